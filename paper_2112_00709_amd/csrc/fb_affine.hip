@@ -1,0 +1,353 @@
+// Affine layer and its gradient (fb_layers.h): the calls, the plain product kernel and what stands beside the products.
+#include "fb_affine.h"
+
+namespace fb {
+
+int launch_column_sum(const float *part, int64_t P, int64_t C, int sets, float *out0, float *out1, void *stream);
+
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kTile = 128, kDeep = 16, kTileLd = kTile + 4;
+
+// A tile's share of a factor, 128 x 16, as floats in LDS, [k][i].
+template <class T>
+__device__ __forceinline__ void fetch(const Factor &f, int64_t i0, int64_t rows, int64_t k0, int64_t k1, float (&v)[8])
+{
+    constexpr int VE = Vec<T>::kN;
+    const int t = threadIdx.x;
+    const T *p = (const T *)f.p;
+    const int64_t i = i0 + (f.along ? t >> 1 : (t & 15) * 8), k = k0 + (f.along ? (t & 1) * 8 : t >> 4);
+    int64_t n = f.along ? (i < rows ? k1 - k : 0) : (k < k1 ? rows - i : 0);
+    n = n < 0 ? 0 : n > 8 ? 8 : n;
+    const T *q = p + (f.along ? i * f.ld + k : k * f.ld + i);
+#pragma unroll
+    for (int e = 0; e < 8; e += VE) unpack<T>(load_piece(q + e, (int)n - e), v + e);
+}
+
+__device__ __forceinline__ void put(const Factor &f, float *tile, const float (&v)[8])
+{
+    const int t = threadIdx.x;
+    if (f.along) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) tile[((t & 1) * 8 + e) * kTileLd + (t >> 1)] = v[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) tile[(t >> 4) * kTileLd + (t & 15) * 8 + e] = v[e];
+    }
+}
+
+// C = A B^T by 128 x 128 tiles, four waves with 64 x 64 each, on the single-precision matrix instruction, 16 k at a time
+// through LDS.  Sums of 256 k are closed and added to a second set, so that roundings do not pile up along k.
+template <class T>
+__global__ __launch_bounds__(256) void fb_product_kernel(Product q)
+{
+    __shared__ float ta[kDeep * kTileLd], tb[kDeep * kTileLd];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t i0 = (int64_t)blockIdx.y * kTile, j0 = (int64_t)blockIdx.x * kTile;
+    const int64_t k0 = blockIdx.z * q.share, k1 = k0 + q.share < q.K ? k0 + q.share : q.K;
+    const int wi = (wave & 1) * 64, wj = (wave >> 1) * 64, l = lane & 31, h = lane >> 5;
+    f32x16 acc[2][2] = {}, sum[2][2] = {};
+    float va[8], vb[8];
+    fetch<T>(q.A, i0, q.M, k0, k1, va);
+    fetch<T>(q.B, j0, q.N, k0, k1, vb);
+    int since = 0;
+    for (int64_t k = k0; k < k1; k += kDeep) {
+        __syncthreads();
+        put(q.A, ta, va);
+        put(q.B, tb, vb);
+        __syncthreads();
+        if (k + kDeep < k1) {
+            fetch<T>(q.A, i0, q.M, k + kDeep, k1, va);
+            fetch<T>(q.B, j0, q.N, k + kDeep, k1, vb);
+        }
+#pragma unroll
+        for (int d = 0; d < kDeep; d += 2) {
+            float a[2], b[2];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                a[s] = ta[(d + h) * kTileLd + wi + s * 32 + l];
+                b[s] = tb[(d + h) * kTileLd + wj + s * 32 + l];
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) acc[s][u] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[s], b[u], acc[s][u], 0, 0, 0);
+        }
+        if (++since == 256 / kDeep) {
+            since = 0;
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    sum[s][u] += acc[s][u];
+                    acc[s][u] = (f32x16)(0.0f);
+                }
+        }
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const f32x16 c = sum[s][u] + acc[s][u];
+            const int64_t j = j0 + wj + u * 32 + l;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int64_t i = i0 + wi + s * 32 + 8 * (e / 4) + 4 * h + e % 4;
+                if (i < q.M && j < q.N) {
+                    if (q.split > 1)
+                        q.part[((size_t)blockIdx.z * q.M + i) * q.N + j] = c[e];
+                    else
+                        finish_one<T>(q.f, i, j, c[e]);
+                }
+            }
+        }
+}
+
+// The shares of a split product added in their order and finished.
+template <class T>
+__global__ __launch_bounds__(256) void fb_product_join_kernel(Product q)
+{
+    const int64_t n = q.M * q.N;
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < n; at += (int64_t)gridDim.x * 256) {
+        float s = 0.0f;
+        for (int c = 0; c < q.split; ++c) s += q.part[(size_t)c * n + at];
+        finish_one<T>(q.f, at / q.N, at % q.N, s);
+    }
+}
+
+struct SlopeParams {
+    const void *dy, *z;
+    int64_t lddy, ldz, M, N, ldo;
+    int act;
+    void *out;           // dz as the products take it, nullable
+    float *part;         // [gridDim.y][N]: shares of the sums over rows, nullable
+};
+
+// dz = dy act'(z), rounded to the factors' type, and the sums of its columns before the rounding.  A thread has one piece of
+// the width and every fourth of a workgroup's rows.
+template <class T, class D>
+__global__ __launch_bounds__(256) void fb_slope_kernel(SlopeParams p)
+{
+    constexpr int VE = Vec<T>::kN, VD = Vec<D>::kN;
+    __shared__ float slots[4][64][VE + 1];
+    const int lane = threadIdx.x & 63, sub = threadIdx.x >> 6;
+    const int64_t at = ((int64_t)blockIdx.x * 64 + lane) * VE;
+    const int n = (int)(p.N - at < VE ? p.N - at : VE);
+    float sum[VE] = {};
+    if (n > 0) {
+        for (int64_t r = (int64_t)blockIdx.y * 4 + sub; r < p.M; r += (int64_t)gridDim.y * 4) {
+            float g[VE];
+#pragma unroll
+            for (int e = 0; e < VE; e += VD) unpack<D>(load_piece((const D *)p.dy + r * p.lddy + at + e, n - e), g + e);
+            if (p.act != FB_ACT_NONE) {
+                float z[VE];
+                unpack<T>(load_piece((const T *)p.z + r * p.ldz + at, n), z);
+#pragma unroll
+                for (int e = 0; e < VE; ++e) g[e] = e < n ? g[e] * act_slope(z[e], p.act) : 0.0f;
+            }
+#pragma unroll
+            for (int e = 0; e < VE; ++e) sum[e] += g[e];
+            if (p.out) store_piece((T *)p.out + r * p.ldo + at, n, pack<T>(g));
+        }
+    }
+    if (!p.part) return;
+#pragma unroll
+    for (int e = 0; e < VE; ++e) slots[sub][lane][e] = sum[e];
+    __syncthreads();
+    if (sub == 0) {
+#pragma unroll
+        for (int e = 0; e < VE; ++e)
+            if (e < n) p.part[(size_t)blockIdx.y * p.N + at + e] = (slots[0][lane][e] + slots[1][lane][e]) + (slots[2][lane][e] + slots[3][lane][e]);
+    }
+}
+
+constexpr int64_t kSlopeGroups = 256;   // shares of the rows
+
+int64_t slope_groups(int64_t M) { return std::max<int64_t>(1, std::min<int64_t>((M + 3) / 4, kSlopeGroups)); }
+
+size_t aligned(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// Shares of k: as many as fill the GPU with tiles, of at least 256 k each.
+void plan_split(Product &q)
+{
+    const int64_t tiles = ((q.M + kTile - 1) / kTile) * ((q.N + kTile - 1) / kTile);
+    int64_t split = std::min<int64_t>(2 * kCUs / std::max<int64_t>(tiles, 1), (q.K + 255) / 256);
+    split = std::max<int64_t>(1, std::min<int64_t>(split, 64));
+    q.share = std::max<int64_t>(kDeep, ((q.K + split - 1) / split + kDeep - 1) / kDeep * kDeep);
+    q.split = (int)std::max<int64_t>(1, (q.K + q.share - 1) / q.share);   // (K = 0, a gradient over no rows: sums of nothing)
+}
+
+size_t product_bytes(const Product &q) { return q.split > 1 ? aligned((size_t)q.split * (size_t)q.M * (size_t)q.N * sizeof(float)) : 0; }
+
+template <class T>
+int launch_product(const Product &q, hipStream_t stream)
+{
+    const int64_t ti = (q.M + kTile - 1) / kTile, tj = (q.N + kTile - 1) / kTile;
+    hipLaunchKernelGGL(fb_product_kernel<T>, dim3((unsigned)tj, (unsigned)ti, (unsigned)q.split), dim3(256), 0, stream, q);
+    int rc = launched("product kernel launch: ");
+    if (rc == FB_OK && q.split > 1) {
+        const int64_t groups = std::min<int64_t>((q.M * q.N + 255) / 256, 8 * kCUs);
+        hipLaunchKernelGGL(fb_product_join_kernel<T>, dim3((unsigned)groups), dim3(256), 0, stream, q);
+        rc = launched("product join kernel launch: ");
+    }
+    return rc;
+}
+
+int launch_product(const Product &q, hipStream_t stream)
+{
+    if (q.M == 0) return FB_OK;
+    if (q.type == FB_TYPE_F32) return launch_product<float>(q, stream);
+    if (q.type == FB_TYPE_BF16) return launch_product<bf16>(q, stream);
+    return launch_product<f16>(q, stream);
+}
+
+bool bad_sizes(int64_t M, int64_t N, int64_t K) { return bad_rows(M) || bad_width(N) || bad_width(K); }
+
+Product forward_product(int64_t M, int64_t N, int64_t K, int type)
+{
+    Product q{};
+    q.M = M; q.N = N; q.K = K; q.type = type;
+    plan_split(q);
+    return q;
+}
+
+// The two products of the gradient.
+struct GradPlan {
+    Product dx, dw;
+    bool slope;           // dz has to be made
+    int64_t ldz;
+    size_t dz, sums, part, bytes;
+};
+
+GradPlan grad_plan(int64_t M, int64_t N, int64_t K, int type, int dy_type, int act)
+{
+    GradPlan g{};
+    g.dx.M = M; g.dx.N = K; g.dx.K = N; g.dx.type = type;
+    g.dw.M = N; g.dw.N = K; g.dw.K = M; g.dw.type = type;
+    plan_split(g.dx);
+    plan_split(g.dw);
+    g.slope = act != FB_ACT_NONE || dy_type != type;
+    g.ldz = (N + 7) & ~(int64_t)7;
+    g.dz = g.slope ? aligned((size_t)M * (size_t)g.ldz * type_bytes(type)) : 0;
+    g.sums = aligned((size_t)slope_groups(M) * (size_t)N * sizeof(float));
+    g.part = std::max(product_bytes(g.dx), product_bytes(g.dw));
+    g.bytes = g.dz + g.sums + g.part;
+    return g;
+}
+
+template <class T, class D>
+int launch_slope(const SlopeParams &p, int64_t groups, hipStream_t stream)
+{
+    const int64_t wide = 64 * Vec<T>::kN;
+    hipLaunchKernelGGL((fb_slope_kernel<T, D>), dim3((unsigned)((p.N + wide - 1) / wide), (unsigned)groups), dim3(256), 0, stream, p);
+    return launched("activation slope kernel launch: ");
+}
+
+int check_affine(const char *who, const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t N, int64_t K, int type, int act)
+{
+    const std::string w(who);
+    if (!known_type(type)) return fail(FB_EINVAL, w + ": unknown type");
+    if (act < FB_ACT_NONE || act > FB_ACT_SILU) return fail(FB_EINVAL, w + ": unknown activation");
+    if (bad_sizes(M, N, K)) return fail(FB_EINVAL, w + ": M must be 0 or more, N and K 1 or more, all below 2^31");
+    if ((!x && M > 0) || !weight) return fail(FB_EINVAL, w + ": x or weight is NULL");
+    if (bad_ld(ldx, K) || bad_ld(ldw, K)) return fail(FB_EINVAL, w + ": rows of x or weight closer than K elements");
+    return FB_OK;
+}
+
+}  // namespace
+
+}  // namespace fb
+
+extern "C" {
+
+size_t fb_affine_workspace_bytes(int64_t M, int64_t N, int64_t K, int type, int64_t ldx, int64_t ldw)
+{
+    using namespace fb;
+    (void)ldx; (void)ldw;
+    if (bad_sizes(M, N, K) || !known_type(type)) return 0;
+    return product_bytes(forward_product(M, N, K, type));
+}
+
+int fb_affine(const void *x, int64_t ldx, const void *weight, int64_t ldw, const float *bias, const void *residual, int64_t ldr,
+              int64_t M, int64_t N, int64_t K, int type, int act, void *y, int64_t ldy, int out_type, void *preact, int64_t ldp,
+              void *ws, size_t ws_bytes, fb_stream stream)
+{
+    using namespace fb;
+    return guarded([&]() -> int {
+        const int rc = check_affine("fb_affine", x, ldx, weight, ldw, M, N, K, type, act);
+        if (rc != FB_OK) return rc;
+        if (out_type != type && out_type != FB_TYPE_F32) return fail(FB_EINVAL, "fb_affine: the output's type is neither float nor the factors'");
+        if (!y && M > 0) return fail(FB_EINVAL, "fb_affine: y is NULL");
+        if (bad_ld(ldy, N) || (residual && bad_ld(ldr, N)) || (preact && bad_ld(ldp, N))) return fail(FB_EINVAL, "fb_affine: rows closer than N elements");
+        Product q = forward_product(M, N, K, type);
+        if (product_bytes(q) && (!ws || ws_bytes < product_bytes(q))) return fail(FB_EINVAL, "fb_affine: workspace missing or too small");
+        q.A = {x, ldx, true};
+        q.B = {weight, ldw, true};
+        q.f = {bias, residual, ldr, act, y, ldy, out_type, preact, ldp};
+        q.part = (float *)ws;
+        return launch_product(q, (hipStream_t)stream);
+    });
+}
+
+size_t fb_affine_grad_workspace_bytes(int64_t M, int64_t N, int64_t K, int type, int dy_type, int act, int64_t lddy, int64_t ldx, int64_t ldw)
+{
+    using namespace fb;
+    (void)lddy; (void)ldx; (void)ldw;
+    if (bad_sizes(M, N, K) || !known_type(type) || (dy_type != type && dy_type != FB_TYPE_F32) || act < FB_ACT_NONE || act > FB_ACT_SILU) return 0;
+    return grad_plan(M, N, K, type, dy_type, act).bytes;
+}
+
+int fb_affine_grad(const void *dy, int64_t lddy, int dy_type, const void *x, int64_t ldx, const void *weight, int64_t ldw,
+                   const void *preact, int64_t ldp, int64_t M, int64_t N, int64_t K, int type, int act, void *dx, int64_t lddx,
+                   void *dweight, float *dbias, void *ws, size_t ws_bytes, fb_stream stream)
+{
+    using namespace fb;
+    return guarded([&]() -> int {
+        int rc = check_affine("fb_affine_grad", x, ldx, weight, ldw, M, N, K, type, act);
+        if (rc != FB_OK) return rc;
+        if (dy_type != type && dy_type != FB_TYPE_F32) return fail(FB_EINVAL, "fb_affine_grad: the type of dy is neither float nor the factors'");
+        if (!dy && M > 0) return fail(FB_EINVAL, "fb_affine_grad: dy is NULL");
+        if (act != FB_ACT_NONE && !preact && M > 0) return fail(FB_EINVAL, "fb_affine_grad: this activation needs preact");
+        if (bad_ld(lddy, N) || (act != FB_ACT_NONE && bad_ld(ldp, N)) || (dx && bad_ld(lddx, K))) return fail(FB_EINVAL, "fb_affine_grad: rows closer than their width");
+        if (!dx && !dweight && !dbias) return FB_OK;
+        GradPlan g = grad_plan(M, N, K, type, dy_type, act);
+        if (!ws || ws_bytes < g.bytes) return fail(FB_EINVAL, "fb_affine_grad: workspace missing or too small");
+        hipStream_t st = (hipStream_t)stream;
+        char *w = (char *)ws;
+        void *dz = w;
+        float *sums = (float *)(w + g.dz), *part = (float *)(w + g.dz + g.sums);
+        const bool make = g.slope && (dx || dweight);
+        if (M > 0 && (make || dbias)) {
+            SlopeParams p{dy, preact, lddy, ldp, M, N, g.ldz, act, make ? dz : nullptr, dbias ? sums : nullptr};
+            const int64_t groups = slope_groups(M);
+            if (type == FB_TYPE_F32)
+                rc = launch_slope<float, float>(p, groups, st);
+            else if (type == FB_TYPE_BF16)
+                rc = dy_type == type ? launch_slope<bf16, bf16>(p, groups, st) : launch_slope<bf16, float>(p, groups, st);
+            else
+                rc = dy_type == type ? launch_slope<f16, f16>(p, groups, st) : launch_slope<f16, float>(p, groups, st);
+            if (rc != FB_OK) return rc;
+        }
+        if (dbias && (rc = launch_column_sum(sums, M > 0 ? slope_groups(M) : 0, N, 1, dbias, nullptr, stream)) != FB_OK) return rc;
+        const Factor d{make ? dz : dy, make ? g.ldz : lddy, true};
+        if (dx) {
+            g.dx.A = d;
+            g.dx.B = {weight, ldw, false};
+            g.dx.f.y = dx; g.dx.f.ldy = lddx; g.dx.f.out_type = type;
+            g.dx.part = part;
+            if ((rc = launch_product(g.dx, st)) != FB_OK) return rc;
+        }
+        if (dweight) {
+            g.dw.A = {d.p, d.ld, false};
+            g.dw.B = {x, ldx, false};
+            g.dw.f.y = dweight; g.dw.f.ldy = K; g.dw.f.out_type = type;
+            g.dw.part = part;
+            if ((rc = launch_product(g.dw, st)) != FB_OK) return rc;
+        }
+        return FB_OK;
+    });
+}
+
+}  // extern "C"

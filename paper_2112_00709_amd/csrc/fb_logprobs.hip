@@ -1,0 +1,541 @@
+// Log probabilities of given tokens, entropy and best alternatives, and their gradient (fb_layers.h).
+//
+// One pass over the logits.  A wave holds a piece of a row in registers (as stored, 16 bytes a piece and lane), takes its
+// maximum m and with d = x - m the sums S = sum e^d and T = sum e^d d; then log Z = m + log S and H = log S - T / S.  Pieces
+// of a row are joined by (m, S, T) -> (M, S e^(m-M), (T + S (m - M)) e^(m-M)), so a long row is split over as many waves
+// and workgroups as it takes, and the logits are never read twice.
+#include "fb_layers_device.h"
+
+namespace fb {
+
+namespace {
+
+constexpr float kLog2E = 1.44269504088896340736f;
+constexpr float kInf = __builtin_huge_valf();
+
+struct TokenParams {
+    const void *logits;
+    int64_t ld, R, V;
+    const int32_t *tokens;
+    int top;
+    float *logprobs, *entropy, *logz;
+    int32_t *top_ids;
+    float *top_logprobs;
+    int split;                 // workgroups a row
+    int64_t chunk;             // elements of the row that each of them has
+    float *part;               // [R][split][3]: m, S, T
+    uint64_t *part_top;        // [R][split][top] keys
+};
+
+// Total order of (value, number): larger values first, then smaller numbers.  -0 counts as 0.
+__device__ __forceinline__ uint32_t order_of(float x)
+{
+    const uint32_t u = __float_as_uint(x + 0.0f);
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o ^ ((o & 0x80000000u) ? 0x80000000u : 0xffffffffu)); }
+__device__ __forceinline__ uint64_t key_of(float x, uint32_t j) { return (uint64_t)order_of(x) << 32 | (uint32_t)~j; }
+
+// Largest key of a wave; 0 stands for none.
+__device__ __forceinline__ uint64_t max_wave_key(uint64_t k)
+{
+    const uint32_t hi = max_wave_u((uint32_t)(k >> 32));
+    const uint32_t lo = max_wave_u((uint32_t)(k >> 32) == hi ? (uint32_t)k : 0u);
+    return (uint64_t)hi << 32 | lo;
+}
+
+// What a wave's lanes have written to LDS, its other lanes read from here on (LDS serves a wave in order: only the compiler
+// is held).
+__device__ __forceinline__ void lds_settled() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+
+struct Stats {
+    float m, S, T;
+};
+
+__device__ __forceinline__ Stats join(const Stats &a, const Stats &b)
+{
+    const float M = fmaxf(a.m, b.m);
+    if (M == -kInf) return {M, a.S + b.S, a.T + b.T};           // nothing but -inf so far (or NaN, which the sums carry on)
+    const float da = a.m == -kInf ? 0.0f : a.m - M, db = b.m == -kInf ? 0.0f : b.m - M;   // (an empty side has no sums to scale)
+    const float ea = __builtin_amdgcn_exp2f(da * kLog2E), eb = __builtin_amdgcn_exp2f(db * kLog2E);
+    return {M, fmaf(a.S, ea, b.S * eb), fmaf(fmaf(a.S, da, a.T), ea, fmaf(b.S, db, b.T) * eb)};
+}
+
+// The best `top` of n keys, descending, to `out`; missing ones are 0.  For one wave.
+__device__ __forceinline__ void best_of_keys(const uint64_t *keys, int n, int top, uint64_t *out)
+{
+    const int lane = threadIdx.x & 63;
+    uint64_t last = ~0ull;
+    for (int t = 0; t < top; ++t) {
+        uint64_t best = 0;
+        for (int i = lane; i < n; i += 64) {
+            const uint64_t k = keys[i];
+            if (k < last && k > best) best = k;
+        }
+        last = max_wave_key(best);
+        if (lane == 0) out[t] = last;
+    }
+}
+
+// The best `top` of the elements that a wave holds pieces of (in memory: piece i of a lane starts at element first + i * stride
+// of n), as keys, descending, to out[0 .. top) in LDS; peak[i] is the largest element of the lane's piece i.  The top-th
+// largest of the lanes' own maxima bounds the top-th best from below; what reaches it are few elements (about `top`) of few
+// pieces, which are read once more, put on a list and ranked there, one a lane.  Where ties, or rows of almost nothing but
+// -inf, make them more than 64 the elements are searched once per place.  (From memory: the pieces in registers, indexed at
+// run time, would take a copy of all this per element.)
+template <class T, int NV>
+__device__ __forceinline__ void best_of_wave(const T *row, const float (&peak)[NV], float lane_max, int first, int stride, int n, int top, uint64_t *list, uint64_t *out)
+{
+    constexpr int VE = Vec<T>::kN;
+    const int lane = threadIdx.x & 63;
+    float cur = lane_max, bound = -kInf;
+    for (int found = 0; found < top;) {
+        bound = max_wave(cur);
+        const uint64_t hit = __ballot(cur == bound);
+        if (bound == -kInf || hit == 0) break;
+        found += __popcll(hit);
+        if (cur == bound) cur = -kInf;
+    }
+    uint32_t pieces = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) pieces |= peak[i] >= bound ? 1u << i : 0u;
+    int count = 0;
+    while (count <= 64 && __ballot(pieces != 0) != 0) {
+        const int at = first + (pieces ? __ffs(pieces) - 1 : 0) * stride;
+        const int left = pieces ? n - at : 0;
+        pieces &= pieces - 1;
+        float v[VE];
+        unpack<T>(load_piece(row + at, left), v);
+#pragma unroll
+        for (int j = 0; j < VE; ++j) {
+            const uint64_t hit = __ballot(j < left && v[j] >= bound);
+            const int at_list = count + __popcll(hit & ((1ull << lane) - 1));
+            if ((hit >> lane & 1) && at_list < 64) list[at_list] = key_of(v[j], (uint32_t)(at + j));
+            count += __popcll(hit);
+        }
+    }
+    lds_settled();
+    if (count <= 64) {
+        const uint64_t mine = lane < count ? list[lane] : 0;
+        int rank = 0;
+        for (int c = 0; c < count; ++c) {
+            const uint64_t k = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(mine >> 32), c) << 32 |
+                               (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)mine, c);
+            rank += k > mine ? 1 : 0;
+        }
+        if (lane < count && rank < top) out[rank] = mine;
+        if (lane >= count && lane < top) out[lane] = 0;
+        return;
+    }
+    uint64_t last = ~0ull;
+    for (int t = 0; t < top; ++t) {
+        uint64_t best = 0;
+#pragma unroll 1
+        for (int i = 0; i < NV; ++i) {
+            float v[VE];
+            const int at = first + i * stride;
+            unpack<T>(load_piece(row + at, n - at), v);
+#pragma unroll
+            for (int j = 0; j < VE; ++j) {
+                const uint64_t k = key_of(v[j], (uint32_t)(at + j));
+                if (at + j < n && k < last && k > best) best = k;
+            }
+        }
+        last = max_wave_key(best);
+        if (lane == 0) out[t] = last;
+    }
+}
+
+// A row's results from its statistics and the keys of its best elements (one lane a place).
+template <class T>
+__device__ __forceinline__ void write_row(const TokenParams &p, int64_t r, int32_t token, const Stats &st, const uint64_t *keys, int lane)
+{
+    const float ls = logf(st.S);
+    const bool dead = st.m == -kInf && st.S == 0.0f;
+    const float logz = dead ? -kInf : st.m + ls;
+    if (lane == 0) {
+        if (p.logz) p.logz[r] = logz;
+        if (p.entropy) p.entropy[r] = dead ? 0.0f : ls - st.T / st.S;
+        if (p.logprobs) {
+            const float x = token < p.V ? load_one((const T *)p.logits + r * p.ld + token) : __builtin_nanf("");
+            p.logprobs[r] = dead && token < p.V ? -kInf : x - logz;
+        }
+    }
+    if (lane < p.top) {
+        const uint64_t k = keys[lane];
+        const float x = value_of((uint32_t)(k >> 32));
+        p.top_ids[r * p.top + lane] = k ? (int32_t)~(uint32_t)k : -1;
+        p.top_logprobs[r * p.top + lane] = !k ? __builtin_nanf("") : x == -kInf ? -kInf : x - logz;
+    }
+}
+
+__device__ __forceinline__ void write_padding(const TokenParams &p, int64_t r, int lane)
+{
+    if (lane == 0) {
+        if (p.logz) p.logz[r] = 0.0f;
+        if (p.entropy) p.entropy[r] = 0.0f;
+        if (p.logprobs) p.logprobs[r] = 0.0f;
+    }
+    if (lane < p.top) {
+        p.top_ids[r * p.top + lane] = -1;
+        p.top_logprobs[r * p.top + lane] = 0.0f;
+    }
+}
+
+// Statistics of what a wave holds: elements first + i * stride + j < n.
+template <class T, int NV>
+__device__ __forceinline__ Stats wave_stats(u32x4 (&raw)[NV], int first, int stride, int n, float (&peak)[NV], float &lane_max)
+{
+    constexpr int VE = Vec<T>::kN;
+    float m = -kInf;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        float v[VE];
+        unpack<T>(raw[i], v);
+        const int at = first + i * stride;
+        if (at + VE > n) {                                    // places past the end hold -inf from here on
+#pragma unroll
+            for (int j = 0; j < VE; ++j) v[j] = at + j < n ? v[j] : -kInf;
+            raw[i] = pack<T>(v);
+        }
+        peak[i] = -kInf;
+#pragma unroll
+        for (int j = 0; j < VE; ++j) peak[i] = fmaxf(peak[i], v[j]);
+        m = fmaxf(m, peak[i]);
+    }
+    lane_max = m;
+    m = max_wave(m);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(raw[i]));   // (unpacked anew below, not kept as floats in twice the registers)
+    const float base = m == -kInf ? 0.0f : m;
+    float S = 0.0f, U = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        float v[VE];
+        unpack<T>(raw[i], v);
+#pragma unroll
+        for (int j = 0; j < VE; ++j) {
+            const float d = v[j] - base, e = __builtin_amdgcn_exp2f(d * kLog2E);
+            S += e;
+            U = fmaf(e, fmaxf(d, -1e30f), U);                 // (e is 0 where d is -inf)
+        }
+    }
+    return {m, sum_wave(S), sum_wave(U)};
+}
+
+// WAVES waves hold a row, or a workgroup's chunk of one (SPLIT); with one wave a row a workgroup has four rows at a time.
+template <class T, int WAVES, int NV, bool SPLIT>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64, NV * Vec<T>::kN <= 16 ? 8 : NV * Vec<T>::kN <= 32 ? 6 : 4) void fb_token_logprobs_kernel(TokenParams p)
+{
+    constexpr int VE = Vec<T>::kN, kRows = WAVES == 1 ? 4 : 1, kW = WAVES == 1 ? 4 : WAVES;
+    __shared__ uint64_t list[kW][64], best[kW][FB_TOP_MAX];
+    __shared__ Stats stats[kW];
+    __shared__ uint64_t row_best[FB_TOP_MAX];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t item = (int64_t)blockIdx.x * kRows + (WAVES == 1 ? wave : 0);
+    const int64_t r = SPLIT ? item / p.split : item;
+    const int c = SPLIT ? (int)(item - r * p.split) : 0;
+    if (r >= p.R) return;                                     // (a whole wave; with WAVES > 1 the whole workgroup)
+    const int32_t token = p.tokens[r];
+    if (token < 0) {
+        if ((WAVES == 1 || wave == 0) && c == 0 && !SPLIT) write_padding(p, r, lane);
+        return;
+    }
+    const int64_t at0 = SPLIT ? c * p.chunk : 0;
+    const int n = (int)((SPLIT ? (p.V - at0 < p.chunk ? p.V - at0 : p.chunk) : p.V));
+    const T *row = (const T *)p.logits + r * p.ld + at0;
+    const int first = ((WAVES == 1 ? 0 : wave) * NV * 64 + lane) * VE;   // a wave's pieces lie side by side
+    u32x4 raw[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) raw[i] = load_piece(row + first + i * 64 * VE, n - (first + i * 64 * VE));
+    float peak[NV], lane_max;
+    Stats st = wave_stats<T, NV>(raw, first, 64 * VE, n, peak, lane_max);
+    if (p.top) best_of_wave<T, NV>(row, peak, lane_max, first, 64 * VE, n, p.top, list[wave], best[wave]);
+    lds_settled();
+    const uint64_t *keys = best[wave];
+    if constexpr (WAVES > 1) {
+        if (lane == 0) stats[wave] = st;
+        __syncthreads();
+        if (wave != 0) return;
+        st = stats[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) st = join(st, stats[w]);
+        if (p.top) {
+            // (`best` is one array; its rows hold `top` keys each and zeros are no keys)
+            uint64_t last = ~0ull;
+            for (int t = 0; t < p.top; ++t) {
+                uint64_t b = 0;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) {
+                    const uint64_t k = lane < p.top ? best[w][lane] : 0;
+                    if (k < last && k > b) b = k;
+                }
+                last = max_wave_key(b);
+                if (lane == 0) row_best[t] = last;
+            }
+            lds_settled();
+            keys = row_best;
+        }
+    }
+    if constexpr (SPLIT) {
+        float *q = p.part + (size_t)item * 3;
+        if (lane == 0) {
+            q[0] = st.m;
+            q[1] = st.S;
+            q[2] = st.T;
+        }
+        if (lane < p.top) {
+            const uint64_t k = keys[lane];                    // numbers in the row instead of the chunk
+            p.part_top[(size_t)item * p.top + lane] = k ? (k & 0xffffffff00000000ull) | (uint32_t)~(~(uint32_t)k + (uint32_t)at0) : 0;
+        }
+    } else {
+        write_row<T>(p, r, token, st, keys, lane);
+    }
+}
+
+// The chunks of a row joined, one wave a row.
+template <class T>
+__global__ __launch_bounds__(64) void fb_token_join_kernel(TokenParams p)
+{
+    __shared__ uint64_t best[FB_TOP_MAX];
+    const int lane = threadIdx.x;
+    const int64_t r = blockIdx.x;
+    const int32_t token = p.tokens[r];
+    if (token < 0) {
+        write_padding(p, r, lane);
+        return;
+    }
+    const float *q = p.part + (size_t)r * p.split * 3;
+    Stats st = {-kInf, 0.0f, 0.0f};
+    for (int c = lane; c < p.split; c += 64) st = join(st, {q[3 * c], q[3 * c + 1], q[3 * c + 2]});
+#pragma unroll
+    for (int step = 1; step < 64; step <<= 1) {
+        const Stats o = {__shfl_xor(st.m, step), __shfl_xor(st.S, step), __shfl_xor(st.T, step)};
+        st = join(st, o);
+    }
+    if (p.top) best_of_keys(p.part_top + (size_t)r * p.split * p.top, p.split * p.top, p.top, best);
+    __syncthreads();
+    write_row<T>(p, r, token, st, best, lane);
+}
+
+struct TokenGradParams {
+    const void *logits;
+    int64_t ld, R, V, ldd;
+    const int32_t *tokens;
+    const float *logz, *entropy, *g_logprobs, *g_entropy;
+    void *dlogits;
+    int64_t pieces, items;     // pieces of 64 * kGradPieces vectors a row, and of all rows
+};
+
+constexpr int kGradPieces = 4;
+
+// One element at a time is all there is to it: bound by memory.  A wave has 4 KB of a row.
+template <class T>
+__global__ __launch_bounds__(256) void fb_token_logprobs_grad_kernel(TokenGradParams p)
+{
+    constexpr int VE = Vec<T>::kN, kWide = 64 * VE * kGradPieces;
+    const int lane = threadIdx.x & 63;
+    const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (item >= p.items) return;
+    const int64_t r = item / p.pieces;
+    const int64_t at0 = (item - r * p.pieces) * kWide;
+    const int n = (int)(p.V - at0 < kWide ? p.V - at0 : kWide);
+    const int32_t token = p.tokens[r];
+    const float logz = p.logz[r];
+    const bool live = token >= 0 && logz != -kInf;
+    const T *row = (const T *)p.logits + r * p.ld + at0;
+    T *out = (T *)p.dlogits + r * p.ldd + at0;
+    const float g = p.g_logprobs ? p.g_logprobs[r] : 0.0f, h = p.g_entropy ? p.g_entropy[r] : 0.0f, ent = p.g_entropy ? p.entropy[r] : 0.0f;
+    const float a = fmaf(h, ent, g);                          // -p (g + h (log p + H)) = -p (a + h log p)
+    const int64_t hit = (int64_t)token - at0;
+    u32x4 raw[kGradPieces];
+    if (live) {
+#pragma unroll
+        for (int i = 0; i < kGradPieces; ++i) raw[i] = load_piece(row + (i * 64 + lane) * VE, n - (i * 64 + lane) * VE);
+    }
+#pragma unroll
+    for (int i = 0; i < kGradPieces; ++i) {
+        const int at = (i * 64 + lane) * VE;
+        float v[VE];
+        if (live) {
+            unpack<T>(raw[i], v);
+#pragma unroll
+            for (int j = 0; j < VE; ++j) {
+                const float lp = v[j] - logz, q = __builtin_amdgcn_exp2f(lp * kLog2E);
+                v[j] = -q * fmaf(h, fmaxf(lp, -1e30f), a);
+                if (at + j == hit) v[j] += g;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < VE; ++j) v[j] = 0.0f;
+        }
+        store_piece(out + at, n - at, pack<T>(v));
+    }
+}
+
+// How a call is laid out.  A wave holds up to 64 elements a lane: rows of up to 4096 elements go to a wave each where there
+// are enough of them to fill the GPU, else to four waves; rows that four waves cannot hold are split over workgroups,
+// and so are long rows that are few.
+struct TokenPlan {
+    int waves, nv, split;
+    int64_t chunk;
+};
+
+constexpr int kMostElements = 64;   // of a row, in a lane's registers
+
+TokenPlan token_plan(int64_t R, int64_t V, int type)
+{
+    const int64_t ve = 16 / (int64_t)type_bytes(type);
+    const int64_t vecs = (V + ve - 1) / ve, most = kMostElements / ve;
+    TokenPlan t{};
+    t.split = 1;
+    const int64_t one = 64, four = 256;
+    if (vecs <= one * 2 || (vecs <= one * most && R >= 4 * kCUs)) {
+        t.waves = 1;
+        t.nv = (int)((vecs + one - 1) / one);
+    } else {
+        t.waves = 4;
+        int64_t split = (vecs + four * most - 1) / (four * most);
+        // few rows: as many workgroups as the GPU has compute units, as long as each has 2 vectors a lane
+        const int64_t fill = (kCUs + R - 1) / std::max<int64_t>(R, 1);
+        if (split < fill) split = std::max(split, std::min(fill, (vecs + four * 2 - 1) / (four * 2)));
+        const int64_t each = (vecs + split - 1) / split;
+        t.nv = (int)((each + four - 1) / four);
+        t.split = (int)((vecs + each - 1) / each);
+        t.chunk = each * ve;
+    }
+    t.nv = t.nv <= 1 ? 1 : t.nv <= 2 ? 2 : t.nv <= 4 ? 4 : t.nv <= 8 ? 8 : t.nv <= 12 ? 12 : 16;
+    return t;
+}
+
+template <class T, int WAVES, int NV>
+void launch_tokens(const TokenParams &p, hipStream_t stream)
+{
+    const int64_t items = p.R * p.split, groups = WAVES == 1 ? (items + 3) / 4 : items;
+    const dim3 block(WAVES == 1 ? 256 : WAVES * 64);
+    if constexpr (NV * Vec<T>::kN <= kMostElements) {
+        if constexpr (WAVES > 1) {
+            if (p.split > 1) {
+                hipLaunchKernelGGL((fb_token_logprobs_kernel<T, WAVES, NV, true>), dim3((unsigned)groups), block, 0, stream, p);
+                return;
+            }
+        }
+        hipLaunchKernelGGL((fb_token_logprobs_kernel<T, WAVES, NV, false>), dim3((unsigned)groups), block, 0, stream, p);
+    }
+}
+
+template <class T>
+int launch_tokens(const TokenParams &p, const TokenPlan &t, hipStream_t stream)
+{
+#define FB_TOKENS(W, N) launch_tokens<T, W, N>(p, stream)
+    if (t.waves == 1) {
+        switch (t.nv) {
+        case 1: FB_TOKENS(1, 1); break;
+        case 2: FB_TOKENS(1, 2); break;
+        case 4: FB_TOKENS(1, 4); break;
+        case 8: FB_TOKENS(1, 8); break;
+        case 12: FB_TOKENS(1, 12); break;
+        default: FB_TOKENS(1, 16); break;
+        }
+    } else {
+        switch (t.nv) {
+        case 1: FB_TOKENS(4, 1); break;
+        case 2: FB_TOKENS(4, 2); break;
+        case 4: FB_TOKENS(4, 4); break;
+        case 8: FB_TOKENS(4, 8); break;
+        case 12: FB_TOKENS(4, 12); break;
+        default: FB_TOKENS(4, 16); break;
+        }
+    }
+#undef FB_TOKENS
+    int rc = launched("token log probability kernel launch: ");
+    if (rc == FB_OK && p.split > 1) {
+        hipLaunchKernelGGL((fb_token_join_kernel<T>), dim3((unsigned)p.R), dim3(64), 0, stream, p);
+        rc = launched("token join kernel launch: ");
+    }
+    return rc;
+}
+
+size_t stats_bytes(int64_t R, int split) { return ((size_t)R * split * 3 * sizeof(float) + 255) & ~(size_t)255; }
+
+int check_tokens(const char *who, const void *logits, int64_t ld, const int32_t *tokens, int64_t R, int64_t V, int type)
+{
+    const std::string w(who);
+    if (!known_type(type)) return fail(FB_EINVAL, w + ": unknown type");
+    if (bad_rows(R) || bad_width(V)) return fail(FB_EINVAL, w + ": R must be 0 or more, V 1 or more, both below 2^31");
+    if ((!logits || !tokens) && R > 0) return fail(FB_EINVAL, w + ": logits or tokens is NULL");
+    if (bad_ld(ld, V)) return fail(FB_EINVAL, w + ": rows closer than V elements");
+    return FB_OK;
+}
+
+}  // namespace
+
+}  // namespace fb
+
+extern "C" {
+
+size_t fb_token_logprobs_workspace_bytes(int64_t R, int64_t V, int type, int top)
+{
+    using namespace fb;
+    if (bad_rows(R) || bad_width(V) || !known_type(type) || top < 0 || top > FB_TOP_MAX || top > V) return 0;
+    const TokenPlan t = token_plan(R, V, type);
+    return t.split == 1 ? 0 : stats_bytes(R, t.split) + (((size_t)R * t.split * top * sizeof(uint64_t) + 255) & ~(size_t)255);
+}
+
+int fb_token_logprobs(const void *logits, int64_t ld, const int32_t *tokens, int64_t R, int64_t V, int type, int top,
+                      float *logprobs, float *entropy, float *logz, int32_t *top_ids, float *top_logprobs, void *ws,
+                      size_t ws_bytes, fb_stream stream)
+{
+    using namespace fb;
+    return guarded([&]() -> int {
+        const int rc = check_tokens("fb_token_logprobs", logits, ld, tokens, R, V, type);
+        if (rc != FB_OK) return rc;
+        if (top < 0 || top > FB_TOP_MAX || top > V) return fail(FB_EINVAL, "fb_token_logprobs: top must lie in 0 .. min(FB_TOP_MAX, V)");
+        if (top > 0 && (!top_ids || !top_logprobs) && R > 0) return fail(FB_EINVAL, "fb_token_logprobs: top_ids or top_logprobs is NULL");
+        const size_t need = fb_token_logprobs_workspace_bytes(R, V, type, top);
+        if (need && (!ws || ws_bytes < need)) return fail(FB_EINVAL, "fb_token_logprobs: workspace missing or too small");
+        if (R == 0) return FB_OK;
+        const TokenPlan t = token_plan(R, V, type);
+        TokenParams p{};
+        p.logits = logits; p.ld = ld; p.R = R; p.V = V; p.tokens = tokens; p.top = top;
+        p.logprobs = logprobs; p.entropy = entropy; p.logz = logz; p.top_ids = top_ids; p.top_logprobs = top_logprobs;
+        p.split = t.split; p.chunk = t.chunk;
+        p.part = (float *)ws;
+        p.part_top = (uint64_t *)((char *)ws + (t.split > 1 ? stats_bytes(R, t.split) : 0));
+        if (R * t.split >= kMostSize) return fail(FB_EUNSUPPORTED, "fb_token_logprobs: more than 2^31 pieces of rows");
+        if (type == FB_TYPE_F32) return launch_tokens<float>(p, t, (hipStream_t)stream);
+        if (type == FB_TYPE_BF16) return launch_tokens<bf16>(p, t, (hipStream_t)stream);
+        return launch_tokens<f16>(p, t, (hipStream_t)stream);
+    });
+}
+
+int fb_token_logprobs_grad(const void *logits, int64_t ld, const int32_t *tokens, const float *logz, const float *entropy,
+                           const float *g_logprobs, const float *g_entropy, int64_t R, int64_t V, int type, void *dlogits,
+                           int64_t ldd, fb_stream stream)
+{
+    using namespace fb;
+    return guarded([&]() -> int {
+        const int rc = check_tokens("fb_token_logprobs_grad", logits, ld, tokens, R, V, type);
+        if (rc != FB_OK) return rc;
+        if ((!logz || !dlogits || (g_entropy && !entropy)) && R > 0) return fail(FB_EINVAL, "fb_token_logprobs_grad: logz, dlogits or entropy is NULL");
+        if (bad_ld(ldd, V)) return fail(FB_EINVAL, "fb_token_logprobs_grad: rows closer than V elements");
+        if (R == 0) return FB_OK;
+        TokenGradParams p{};
+        p.logits = logits; p.ld = ld; p.R = R; p.V = V; p.ldd = ldd; p.tokens = tokens; p.logz = logz; p.entropy = entropy;
+        p.g_logprobs = g_logprobs; p.g_entropy = g_entropy; p.dlogits = dlogits;
+        const int64_t wide = 64 * kGradPieces * (16 / (int64_t)type_bytes(type));
+        p.pieces = (V + wide - 1) / wide;
+        p.items = R * p.pieces;
+        if (p.items >= 4 * (kMostSize - 1)) return fail(FB_EUNSUPPORTED, "fb_token_logprobs_grad: more than 2^33 pieces of rows");
+        const dim3 grid((unsigned)((p.items + 3) / 4)), block(256);
+        if (type == FB_TYPE_F32)
+            hipLaunchKernelGGL(fb_token_logprobs_grad_kernel<float>, grid, block, 0, (hipStream_t)stream, p);
+        else if (type == FB_TYPE_BF16)
+            hipLaunchKernelGGL(fb_token_logprobs_grad_kernel<bf16>, grid, block, 0, (hipStream_t)stream, p);
+        else
+            hipLaunchKernelGGL(fb_token_logprobs_grad_kernel<f16>, grid, block, 0, (hipStream_t)stream, p);
+        return launched("token log probability gradient kernel launch: ");
+    });
+}
+
+}  // extern "C"
