@@ -63,8 +63,9 @@ int fb_layer_norm_grad(const void *dy, int64_t lddy, const void *x, int64_t ldx,
                        const void *weight, int wtype, int64_t R, int64_t H, int type, void *dx, int64_t lddx, float *dweight,
                        float *dbias, void *ws, size_t ws_bytes, fb_stream stream);
 
-/* Bytes of workspace fb_affine needs for these sizes, types and row distances (0: none, or bad arguments). */
-size_t fb_affine_workspace_bytes(int64_t M, int64_t N, int64_t K, int type, int64_t ldx, int64_t ldw);
+/* Bytes of workspace fb_affine needs for these arguments (0: none, or bad arguments).  Of x and weight only the address counts:
+ * 16-bit matrices whose rows are not whole 16-byte pieces at multiples of 16 bytes are copied to such rows first. */
+size_t fb_affine_workspace_bytes(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t N, int64_t K, int type);
 
 /*
  * Affine layer:  z = x W^T + bias,  y = act(z) + residual
@@ -80,9 +81,10 @@ int fb_affine(const void *x, int64_t ldx, const void *weight, int64_t ldw, const
               int64_t M, int64_t N, int64_t K, int type, int act, void *y, int64_t ldy, int out_type, void *preact, int64_t ldp,
               void *ws, size_t ws_bytes, fb_stream stream);
 
-/* Bytes of workspace fb_affine_grad needs (0: none, or bad arguments). */
-size_t fb_affine_grad_workspace_bytes(int64_t M, int64_t N, int64_t K, int type, int dy_type, int act, int64_t lddy, int64_t ldx,
-                                      int64_t ldw);
+/* Bytes of workspace fb_affine_grad needs for these arguments (0: bad arguments); addresses count as in
+ * fb_affine_workspace_bytes. */
+size_t fb_affine_grad_workspace_bytes(const void *dy, int64_t lddy, int dy_type, const void *x, int64_t ldx, const void *weight, int64_t ldw,
+                                      int64_t M, int64_t N, int64_t K, int type, int act);
 
 /*
  * Its gradient:  dz = dy act'(preact),  dx = dz W,  dweight = dz^T x,  dbias = sum over rows of dz

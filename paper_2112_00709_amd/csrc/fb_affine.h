@@ -34,7 +34,17 @@ struct Product {
     float *part;         // split > 1: [split][M][N] sums of shares of k
     int split;
     int64_t share;       // length of a share
+    int tile;            // 16-bit factors: 256 or 128, the side of the tiles
 };
+
+int launch_mfma_product(const Product &q, hipStream_t stream);   // 16-bit factors, see ready()
+
+// Whether the matrix units' kernel can take a factor as it is: whole 16-byte pieces, at addresses and distances that are
+// multiples of 16 bytes, and a tile's rows within the 2^31 bytes of a buffer.  `width`: the length of its rows in memory.
+inline bool ready(const void *p, int64_t ld, int64_t width)
+{
+    return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && width % 8 == 0 && ld < (int64_t)1 << 21;
+}
 
 namespace {
 

@@ -11,19 +11,18 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kTile = 128, kDeep = 16, kTileLd = kTile + 4;
 
-// A tile's share of a factor, 128 x 16, as floats in LDS, [k][i].
-template <class T>
+// A tile's share of a factor, 128 x 16, [k][i] in LDS.
 __device__ __forceinline__ void fetch(const Factor &f, int64_t i0, int64_t rows, int64_t k0, int64_t k1, float (&v)[8])
 {
-    constexpr int VE = Vec<T>::kN;
+    constexpr int VE = Vec<float>::kN;
     const int t = threadIdx.x;
-    const T *p = (const T *)f.p;
+    const float *p = (const float *)f.p;
     const int64_t i = i0 + (f.along ? t >> 1 : (t & 15) * 8), k = k0 + (f.along ? (t & 1) * 8 : t >> 4);
     int64_t n = f.along ? (i < rows ? k1 - k : 0) : (k < k1 ? rows - i : 0);
     n = n < 0 ? 0 : n > 8 ? 8 : n;
-    const T *q = p + (f.along ? i * f.ld + k : k * f.ld + i);
+    const float *q = p + (f.along ? i * f.ld + k : k * f.ld + i);
 #pragma unroll
-    for (int e = 0; e < 8; e += VE) unpack<T>(load_piece(q + e, (int)n - e), v + e);
+    for (int e = 0; e < 8; e += VE) unpack<float>(load_piece(q + e, (int)n - e), v + e);
 }
 
 __device__ __forceinline__ void put(const Factor &f, float *tile, const float (&v)[8])
@@ -38,9 +37,8 @@ __device__ __forceinline__ void put(const Factor &f, float *tile, const float (&
     }
 }
 
-// C = A B^T by 128 x 128 tiles, four waves with 64 x 64 each, on the single-precision matrix instruction, 16 k at a time
+// Single-precision factors: C = A B^T by 128 x 128 tiles, four waves with 64 x 64 each, on the single-precision matrix instruction, 16 k at a time
 // through LDS.  Sums of 256 k are closed and added to a second set, so that roundings do not pile up along k.
-template <class T>
 __global__ __launch_bounds__(256) void fb_product_kernel(Product q)
 {
     __shared__ float ta[kDeep * kTileLd], tb[kDeep * kTileLd];
@@ -50,8 +48,8 @@ __global__ __launch_bounds__(256) void fb_product_kernel(Product q)
     const int wi = (wave & 1) * 64, wj = (wave >> 1) * 64, l = lane & 31, h = lane >> 5;
     f32x16 acc[2][2] = {}, sum[2][2] = {};
     float va[8], vb[8];
-    fetch<T>(q.A, i0, q.M, k0, k1, va);
-    fetch<T>(q.B, j0, q.N, k0, k1, vb);
+    fetch(q.A, i0, q.M, k0, k1, va);
+    fetch(q.B, j0, q.N, k0, k1, vb);
     int since = 0;
     for (int64_t k = k0; k < k1; k += kDeep) {
         __syncthreads();
@@ -59,8 +57,8 @@ __global__ __launch_bounds__(256) void fb_product_kernel(Product q)
         put(q.B, tb, vb);
         __syncthreads();
         if (k + kDeep < k1) {
-            fetch<T>(q.A, i0, q.M, k + kDeep, k1, va);
-            fetch<T>(q.B, j0, q.N, k + kDeep, k1, vb);
+            fetch(q.A, i0, q.M, k + kDeep, k1, va);
+            fetch(q.B, j0, q.N, k + kDeep, k1, vb);
         }
 #pragma unroll
         for (int d = 0; d < kDeep; d += 2) {
@@ -99,7 +97,7 @@ __global__ __launch_bounds__(256) void fb_product_kernel(Product q)
                     if (q.split > 1)
                         q.part[((size_t)blockIdx.z * q.M + i) * q.N + j] = c[e];
                     else
-                        finish_one<T>(q.f, i, j, c[e]);
+                        finish_one<float>(q.f, i, j, c[e]);
                 }
             }
         }
@@ -125,7 +123,7 @@ struct SlopeParams {
     float *part;         // [gridDim.y][N]: shares of the sums over rows, nullable
 };
 
-// dz = dy act'(z), rounded to the factors' type, and the sums of its columns before the rounding.  A thread has one piece of
+// dz = dy act'(z) (or a copy of dy in rows of whole pieces), rounded to the factors' type, and the sums of its columns before the rounding.  A thread has one piece of
 // the width and every fourth of a workgroup's rows.
 template <class T, class D>
 __global__ __launch_bounds__(256) void fb_slope_kernel(SlopeParams p)
@@ -149,7 +147,7 @@ __global__ __launch_bounds__(256) void fb_slope_kernel(SlopeParams p)
             }
 #pragma unroll
             for (int e = 0; e < VE; ++e) sum[e] += g[e];
-            if (p.out) store_piece((T *)p.out + r * p.ldo + at, n, pack<T>(g));
+            if (p.out) store_piece((T *)p.out + r * p.ldo + at, sizeof(T) == 2 ? VE : n, pack<T>(g));   // (16 bits: rows of whole pieces)
         }
     }
     if (!p.part) return;
@@ -169,72 +167,64 @@ int64_t slope_groups(int64_t M) { return std::max<int64_t>(1, std::min<int64_t>(
 
 size_t aligned(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Shares of k: as many as fill the GPU with tiles, of at least 256 k each.
-void plan_split(Product &q)
+// Tiles and shares of k, by estimated time in units of a compute unit's work on one k of a 256 x 256 tile: rounds of
+// workgroups (one 256 or two 128 tiles a compute unit at a time, the latter at kSmallCost of the former's time per product),
+// a start and end of kEnds a workgroup, and, where k is shared, the sums' way through memory and a launch to join them.
+constexpr double kSmallCost = 1.25, kEnds = 400.0, kJoinPerSum = 2.0e-4, kJoinLaunch = 300.0;
+
+void plan(Product &q)
 {
-    const int64_t tiles = ((q.M + kTile - 1) / kTile) * ((q.N + kTile - 1) / kTile);
-    int64_t split = std::min<int64_t>(2 * kCUs / std::max<int64_t>(tiles, 1), (q.K + 255) / 256);
-    split = std::max<int64_t>(1, std::min<int64_t>(split, 64));
-    q.share = std::max<int64_t>(kDeep, ((q.K + split - 1) / split + kDeep - 1) / kDeep * kDeep);
-    q.split = (int)std::max<int64_t>(1, (q.K + q.share - 1) / q.share);   // (K = 0, a gradient over no rows: sums of nothing)
+    if (q.type == FB_TYPE_F32) {            // as many shares as fill the GPU with tiles, of at least 256 k each
+        const int64_t tiles = ((q.M + kTile - 1) / kTile) * ((q.N + kTile - 1) / kTile);
+        int64_t split = std::min<int64_t>(2 * kCUs / std::max<int64_t>(tiles, 1), (q.K + 255) / 256);
+        split = std::max<int64_t>(1, std::min<int64_t>(split, 64));
+        q.share = std::max<int64_t>(kDeep, ((q.K + split - 1) / split + kDeep - 1) / kDeep * kDeep);
+        q.split = (int)std::max<int64_t>(1, (q.K + q.share - 1) / q.share);   // (K = 0, a gradient over no rows: sums of nothing)
+        return;
+    }
+    double best = 0.0;
+    for (int tile = 128; tile <= 256; tile += 128) {
+        const int64_t tiles = ((q.M + tile - 1) / tile) * ((q.N + tile - 1) / tile), slots = tile == 256 ? kCUs : 2 * kCUs;
+        for (int64_t split = 1; split <= 32; ++split) {
+            const int64_t share = std::max<int64_t>(64, ((q.K + split - 1) / split + 63) / 64 * 64);
+            if (split > 1 && (split - 1) * share >= q.K) break;
+            const double rounds = (double)((tiles * split + slots - 1) / slots);
+            double cost = rounds * ((double)share * (tile == 256 ? 1.0 : kSmallCost / 2) + kEnds);
+            if (split > 1) cost += kJoinLaunch + kJoinPerSum * (double)(split + 1) * (double)q.M * (double)q.N / 16.0;
+            if (best == 0.0 || cost < best) {
+                best = cost;
+                q.tile = tile;
+                q.share = share;
+                q.split = (int)split;
+            }
+        }
+    }
 }
 
 size_t product_bytes(const Product &q) { return q.split > 1 ? aligned((size_t)q.split * (size_t)q.M * (size_t)q.N * sizeof(float)) : 0; }
 
 template <class T>
-int launch_product(const Product &q, hipStream_t stream)
+int launch_join(const Product &q, hipStream_t stream)
 {
-    const int64_t ti = (q.M + kTile - 1) / kTile, tj = (q.N + kTile - 1) / kTile;
-    hipLaunchKernelGGL(fb_product_kernel<T>, dim3((unsigned)tj, (unsigned)ti, (unsigned)q.split), dim3(256), 0, stream, q);
-    int rc = launched("product kernel launch: ");
-    if (rc == FB_OK && q.split > 1) {
-        const int64_t groups = std::min<int64_t>((q.M * q.N + 255) / 256, 8 * kCUs);
-        hipLaunchKernelGGL(fb_product_join_kernel<T>, dim3((unsigned)groups), dim3(256), 0, stream, q);
-        rc = launched("product join kernel launch: ");
-    }
-    return rc;
+    const int64_t groups = std::min<int64_t>((q.M * q.N + 255) / 256, 8 * kCUs);
+    hipLaunchKernelGGL(fb_product_join_kernel<T>, dim3((unsigned)groups), dim3(256), 0, stream, q);
+    return launched("product join kernel launch: ");
 }
 
 int launch_product(const Product &q, hipStream_t stream)
 {
     if (q.M == 0) return FB_OK;
-    if (q.type == FB_TYPE_F32) return launch_product<float>(q, stream);
-    if (q.type == FB_TYPE_BF16) return launch_product<bf16>(q, stream);
-    return launch_product<f16>(q, stream);
-}
-
-bool bad_sizes(int64_t M, int64_t N, int64_t K) { return bad_rows(M) || bad_width(N) || bad_width(K); }
-
-Product forward_product(int64_t M, int64_t N, int64_t K, int type)
-{
-    Product q{};
-    q.M = M; q.N = N; q.K = K; q.type = type;
-    plan_split(q);
-    return q;
-}
-
-// The two products of the gradient.
-struct GradPlan {
-    Product dx, dw;
-    bool slope;           // dz has to be made
-    int64_t ldz;
-    size_t dz, sums, part, bytes;
-};
-
-GradPlan grad_plan(int64_t M, int64_t N, int64_t K, int type, int dy_type, int act)
-{
-    GradPlan g{};
-    g.dx.M = M; g.dx.N = K; g.dx.K = N; g.dx.type = type;
-    g.dw.M = N; g.dw.N = K; g.dw.K = M; g.dw.type = type;
-    plan_split(g.dx);
-    plan_split(g.dw);
-    g.slope = act != FB_ACT_NONE || dy_type != type;
-    g.ldz = (N + 7) & ~(int64_t)7;
-    g.dz = g.slope ? aligned((size_t)M * (size_t)g.ldz * type_bytes(type)) : 0;
-    g.sums = aligned((size_t)slope_groups(M) * (size_t)N * sizeof(float));
-    g.part = std::max(product_bytes(g.dx), product_bytes(g.dw));
-    g.bytes = g.dz + g.sums + g.part;
-    return g;
+    int rc;
+    if (q.type == FB_TYPE_F32) {
+        const int64_t ti = (q.M + kTile - 1) / kTile, tj = (q.N + kTile - 1) / kTile;
+        hipLaunchKernelGGL(fb_product_kernel, dim3((unsigned)tj, (unsigned)ti, (unsigned)q.split), dim3(256), 0, stream, q);
+        rc = launched("product kernel launch: ");
+    } else {
+        rc = launch_mfma_product(q, stream);
+    }
+    if (rc != FB_OK || q.split == 1) return rc;
+    if (q.type == FB_TYPE_F32) return launch_join<float>(q, stream);
+    return q.type == FB_TYPE_BF16 ? launch_join<bf16>(q, stream) : launch_join<f16>(q, stream);
 }
 
 template <class T, class D>
@@ -243,6 +233,85 @@ int launch_slope(const SlopeParams &p, int64_t groups, hipStream_t stream)
     const int64_t wide = 64 * Vec<T>::kN;
     hipLaunchKernelGGL((fb_slope_kernel<T, D>), dim3((unsigned)((p.N + wide - 1) / wide), (unsigned)groups), dim3(256), 0, stream, p);
     return launched("activation slope kernel launch: ");
+}
+
+int launch_slope(const SlopeParams &p, int type, int dy_type, hipStream_t stream)
+{
+    const int64_t groups = slope_groups(p.M);
+    if (type == FB_TYPE_F32) return launch_slope<float, float>(p, groups, stream);
+    if (type == FB_TYPE_BF16)
+        return dy_type == type ? launch_slope<bf16, bf16>(p, groups, stream) : launch_slope<bf16, float>(p, groups, stream);
+    return dy_type == type ? launch_slope<f16, f16>(p, groups, stream) : launch_slope<f16, float>(p, groups, stream);
+}
+
+// A 16-bit matrix that the matrix units' kernel cannot take as it is, copied to rows of whole pieces (padded with zeros).
+struct Packed {
+    bool copy;
+    int64_t ld;
+    size_t bytes;
+};
+
+Packed packed(const void *p, int64_t ld, int64_t rows, int64_t width, int type)
+{
+    Packed k{};
+    k.copy = type != FB_TYPE_F32 && !ready(p, ld, width);
+    k.ld = k.copy ? (width + 7) & ~(int64_t)7 : ld;
+    k.bytes = k.copy ? aligned((size_t)rows * (size_t)k.ld * 2) : 0;
+    return k;
+}
+
+int launch_pack(const Packed &k, const void *p, int64_t ld, int64_t rows, int64_t width, int type, void *to, hipStream_t stream)
+{
+    if (!k.copy || rows == 0) return FB_OK;
+    const SlopeParams s{p, nullptr, ld, 0, rows, width, k.ld, FB_ACT_NONE, to, nullptr};
+    return launch_slope(s, type, type, stream);
+}
+
+bool bad_sizes(int64_t M, int64_t N, int64_t K) { return bad_rows(M) || bad_width(N) || bad_width(K); }
+
+struct ForwardPlan {
+    Product q;
+    Packed x, w;
+    size_t bytes;
+};
+
+ForwardPlan forward_plan(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t N, int64_t K, int type)
+{
+    ForwardPlan f{};
+    f.q.M = M; f.q.N = N; f.q.K = K; f.q.type = type;
+    plan(f.q);
+    f.x = packed(x, ldx, M, K, type);
+    f.w = packed(weight, ldw, N, K, type);
+    f.bytes = f.x.bytes + f.w.bytes + product_bytes(f.q);
+    return f;
+}
+
+// The two products of the gradient.
+struct GradPlan {
+    Product dx, dw;
+    bool slope;           // dz has to be made, or dy laid out anew
+    int64_t ldz;
+    Packed x, w;
+    size_t dz, sums, part, bytes;
+};
+
+GradPlan grad_plan(const void *dy, int64_t lddy, int dy_type, const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t N,
+                   int64_t K, int type, int act)
+{
+    GradPlan g{};
+    g.dx.M = M; g.dx.N = K; g.dx.K = N; g.dx.type = type;
+    g.dw.M = N; g.dw.N = K; g.dw.K = M; g.dw.type = type;
+    plan(g.dx);
+    plan(g.dw);
+    g.slope = act != FB_ACT_NONE || dy_type != type || packed(dy, lddy, M, N, type).copy;
+    g.ldz = (N + 7) & ~(int64_t)7;
+    g.dz = g.slope ? aligned((size_t)M * (size_t)g.ldz * type_bytes(type)) : 0;
+    g.x = packed(x, ldx, M, K, type);
+    g.w = packed(weight, ldw, N, K, type);
+    g.sums = aligned((size_t)slope_groups(M) * (size_t)N * sizeof(float));
+    g.part = std::max(product_bytes(g.dx), product_bytes(g.dw));
+    g.bytes = g.dz + g.x.bytes + g.w.bytes + g.sums + g.part;
+    return g;
 }
 
 int check_affine(const char *who, const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t N, int64_t K, int type, int act)
@@ -262,12 +331,11 @@ int check_affine(const char *who, const void *x, int64_t ldx, const void *weight
 
 extern "C" {
 
-size_t fb_affine_workspace_bytes(int64_t M, int64_t N, int64_t K, int type, int64_t ldx, int64_t ldw)
+size_t fb_affine_workspace_bytes(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t N, int64_t K, int type)
 {
     using namespace fb;
-    (void)ldx; (void)ldw;
     if (bad_sizes(M, N, K) || !known_type(type)) return 0;
-    return product_bytes(forward_product(M, N, K, type));
+    return forward_plan(x, ldx, weight, ldw, M, N, K, type).bytes;
 }
 
 int fb_affine(const void *x, int64_t ldx, const void *weight, int64_t ldw, const float *bias, const void *residual, int64_t ldr,
@@ -276,27 +344,32 @@ int fb_affine(const void *x, int64_t ldx, const void *weight, int64_t ldw, const
 {
     using namespace fb;
     return guarded([&]() -> int {
-        const int rc = check_affine("fb_affine", x, ldx, weight, ldw, M, N, K, type, act);
+        int rc = check_affine("fb_affine", x, ldx, weight, ldw, M, N, K, type, act);
         if (rc != FB_OK) return rc;
         if (out_type != type && out_type != FB_TYPE_F32) return fail(FB_EINVAL, "fb_affine: the output's type is neither float nor the factors'");
         if (!y && M > 0) return fail(FB_EINVAL, "fb_affine: y is NULL");
         if (bad_ld(ldy, N) || (residual && bad_ld(ldr, N)) || (preact && bad_ld(ldp, N))) return fail(FB_EINVAL, "fb_affine: rows closer than N elements");
-        Product q = forward_product(M, N, K, type);
-        if (product_bytes(q) && (!ws || ws_bytes < product_bytes(q))) return fail(FB_EINVAL, "fb_affine: workspace missing or too small");
-        q.A = {x, ldx, true};
-        q.B = {weight, ldw, true};
+        const ForwardPlan f = forward_plan(x, ldx, weight, ldw, M, N, K, type);
+        if (f.bytes && (!ws || ws_bytes < f.bytes)) return fail(FB_EINVAL, "fb_affine: workspace missing or too small");
+        hipStream_t st = (hipStream_t)stream;
+        char *xs = (char *)ws, *wts = xs + f.x.bytes;
+        if ((rc = launch_pack(f.x, x, ldx, M, K, type, xs, st)) != FB_OK || (M > 0 && (rc = launch_pack(f.w, weight, ldw, N, K, type, wts, st)) != FB_OK))
+            return rc;
+        Product q = f.q;
+        q.A = {f.x.copy ? xs : x, f.x.ld, true};
+        q.B = {f.w.copy ? wts : weight, f.w.ld, true};
         q.f = {bias, residual, ldr, act, y, ldy, out_type, preact, ldp};
-        q.part = (float *)ws;
-        return launch_product(q, (hipStream_t)stream);
+        q.part = (float *)(wts + f.w.bytes);
+        return launch_product(q, st);
     });
 }
 
-size_t fb_affine_grad_workspace_bytes(int64_t M, int64_t N, int64_t K, int type, int dy_type, int act, int64_t lddy, int64_t ldx, int64_t ldw)
+size_t fb_affine_grad_workspace_bytes(const void *dy, int64_t lddy, int dy_type, const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M,
+                                      int64_t N, int64_t K, int type, int act)
 {
     using namespace fb;
-    (void)lddy; (void)ldx; (void)ldw;
     if (bad_sizes(M, N, K) || !known_type(type) || (dy_type != type && dy_type != FB_TYPE_F32) || act < FB_ACT_NONE || act > FB_ACT_SILU) return 0;
-    return grad_plan(M, N, K, type, dy_type, act).bytes;
+    return grad_plan(dy, lddy, dy_type, x, ldx, weight, ldw, M, N, K, type, act).bytes;
 }
 
 int fb_affine_grad(const void *dy, int64_t lddy, int dy_type, const void *x, int64_t ldx, const void *weight, int64_t ldw,
@@ -312,36 +385,30 @@ int fb_affine_grad(const void *dy, int64_t lddy, int dy_type, const void *x, int
         if (act != FB_ACT_NONE && !preact && M > 0) return fail(FB_EINVAL, "fb_affine_grad: this activation needs preact");
         if (bad_ld(lddy, N) || (act != FB_ACT_NONE && bad_ld(ldp, N)) || (dx && bad_ld(lddx, K))) return fail(FB_EINVAL, "fb_affine_grad: rows closer than their width");
         if (!dx && !dweight && !dbias) return FB_OK;
-        GradPlan g = grad_plan(M, N, K, type, dy_type, act);
+        GradPlan g = grad_plan(dy, lddy, dy_type, x, ldx, weight, ldw, M, N, K, type, act);
         if (!ws || ws_bytes < g.bytes) return fail(FB_EINVAL, "fb_affine_grad: workspace missing or too small");
         hipStream_t st = (hipStream_t)stream;
-        char *w = (char *)ws;
-        void *dz = w;
-        float *sums = (float *)(w + g.dz), *part = (float *)(w + g.dz + g.sums);
+        char *dz = (char *)ws, *xs = dz + g.dz, *wts = xs + g.x.bytes;
+        float *sums = (float *)(wts + g.w.bytes), *part = (float *)(wts + g.w.bytes + g.sums);
         const bool make = g.slope && (dx || dweight);
         if (M > 0 && (make || dbias)) {
-            SlopeParams p{dy, preact, lddy, ldp, M, N, g.ldz, act, make ? dz : nullptr, dbias ? sums : nullptr};
-            const int64_t groups = slope_groups(M);
-            if (type == FB_TYPE_F32)
-                rc = launch_slope<float, float>(p, groups, st);
-            else if (type == FB_TYPE_BF16)
-                rc = dy_type == type ? launch_slope<bf16, bf16>(p, groups, st) : launch_slope<bf16, float>(p, groups, st);
-            else
-                rc = dy_type == type ? launch_slope<f16, f16>(p, groups, st) : launch_slope<f16, float>(p, groups, st);
-            if (rc != FB_OK) return rc;
+            const SlopeParams p{dy, preact, lddy, ldp, M, N, g.ldz, act, make ? dz : nullptr, dbias ? sums : nullptr};
+            if ((rc = launch_slope(p, type, dy_type, st)) != FB_OK) return rc;
         }
         if (dbias && (rc = launch_column_sum(sums, M > 0 ? slope_groups(M) : 0, N, 1, dbias, nullptr, stream)) != FB_OK) return rc;
-        const Factor d{make ? dz : dy, make ? g.ldz : lddy, true};
+        const Factor d{make ? (const void *)dz : dy, make ? g.ldz : lddy, true};
         if (dx) {
+            if (M > 0 && (rc = launch_pack(g.w, weight, ldw, N, K, type, wts, st)) != FB_OK) return rc;
             g.dx.A = d;
-            g.dx.B = {weight, ldw, false};
+            g.dx.B = {g.w.copy ? wts : weight, g.w.ld, false};
             g.dx.f.y = dx; g.dx.f.ldy = lddx; g.dx.f.out_type = type;
             g.dx.part = part;
             if ((rc = launch_product(g.dx, st)) != FB_OK) return rc;
         }
         if (dweight) {
+            if ((rc = launch_pack(g.x, x, ldx, M, K, type, xs, st)) != FB_OK) return rc;
             g.dw.A = {d.p, d.ld, false};
-            g.dw.B = {x, ldx, false};
+            g.dw.B = {g.x.copy ? xs : x, g.x.ld, false};
             g.dw.f.y = dweight; g.dw.f.ldy = K; g.dw.f.out_type = type;
             g.dw.part = part;
             if ((rc = launch_product(g.dw, st)) != FB_OK) return rc;

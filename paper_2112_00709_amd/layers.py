@@ -37,9 +37,9 @@ def lib() -> ctypes.CDLL:
         L.fb_layer_norm.argtypes = [vp, i64, vp, vp, i32, i64, i64, i32, f32, vp, i64, vp, vp, vp]
         L.fb_layer_norm_grad_workspace_bytes.argtypes = [i64, i64]
         L.fb_layer_norm_grad.argtypes = [vp, i64, vp, i64, vp, vp, vp, i32, i64, i64, i32, vp, i64, vp, vp, vp, sz, vp]
-        L.fb_affine_workspace_bytes.argtypes = [i64, i64, i64, i32, i64, i64]
+        L.fb_affine_workspace_bytes.argtypes = [vp, i64, vp, i64, i64, i64, i64, i32]
         L.fb_affine.argtypes = [vp, i64, vp, i64, vp, vp, i64, i64, i64, i64, i32, i32, vp, i64, i32, vp, i64, vp, sz, vp]
-        L.fb_affine_grad_workspace_bytes.argtypes = [i64, i64, i64, i32, i32, i32, i64, i64, i64]
+        L.fb_affine_grad_workspace_bytes.argtypes = [vp, i64, i32, vp, i64, vp, i64, i64, i64, i64, i32, i32]
         L.fb_affine_grad.argtypes = [vp, i64, i32, vp, i64, vp, i64, vp, i64, i64, i64, i64, i32, i32, vp, i64, vp, vp, vp, sz, vp]
         L.fb_token_logprobs_workspace_bytes.argtypes = [i64, i64, i32, i32]
         L.fb_token_logprobs.argtypes = [vp, i64, vp, i64, i64, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]
@@ -195,7 +195,7 @@ def fb_affine(x, weight, bias=None, activation: str = "none", residual=None, out
         pr, ldr, _, _ = _rows(residual, "residual", N, out, lead)
     y = _new((*lead, N), out, x.device)
     z = _new((*lead, N), x.dtype, x.device) if want_preact else None
-    need = int(L.fb_affine_workspace_bytes(M, N, K, code, ldx, ldw))
+    need = int(L.fb_affine_workspace_bytes(px, ldx, pw, ldw, M, N, K, code))
     ws, pws = _workspace(need, x.device)
     _check(L.fb_affine(px, ldx, pw, ldw, pb, pr, ldr, M, N, K, code, act, y.data_ptr(), N, _types[out],
                        z.data_ptr() if want_preact else None, N, pws, need, _stream()))
@@ -228,7 +228,7 @@ def fb_affine_grad(dy, x, weight, activation: str = "none", preact=None, want_dx
     dw = _new((N, K), x.dtype, x.device) if want_dweight else None
     db = _new((N,), torch.float32, x.device) if want_dbias else None
     dtype = _types[dy.dtype]
-    need = int(L.fb_affine_grad_workspace_bytes(M, N, K, code, dtype, act, lddy, ldx, ldw))
+    need = int(L.fb_affine_grad_workspace_bytes(pdy, lddy, dtype, px, ldx, pw, ldw, M, N, K, code, act))
     ws, pws = _workspace(need, x.device)
     _check(L.fb_affine_grad(pdy, lddy, dtype, px, ldx, pw, ldw, pz, ldz, M, N, K, code, act, dx.data_ptr() if want_dx else None, K,
                             dw.data_ptr() if want_dweight else None, db.data_ptr() if want_dbias else None, pws, need, _stream()))

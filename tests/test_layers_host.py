@@ -70,8 +70,10 @@ def test_workspaces():
     assert L.fb_token_logprobs_workspace_bytes(4, 100, 0, 3) == 0                    # one launch, nothing kept
     assert L.fb_token_logprobs_workspace_bytes(1, 1 << 17, 1, 3) > 0
     assert L.fb_token_logprobs_workspace_bytes(1, 1 << 17, 1, 65) == 0
-    assert L.fb_affine_grad_workspace_bytes(10, 10, 10, 1, 2, 0, 10, 10, 10) == 0    # dy of another 16-bit type
-    assert L.fb_affine_grad_workspace_bytes(10, 10, 10, 1, 0, 0, 10, 10, 10) > 0
+    assert L.fb_affine_grad_workspace_bytes(_one(), 10, 2, _one(), 10, _one(), 10, 10, 10, 10, 1, 0) == 0    # dy of another 16-bit type
+    assert L.fb_affine_grad_workspace_bytes(_one(), 10, 0, _one(), 10, _one(), 10, 10, 10, 10, 1, 0) > 0
+    assert L.fb_affine_workspace_bytes(_one(), 64, _one(), 64, 999, 64, 64, 1) == 0       # whole pieces, one share of k
+    assert L.fb_affine_workspace_bytes(_one(), 65, _one(), 64, 999, 64, 64, 1) >= 999 * 128
 
 
 def test_no_rows_is_no_work():
