@@ -10,13 +10,6 @@
 // different quarters of the banks.  The copies write LDS in order of lanes, so the exchange is in the address a lane reads.
 #include "fb_affine.h"
 
-#ifndef FB_WI
-#define FB_WI 2
-#define FB_WJ 4
-#define FB_FI 4
-#define FB_FJ 2
-#endif
-
 namespace fb {
 
 namespace {
@@ -62,12 +55,11 @@ struct Side {
     uint32_t at[ALONG ? 4 : 2];
     int chunk;               // ALONG: a lane's piece along k
 
-    __device__ __forceinline__ void start(const Factor &f, int64_t r0, int64_t n, int64_t k0, uint32_t lds_at, int wave, int w0)
+    // What does not depend on the tile.
+    __device__ __forceinline__ void start(const Factor &f, uint32_t lds_at, int wave, int w0)
     {
         const int lane = threadIdx.x & 63;
         ld2 = (uint32_t)f.ld * 2;
-        rows = (int)(n - r0 < ROWS ? n - r0 : ROWS);
-        base = (uint64_t)(uintptr_t)f.p + (uint64_t)(ALONG ? r0 * f.ld + k0 : k0 * f.ld + r0) * 2;
         lds = lds_at;
         const int l = lane & 31, h = lane >> 5;
         if constexpr (ALONG) {
@@ -87,6 +79,12 @@ struct Side {
             for (int odd = 0; odd < 2; ++odd)
                 at[odd] = lds + ((g >> 1) * 8 + kq) * (ROWS * 2) + w0 * 2 + (((c + odd * 4) ^ (kq << 1)) * 16) + (lane & 1) * 8;
         }
+    }
+
+    __device__ __forceinline__ void tile(const Factor &f, int64_t r0, int64_t n, int64_t k0)
+    {
+        rows = (int)(n - r0 < ROWS ? n - r0 : ROWS);
+        base = (uint64_t)(uintptr_t)f.p + (uint64_t)(ALONG ? r0 * f.ld + k0 : k0 * f.ld + r0) * 2;
     }
 
     // The factor's share of the next 64 of `left` k, into buffer `b`.
@@ -125,54 +123,184 @@ struct Side {
     }
 };
 
-// Four neighbouring sums of a row finished and stored; n of them exist.
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+
 template <class T>
-__device__ __forceinline__ void finish_four(const Finish &f, int64_t i, int64_t j, int n, const f32x4 &sums, const f32x4 &bias)
+__device__ __forceinline__ f32x4 load_four(const T *p)
 {
-    float s[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) s[e] = sums[e] + bias[e];
-    auto put = [&](T *to) {
-        const u32x2 v = {pack2<T>(s[0], s[1]), pack2<T>(s[2], s[3])};
-        if (n == 4) {
-            typedef u32x2 u32x2_any __attribute__((aligned(2)));
-            *(u32x2_any *)to = v;
-        } else {
-#pragma unroll
-            for (int e = 0; e < 3; ++e)
-                if (e < n) to[e] = (T)s[e];
-        }
-    };
-    if (f.preact) put((T *)f.preact + i * f.ldp + j);
-    if (f.act != FB_ACT_NONE) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[e] = act_of(s[e], f.act);
-    }
-    if (f.out_type == FB_TYPE_F32) {
-        typedef f32x4 f32x4_any __attribute__((aligned(4)));
-        float *to = (float *)f.y + i * f.ldy + j;
-        const float *from = (const float *)f.residual + i * f.ldr + j;
-        if (n == 4) {
-            f32x4 v = {s[0], s[1], s[2], s[3]};
-            if (f.residual) v += *(const f32x4_any *)from;
-            *(f32x4_any *)to = v;
-        } else {
-#pragma unroll
-            for (int e = 0; e < 3; ++e)
-                if (e < n) to[e] = s[e] + (f.residual ? from[e] : 0.0f);
-        }
+    if constexpr (sizeof(T) == 4) {
+        return *(const f32x4_any *)p;
     } else {
-        if (f.residual) {
-            const T *from = (const T *)f.residual + i * f.ldr + j;
+        const u32x2 r = *(const u32x2_any *)p;
+        float v[8];
+        unpack<T>(u32x4{r[0], r[1], 0, 0}, v);
+        return f32x4{v[0], v[1], v[2], v[3]};
+    }
+}
+template <class T>
+__device__ __forceinline__ void store_four(T *p, const f32x4 &v)
+{
+    if constexpr (sizeof(T) == 4)
+        *(f32x4_any *)p = v;
+    else
+        *(u32x2_any *)p = u32x2{pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3])};
+}
+
+// R times four neighbouring sums, `step` rows apart: those of a lane's row `row`, row + step, .. below `rows`, n of the four
+// below N (1 .. 4).  The first of the tile's rows is at i, its first column at j, the lane's own `col` further: addresses are
+// a wave's 64-bit base and a lane's 32-bit offset.  Each thing that may have to be done is asked for once for all R.
+struct Spot {
+    int64_t i, j;
+    int row, col, rows, n;
+};
+
+template <class T, class O, int R, int STEP>
+__device__ __forceinline__ void store_rows(O *p, int64_t ld, const Spot &at, const f32x4 (&w)[R])
+{
+    O *base = p + at.i * ld + at.j;
+    const uint32_t off = (uint32_t)at.row * (uint32_t)ld + (uint32_t)at.col;
+    if (at.n == 4) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (e < n) s[e] += (float)from[e];
+        for (int r = 0; r < R; ++r, base += STEP * ld)
+            if (at.row + r * STEP < at.rows) store_four(base + off, w[r]);
+    } else {
+#pragma unroll 1
+        for (int e = 0; e < at.n; ++e) {
+            O *q = base + e;
+#pragma unroll
+            for (int r = 0; r < R; ++r, q += STEP * ld)
+                if (at.row + r * STEP < at.rows) q[off] = (O)(e == 0 ? w[r][0] : e == 1 ? w[r][1] : w[r][2]);
         }
-        put((T *)f.y + i * f.ldy + j);
+    }
+}
+// What the residual has at the same places, as it is stored.  (A lane at the right edge, n < 4, takes its few elements later.)
+template <class T, int R, int STEP>
+__device__ __forceinline__ void ask_rows(const void *p, int type, int64_t ld, const Spot &at, u32x4 (&raw)[R])
+{
+    const uint32_t off = (uint32_t)at.row * (uint32_t)ld + (uint32_t)at.col;
+    if (type == FB_TYPE_F32) {
+        const float *base = (const float *)p + at.i * ld + at.j;
+#pragma unroll
+        for (int r = 0; r < R; ++r, base += STEP * ld)
+            if (at.row + r * STEP < at.rows && at.n == 4) raw[r] = __builtin_bit_cast(u32x4, (f32x4) * (const f32x4_any *)(base + off));
+    } else {
+        const T *base = (const T *)p + at.i * ld + at.j;
+#pragma unroll
+        for (int r = 0; r < R; ++r, base += STEP * ld)
+            if (at.row + r * STEP < at.rows && at.n == 4) {
+                const u32x2 v = *(const u32x2_any *)(base + off);
+                raw[r][0] = v[0];
+                raw[r][1] = v[1];
+            }
+    }
+}
+template <class O, int R, int STEP>
+__device__ __forceinline__ void add_edge(const O *p, int64_t ld, const Spot &at, f32x4 (&w)[R])
+{
+    const O *base = p + at.i * ld + at.j;
+    const uint32_t off = (uint32_t)at.row * (uint32_t)ld + (uint32_t)at.col;
+#pragma unroll
+    for (int r = 0; r < R; ++r, base += STEP * ld)
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (at.row + r * STEP < at.rows && e < at.n) w[r][e] += (float)base[off + e];
+}
+template <class T, int R, int STEP>
+__device__ __forceinline__ void add_rows(const void *p, int type, int64_t ld, const Spot &at, const u32x4 (&raw)[R], f32x4 (&w)[R])
+{
+    if (at.n < 4) {
+        if (type == FB_TYPE_F32)
+            add_edge<float, R, STEP>((const float *)p, ld, at, w);
+        else
+            add_edge<T, R, STEP>((const T *)p, ld, at, w);
+    } else if (type == FB_TYPE_F32) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) w[r] += __builtin_bit_cast(f32x4, raw[r]);
+    } else {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float v[8];
+            unpack<T>(u32x4{raw[r][0], raw[r][1], 0, 0}, v);
+            w[r] += f32x4{v[0], v[1], v[2], v[3]};
+        }
     }
 }
 
-template <class T, bool ALONG_A, bool ALONG_B, int WI, int WJ, int FI, int FJ>
+// How sums leave: as they are, with bias and perhaps max(z, 0); or with any of activation (one an instantiation), residual, preact.
+constexpr int kPlain = -1;
+
+// The sums of a wave's part of a tile finished and stored.  They pass through LDS, 16 rows of C at a time and each wave in a
+// region of its own, so that whole runs of a row are stored: a lane's own are 4 neighbours, 8 apart in every 32 columns, of
+// one row in 32.  Piece c of a row lies at c ^ row, as eight lanes that write or read at once are to cover all banks.
+template <class T, int FI, int FJ, int KIND, class Between>
+__device__ __forceinline__ void leave(const f32x16 (&acc)[FI][FJ], const f32x4 &bias, int share, int64_t i0, int64_t j0, float *mine, Between between)
+{
+    // What is needed here alone is fetched and computed here: kept over the loops before it costs registers that they need.
+    const __attribute__((address_space(4))) Product *args = (const __attribute__((address_space(4))) Product *)__builtin_amdgcn_kernarg_segment_ptr();
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+s"(args), "+v"(lane));
+    constexpr int kPer = FJ * 8, kRows = 64 / kPer, kR = 16 / kRows;
+    const int64_t M = args->M, N = args->N, j = j0 + (lane % kPer) * 4;
+    const int nj = (int)(N - j < 4 ? (N - j < 0 ? 0 : N - j) : 4), in_row = lane / kPer;
+    const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)mine + (lane & 15) * FJ * 128;
+    const bool split = KIND == kPlain && args->split > 1, relu = KIND == FB_ACT_RELU || (KIND == kPlain && !split && args->f.act == FB_ACT_RELU);
+    const int out_type = split ? FB_TYPE_F32 : args->f.out_type;
+    const int64_t ld = split ? N : args->f.ldy;
+    void *y = split ? (void *)(args->part + (size_t)share * M * N) : args->f.y;
+    const void *residual = KIND == kPlain ? nullptr : args->f.residual;
+    auto spot = [&](int pass) {
+        const int64_t i = i0 + pass * 16;
+        return Spot{i, j0, in_row, (lane % kPer) * 4, (int)(M - i < 16 ? M - i : 16), nj};
+    };
+    u32x4 raw[2][kR] = {};
+    if (residual) ask_rows<T, kR, kRows>(residual, out_type, args->f.ldr, spot(0), raw[0]);
+    between();
+#pragma unroll
+    for (int pass = 0; pass < 2 * FI; ++pass) {
+        if ((lane >> 4 & 1) == (pass & 1)) {
+#pragma unroll
+            for (int y = 0; y < FJ; ++y)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const f32x16 &sums = acc[pass / 2][y];
+                    const f32x4 w = {sums[4 * e], sums[4 * e + 1], sums[4 * e + 2], sums[4 * e + 3]};
+                    const int c = (y * 8 + 2 * e + (lane >> 5)) ^ (lane & 15 & (kPer - 1));
+                    *(__attribute__((address_space(3))) f32x4 *)(uintptr_t)(to + c * 16) = w;
+                }
+        }
+        if (residual && pass + 1 < 2 * FI) ask_rows<T, kR, kRows>(residual, out_type, args->f.ldr, spot(pass + 1), raw[(pass + 1) & 1]);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        f32x4 w[kR];
+#pragma unroll
+        for (int r = 0; r < kR; ++r) {
+            const int row = r * kRows + in_row;
+            w[r] = *(const f32x4 *)(mine + row * FJ * 32 + ((lane % kPer) ^ (row & (kPer - 1))) * 4);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const Spot at = spot(pass);
+        if (at.rows > in_row && nj > 0) {
+#pragma unroll
+            for (int r = 0; r < kR; ++r) w[r] += bias;
+            if (KIND != kPlain && args->f.preact) store_rows<T, T, kR, kRows>((T *)args->f.preact, args->f.ldp, at, w);
+            constexpr int kAct = KIND == kPlain ? FB_ACT_RELU : KIND;
+            if (KIND != kPlain || relu) {
+#pragma unroll
+                for (int r = 0; r < kR; ++r)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[r][e] = act_of(w[r][e], kAct);
+            }
+            if (residual) add_rows<T, kR, kRows>(residual, out_type, args->f.ldr, at, raw[pass & 1], w);
+            if (out_type == FB_TYPE_F32)
+                store_rows<T, float, kR, kRows>((float *)y, ld, at, w);
+            else
+                store_rows<T, T, kR, kRows>((T *)y, ld, at, w);
+        }
+    }
+}
+
+// Workgroups stay and take tile after tile, so that the copies for the next tile are under way while this one's sums leave.
+template <class T, bool ALONG_A, bool ALONG_B, int WI, int WJ, int FI, int FJ, int KIND>
 __global__ __launch_bounds__(WI * WJ * 64) void fb_mfma_product_kernel(Product q, int tiles_i, int tiles_j)
 {
     constexpr int kI = WI * FI * 32, kJ = WJ * FJ * 32, kNW = WI * WJ;
@@ -181,29 +309,38 @@ __global__ __launch_bounds__(WI * WJ * 64) void fb_mfma_product_kernel(Product q
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wi = wave / WJ, wj = wave % WJ;
 
-    // Workgroups go to the eight chiplets in turn: each chiplet gets a run of neighbouring tiles, so that its L2 holds what
+    // Workgroups go to the eight chiplets in turn: each chiplet has a run of neighbouring tiles, so that its L2 holds what
     // they share; within a run eight tiles down, then one across.
-    const int n = tiles_i * tiles_j * q.split, xcd = blockIdx.x % 8, in_xcd = blockIdx.x / 8;
-    const int t = xcd * (n / 8) + (xcd < n % 8 ? xcd : n % 8) + in_xcd;
-    const int share = t / (tiles_i * tiles_j), u = t - share * tiles_i * tiles_j;
-    const int group = u / (8 * tiles_j), first = group * 8, down = tiles_i - first < 8 ? tiles_i - first : 8;
-    const int v = u - group * 8 * tiles_j;
-    const int64_t i0 = (int64_t)(first + v % down) * kI, j0 = (int64_t)(v / down) * kJ;
-    const int64_t k0 = (int64_t)share * q.share, k1 = k0 + q.share < q.K ? k0 + q.share : q.K;
-    const int steps = (int)((k1 - k0 + kDeep - 1) / kDeep);
+    const int n = tiles_i * tiles_j * q.split, xcd = blockIdx.x % 8, run = n / 8 + (xcd < n % 8 ? 1 : 0);
+    const int run0 = xcd * (n / 8) + (xcd < n % 8 ? xcd : n % 8);
+    struct Place {
+        int share;
+        int64_t i0, j0, length;
+    };
+    auto place = [&](int in_run) {
+        const int t = run0 + in_run, share = t / (tiles_i * tiles_j), u = t - share * tiles_i * tiles_j;
+        const int group = u / (8 * tiles_j), first = group * 8, down = tiles_i - first < 8 ? tiles_i - first : 8;
+        const int v = u - group * 8 * tiles_j;
+        const int64_t k0 = (int64_t)share * q.share;
+        return Place{share, (int64_t)(first + v % down) * kI, (int64_t)(v / down) * kJ, k0 + q.share < q.K ? q.share : q.K - k0};
+    };
 
     Side<ALONG_A, kI, kNW, FI> a;
     Side<ALONG_B, kJ, kNW, FJ> b;
-    a.start(q.A, i0, q.M, k0, lds0, wave, wi * FI * 32);
-    b.start(q.B, j0, q.N, k0, lds0 + 2 * a.kBytes, wave, wj * FJ * 32);
-
-    f32x16 acc[FI][FJ] = {};
-    u32x4 fa[2][FI], fb_[2][FJ];
-    auto bring = [&](int step) {
-        const int64_t left = k1 - k0 - (int64_t)step * kDeep;
-        a.copy(left, step & 1, wave);
-        b.copy(left, step & 1, wave);
+    a.start(q.A, lds0, wave, wi * FI * 32);
+    b.start(q.B, lds0 + 2 * a.kBytes, wave, wj * FJ * 32);
+    auto begin = [&](const Place &p) {
+        a.tile(q.A, p.i0, q.M, (int64_t)p.share * q.share);
+        b.tile(q.B, p.j0, q.N, (int64_t)p.share * q.share);
     };
+    auto bring = [&](const Place &p, int step) {
+        const int64_t left = p.length - (int64_t)step * kDeep;
+        if (left > 0) {
+            a.copy(left, step & 1, wave);
+            b.copy(left, step & 1, wave);
+        }
+    };
+    u32x4 fa[2][FI], fb_[2][FJ];
     auto read = [&](int buffer, int s, int set) {
 #pragma unroll
         for (int f = 0; f < FI; ++f) fa[set][f] = a.read(buffer, s, f);
@@ -212,108 +349,95 @@ __global__ __launch_bounds__(WI * WJ * 64) void fb_mfma_product_kernel(Product q
     };
     // What has been asked for has come, in every wave; and every wave has read what it wanted of the other buffer.
     auto meet = [&]() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
-    if (steps > 0) {
-        bring(0);
-        meet();
-        if (steps > 1) bring(1);
-        read(0, 0, 0);
-    }
-    for (int step = 0; step < steps; ++step) {
-        const int cur = step & 1;
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            if (s < 3) {
-                read(cur, s + 1, (s + 1) & 1);
-            } else if (step + 1 < steps) {
-                meet();
-                if (step + 2 < steps) bring(step + 2);
-                read(cur ^ 1, 0, 0);
-            }
-#pragma unroll
-            for (int x = 0; x < FI; ++x)
-#pragma unroll
-                for (int y = 0; y < FJ; ++y) acc[x][y] = multiply<T>(fb_[s & 1][y], fa[s & 1][x], acc[x][y]);
-        }
-    }
 
-    // The sums pass through LDS, 32 rows of C at a time and each wave in a region of its own, so that whole runs of a row are
-    // stored: a lane's own are 4 neighbours of 4 rows 8 apart in every 32 columns.
-    constexpr int kLd = FJ * 32 + 4, kPer = FJ * 8, kRows = 64 / kPer;
-    __syncthreads();
-    float *mine = (float *)lds_raw + wave * 32 * kLd;
-    const int64_t j = j0 + wj * FJ * 32 + (lane % kPer) * 4;
-    const int nj = (int)(q.N - j < 4 ? (q.N - j < 0 ? 0 : q.N - j) : 4);
-    f32x4 bias = {};
-    if (q.split == 1 && q.f.bias) {
+    int in_run = blockIdx.x / 8;
+    if (in_run >= run) return;
+    Place p = place(in_run);
+    begin(p);
+    bring(p, 0);
+    for (;;) {
+        const int steps = (int)((p.length + kDeep - 1) / kDeep);
+        f32x16 acc[FI][FJ] = {};
+        f32x4 bias = {};
+        if (q.split == 1 && q.f.bias) {
+            const int64_t j = p.j0 + wj * FJ * 32 + lane % (FJ * 8) * 4;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < nj) bias[e] = q.f.bias[j + e];
-    }
+            for (int e = 0; e < 4; ++e)
+                if (j + e < q.N) bias[e] = q.f.bias[j + e];
+        }
+        if (steps > 0) {
+            meet();
+            asm volatile("" : "+v"(bias));   // (it has come with the rest: no wait for it later, behind the next tile's copies)
+            bring(p, 1);
+            read(0, 0, 0);
+        }
+        for (int step = 0; step < steps; ++step) {
+            const int cur = step & 1;
 #pragma unroll
-    for (int x = 0; x < FI; ++x) {
-#pragma unroll
-        for (int y = 0; y < FJ; ++y)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const f32x4 w = {acc[x][y][4 * e], acc[x][y][4 * e + 1], acc[x][y][4 * e + 2], acc[x][y][4 * e + 3]};
-                *(f32x4 *)(mine + (lane & 31) * kLd + y * 32 + 8 * e + 4 * (lane >> 5)) = w;
-            }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll 4
-        for (int r = 0; r < 32; r += kRows) {
-            const int row = r + lane / kPer;
-            const f32x4 w = *(const f32x4 *)(mine + row * kLd + (lane % kPer) * 4);
-            const int64_t i = i0 + wi * FI * 32 + x * 32 + row;
-            if (i < q.M && nj > 0) {
-                if (q.split > 1) {
-                    typedef f32x4 f32x4_any __attribute__((aligned(4)));
-                    float *to = q.part + ((size_t)share * q.M + i) * q.N + j;
-                    if (nj == 4) {
-                        *(f32x4_any *)to = w;
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 3; ++e)
-                            if (e < nj) to[e] = w[e];
-                    }
-                } else {
-                    finish_four<T>(q.f, i, j, nj, w, bias);
+            for (int s = 0; s < 4; ++s) {
+                if (s < 3) {
+                    read(cur, s + 1, (s + 1) & 1);
+                } else if (step + 1 < steps) {
+                    meet();
+                    bring(p, step + 2);
+                    read(cur ^ 1, 0, 0);
                 }
+#pragma unroll
+                for (int x = 0; x < FI; ++x)
+#pragma unroll
+                    for (int y = 0; y < FJ; ++y) acc[x][y] = multiply<T>(fb_[s & 1][y], fa[s & 1][x], acc[x][y]);
             }
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const Place done = p;
+        in_run += gridDim.x / 8;
+        const bool more = in_run < run;
+        leave<T, FI, FJ, KIND>(acc, bias, done.share, done.i0 + wi * FI * 32, done.j0 + wj * FJ * 32,
+                               (float *)(lds_raw + 2 * (a.kBytes + b.kBytes)) + wave * 16 * FJ * 32, [&]() {
+                                   if (!more) return;
+                                   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // (no wave reads the buffers any longer)
+                                   p = place(in_run);
+                                   begin(p);
+                                   bring(p, 0);
+                               });
+        if (!more) return;
     }
 }
 
-template <class T, bool ALONG_A, bool ALONG_B, int WI, int WJ, int FI, int FJ>
+template <class T, bool ALONG_A, bool ALONG_B, int WI, int WJ, int FI, int FJ, int KIND>
 int launch(const Product &q, hipStream_t stream)
 {
     constexpr int kI = WI * FI * 32, kJ = WJ * FJ * 32;
     const int64_t ti = (q.M + kI - 1) / kI, tj = (q.N + kJ - 1) / kJ;
     if (ti * tj * q.split >= kMostSize) return fail(FB_EUNSUPPORTED, "affine product: more than 2^31 tiles");
-    constexpr size_t copies = (size_t)2 * (kI + kJ) * kDeep * 2, sums = (size_t)WI * WJ * 32 * (FJ * 32 + 4) * 4;
-    constexpr size_t bytes = copies > sums ? copies : sums;
-    const void *k = (const void *)fb_mfma_product_kernel<T, ALONG_A, ALONG_B, WI, WJ, FI, FJ>;
+    constexpr size_t bytes = (size_t)2 * (kI + kJ) * kDeep * 2 + (size_t)WI * WJ * 16 * FJ * 32 * 4;
+    constexpr int64_t slots = (int64_t)kCUs * (int64_t)(kLdsBytes / bytes);      // workgroups that the GPU holds
+    const auto kernel = fb_mfma_product_kernel<T, ALONG_A, ALONG_B, WI, WJ, FI, FJ, KIND>;
     if (bytes > 64 * 1024) {
-        const hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
         if (e != hipSuccess) return fail(FB_EHIP, std::string("hipFuncSetAttribute(LDS size): ") + hipGetErrorString(e));
     }
-    hipLaunchKernelGGL((fb_mfma_product_kernel<T, ALONG_A, ALONG_B, WI, WJ, FI, FJ>), dim3((unsigned)(ti * tj * q.split)), dim3(WI * WJ * 64), bytes,
-                       stream, q, (int)ti, (int)tj);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(slots, (ti * tj * q.split + 7) / 8 * 8)), dim3(WI * WJ * 64), bytes, stream, q, (int)ti, (int)tj);
     return launched("matrix product kernel launch: ");
 }
 
-template <class T, bool ALONG_A, bool ALONG_B>
+template <class T, bool ALONG_A, bool ALONG_B, int KIND>
 int launch(const Product &q, hipStream_t stream)
 {
-    return q.tile == 256 ? launch<T, ALONG_A, ALONG_B, FB_WI, FB_WJ, FB_FI, FB_FJ>(q, stream) : launch<T, ALONG_A, ALONG_B, 2, 2, 2, 2>(q, stream);
+    return q.tile == 256 ? launch<T, ALONG_A, ALONG_B, 2, 4, 4, 2, KIND>(q, stream) : launch<T, ALONG_A, ALONG_B, 2, 2, 2, 2, KIND>(q, stream);
 }
 
 template <class T>
 int launch(const Product &q, hipStream_t stream)
 {
-    if (q.A.along && q.B.along) return launch<T, true, true>(q, stream);
-    if (q.A.along) return launch<T, true, false>(q, stream);
-    return launch<T, false, false>(q, stream);
+    if (!q.A.along) return launch<T, false, false, kPlain>(q, stream);
+    if (!q.B.along) return launch<T, true, false, kPlain>(q, stream);
+    if (q.split > 1 || (q.f.act <= FB_ACT_RELU && !q.f.residual && !q.f.preact)) return launch<T, true, true, kPlain>(q, stream);
+    switch (q.f.act) {
+    case FB_ACT_NONE: return launch<T, true, true, FB_ACT_NONE>(q, stream);
+    case FB_ACT_RELU: return launch<T, true, true, FB_ACT_RELU>(q, stream);
+    case FB_ACT_GELU: return launch<T, true, true, FB_ACT_GELU>(q, stream);
+    default: return launch<T, true, true, FB_ACT_SILU>(q, stream);
+    }
 }
 
 }  // namespace
