@@ -87,11 +87,14 @@ struct Side {
         base = (uint64_t)(uintptr_t)f.p + (uint64_t)(ALONG ? r0 * f.ld + k0 : k0 * f.ld + r0) * 2;
     }
 
-    // The factor's share of the next 64 of `left` k, into buffer `b`.
-    __device__ __forceinline__ void copy(int64_t left, int b, int wave)
+    // The copies that bring the factor's share of the next 64 of `left` k into buffer `b`: where they read and write, then
+    // each of the wave's kCopies.
+    i32x4 buffer;
+    uint32_t past, to;
+    __device__ __forceinline__ void aim(int64_t left, int b, int wave)     // (left = 0: zeros, which nobody reads)
     {
-        i32x4 buffer;
-        uint32_t bytes, past = 0;
+        uint32_t bytes;
+        past = 0;
         if constexpr (ALONG) {
             bytes = (uint32_t)(rows - 1) * ld2 + (uint32_t)(left < kDeep ? (left + 7) & ~7 : kDeep) * 2;   // (whole pieces)
             past = chunk * 8 < left ? 0u : 0x80000000u;                // (`bytes` is below 2^31)
@@ -100,14 +103,15 @@ struct Side {
         }
         buffer[0] = __builtin_amdgcn_readfirstlane((int)(uint32_t)base);
         buffer[1] = __builtin_amdgcn_readfirstlane((int)(uint32_t)(base >> 32) & 0xffff);
-        buffer[2] = __builtin_amdgcn_readfirstlane((int)bytes);
+        buffer[2] = __builtin_amdgcn_readfirstlane(left > 0 ? (int)bytes : 0);
         buffer[3] = 0x00020000;
-        const uint32_t to = lds + b * kBytes + wave * kCopies * 1024;
-        constexpr int kStep = ALONG ? 8 : 64 / (ROWS / 8);
-#pragma unroll
-        for (int u = 0; u < kCopies; ++u)
-            copy_to_lds(__builtin_amdgcn_readfirstlane(to + u * 1024), from[u & 1] + (uint32_t)(u * kStep) * ld2 + past, buffer);
+        to = lds + b * kBytes + wave * kCopies * 1024;
         base += ALONG ? kDeep * 2 : (uint64_t)kDeep * ld2;
+    }
+    __device__ __forceinline__ void copy(int u) const
+    {
+        constexpr int kStep = ALONG ? 8 : 64 / (ROWS / 8);
+        copy_to_lds(__builtin_amdgcn_readfirstlane(to + u * 1024), from[u & 1] + (uint32_t)(u * kStep) * ld2 + past, buffer);
     }
 
     // Fragment f of step s (16 k) from buffer `b`: row lane % 32, k = 8 (lane / 32) + 0 .. 7.
@@ -233,8 +237,8 @@ constexpr int kPlain = -1;
 // The sums of a wave's part of a tile finished and stored.  They pass through LDS, 16 rows of C at a time and each wave in a
 // region of its own, so that whole runs of a row are stored: a lane's own are 4 neighbours, 8 apart in every 32 columns, of
 // one row in 32.  Piece c of a row lies at c ^ row, as eight lanes that write or read at once are to cover all banks.
-template <class T, int FI, int FJ, int KIND, class Between>
-__device__ __forceinline__ void leave(const f32x16 (&acc)[FI][FJ], const f32x4 &bias, int share, int64_t i0, int64_t j0, float *mine, Between between)
+template <class T, int FI, int FJ, int KIND>
+__device__ __forceinline__ void leave(const f32x16 (&acc)[FI][FJ], const f32x4 &bias, int share, int64_t i0, int64_t j0, float *mine)
 {
     // What is needed here alone is fetched and computed here: kept over the loops before it costs registers that they need.
     const __attribute__((address_space(4))) Product *args = (const __attribute__((address_space(4))) Product *)__builtin_amdgcn_kernarg_segment_ptr();
@@ -255,7 +259,6 @@ __device__ __forceinline__ void leave(const f32x16 (&acc)[FI][FJ], const f32x4 &
     };
     u32x4 raw[2][kR] = {};
     if (residual) ask_rows<T, kR, kRows>(residual, out_type, args->f.ldr, spot(0), raw[0]);
-    between();
 #pragma unroll
     for (int pass = 0; pass < 2 * FI; ++pass) {
         if ((lane >> 4 & 1) == (pass & 1)) {
@@ -329,33 +332,57 @@ __global__ __launch_bounds__(WI * WJ * 64) void fb_mfma_product_kernel(Product q
     Side<ALONG_B, kJ, kNW, FJ> b;
     a.start(q.A, lds0, wave, wi * FI * 32);
     b.start(q.B, lds0 + 2 * a.kBytes, wave, wj * FJ * 32);
-    auto begin = [&](const Place &p) {
+    // The copies run two steps of 64 k ahead of the products, over the ends of tiles.
+    constexpr int kCopies = a.kCopies + b.kCopies, kReads = FI + FJ, kSlots = FI * FJ;
+    int ahead = blockIdx.x / 8;                 // the tile that they are at, and what is left of its k
+    int64_t left = 0;
+    auto enter = [&]() {
+        if (ahead >= run) return;
+        const Place p = place(ahead);
         a.tile(q.A, p.i0, q.M, (int64_t)p.share * q.share);
         b.tile(q.B, p.j0, q.N, (int64_t)p.share * q.share);
+        left = p.length;
     };
-    auto bring = [&](const Place &p, int step) {
-        const int64_t left = p.length - (int64_t)step * kDeep;
+    auto aim = [&](int buffer) {
+        a.aim(left, buffer, wave);
+        b.aim(left, buffer, wave);
         if (left > 0) {
-            a.copy(left, step & 1, wave);
-            b.copy(left, step & 1, wave);
+            left = left > kDeep ? left - kDeep : 0;
+            if (left == 0) {
+                ahead += gridDim.x / 8;
+                enter();
+            }
         }
     };
+    auto copy = [&](int u) {
+        if (u < a.kCopies)
+            a.copy(u);
+        else
+            b.copy(u - a.kCopies);
+    };
     u32x4 fa[2][FI], fb_[2][FJ];
-    auto read = [&](int buffer, int s, int set) {
-#pragma unroll
-        for (int f = 0; f < FI; ++f) fa[set][f] = a.read(buffer, s, f);
-#pragma unroll
-        for (int f = 0; f < FJ; ++f) fb_[set][f] = b.read(buffer, s, f);
+    auto read = [&](int buffer, int s, int set, int f) {
+        if (f < FI)
+            fa[set][f] = a.read(buffer, s, f);
+        else
+            fb_[set][f - FI] = b.read(buffer, s, f - FI);
     };
     // What has been asked for has come, in every wave; and every wave has read what it wanted of the other buffer.
     auto meet = [&]() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
 
-    int in_run = blockIdx.x / 8;
-    if (in_run >= run) return;
-    Place p = place(in_run);
-    begin(p);
-    bring(p, 0);
-    for (;;) {
+    if (ahead >= run) return;
+    if (q.K > 0) {
+        enter();
+        for (int buffer = 0; buffer < 2; ++buffer) {
+            aim(buffer);
+#pragma unroll
+            for (int u = 0; u < kCopies; ++u) copy(u);
+            if (buffer == 0) meet();
+        }
+    }
+    int turn = 0;                               // the buffer that holds this step's share
+    for (int in_run = blockIdx.x / 8; in_run < run; in_run += gridDim.x / 8) {
+        const Place p = place(in_run);
         const int steps = (int)((p.length + kDeep - 1) / kDeep);
         f32x16 acc[FI][FJ] = {};
         f32x4 bias = {};
@@ -365,42 +392,49 @@ __global__ __launch_bounds__(WI * WJ * 64) void fb_mfma_product_kernel(Product q
             for (int e = 0; e < 4; ++e)
                 if (j + e < q.N) bias[e] = q.f.bias[j + e];
         }
+        // One matrix instruction at a time, and behind it a read for the next 16 k, and after the meeting also a copy: in this
+        // order, which the compiler left to itself does not keep (it puts the reads right before their use).
+        auto times = [&](int m, int set) {
+            const int x = m / FJ, y = m % FJ;
+            acc[x][y] = multiply<T>(fb_[set][y], fa[set][x], acc[x][y]);
+        };
         if (steps > 0) {
-            meet();
-            asm volatile("" : "+v"(bias));   // (it has come with the rest: no wait for it later, behind the next tile's copies)
-            bring(p, 1);
-            read(0, 0, 0);
+#pragma unroll
+            for (int f = 0; f < kReads; ++f) read(turn, 0, 0, f);
         }
-        for (int step = 0; step < steps; ++step) {
-            const int cur = step & 1;
+        for (int step = 0; step < steps; ++step, turn ^= 1) {
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                if (s < 3) {
-                    read(cur, s + 1, (s + 1) & 1);
-                } else if (step + 1 < steps) {
-                    meet();
-                    bring(p, step + 2);
-                    read(cur ^ 1, 0, 0);
+            for (int s = 0; s < 3; ++s)
+#pragma unroll
+                for (int m = 0; m < kSlots; ++m) {
+                    times(m, s & 1);
+#pragma unroll
+                    for (int f = 0; f < kReads; ++f)
+                        if (f * kSlots / kReads == m) read(turn, s + 1, (s + 1) & 1, f);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
+            times(0, 1);
+            __builtin_amdgcn_sched_barrier(0);
+            meet();
+            asm volatile("" : "+v"(bias));      // (it has come with the rest: no wait for it later, behind further copies)
+            aim(turn);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int x = 0; x < FI; ++x)
+            for (int m = 1; m < kSlots; ++m) {  // (behind a tile's last step: of the next tile's first, and read again then)
+                times(m, 1);
 #pragma unroll
-                    for (int y = 0; y < FJ; ++y) acc[x][y] = multiply<T>(fb_[s & 1][y], fa[s & 1][x], acc[x][y]);
+                for (int f = 0; f < kReads; ++f)
+                    if (f * (kSlots - 1) / kReads == m - 1) read(turn ^ 1, 0, 0, f);
+#pragma unroll
+                for (int u = 0; u < kCopies; ++u)
+                    if (u * (kSlots - 1) / kCopies == m - 1) copy(u);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
-        const Place done = p;
-        in_run += gridDim.x / 8;
-        const bool more = in_run < run;
-        leave<T, FI, FJ, KIND>(acc, bias, done.share, done.i0 + wi * FI * 32, done.j0 + wj * FJ * 32,
-                               (float *)(lds_raw + 2 * (a.kBytes + b.kBytes)) + wave * 16 * FJ * 32, [&]() {
-                                   if (!more) return;
-                                   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // (no wave reads the buffers any longer)
-                                   p = place(in_run);
-                                   begin(p);
-                                   bring(p, 0);
-                               });
-        if (!more) return;
+        leave<T, FI, FJ, KIND>(acc, bias, p.share, p.i0 + wi * FI * 32, p.j0 + wj * FJ * 32,
+                               (float *)(lds_raw + 2 * (a.kBytes + b.kBytes)) + wave * 16 * FJ * 32);
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (no copy into LDS outlives the workgroup)
 }
 
 template <class T, bool ALONG_A, bool ALONG_B, int WI, int WJ, int FI, int FJ, int KIND>
