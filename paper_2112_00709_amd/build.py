@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfb_amd.so")
 SOURCES = ["fb_kernels.hip", "fb_graph.cpp", "fb_sell.cpp", "fb_stream.cpp", "fb_pstream.cpp", "fb_small.cpp", "fb_api.cpp", "fb_leaky.hip",
            "fb_small.hip", "fb_small_linear.hip", "fb_post_small.hip", "fb_layer_norm.hip", "fb_logprobs.hip",
-           "fb_affine.hip", "fb_affine_mfma.hip"]
+           "fb_affine.hip", "fb_affine_mfma.hip", "fb_affine_few.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",

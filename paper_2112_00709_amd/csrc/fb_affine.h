@@ -39,6 +39,10 @@ struct Product {
 
 int launch_mfma_product(const Product &q, hipStream_t stream);   // 16-bit factors, see ready()
 
+// Few rows of x (M <= kFewRows), both factors along k, at any address and distance.
+constexpr int64_t kFewRows = 64;
+int launch_few_rows(const Product &q, hipStream_t stream);
+
 // Whether the matrix units' kernel can take a factor as it is: whole 16-byte pieces, at addresses and distances that are
 // multiples of 16 bytes, and a tile's rows within the 2^31 bytes of a buffer.  `width`: the length of its rows in memory.
 inline bool ready(const void *p, int64_t ld, int64_t width)

@@ -271,6 +271,7 @@ bool bad_sizes(int64_t M, int64_t N, int64_t K) { return bad_rows(M) || bad_widt
 
 struct ForwardPlan {
     Product q;
+    bool few;             // by launch_few_rows
     Packed x, w;
     size_t bytes;
 };
@@ -279,6 +280,8 @@ ForwardPlan forward_plan(const void *x, int64_t ldx, const void *weight, int64_t
 {
     ForwardPlan f{};
     f.q.M = M; f.q.N = N; f.q.K = K; f.q.type = type;
+    f.few = M <= kFewRows;
+    if (f.few) return f;
     plan(f.q);
     f.x = packed(x, ldx, M, K, type);
     f.w = packed(weight, ldw, N, K, type);
@@ -356,9 +359,14 @@ int fb_affine(const void *x, int64_t ldx, const void *weight, int64_t ldw, const
         if ((rc = launch_pack(f.x, x, ldx, M, K, type, xs, st)) != FB_OK || (M > 0 && (rc = launch_pack(f.w, weight, ldw, N, K, type, wts, st)) != FB_OK))
             return rc;
         Product q = f.q;
+        q.f = {bias, residual, ldr, act, y, ldy, out_type, preact, ldp};
+        if (f.few) {
+            q.A = {x, ldx, true};
+            q.B = {weight, ldw, true};
+            return M > 0 ? launch_few_rows(q, st) : FB_OK;
+        }
         q.A = {f.x.copy ? xs : x, f.x.ld, true};
         q.B = {f.w.copy ? wts : weight, f.w.ld, true};
-        q.f = {bias, residual, ldr, act, y, ldy, out_type, preact, ldp};
         q.part = (float *)(wts + f.w.bytes);
         return launch_product(q, st);
     });
