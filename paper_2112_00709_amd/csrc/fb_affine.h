@@ -31,7 +31,8 @@ struct Product {
     int64_t M, N, K;     // i < M, j < N, k < K
     int type;            // of the factors
     Finish f;
-    float *part;         // split > 1: [split][M][N] sums of shares of k
+    bool parts;          // the sums of shares of k go to part, [split][M][N], to be joined and finished
+    float *part;
     int split;
     int64_t share;       // length of a share
     int tile;            // 16-bit factors: 256 or 128, the side of the tiles

@@ -37,11 +37,35 @@ __device__ __forceinline__ void put(const Factor &f, float *tile, const float (&
     }
 }
 
-// Single-precision factors: C = A B^T by 128 x 128 tiles, four waves with 64 x 64 each, on the single-precision matrix instruction, 16 k at a time
-// through LDS.  Sums of 256 k are closed and added to a second set, so that roundings do not pile up along k.
+// Four neighbouring sums of a row finished and stored, n of them (1 .. 4) below N.
+__device__ __forceinline__ void finish_four(const Finish &f, int64_t i, int64_t j, int n, f32x4 s)
+{
+    typedef f32x4 f32x4_any __attribute__((aligned(4)));
+    if (n < 4) {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (e < n) finish_one<float>(f, i, j + e, s[e]);
+        return;
+    }
+    if (f.bias) s += *(const f32x4_any *)(f.bias + j);
+    if (f.preact) *(f32x4_any *)((float *)f.preact + i * f.ldp + j) = s;
+    if (f.act != FB_ACT_NONE) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] = act_of(s[e], f.act);
+    }
+    if (f.residual) s += *(const f32x4_any *)((const float *)f.residual + i * f.ldr + j);
+    *(f32x4_any *)((float *)f.y + i * f.ldy + j) = s;
+}
+
+// Single-precision factors: C = A B^T by 128 x 128 tiles, four waves with 64 x 64 each, on the single-precision matrix
+// instruction, 16 k at a time through two buffers in LDS.  Sums of 256 k are closed and added to a second set, so that
+// roundings do not pile up along k.  The matrix instruction is slow enough (64 cycles for 128 bytes a wave from LDS) that
+// nothing else of the loop counts.
 __global__ __launch_bounds__(256) void fb_product_kernel(Product q)
 {
-    __shared__ float ta[kDeep * kTileLd], tb[kDeep * kTileLd];
+    constexpr int kFactor = kDeep * kTileLd;
+    __shared__ float lds[4 * kFactor];                      // two buffers of both factors; then 64 rows of the tile's sums
+    static_assert(4 * kFactor >= 64 * kTileLd, "sums do not fit");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t i0 = (int64_t)blockIdx.y * kTile, j0 = (int64_t)blockIdx.x * kTile;
     const int64_t k0 = blockIdx.z * q.share, k1 = k0 + q.share < q.K ? k0 + q.share : q.K;
@@ -50,13 +74,14 @@ __global__ __launch_bounds__(256) void fb_product_kernel(Product q)
     float va[8], vb[8];
     fetch(q.A, i0, q.M, k0, k1, va);
     fetch(q.B, j0, q.N, k0, k1, vb);
-    int since = 0;
-    for (int64_t k = k0; k < k1; k += kDeep) {
-        __syncthreads();
-        put(q.A, ta, va);
-        put(q.B, tb, vb);
-        __syncthreads();
-        if (k + kDeep < k1) {
+    put(q.A, lds, va);
+    put(q.B, lds + kFactor, vb);
+    __syncthreads();
+    int since = 0, turn = 0;
+    for (int64_t k = k0; k < k1; k += kDeep, turn ^= 1) {
+        const float *ta = lds + turn * 2 * kFactor, *tb = ta + kFactor;
+        const bool more = k + kDeep < k1;
+        if (more) {
             fetch(q.A, i0, q.M, k + kDeep, k1, va);
             fetch(q.B, j0, q.N, k + kDeep, k1, vb);
         }
@@ -71,7 +96,7 @@ __global__ __launch_bounds__(256) void fb_product_kernel(Product q)
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
-                for (int u = 0; u < 2; ++u) acc[s][u] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[s], b[u], acc[s][u], 0, 0, 0);
+                for (int u = 0; u < 2; ++u) acc[s][u] = __builtin_amdgcn_mfma_f32_32x32x2f32(b[u], a[s], acc[s][u], 0, 0, 0);
         }
         if (++since == 256 / kDeep) {
             since = 0;
@@ -83,33 +108,52 @@ __global__ __launch_bounds__(256) void fb_product_kernel(Product q)
                     acc[s][u] = (f32x16)(0.0f);
                 }
         }
+        if (more) {                                         // (the other buffer was read before the last barrier)
+            put(q.A, lds + (turn ^ 1) * 2 * kFactor, va);
+            put(q.B, lds + (turn ^ 1) * 2 * kFactor + kFactor, vb);
+        }
+        __syncthreads();
     }
+    // The sums leave through LDS, half of the tile's rows at a time, so that whole runs of a row are stored.
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+    for (int s = 0; s < 2; ++s) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const f32x16 c = sum[s][u] + acc[s][u];
-            const int64_t j = j0 + wj + u * 32 + l;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int64_t i = i0 + wi + s * 32 + 8 * (e / 4) + 4 * h + e % 4;
-                if (i < q.M && j < q.N) {
-                    if (q.split > 1)
-                        q.part[((size_t)blockIdx.z * q.M + i) * q.N + j] = c[e];
-                    else
-                        finish_one<float>(q.f, i, j, c[e]);
+            for (int e = 0; e < 4; ++e)
+                *(f32x4 *)(lds + ((wave & 1) * 32 + l) * kTileLd + wj + u * 32 + 8 * e + 4 * h) = f32x4{c[4 * e], c[4 * e + 1], c[4 * e + 2], c[4 * e + 3]};
+        }
+        __syncthreads();
+        const int64_t j = j0 + (threadIdx.x & 31) * 4;
+        const int n = (int)(q.N - j < 4 ? q.N - j : 4);
+#pragma unroll 1
+        for (int r = threadIdx.x >> 5; r < 64; r += 8) {
+            const int64_t i = i0 + (r >> 5) * 64 + s * 32 + (r & 31);
+            const f32x4 c = *(const f32x4 *)(lds + r * kTileLd + (threadIdx.x & 31) * 4);
+            if (i < q.M && n > 0) {
+                if (q.parts) {
+                    float *to = q.part + ((size_t)blockIdx.z * q.M + i) * q.N + j;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (e < n) to[e] = c[e];
+                } else {
+                    finish_four(q.f, i, j, n, c);
                 }
             }
         }
+        __syncthreads();
+    }
 }
 
-// The shares of a split product added in their order and finished.
+// The shares of a product added in their order and finished.
 template <class T>
 __global__ __launch_bounds__(256) void fb_product_join_kernel(Product q)
 {
     const int64_t n = q.M * q.N;
     for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < n; at += (int64_t)gridDim.x * 256) {
         float s = 0.0f;
+#pragma unroll 8
         for (int c = 0; c < q.split; ++c) s += q.part[(size_t)c * n + at];
         finish_one<T>(q.f, at / q.N, at % q.N, s);
     }
@@ -174,12 +218,13 @@ constexpr double kSmallCost = 1.25, kEnds = 400.0, kJoinPerSum = 2.0e-4, kJoinLa
 
 void plan(Product &q)
 {
-    if (q.type == FB_TYPE_F32) {            // as many shares as fill the GPU with tiles, of at least 256 k each
+    if (q.type == FB_TYPE_F32) {            // as many shares as fill the GPU with tiles, of at least 128 k each
         const int64_t tiles = ((q.M + kTile - 1) / kTile) * ((q.N + kTile - 1) / kTile);
-        int64_t split = std::min<int64_t>(2 * kCUs / std::max<int64_t>(tiles, 1), (q.K + 255) / 256);
-        split = std::max<int64_t>(1, std::min<int64_t>(split, 64));
+        int64_t split = std::min<int64_t>(2 * kCUs / std::max<int64_t>(tiles, 1), (q.K + 127) / 128);
+        split = std::max<int64_t>(1, std::min<int64_t>(split, 128));
         q.share = std::max<int64_t>(kDeep, ((q.K + split - 1) / split + kDeep - 1) / kDeep * kDeep);
         q.split = (int)std::max<int64_t>(1, (q.K + q.share - 1) / q.share);   // (K = 0, a gradient over no rows: sums of nothing)
+        q.parts = q.split > 1;
         return;
     }
     double best = 0.0;
@@ -199,9 +244,10 @@ void plan(Product &q)
             }
         }
     }
+    q.parts = q.split > 1 || q.N < 4;       // (the matrix units' kernel takes a residual by fours)
 }
 
-size_t product_bytes(const Product &q) { return q.split > 1 ? aligned((size_t)q.split * (size_t)q.M * (size_t)q.N * sizeof(float)) : 0; }
+size_t product_bytes(const Product &q) { return q.parts ? aligned((size_t)q.split * (size_t)q.M * (size_t)q.N * sizeof(float)) : 0; }
 
 template <class T>
 int launch_join(const Product &q, hipStream_t stream)
@@ -222,7 +268,7 @@ int launch_product(const Product &q, hipStream_t stream)
     } else {
         rc = launch_mfma_product(q, stream);
     }
-    if (rc != FB_OK || q.split == 1) return rc;
+    if (rc != FB_OK || !q.parts) return rc;
     if (q.type == FB_TYPE_F32) return launch_join<float>(q, stream);
     return q.type == FB_TYPE_BF16 ? launch_join<bf16>(q, stream) : launch_join<f16>(q, stream);
 }

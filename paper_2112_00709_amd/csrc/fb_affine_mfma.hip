@@ -178,57 +178,40 @@ __device__ __forceinline__ void store_rows(O *p, int64_t ld, const Spot &at, con
         }
     }
 }
-// What the residual has at the same places, as it is stored.  (A lane at the right edge, n < 4, takes its few elements later.)
+// What a 16-bit residual has at the same places, as it is stored.  (At the right edge the last four of a row are read, so that
+// such a lane waits no longer than the others; there are four, see Product::parts.)
 template <class T, int R, int STEP>
-__device__ __forceinline__ void ask_rows(const void *p, int type, int64_t ld, const Spot &at, u32x4 (&raw)[R])
+__device__ __forceinline__ void ask_rows(const T *p, int64_t ld, const Spot &at, u32x2 (&raw)[R])
 {
-    const uint32_t off = (uint32_t)at.row * (uint32_t)ld + (uint32_t)at.col;
-    if (type == FB_TYPE_F32) {
-        const float *base = (const float *)p + at.i * ld + at.j;
-#pragma unroll
-        for (int r = 0; r < R; ++r, base += STEP * ld)
-            if (at.row + r * STEP < at.rows && at.n == 4) raw[r] = __builtin_bit_cast(u32x4, (f32x4) * (const f32x4_any *)(base + off));
-    } else {
-        const T *base = (const T *)p + at.i * ld + at.j;
-#pragma unroll
-        for (int r = 0; r < R; ++r, base += STEP * ld)
-            if (at.row + r * STEP < at.rows && at.n == 4) {
-                const u32x2 v = *(const u32x2_any *)(base + off);
-                raw[r][0] = v[0];
-                raw[r][1] = v[1];
-            }
-    }
-}
-template <class O, int R, int STEP>
-__device__ __forceinline__ void add_edge(const O *p, int64_t ld, const Spot &at, f32x4 (&w)[R])
-{
-    const O *base = p + at.i * ld + at.j;
-    const uint32_t off = (uint32_t)at.row * (uint32_t)ld + (uint32_t)at.col;
+    const T *base = p + at.i * ld + at.j;
+    const uint32_t off = (uint32_t)at.row * (uint32_t)ld + (uint32_t)at.col - (uint32_t)(4 - at.n);
 #pragma unroll
     for (int r = 0; r < R; ++r, base += STEP * ld)
-#pragma unroll
-        for (int e = 0; e < 3; ++e)
-            if (at.row + r * STEP < at.rows && e < at.n) w[r][e] += (float)base[off + e];
+        if (at.row + r * STEP < at.rows && at.n > 0) raw[r] = *(const u32x2_any *)(base + (int32_t)off);
 }
-template <class T, int R, int STEP>
-__device__ __forceinline__ void add_rows(const void *p, int type, int64_t ld, const Spot &at, const u32x4 (&raw)[R], f32x4 (&w)[R])
+template <class T, int R>
+__device__ __forceinline__ void add_rows(const Spot &at, const u32x2 (&raw)[R], f32x4 (&w)[R])
 {
-    if (at.n < 4) {
-        if (type == FB_TYPE_F32)
-            add_edge<float, R, STEP>((const float *)p, ld, at, w);
-        else
-            add_edge<T, R, STEP>((const T *)p, ld, at, w);
-    } else if (type == FB_TYPE_F32) {
 #pragma unroll
-        for (int r = 0; r < R; ++r) w[r] += __builtin_bit_cast(f32x4, raw[r]);
-    } else {
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            float v[8];
-            unpack<T>(u32x4{raw[r][0], raw[r][1], 0, 0}, v);
-            w[r] += f32x4{v[0], v[1], v[2], v[3]};
-        }
+    for (int r = 0; r < R; ++r) {
+        const uint64_t four = __builtin_bit_cast(uint64_t, raw[r]) >> (16 * (4 - at.n));
+        float v[8];
+        unpack<T>(u32x4{(uint32_t)four, (uint32_t)(four >> 32), 0, 0}, v);
+        w[r] += f32x4{v[0], v[1], v[2], v[3]};
     }
+}
+template <int R, int STEP>
+__device__ __forceinline__ void add_rows(const float *p, int64_t ld, const Spot &at, f32x4 (&w)[R])
+{
+    const float *base = p + at.i * ld + at.j;
+    const uint32_t off = (uint32_t)at.row * (uint32_t)ld + (uint32_t)at.col - (uint32_t)(4 - at.n);
+    f32x4 v[R] = {};
+#pragma unroll
+    for (int r = 0; r < R; ++r, base += STEP * ld)
+        if (at.row + r * STEP < at.rows) v[r] = *(const f32x4_any *)(base + (int32_t)off);
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        w[r] += at.n == 4 ? v[r] : at.n == 3 ? f32x4{v[r][1], v[r][2], v[r][3], 0.0f} : at.n == 2 ? f32x4{v[r][2], v[r][3], 0.0f, 0.0f} : f32x4{v[r][3], 0.0f, 0.0f, 0.0f};
 }
 
 // How sums leave: as they are, with bias and perhaps max(z, 0); or with any of activation (one an instantiation), residual, preact.
@@ -248,7 +231,7 @@ __device__ __forceinline__ void leave(const f32x16 (&acc)[FI][FJ], const f32x4 &
     const int64_t M = args->M, N = args->N, j = j0 + (lane % kPer) * 4;
     const int nj = (int)(N - j < 4 ? (N - j < 0 ? 0 : N - j) : 4), in_row = lane / kPer;
     const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)mine + (lane & 15) * FJ * 128;
-    const bool split = KIND == kPlain && args->split > 1, relu = KIND == FB_ACT_RELU || (KIND == kPlain && !split && args->f.act == FB_ACT_RELU);
+    const bool split = KIND == kPlain && args->parts, relu = KIND == FB_ACT_RELU || (KIND == kPlain && !split && args->f.act == FB_ACT_RELU);
     const int out_type = split ? FB_TYPE_F32 : args->f.out_type;
     const int64_t ld = split ? N : args->f.ldy;
     void *y = split ? (void *)(args->part + (size_t)share * M * N) : args->f.y;
@@ -257,47 +240,77 @@ __device__ __forceinline__ void leave(const f32x16 (&acc)[FI][FJ], const f32x4 &
         const int64_t i = i0 + pass * 16;
         return Spot{i, j0, in_row, (lane % kPer) * 4, (int)(M - i < 16 ? M - i : 16), nj};
     };
-    u32x4 raw[2][kR] = {};
-    if (residual) ask_rows<T, kR, kRows>(residual, out_type, args->f.ldr, spot(0), raw[0]);
+    auto put = [&](const f32x16 (&sums)[FJ]) {
 #pragma unroll
-    for (int pass = 0; pass < 2 * FI; ++pass) {
-        if ((lane >> 4 & 1) == (pass & 1)) {
+        for (int y = 0; y < FJ; ++y)
 #pragma unroll
-            for (int y = 0; y < FJ; ++y)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const f32x16 &sums = acc[pass / 2][y];
-                    const f32x4 w = {sums[4 * e], sums[4 * e + 1], sums[4 * e + 2], sums[4 * e + 3]};
-                    const int c = (y * 8 + 2 * e + (lane >> 5)) ^ (lane & 15 & (kPer - 1));
-                    *(__attribute__((address_space(3))) f32x4 *)(uintptr_t)(to + c * 16) = w;
-                }
-        }
-        if (residual && pass + 1 < 2 * FI) ask_rows<T, kR, kRows>(residual, out_type, args->f.ldr, spot(pass + 1), raw[(pass + 1) & 1]);
+            for (int e = 0; e < 4; ++e) {
+                const f32x4 w = {sums[y][4 * e], sums[y][4 * e + 1], sums[y][4 * e + 2], sums[y][4 * e + 3]};
+                const int c = (y * 8 + 2 * e + (lane >> 5)) ^ (lane & 15 & (kPer - 1));
+                *(__attribute__((address_space(3))) f32x4 *)(uintptr_t)(to + c * 16) = w;
+            }
+    };
+    auto get = [&](f32x4 (&w)[kR]) {
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        f32x4 w[kR];
 #pragma unroll
         for (int r = 0; r < kR; ++r) {
             const int row = r * kRows + in_row;
-            w[r] = *(const f32x4 *)(mine + row * FJ * 32 + ((lane % kPer) ^ (row & (kPer - 1))) * 4);
+            w[r] = *(const f32x4 *)(mine + row * FJ * 32 + ((lane % kPer) ^ (row & (kPer - 1))) * 4) + bias;
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        const Spot at = spot(pass);
-        if (at.rows > in_row && nj > 0) {
+    };
+    auto act = [&](f32x4 (&w)[kR], int which) {
 #pragma unroll
-            for (int r = 0; r < kR; ++r) w[r] += bias;
-            if (KIND != kPlain && args->f.preact) store_rows<T, T, kR, kRows>((T *)args->f.preact, args->f.ldp, at, w);
-            constexpr int kAct = KIND == kPlain ? FB_ACT_RELU : KIND;
-            if (KIND != kPlain || relu) {
+        for (int r = 0; r < kR; ++r)
 #pragma unroll
-                for (int r = 0; r < kR; ++r)
+            for (int e = 0; e < 4; ++e) w[r][e] = act_of(w[r][e], which);
+    };
+    auto store = [&](const Spot &at, const f32x4 (&w)[kR]) {
+        if (out_type == FB_TYPE_F32)
+            store_rows<T, float, kR, kRows>((float *)y, ld, at, w);
+        else
+            store_rows<T, T, kR, kRows>((T *)y, ld, at, w);
+    };
+    if constexpr (KIND == kPlain) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) w[r][e] = act_of(w[r][e], kAct);
+        for (int pass = 0; pass < 2 * FI; ++pass) {
+            if ((lane >> 4 & 1) == (pass & 1)) put(acc[pass / 2]);
+            f32x4 w[kR];
+            get(w);
+            const Spot at = spot(pass);
+            if (at.rows > in_row && nj > 0) {
+                if (relu) act(w, FB_ACT_RELU);
+                store(at, w);
             }
-            if (residual) add_rows<T, kR, kRows>(residual, out_type, args->f.ldr, at, raw[pass & 1], w);
-            if (out_type == FB_TYPE_F32)
-                store_rows<T, float, kR, kRows>((float *)y, ld, at, w);
-            else
-                store_rows<T, T, kR, kRows>((T *)y, ld, at, w);
+        }
+    } else {
+        // (A loop: unrolled, the addresses of three matrices in every pass take all scalar registers and more.)
+        const T *res16 = out_type == FB_TYPE_F32 ? nullptr : (const T *)residual;
+        const float *res32 = out_type == FB_TYPE_F32 ? (const float *)residual : nullptr;
+        u32x2 next[kR] = {};
+        if (res16) ask_rows<T, kR, kRows>(res16, args->f.ldr, spot(0), next);
+#pragma unroll 1
+        for (int pass = 0; pass < 2 * FI; ++pass) {
+            if ((lane >> 4 & 1) == (pass & 1)) {
+                if (pass < 2) put(acc[0]);
+                else if (FI == 2 || pass < 4) put(acc[1 % FI]);
+                else if (pass < 6) put(acc[2 % FI]);
+                else put(acc[3 % FI]);
+            }
+            u32x2 raw[kR];
+#pragma unroll
+            for (int r = 0; r < kR; ++r) raw[r] = next[r];
+            if (res16 && pass + 1 < 2 * FI) ask_rows<T, kR, kRows>(res16, args->f.ldr, spot(pass + 1), next);
+            f32x4 w[kR];
+            get(w);
+            const Spot at = spot(pass);
+            if (at.rows > in_row && nj > 0) {
+                if (args->f.preact) store_rows<T, T, kR, kRows>((T *)args->f.preact, args->f.ldp, at, w);
+                act(w, KIND);
+                if (res16) add_rows<T, kR>(at, raw, w);
+                if (res32) add_rows<kR, kRows>(res32, args->f.ldr, at, w);
+                store(at, w);
+            }
         }
     }
 }
@@ -386,7 +399,7 @@ __global__ __launch_bounds__(WI * WJ * 64) void fb_mfma_product_kernel(Product q
         const int steps = (int)((p.length + kDeep - 1) / kDeep);
         f32x16 acc[FI][FJ] = {};
         f32x4 bias = {};
-        if (q.split == 1 && q.f.bias) {
+        if (!q.parts && q.f.bias) {
             const int64_t j = p.j0 + wj * FJ * 32 + lane % (FJ * 8) * 4;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -465,7 +478,7 @@ int launch(const Product &q, hipStream_t stream)
 {
     if (!q.A.along) return launch<T, false, false, kPlain>(q, stream);
     if (!q.B.along) return launch<T, true, false, kPlain>(q, stream);
-    if (q.split > 1 || (q.f.act <= FB_ACT_RELU && !q.f.residual && !q.f.preact)) return launch<T, true, true, kPlain>(q, stream);
+    if (q.parts || (q.f.act <= FB_ACT_RELU && !q.f.residual && !q.f.preact)) return launch<T, true, true, kPlain>(q, stream);
     switch (q.f.act) {
     case FB_ACT_NONE: return launch<T, true, true, FB_ACT_NONE>(q, stream);
     case FB_ACT_RELU: return launch<T, true, true, FB_ACT_RELU>(q, stream);
