@@ -64,7 +64,7 @@ int fb_layer_norm_grad(const void *dy, int64_t lddy, const void *x, int64_t ldx,
                        float *dbias, void *ws, size_t ws_bytes, fb_stream stream);
 
 /* Bytes of workspace fb_affine needs for these arguments (0: none, or bad arguments).  Of x and weight only the address counts:
- * 16-bit matrices whose rows are not whole 16-byte pieces at multiples of 16 bytes are copied to such rows first. */
+ * matrices whose rows are not whole 16-byte pieces at multiples of 16 bytes are copied to such rows first (unless M <= 64). */
 size_t fb_affine_workspace_bytes(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t N, int64_t K, int type);
 
 /*

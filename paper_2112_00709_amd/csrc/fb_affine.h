@@ -35,10 +35,10 @@ struct Product {
     float *part;
     int split;
     int64_t share;       // length of a share
-    int tile;            // 16-bit factors: 256 or 128, the side of the tiles
+    int tile;            // 256, 128 or 64, the side of the tiles
 };
 
-int launch_mfma_product(const Product &q, hipStream_t stream);   // 16-bit factors, see ready()
+int launch_mfma_product(const Product &q, hipStream_t stream);   // factors as ready() wants them
 
 // Few rows of x (M <= kFewRows), both factors along k, at any address and distance.
 constexpr int64_t kFewRows = 64;
@@ -46,9 +46,10 @@ int launch_few_rows(const Product &q, hipStream_t stream);
 
 // Whether the matrix units' kernel can take a factor as it is: whole 16-byte pieces, at addresses and distances that are
 // multiples of 16 bytes, and a tile's rows within the 2^31 bytes of a buffer.  `width`: the length of its rows in memory.
-inline bool ready(const void *p, int64_t ld, int64_t width)
+inline bool ready(const void *p, int64_t ld, int64_t width, int type)
 {
-    return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && width % 8 == 0 && ld < (int64_t)1 << 21;
+    const int64_t piece = 16 / (int64_t)type_bytes(type);
+    return ((uintptr_t)p & 15) == 0 && ld % piece == 0 && width % piece == 0 && ld * (int64_t)type_bytes(type) < (int64_t)1 << 22;
 }
 
 namespace {

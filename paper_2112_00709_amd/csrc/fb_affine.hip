@@ -1,4 +1,4 @@
-// Affine layer and its gradient (fb_layers.h): the calls, the plain product kernel and what stands beside the products.
+// Affine layer and its gradient (fb_layers.h): the calls, how their products are laid out, and what stands beside the products.
 #include "fb_affine.h"
 
 namespace fb {
@@ -6,145 +6,6 @@ namespace fb {
 int launch_column_sum(const float *part, int64_t P, int64_t C, int sets, float *out0, float *out1, void *stream);
 
 namespace {
-
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-
-constexpr int kTile = 128, kDeep = 16, kTileLd = kTile + 4;
-
-// A tile's share of a factor, 128 x 16, [k][i] in LDS.
-__device__ __forceinline__ void fetch(const Factor &f, int64_t i0, int64_t rows, int64_t k0, int64_t k1, float (&v)[8])
-{
-    constexpr int VE = Vec<float>::kN;
-    const int t = threadIdx.x;
-    const float *p = (const float *)f.p;
-    const int64_t i = i0 + (f.along ? t >> 1 : (t & 15) * 8), k = k0 + (f.along ? (t & 1) * 8 : t >> 4);
-    int64_t n = f.along ? (i < rows ? k1 - k : 0) : (k < k1 ? rows - i : 0);
-    n = n < 0 ? 0 : n > 8 ? 8 : n;
-    const float *q = p + (f.along ? i * f.ld + k : k * f.ld + i);
-#pragma unroll
-    for (int e = 0; e < 8; e += VE) unpack<float>(load_piece(q + e, (int)n - e), v + e);
-}
-
-__device__ __forceinline__ void put(const Factor &f, float *tile, const float (&v)[8])
-{
-    const int t = threadIdx.x;
-    if (f.along) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) tile[((t & 1) * 8 + e) * kTileLd + (t >> 1)] = v[e];
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) tile[(t >> 4) * kTileLd + (t & 15) * 8 + e] = v[e];
-    }
-}
-
-// Four neighbouring sums of a row finished and stored, n of them (1 .. 4) below N.
-__device__ __forceinline__ void finish_four(const Finish &f, int64_t i, int64_t j, int n, f32x4 s)
-{
-    typedef f32x4 f32x4_any __attribute__((aligned(4)));
-    if (n < 4) {
-#pragma unroll
-        for (int e = 0; e < 3; ++e)
-            if (e < n) finish_one<float>(f, i, j + e, s[e]);
-        return;
-    }
-    if (f.bias) s += *(const f32x4_any *)(f.bias + j);
-    if (f.preact) *(f32x4_any *)((float *)f.preact + i * f.ldp + j) = s;
-    if (f.act != FB_ACT_NONE) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[e] = act_of(s[e], f.act);
-    }
-    if (f.residual) s += *(const f32x4_any *)((const float *)f.residual + i * f.ldr + j);
-    *(f32x4_any *)((float *)f.y + i * f.ldy + j) = s;
-}
-
-// Single-precision factors: C = A B^T by 128 x 128 tiles, four waves with 64 x 64 each, on the single-precision matrix
-// instruction, 16 k at a time through two buffers in LDS.  Sums of 256 k are closed and added to a second set, so that
-// roundings do not pile up along k.  The matrix instruction is slow enough (64 cycles for 128 bytes a wave from LDS) that
-// nothing else of the loop counts.
-__global__ __launch_bounds__(256) void fb_product_kernel(Product q)
-{
-    constexpr int kFactor = kDeep * kTileLd;
-    __shared__ float lds[4 * kFactor];                      // two buffers of both factors; then 64 rows of the tile's sums
-    static_assert(4 * kFactor >= 64 * kTileLd, "sums do not fit");
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t i0 = (int64_t)blockIdx.y * kTile, j0 = (int64_t)blockIdx.x * kTile;
-    const int64_t k0 = blockIdx.z * q.share, k1 = k0 + q.share < q.K ? k0 + q.share : q.K;
-    const int wi = (wave & 1) * 64, wj = (wave >> 1) * 64, l = lane & 31, h = lane >> 5;
-    f32x16 acc[2][2] = {}, sum[2][2] = {};
-    float va[8], vb[8];
-    fetch(q.A, i0, q.M, k0, k1, va);
-    fetch(q.B, j0, q.N, k0, k1, vb);
-    put(q.A, lds, va);
-    put(q.B, lds + kFactor, vb);
-    __syncthreads();
-    int since = 0, turn = 0;
-    for (int64_t k = k0; k < k1; k += kDeep, turn ^= 1) {
-        const float *ta = lds + turn * 2 * kFactor, *tb = ta + kFactor;
-        const bool more = k + kDeep < k1;
-        if (more) {
-            fetch(q.A, i0, q.M, k + kDeep, k1, va);
-            fetch(q.B, j0, q.N, k + kDeep, k1, vb);
-        }
-#pragma unroll
-        for (int d = 0; d < kDeep; d += 2) {
-            float a[2], b[2];
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                a[s] = ta[(d + h) * kTileLd + wi + s * 32 + l];
-                b[s] = tb[(d + h) * kTileLd + wj + s * 32 + l];
-            }
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int u = 0; u < 2; ++u) acc[s][u] = __builtin_amdgcn_mfma_f32_32x32x2f32(b[u], a[s], acc[s][u], 0, 0, 0);
-        }
-        if (++since == 256 / kDeep) {
-            since = 0;
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    sum[s][u] += acc[s][u];
-                    acc[s][u] = (f32x16)(0.0f);
-                }
-        }
-        if (more) {                                         // (the other buffer was read before the last barrier)
-            put(q.A, lds + (turn ^ 1) * 2 * kFactor, va);
-            put(q.B, lds + (turn ^ 1) * 2 * kFactor + kFactor, vb);
-        }
-        __syncthreads();
-    }
-    // The sums leave through LDS, half of the tile's rows at a time, so that whole runs of a row are stored.
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const f32x16 c = sum[s][u] + acc[s][u];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                *(f32x4 *)(lds + ((wave & 1) * 32 + l) * kTileLd + wj + u * 32 + 8 * e + 4 * h) = f32x4{c[4 * e], c[4 * e + 1], c[4 * e + 2], c[4 * e + 3]};
-        }
-        __syncthreads();
-        const int64_t j = j0 + (threadIdx.x & 31) * 4;
-        const int n = (int)(q.N - j < 4 ? q.N - j : 4);
-#pragma unroll 1
-        for (int r = threadIdx.x >> 5; r < 64; r += 8) {
-            const int64_t i = i0 + (r >> 5) * 64 + s * 32 + (r & 31);
-            const f32x4 c = *(const f32x4 *)(lds + r * kTileLd + (threadIdx.x & 31) * 4);
-            if (i < q.M && n > 0) {
-                if (q.parts) {
-                    float *to = q.part + ((size_t)blockIdx.z * q.M + i) * q.N + j;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (e < n) to[e] = c[e];
-                } else {
-                    finish_four(q.f, i, j, n, c);
-                }
-            }
-        }
-        __syncthreads();
-    }
-}
 
 // The shares of a product added in their order and finished.
 template <class T>
@@ -191,7 +52,7 @@ __global__ __launch_bounds__(256) void fb_slope_kernel(SlopeParams p)
             }
 #pragma unroll
             for (int e = 0; e < VE; ++e) sum[e] += g[e];
-            if (p.out) store_piece((T *)p.out + r * p.ldo + at, sizeof(T) == 2 ? VE : n, pack<T>(g));   // (16 bits: rows of whole pieces)
+            if (p.out) store_piece((T *)p.out + r * p.ldo + at, VE, pack<T>(g));   // (rows of whole pieces)
         }
     }
     if (!p.part) return;
@@ -211,40 +72,40 @@ int64_t slope_groups(int64_t M) { return std::max<int64_t>(1, std::min<int64_t>(
 
 size_t aligned(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Tiles and shares of k, by estimated time in units of a compute unit's work on one k of a 256 x 256 tile: rounds of
-// workgroups (one 256 or two 128 tiles a compute unit at a time, the latter at kSmallCost of the former's time per product),
-// a start and end of kEnds a workgroup, and, where k is shared, the sums' way through memory and a launch to join them.
-constexpr double kSmallCost = 1.25, kEnds = 400.0, kJoinPerSum = 2.0e-4, kJoinLaunch = 300.0;
-
+// Tiles and shares of k, by estimated clocks of the busiest compute unit: its tiles' work, for every round of workgroups that
+// it holds at a time (1, 2 or 4) a start, an end and the latency of every step, and, where k is shared, the sums' way through
+// memory and a launch to join them.  In single precision a share is at most 4096 long, so that roundings do not pile up.
 void plan(Product &q)
 {
-    if (q.type == FB_TYPE_F32) {            // as many shares as fill the GPU with tiles, of at least 128 k each
-        const int64_t tiles = ((q.M + kTile - 1) / kTile) * ((q.N + kTile - 1) / kTile);
-        int64_t split = std::min<int64_t>(2 * kCUs / std::max<int64_t>(tiles, 1), (q.K + 127) / 128);
-        split = std::max<int64_t>(1, std::min<int64_t>(split, 128));
-        q.share = std::max<int64_t>(kDeep, ((q.K + split - 1) / split + kDeep - 1) / kDeep * kDeep);
-        q.split = (int)std::max<int64_t>(1, (q.K + q.share - 1) / q.share);   // (K = 0, a gradient over no rows: sums of nothing)
-        q.parts = q.split > 1;
-        return;
-    }
+    static constexpr int kSplits[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64, 96, 128};
+    struct Shape {
+        int tile, resident;
+        double per_k16, per_k32;            // clocks of a compute unit on one k of a tile, measured
+    };
+    static constexpr Shape kShapes[] = {{256, 1, 62.0, 540.0}, {128, 2, 20.0, 140.0}, {64, 4, 9.0, 34.0}};
+    constexpr double kEnds = 8000.0, kStep = 500.0, kJoin = 11000.0, kBytesPerClock = 1800.0;
+    const bool wide = q.type == FB_TYPE_F32;
+    const int64_t deep = wide ? 32 : 64;
     double best = 0.0;
-    for (int tile = 128; tile <= 256; tile += 128) {
-        const int64_t tiles = ((q.M + tile - 1) / tile) * ((q.N + tile - 1) / tile), slots = tile == 256 ? kCUs : 2 * kCUs;
-        for (int64_t split = 1; split <= 32; ++split) {
-            const int64_t share = std::max<int64_t>(64, ((q.K + split - 1) / split + 63) / 64 * 64);
+    for (const Shape &sh : kShapes) {
+        const int64_t tiles = ((q.M + sh.tile - 1) / sh.tile) * ((q.N + sh.tile - 1) / sh.tile);
+        for (const int64_t split : kSplits) {
+            const int64_t share = std::max<int64_t>(deep, ((q.K + split - 1) / split + deep - 1) / deep * deep);
             if (split > 1 && (split - 1) * share >= q.K) break;
-            const double rounds = (double)((tiles * split + slots - 1) / slots);
-            double cost = rounds * ((double)share * (tile == 256 ? 1.0 : kSmallCost / 2) + kEnds);
-            if (split > 1) cost += kJoinLaunch + kJoinPerSum * (double)(split + 1) * (double)q.M * (double)q.N / 16.0;
+            if (wide && share > 4096 && split < 128) continue;
+            const int64_t busiest = (tiles * split + kCUs - 1) / kCUs, rounds = (busiest + sh.resident - 1) / sh.resident;
+            double cost = (double)rounds * (kEnds + (double)(share / deep) * kStep) + (double)busiest * (double)share * (wide ? sh.per_k32 : sh.per_k16);
+            if (split > 1) cost += kJoin + (double)(split + 1) * (double)q.M * (double)q.N * 4.0 / kBytesPerClock;
             if (best == 0.0 || cost < best) {
                 best = cost;
-                q.tile = tile;
+                q.tile = sh.tile;
                 q.share = share;
-                q.split = (int)split;
+                q.split = (int)((q.K + share - 1) / share);
             }
         }
     }
-    q.parts = q.split > 1 || q.N < 4;       // (the matrix units' kernel takes a residual by fours)
+    q.split = std::max(q.split, 1);         // (K = 0, a gradient over no rows: sums of nothing)
+    q.parts = q.split > 1 || q.N < 4;       // (the kernel takes a residual by fours)
 }
 
 size_t product_bytes(const Product &q) { return q.parts ? aligned((size_t)q.split * (size_t)q.M * (size_t)q.N * sizeof(float)) : 0; }
@@ -260,14 +121,7 @@ int launch_join(const Product &q, hipStream_t stream)
 int launch_product(const Product &q, hipStream_t stream)
 {
     if (q.M == 0) return FB_OK;
-    int rc;
-    if (q.type == FB_TYPE_F32) {
-        const int64_t ti = (q.M + kTile - 1) / kTile, tj = (q.N + kTile - 1) / kTile;
-        hipLaunchKernelGGL(fb_product_kernel, dim3((unsigned)tj, (unsigned)ti, (unsigned)q.split), dim3(256), 0, stream, q);
-        rc = launched("product kernel launch: ");
-    } else {
-        rc = launch_mfma_product(q, stream);
-    }
+    const int rc = launch_mfma_product(q, stream);
     if (rc != FB_OK || !q.parts) return rc;
     if (q.type == FB_TYPE_F32) return launch_join<float>(q, stream);
     return q.type == FB_TYPE_BF16 ? launch_join<bf16>(q, stream) : launch_join<f16>(q, stream);
@@ -290,7 +144,13 @@ int launch_slope(const SlopeParams &p, int type, int dy_type, hipStream_t stream
     return dy_type == type ? launch_slope<f16, f16>(p, groups, stream) : launch_slope<f16, float>(p, groups, stream);
 }
 
-// A 16-bit matrix that the matrix units' kernel cannot take as it is, copied to rows of whole pieces (padded with zeros).
+int64_t whole_pieces(int64_t width, int type)
+{
+    const int64_t piece = 16 / (int64_t)type_bytes(type);
+    return (width + piece - 1) / piece * piece;
+}
+
+// A matrix that the matrix units' kernel cannot take as it is, copied to rows of whole pieces (padded with zeros).
 struct Packed {
     bool copy;
     int64_t ld;
@@ -300,9 +160,9 @@ struct Packed {
 Packed packed(const void *p, int64_t ld, int64_t rows, int64_t width, int type)
 {
     Packed k{};
-    k.copy = type != FB_TYPE_F32 && !ready(p, ld, width);
-    k.ld = k.copy ? (width + 7) & ~(int64_t)7 : ld;
-    k.bytes = k.copy ? aligned((size_t)rows * (size_t)k.ld * 2) : 0;
+    k.copy = !ready(p, ld, width, type);
+    k.ld = k.copy ? whole_pieces(width, type) : ld;
+    k.bytes = k.copy ? aligned((size_t)rows * (size_t)k.ld * type_bytes(type)) : 0;
     return k;
 }
 
@@ -353,7 +213,7 @@ GradPlan grad_plan(const void *dy, int64_t lddy, int dy_type, const void *x, int
     plan(g.dx);
     plan(g.dw);
     g.slope = act != FB_ACT_NONE || dy_type != type || packed(dy, lddy, M, N, type).copy;
-    g.ldz = (N + 7) & ~(int64_t)7;
+    g.ldz = whole_pieces(N, type);
     g.dz = g.slope ? aligned((size_t)M * (size_t)g.ldz * type_bytes(type)) : 0;
     g.x = packed(x, ldx, M, K, type);
     g.w = packed(weight, ldw, N, K, type);

@@ -1,12 +1,14 @@
-// Products of 16-bit factors on the matrix units (see fb_affine.h), for factors whose rows are whole 16-byte pieces.
+// Products on the matrix units (see fb_affine.h), for factors whose rows are whole 16-byte pieces.
 //
-// A workgroup forms a tile of C, 64 k at a time.  Both factors' shares of those k come into LDS by direct copies (16 bytes a
+// A workgroup forms a tile of C, 128 bytes along k at a time: 64 k of 16 bits, 32 of 32.  Both factors' shares of those k come into LDS by direct copies (16 bytes a
 // lane, no registers in between), into one of two buffers while the other is worked on; a wave reads its 32-row fragments of
-// 16 k from LDS one step ahead of the matrix instructions that use them.  A factor that runs along k is kept as [row][k], one
-// that does not as [k][row] and is read by the transposing LDS read, so no factor is ever transposed in memory.
+// 32 bytes along k from LDS one step ahead of the matrix instructions that use them.  A factor that runs along k is kept as [row][k], one
+// that does not as [k][row] and is read by the transposing LDS read (32 bits: by single words), so no factor is ever transposed
+// in memory.  Of 32 bytes along k a lane of the lower half has the first 16 and a lane of the upper half the others: in
+// single precision, whose instruction takes 2 k, the four k of the one are multiplied beside those of the other.
 //
-// LDS banks.  [row][64 k]: the 16-byte piece c of a row lies at piece c ^ (row & 7), so eight rows read at one c cover all
-// banks.  [k][rows]: piece c of a k lies at c ^ ((k & 3) << 1): the four k that a transposing read takes at once lie in
+// LDS banks.  [row][k]: the 16-byte piece c of a row lies at piece c ^ (row & 7), so eight rows read at one c cover all
+// banks.  [k][rows] of 16 bits: piece c of a k lies at c ^ ((k & 3) << 1): the four k that a transposing read takes at once lie in
 // different quarters of the banks.  The copies write LDS in order of lanes, so the exchange is in the address a lane reads.
 #include "fb_affine.h"
 
@@ -20,12 +22,18 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef f16 f16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int kDeep = 64;          // k of a step between barriers
+template <class T>
+constexpr int kDeepOf = 128 / (int)sizeof(T);          // k of a step between barriers
 
 template <class T>
 __device__ __forceinline__ f32x16 multiply(const u32x4 &a, const u32x4 &b, const f32x16 &c)
 {
-    if constexpr (std::is_same<T, bf16>::value)
+    if constexpr (sizeof(T) == 4) {
+        f32x16 d = c;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) d = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[e]), __uint_as_float(b[e]), d, 0, 0, 0);
+        return d;
+    } else if constexpr (std::is_same<T, bf16>::value)
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     else
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
@@ -44,11 +52,13 @@ __device__ __forceinline__ void copy_to_lds(uint32_t to, uint32_t offset, const 
 }
 
 // One factor's way into LDS and out of it.  ROWS of the tile, NW waves that copy, F fragments of 32 rows a wave from row w0 on.
-template <bool ALONG, int ROWS, int NW, int F>
+template <class T, bool ALONG, int ROWS, int NW, int F>
 struct Side {
-    static constexpr int kBytes = ROWS * kDeep * 2, kCopies = kBytes / 1024 / NW;
+    static constexpr int kSize = sizeof(T), kDeep = kDeepOf<T>, kPiece = 16 / kSize;
+    static constexpr int kBytes = ROWS * 128, kCopies = kBytes / 1024 / NW;
+    static constexpr int kPer = ROWS * kSize / 16, kK = 64 / kPer;      // not ALONG: lanes a k, k a copy
     uint64_t base;           // of the tile's first element at the share's first k
-    uint32_t ld2;            // bytes between rows
+    uint32_t ldb;            // bytes between rows
     int rows;                // rows of the factor from the tile's first on
     uint32_t from[2];        // a lane's offset in what a copy brings (two: even and odd copies)
     uint32_t lds;            // the first buffer
@@ -59,35 +69,38 @@ struct Side {
     __device__ __forceinline__ void start(const Factor &f, uint32_t lds_at, int wave, int w0)
     {
         const int lane = threadIdx.x & 63;
-        ld2 = (uint32_t)f.ld * 2;
+        ldb = (uint32_t)f.ld * kSize;
         lds = lds_at;
         const int l = lane & 31, h = lane >> 5;
         if constexpr (ALONG) {
             chunk = (lane & 7) ^ (lane >> 3);
-            from[0] = from[1] = (uint32_t)(wave * kCopies * 8 + (lane >> 3)) * ld2 + chunk * 16;
+            from[0] = from[1] = (uint32_t)(wave * kCopies * 8 + (lane >> 3)) * ldb + chunk * 16;
 #pragma unroll
             for (int s = 0; s < 4; ++s) at[s] = lds + (w0 + l) * 128 + (((s * 2 + h) ^ (l & 7)) * 16);
         } else {
-            constexpr int kPer = ROWS / 8, kK = 64 / kPer;          // lanes a k, k a copy
             const int k = lane / kPer, p = lane % kPer;
             chunk = 0;
 #pragma unroll
             for (int odd = 0; odd < 2; ++odd)
-                from[odd] = (uint32_t)(wave * kCopies * kK + k) * ld2 + ((p ^ (((odd * kK + k) & 3) << 1)) * 16);
+                from[odd] = (uint32_t)(wave * kCopies * kK + k) * ldb + (kSize == 4 ? p : p ^ (((odd * kK + k) & 3) << 1)) * 16;
+            if constexpr (kSize == 4) {
+                at[0] = at[1] = lds + (h * 4 * ROWS + w0 + l) * 4;
+                return;
+            }
             const int g = lane >> 4, kq = (lane & 15) >> 2, c = (g & 1) * 2 + ((lane & 3) >> 1);
 #pragma unroll
             for (int odd = 0; odd < 2; ++odd)
-                at[odd] = lds + ((g >> 1) * 8 + kq) * (ROWS * 2) + w0 * 2 + (((c + odd * 4) ^ (kq << 1)) * 16) + (lane & 1) * 8;
+                at[odd] = lds + ((g >> 1) * 8 + kq) * (ROWS * 2) + (((w0 / 8 + c + odd * 4) ^ (kq << 1)) * 16) + (lane & 1) * 8;
         }
     }
 
     __device__ __forceinline__ void tile(const Factor &f, int64_t r0, int64_t n, int64_t k0)
     {
         rows = (int)(n - r0 < ROWS ? n - r0 : ROWS);
-        base = (uint64_t)(uintptr_t)f.p + (uint64_t)(ALONG ? r0 * f.ld + k0 : k0 * f.ld + r0) * 2;
+        base = (uint64_t)(uintptr_t)f.p + (uint64_t)(ALONG ? r0 * f.ld + k0 : k0 * f.ld + r0) * kSize;
     }
 
-    // The copies that bring the factor's share of the next 64 of `left` k into buffer `b`: where they read and write, then
+    // The copies that bring the factor's share of the next kDeep of `left` k into buffer `b`: where they read and write, then
     // each of the wave's kCopies.
     i32x4 buffer;
     uint32_t past, to;
@@ -96,29 +109,35 @@ struct Side {
         uint32_t bytes;
         past = 0;
         if constexpr (ALONG) {
-            bytes = (uint32_t)(rows - 1) * ld2 + (uint32_t)(left < kDeep ? (left + 7) & ~7 : kDeep) * 2;   // (whole pieces)
-            past = chunk * 8 < left ? 0u : 0x80000000u;                // (`bytes` is below 2^31)
+            bytes = (uint32_t)(rows - 1) * ldb + (uint32_t)(left < kDeep ? (left + kPiece - 1) & ~(kPiece - 1) : kDeep) * kSize;   // (whole pieces)
+            past = chunk * kPiece < left ? 0u : 0x80000000u;                // (`bytes` is below 2^31)
         } else {
-            bytes = (uint32_t)((left < kDeep ? left : kDeep) - 1) * ld2 + (uint32_t)((rows + 7) & ~7) * 2;
+            bytes = (uint32_t)((left < kDeep ? left : kDeep) - 1) * ldb + (uint32_t)((rows + kPiece - 1) & ~(kPiece - 1)) * kSize;
         }
         buffer[0] = __builtin_amdgcn_readfirstlane((int)(uint32_t)base);
         buffer[1] = __builtin_amdgcn_readfirstlane((int)(uint32_t)(base >> 32) & 0xffff);
         buffer[2] = __builtin_amdgcn_readfirstlane(left > 0 ? (int)bytes : 0);
         buffer[3] = 0x00020000;
         to = lds + b * kBytes + wave * kCopies * 1024;
-        base += ALONG ? kDeep * 2 : (uint64_t)kDeep * ld2;
+        base += ALONG ? 128 : (uint64_t)kDeep * ldb;
     }
     __device__ __forceinline__ void copy(int u) const
     {
-        constexpr int kStep = ALONG ? 8 : 64 / (ROWS / 8);
-        copy_to_lds(__builtin_amdgcn_readfirstlane(to + u * 1024), from[u & 1] + (uint32_t)(u * kStep) * ld2 + past, buffer);
+        constexpr int kStep = ALONG ? 8 : kK;
+        copy_to_lds(__builtin_amdgcn_readfirstlane(to + u * 1024), from[u & 1] + (uint32_t)(u * kStep) * ldb + past, buffer);
     }
 
-    // Fragment f of step s (16 k) from buffer `b`: row lane % 32, k = 8 (lane / 32) + 0 .. 7.
+    // Fragment f of step s (32 bytes along k) from buffer `b`: row lane % 32, the (lane / 32)-th 16 bytes.
     __device__ __forceinline__ u32x4 read(int b, int s, int f) const
     {
         if constexpr (ALONG) {
             return lds_read(at[s] + b * kBytes + f * 32 * 128);
+        } else if constexpr (kSize == 4) {
+            u32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] = *(const __attribute__((address_space(3))) uint32_t *)(uintptr_t)(at[0] + b * kBytes + ((s * 8 + e) * ROWS + f * 32) * 4);
+            return v;
         } else {
             const uint32_t a = at[f & 1] + b * kBytes + s * 16 * (ROWS * 2) + (f >> 1) * 128;
             const u32x2 lo = lds_read_across(a), hi = lds_read_across(a + 4 * (ROWS * 2));
@@ -293,7 +312,7 @@ __device__ __forceinline__ void leave(const f32x16 (&acc)[FI][FJ], const f32x4 &
         for (int pass = 0; pass < 2 * FI; ++pass) {
             if ((lane >> 4 & 1) == (pass & 1)) {
                 if (pass < 2) put(acc[0]);
-                else if (FI == 2 || pass < 4) put(acc[1 % FI]);
+                else if (FI <= 2 || pass < 4) put(acc[1 % FI]);
                 else if (pass < 6) put(acc[2 % FI]);
                 else put(acc[3 % FI]);
             }
@@ -341,11 +360,12 @@ __global__ __launch_bounds__(WI * WJ * 64) void fb_mfma_product_kernel(Product q
         return Place{share, (int64_t)(first + v % down) * kI, (int64_t)(v / down) * kJ, k0 + q.share < q.K ? q.share : q.K - k0};
     };
 
-    Side<ALONG_A, kI, kNW, FI> a;
-    Side<ALONG_B, kJ, kNW, FJ> b;
+    constexpr int kDeep = kDeepOf<T>;
+    Side<T, ALONG_A, kI, kNW, FI> a;
+    Side<T, ALONG_B, kJ, kNW, FJ> b;
     a.start(q.A, lds0, wave, wi * FI * 32);
     b.start(q.B, lds0 + 2 * a.kBytes, wave, wj * FJ * 32);
-    // The copies run two steps of 64 k ahead of the products, over the ends of tiles.
+    // The copies run two steps ahead of the products, over the ends of tiles.
     constexpr int kCopies = a.kCopies + b.kCopies, kReads = FI + FJ, kSlots = FI * FJ;
     int ahead = blockIdx.x / 8;                 // the tile that they are at, and what is left of its k
     int64_t left = 0;
@@ -405,7 +425,7 @@ __global__ __launch_bounds__(WI * WJ * 64) void fb_mfma_product_kernel(Product q
             for (int e = 0; e < 4; ++e)
                 if (j + e < q.N) bias[e] = q.f.bias[j + e];
         }
-        // One matrix instruction at a time, and behind it a read for the next 16 k, and after the meeting also a copy: in this
+        // One matrix instruction at a time, and behind it a read for the next 32 bytes of k, and after the meeting also a copy: in this
         // order, which the compiler left to itself does not keep (it puts the reads right before their use).
         auto times = [&](int m, int set) {
             const int x = m / FJ, y = m % FJ;
@@ -432,6 +452,12 @@ __global__ __launch_bounds__(WI * WJ * 64) void fb_mfma_product_kernel(Product q
             asm volatile("" : "+v"(bias));      // (it has come with the rest: no wait for it later, behind further copies)
             aim(turn);
             __builtin_amdgcn_sched_barrier(0);
+            if constexpr (kSlots == 1) {
+#pragma unroll
+                for (int f = 0; f < kReads; ++f) read(turn ^ 1, 0, 0, f);
+#pragma unroll
+                for (int u = 0; u < kCopies; ++u) copy(u);
+            }
 #pragma unroll
             for (int m = 1; m < kSlots; ++m) {  // (behind a tile's last step: of the next tile's first, and read again then)
                 times(m, 1);
@@ -456,7 +482,7 @@ int launch(const Product &q, hipStream_t stream)
     constexpr int kI = WI * FI * 32, kJ = WJ * FJ * 32;
     const int64_t ti = (q.M + kI - 1) / kI, tj = (q.N + kJ - 1) / kJ;
     if (ti * tj * q.split >= kMostSize) return fail(FB_EUNSUPPORTED, "affine product: more than 2^31 tiles");
-    constexpr size_t bytes = (size_t)2 * (kI + kJ) * kDeep * 2 + (size_t)WI * WJ * 16 * FJ * 32 * 4;
+    constexpr size_t bytes = (size_t)2 * (kI + kJ) * 128 + (size_t)WI * WJ * 16 * FJ * 32 * 4;
     constexpr int64_t slots = (int64_t)kCUs * (int64_t)(kLdsBytes / bytes);      // workgroups that the GPU holds
     const auto kernel = fb_mfma_product_kernel<T, ALONG_A, ALONG_B, WI, WJ, FI, FJ, KIND>;
     if (bytes > 64 * 1024) {
@@ -470,7 +496,8 @@ int launch(const Product &q, hipStream_t stream)
 template <class T, bool ALONG_A, bool ALONG_B, int KIND>
 int launch(const Product &q, hipStream_t stream)
 {
-    return q.tile == 256 ? launch<T, ALONG_A, ALONG_B, 2, 4, 4, 2, KIND>(q, stream) : launch<T, ALONG_A, ALONG_B, 2, 2, 2, 2, KIND>(q, stream);
+    if (q.tile == 256) return launch<T, ALONG_A, ALONG_B, 2, 4, 4, 2, KIND>(q, stream);
+    return q.tile == 128 ? launch<T, ALONG_A, ALONG_B, 2, 2, 2, 2, KIND>(q, stream) : launch<T, ALONG_A, ALONG_B, 2, 2, 1, 1, KIND>(q, stream);
 }
 
 template <class T>
@@ -491,6 +518,7 @@ int launch(const Product &q, hipStream_t stream)
 
 int launch_mfma_product(const Product &q, hipStream_t stream)
 {
+    if (q.type == FB_TYPE_F32) return launch<float>(q, stream);
     return q.type == FB_TYPE_BF16 ? launch<bf16>(q, stream) : launch<f16>(q, stream);
 }
 

@@ -21,10 +21,10 @@ struct TokenParams {
     float *logprobs, *entropy, *logz;
     int32_t *top_ids;
     float *top_logprobs;
-    int split;                 // workgroups a row
-    int64_t chunk;             // elements of the row that each of them has
-    float *part;               // [R][split][3]: m, S, T
-    uint64_t *part_top;        // [R][split][top] keys
+    int split;                 // workgroups a row; beyond one, for each of their waves:
+    int64_t chunk;             // (elements of the row that a workgroup has)
+    float *part;               // [R][split * waves][3]: m, S, T
+    uint64_t *part_top;        // [R][split * waves][top] keys, descending
 };
 
 // Total order of (value, number): larger values first, then smaller numbers.  -0 counts as 0.
@@ -61,14 +61,44 @@ __device__ __forceinline__ Stats join(const Stats &a, const Stats &b)
     return {M, fmaf(a.S, ea, b.S * eb), fmaf(fmaf(a.S, da, a.T), ea, fmaf(b.S, db, b.T) * eb)};
 }
 
-// The best `top` of n keys, descending, to `out`; missing ones are 0.  For one wave.
-__device__ __forceinline__ void best_of_keys(const uint64_t *keys, int n, int top, uint64_t *out)
+// The best `top` keys of `lists` descending lists of `top` keys each, descending, to `out`; missing ones are 0.  For one wave:
+// a lane keeps the heads of up to kHeads lists, the largest head of all is taken and its list moved on.  `keys` is read once
+// per key taken, so it may lie in memory.
+constexpr int kHeads = 8;
+
+__device__ __forceinline__ void merge_lists(const uint64_t *keys, int lists, int top, uint64_t *out)
 {
     const int lane = threadIdx.x & 63;
+    if (lists <= 64 * kHeads) {
+        uint64_t head[kHeads], best = 0;
+        int at[kHeads];
+#pragma unroll
+        for (int h = 0; h < kHeads; ++h) {
+            at[h] = (h * 64 + lane) * top;
+            head[h] = h * 64 + lane < lists ? keys[at[h]] : 0;
+            best = head[h] > best ? head[h] : best;
+        }
+        for (int t = 0; t < top; ++t) {
+            const uint64_t win = max_wave_key(best);
+            if (lane == 0) out[t] = win;
+            if (win != 0 && best == win) {                     // (keys are different: one lane)
+                best = 0;
+#pragma unroll
+                for (int h = 0; h < kHeads; ++h) {
+                    if (head[h] == win) {
+                        ++at[h];
+                        head[h] = at[h] < (h * 64 + lane + 1) * top ? keys[at[h]] : 0;
+                    }
+                    best = head[h] > best ? head[h] : best;
+                }
+            }
+        }
+        return;
+    }
     uint64_t last = ~0ull;
     for (int t = 0; t < top; ++t) {
         uint64_t best = 0;
-        for (int i = lane; i < n; i += 64) {
+        for (int i = lane; i < lists * top; i += 64) {
             const uint64_t k = keys[i];
             if (k < last && k > best) best = k;
         }
@@ -82,9 +112,9 @@ __device__ __forceinline__ void best_of_keys(const uint64_t *keys, int n, int to
 // largest of the lanes' own maxima bounds the top-th best from below; what reaches it are few elements (about `top`) of few
 // pieces, which are read once more, put on a list and ranked there, one a lane.  Where ties, or rows of almost nothing but
 // -inf, make them more than 64 the elements are searched once per place.  (From memory: the pieces in registers, indexed at
-// run time, would take a copy of all this per element.)
+// run time, would take a copy of all this per element; up to four are chosen from by selects.)
 template <class T, int NV>
-__device__ __forceinline__ void best_of_wave(const T *row, const float (&peak)[NV], float lane_max, int first, int stride, int n, int top, uint64_t *list, uint64_t *out)
+__device__ __forceinline__ void best_of_wave(const T *row, const u32x4 (&raw)[NV], const float (&peak)[NV], float lane_max, int first, int stride, int n, int top, uint64_t *list, uint64_t *out)
 {
     constexpr int VE = Vec<T>::kN;
     const int lane = threadIdx.x & 63;
@@ -105,7 +135,14 @@ __device__ __forceinline__ void best_of_wave(const T *row, const float (&peak)[N
         const int left = pieces ? n - at : 0;
         pieces &= pieces - 1;
         float v[VE];
-        unpack<T>(load_piece(row + at, left), v);
+        if constexpr (NV <= 4) {
+            u32x4 piece = raw[0];
+#pragma unroll
+            for (int i = 1; i < NV; ++i) piece = at == first + i * stride ? raw[i] : piece;
+            unpack<T>(piece, v);
+        } else {
+            unpack<T>(load_piece(row + at, left), v);
+        }
 #pragma unroll
         for (int j = 0; j < VE; ++j) {
             const uint64_t hit = __ballot(j < left && v[j] >= bound);
@@ -250,9 +287,23 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64, NV * Vec<T>::kN <= 1
     for (int i = 0; i < NV; ++i) raw[i] = load_piece(row + first + i * 64 * VE, n - (first + i * 64 * VE));
     float peak[NV], lane_max;
     Stats st = wave_stats<T, NV>(raw, first, 64 * VE, n, peak, lane_max);
-    if (p.top) best_of_wave<T, NV>(row, peak, lane_max, first, 64 * VE, n, p.top, list[wave], best[wave]);
+    if (p.top) best_of_wave<T, NV>(row, raw, peak, lane_max, first, 64 * VE, n, p.top, list[wave], best[wave]);
     lds_settled();
     const uint64_t *keys = best[wave];
+    if constexpr (SPLIT) {
+        const size_t list = (size_t)item * WAVES + wave;
+        float *q = p.part + list * 3;
+        if (lane == 0) {
+            q[0] = st.m;
+            q[1] = st.S;
+            q[2] = st.T;
+        }
+        if (lane < p.top) {
+            const uint64_t k = keys[lane];                    // numbers in the row instead of the chunk
+            p.part_top[list * p.top + lane] = k ? (k & 0xffffffff00000000ull) | (uint32_t)~(~(uint32_t)k + (uint32_t)at0) : 0;
+        }
+        return;
+    }
     if constexpr (WAVES > 1) {
         if (lane == 0) stats[wave] = st;
         __syncthreads();
@@ -261,8 +312,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64, NV * Vec<T>::kN <= 1
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) st = join(st, stats[w]);
         if (p.top) {
-            // (`best` is one array; its rows hold `top` keys each and zeros are no keys)
-            uint64_t last = ~0ull;
+            uint64_t last = ~0ull;                            // (zeros are no keys)
             for (int t = 0; t < p.top; ++t) {
                 uint64_t b = 0;
 #pragma unroll
@@ -277,24 +327,11 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64, NV * Vec<T>::kN <= 1
             keys = row_best;
         }
     }
-    if constexpr (SPLIT) {
-        float *q = p.part + (size_t)item * 3;
-        if (lane == 0) {
-            q[0] = st.m;
-            q[1] = st.S;
-            q[2] = st.T;
-        }
-        if (lane < p.top) {
-            const uint64_t k = keys[lane];                    // numbers in the row instead of the chunk
-            p.part_top[(size_t)item * p.top + lane] = k ? (k & 0xffffffff00000000ull) | (uint32_t)~(~(uint32_t)k + (uint32_t)at0) : 0;
-        }
-    } else {
-        write_row<T>(p, r, token, st, keys, lane);
-    }
+    write_row<T>(p, r, token, st, keys, lane);
 }
 
-// The chunks of a row joined, one wave a row.
-template <class T>
+// What the waves that share a row have found joined, one wave a row.
+template <class T, int WAVES>
 __global__ __launch_bounds__(64) void fb_token_join_kernel(TokenParams p)
 {
     __shared__ uint64_t best[FB_TOP_MAX];
@@ -305,16 +342,17 @@ __global__ __launch_bounds__(64) void fb_token_join_kernel(TokenParams p)
         write_padding(p, r, lane);
         return;
     }
-    const float *q = p.part + (size_t)r * p.split * 3;
+    const int lists = p.split * WAVES;
+    const float *q = p.part + (size_t)r * lists * 3;
     Stats st = {-kInf, 0.0f, 0.0f};
-    for (int c = lane; c < p.split; c += 64) st = join(st, {q[3 * c], q[3 * c + 1], q[3 * c + 2]});
+    for (int c = lane; c < lists; c += 64) st = join(st, {q[3 * c], q[3 * c + 1], q[3 * c + 2]});
 #pragma unroll
     for (int step = 1; step < 64; step <<= 1) {
         const Stats o = {__shfl_xor(st.m, step), __shfl_xor(st.S, step), __shfl_xor(st.T, step)};
         st = join(st, o);
     }
-    if (p.top) best_of_keys(p.part_top + (size_t)r * p.split * p.top, p.split * p.top, p.top, best);
-    __syncthreads();
+    if (p.top) merge_lists(p.part_top + (size_t)r * lists * p.top, lists, p.top, best);
+    lds_settled();
     write_row<T>(p, r, token, st, best, lane);
 }
 
@@ -381,6 +419,7 @@ struct TokenPlan {
     int64_t chunk;
 };
 
+constexpr int kSplitWaves = 4;      // of a workgroup that has a share of a row
 constexpr int kMostElements = 64;   // of a row, in a lane's registers
 
 TokenPlan token_plan(int64_t R, int64_t V, int type)
@@ -394,7 +433,7 @@ TokenPlan token_plan(int64_t R, int64_t V, int type)
         t.waves = 1;
         t.nv = (int)((vecs + one - 1) / one);
     } else {
-        t.waves = 4;
+        t.waves = kSplitWaves;
         int64_t split = (vecs + four * most - 1) / (four * most);
         // few rows: as many workgroups as the GPU has compute units, as long as each has 2 vectors a lane
         const int64_t fill = (kCUs + R - 1) / std::max<int64_t>(R, 1);
@@ -450,13 +489,13 @@ int launch_tokens(const TokenParams &p, const TokenPlan &t, hipStream_t stream)
 #undef FB_TOKENS
     int rc = launched("token log probability kernel launch: ");
     if (rc == FB_OK && p.split > 1) {
-        hipLaunchKernelGGL((fb_token_join_kernel<T>), dim3((unsigned)p.R), dim3(64), 0, stream, p);
+        hipLaunchKernelGGL((fb_token_join_kernel<T, kSplitWaves>), dim3((unsigned)p.R), dim3(64), 0, stream, p);
         rc = launched("token join kernel launch: ");
     }
     return rc;
 }
 
-size_t stats_bytes(int64_t R, int split) { return ((size_t)R * split * 3 * sizeof(float) + 255) & ~(size_t)255; }
+size_t stats_bytes(int64_t R, int split) { return ((size_t)R * split * kSplitWaves * 3 * sizeof(float) + 255) & ~(size_t)255; }
 
 int check_tokens(const char *who, const void *logits, int64_t ld, const int32_t *tokens, int64_t R, int64_t V, int type)
 {
@@ -479,7 +518,7 @@ size_t fb_token_logprobs_workspace_bytes(int64_t R, int64_t V, int type, int top
     using namespace fb;
     if (bad_rows(R) || bad_width(V) || !known_type(type) || top < 0 || top > FB_TOP_MAX || top > V) return 0;
     const TokenPlan t = token_plan(R, V, type);
-    return t.split == 1 ? 0 : stats_bytes(R, t.split) + (((size_t)R * t.split * top * sizeof(uint64_t) + 255) & ~(size_t)255);
+    return t.split == 1 ? 0 : stats_bytes(R, t.split) + (((size_t)R * t.split * kSplitWaves * top * sizeof(uint64_t) + 255) & ~(size_t)255);
 }
 
 int fb_token_logprobs(const void *logits, int64_t ld, const int32_t *tokens, int64_t R, int64_t V, int type, int top,
@@ -502,7 +541,7 @@ int fb_token_logprobs(const void *logits, int64_t ld, const int32_t *tokens, int
         p.split = t.split; p.chunk = t.chunk;
         p.part = (float *)ws;
         p.part_top = (uint64_t *)((char *)ws + (t.split > 1 ? stats_bytes(R, t.split) : 0));
-        if (R * t.split >= kMostSize) return fail(FB_EUNSUPPORTED, "fb_token_logprobs: more than 2^31 pieces of rows");
+        if (R * t.split * kSplitWaves >= kMostSize) return fail(FB_EUNSUPPORTED, "fb_token_logprobs: more than 2^31 pieces of rows");
         if (type == FB_TYPE_F32) return launch_tokens<float>(p, t, (hipStream_t)stream);
         if (type == FB_TYPE_BF16) return launch_tokens<bf16>(p, t, (hipStream_t)stream);
         return launch_tokens<f16>(p, t, (hipStream_t)stream);
