@@ -26,49 +26,83 @@ struct SlopeParams {
     int act;
     void *out;           // dz as the products take it, nullable
     float *part;         // [gridDim.y][N]: shares of the sums over rows, nullable
+    int lanes;           // a row: a power of two, 64 where the rows are wider than that many pieces
 };
 
-// dz = dy act'(z) (or a copy of dy in rows of whole pieces), rounded to the factors' type, and the sums of its columns before the rounding.  A thread has one piece of
-// the width and every fourth of a workgroup's rows.
+// dz = dy act'(z) (or a copy of dy in rows of whole pieces), rounded to the factors' type, and the sums of its columns before
+// the rounding.  A thread has one piece of the width; `lanes` threads have a row side by side, so narrow rows fill the waves
+// too, and kRowsAhead rows are asked for before the first is worked on.  The sums of a workgroup's threads over its rows are
+// added in a fixed order.
+constexpr int kRowsAhead = 4;
+
 template <class T, class D>
 __global__ __launch_bounds__(256) void fb_slope_kernel(SlopeParams p)
 {
     constexpr int VE = Vec<T>::kN, VD = Vec<D>::kN;
-    __shared__ float slots[4][64][VE + 1];
-    const int lane = threadIdx.x & 63, sub = threadIdx.x >> 6;
-    const int64_t at = ((int64_t)blockIdx.x * 64 + lane) * VE;
-    const int n = (int)(p.N - at < VE ? p.N - at : VE);
+    __shared__ float slots[256][VE + 1];
+    const int lane = threadIdx.x & (p.lanes - 1), sub = threadIdx.x / p.lanes, subs = 256 / p.lanes;
+    const int64_t at = ((int64_t)blockIdx.x * p.lanes + lane) * VE;
+    const int n = at >= p.N ? 0 : (int)(p.N - at < VE ? p.N - at : VE);
     float sum[VE] = {};
     if (n > 0) {
-        for (int64_t r = (int64_t)blockIdx.y * 4 + sub; r < p.M; r += (int64_t)gridDim.y * 4) {
-            float g[VE];
+        const int64_t step = (int64_t)gridDim.y * subs;
+        for (int64_t r0 = (int64_t)blockIdx.y * subs + sub; r0 < p.M; r0 += kRowsAhead * step) {
+            u32x4 rg[kRowsAhead][VE / VD], rz[kRowsAhead];
 #pragma unroll
-            for (int e = 0; e < VE; e += VD) unpack<D>(load_piece((const D *)p.dy + r * p.lddy + at + e, n - e), g + e);
-            if (p.act != FB_ACT_NONE) {
-                float z[VE];
-                unpack<T>(load_piece((const T *)p.z + r * p.ldz + at, n), z);
+            for (int u = 0; u < kRowsAhead; ++u) {
+                const int64_t r = r0 + u * step;
+                const int here = r < p.M ? n : 0;
 #pragma unroll
-                for (int e = 0; e < VE; ++e) g[e] = e < n ? g[e] * act_slope(z[e], p.act) : 0.0f;
+                for (int e = 0; e < VE / VD; ++e) rg[u][e] = load_piece((const D *)p.dy + r * p.lddy + at + e * VD, here - e * VD);
+                if (p.act != FB_ACT_NONE) rz[u] = load_piece((const T *)p.z + r * p.ldz + at, here);
             }
 #pragma unroll
-            for (int e = 0; e < VE; ++e) sum[e] += g[e];
-            if (p.out) store_piece((T *)p.out + r * p.ldo + at, VE, pack<T>(g));   // (rows of whole pieces)
+            for (int u = 0; u < kRowsAhead; ++u) {
+                const int64_t r = r0 + u * step;
+                float g[VE];
+#pragma unroll
+                for (int e = 0; e < VE / VD; ++e) unpack<D>(rg[u][e], g + e * VD);
+                if (p.act != FB_ACT_NONE) {
+                    float z[VE];
+                    unpack<T>(rz[u], z);
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) g[e] = e < n && r < p.M ? g[e] * act_slope(z[e], p.act) : 0.0f;
+                }
+#pragma unroll
+                for (int e = 0; e < VE; ++e) sum[e] += g[e];
+                if (p.out && r < p.M) store_piece((T *)p.out + r * p.ldo + at, VE, pack<T>(g));   // (rows of whole pieces)
+            }
         }
     }
     if (!p.part) return;
 #pragma unroll
-    for (int e = 0; e < VE; ++e) slots[sub][lane][e] = sum[e];
+    for (int e = 0; e < VE; ++e) slots[threadIdx.x][e] = sum[e];
     __syncthreads();
-    if (sub == 0) {
-#pragma unroll
-        for (int e = 0; e < VE; ++e)
-            if (e < n) p.part[(size_t)blockIdx.y * p.N + at + e] = (slots[0][lane][e] + slots[1][lane][e]) + (slots[2][lane][e] + slots[3][lane][e]);
+    for (int c = threadIdx.x; c < p.lanes * VE; c += 256) {
+        const int64_t col = (int64_t)blockIdx.x * p.lanes * VE + c;
+        if (col >= p.N) continue;
+        float s = 0.0f;
+        for (int i = 0; i < subs; ++i) s += slots[i * p.lanes + c / VE][c % VE];
+        p.part[(size_t)blockIdx.y * p.N + col] = s;
     }
 }
 
-constexpr int64_t kSlopeGroups = 256;   // shares of the rows
+// How that kernel is laid out: lanes a row, workgroups along the width and along the rows.
+struct SlopeLayout {
+    int lanes;
+    int64_t wide, down;
+};
 
-int64_t slope_groups(int64_t M) { return std::max<int64_t>(1, std::min<int64_t>((M + 3) / 4, kSlopeGroups)); }
+SlopeLayout slope_layout(int64_t M, int64_t N, int type)
+{
+    const int64_t ve = 16 / (int64_t)type_bytes(type), pieces = (N + ve - 1) / ve;
+    SlopeLayout s{};
+    for (s.lanes = 1; s.lanes < 64 && s.lanes < pieces;) s.lanes *= 2;
+    s.wide = (pieces + s.lanes - 1) / s.lanes;
+    const int64_t rows = 256 / s.lanes;      // at a time
+    s.down = std::max<int64_t>(1, std::min<int64_t>((M + rows - 1) / rows, std::max<int64_t>(64, 4 * kCUs / s.wide)));
+    return s;
+}
 
 size_t aligned(size_t n) { return (n + 255) & ~(size_t)255; }
 
@@ -128,20 +162,20 @@ int launch_product(const Product &q, hipStream_t stream)
 }
 
 template <class T, class D>
-int launch_slope(const SlopeParams &p, int64_t groups, hipStream_t stream)
+int launch_slope(const SlopeParams &p, const SlopeLayout &l, hipStream_t stream)
 {
-    const int64_t wide = 64 * Vec<T>::kN;
-    hipLaunchKernelGGL((fb_slope_kernel<T, D>), dim3((unsigned)((p.N + wide - 1) / wide), (unsigned)groups), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((fb_slope_kernel<T, D>), dim3((unsigned)l.wide, (unsigned)l.down), dim3(256), 0, stream, p);
     return launched("activation slope kernel launch: ");
 }
 
-int launch_slope(const SlopeParams &p, int type, int dy_type, hipStream_t stream)
+int launch_slope(SlopeParams p, int type, int dy_type, hipStream_t stream)
 {
-    const int64_t groups = slope_groups(p.M);
-    if (type == FB_TYPE_F32) return launch_slope<float, float>(p, groups, stream);
+    const SlopeLayout l = slope_layout(p.M, p.N, type);
+    p.lanes = l.lanes;
+    if (type == FB_TYPE_F32) return launch_slope<float, float>(p, l, stream);
     if (type == FB_TYPE_BF16)
-        return dy_type == type ? launch_slope<bf16, bf16>(p, groups, stream) : launch_slope<bf16, float>(p, groups, stream);
-    return dy_type == type ? launch_slope<f16, f16>(p, groups, stream) : launch_slope<f16, float>(p, groups, stream);
+        return dy_type == type ? launch_slope<bf16, bf16>(p, l, stream) : launch_slope<bf16, float>(p, l, stream);
+    return dy_type == type ? launch_slope<f16, f16>(p, l, stream) : launch_slope<f16, float>(p, l, stream);
 }
 
 int64_t whole_pieces(int64_t width, int type)
@@ -169,7 +203,7 @@ Packed packed(const void *p, int64_t ld, int64_t rows, int64_t width, int type)
 int launch_pack(const Packed &k, const void *p, int64_t ld, int64_t rows, int64_t width, int type, void *to, hipStream_t stream)
 {
     if (!k.copy || rows == 0) return FB_OK;
-    const SlopeParams s{p, nullptr, ld, 0, rows, width, k.ld, FB_ACT_NONE, to, nullptr};
+    const SlopeParams s{p, nullptr, ld, 0, rows, width, k.ld, FB_ACT_NONE, to, nullptr, 0};
     return launch_slope(s, type, type, stream);
 }
 
@@ -217,7 +251,7 @@ GradPlan grad_plan(const void *dy, int64_t lddy, int dy_type, const void *x, int
     g.dz = g.slope ? aligned((size_t)M * (size_t)g.ldz * type_bytes(type)) : 0;
     g.x = packed(x, ldx, M, K, type);
     g.w = packed(weight, ldw, N, K, type);
-    g.sums = aligned((size_t)slope_groups(M) * (size_t)N * sizeof(float));
+    g.sums = aligned((size_t)slope_layout(M, N, type).down * (size_t)N * sizeof(float));
     g.part = std::max(product_bytes(g.dx), product_bytes(g.dw));
     g.bytes = g.dz + g.x.bytes + g.w.bytes + g.sums + g.part;
     return g;
@@ -306,10 +340,10 @@ int fb_affine_grad(const void *dy, int64_t lddy, int dy_type, const void *x, int
         float *sums = (float *)(wts + g.w.bytes), *part = (float *)(wts + g.w.bytes + g.sums);
         const bool make = g.slope && (dx || dweight);
         if (M > 0 && (make || dbias)) {
-            const SlopeParams p{dy, preact, lddy, ldp, M, N, g.ldz, act, make ? dz : nullptr, dbias ? sums : nullptr};
+            const SlopeParams p{dy, preact, lddy, ldp, M, N, g.ldz, act, make ? dz : nullptr, dbias ? sums : nullptr, 0};
             if ((rc = launch_slope(p, type, dy_type, st)) != FB_OK) return rc;
         }
-        if (dbias && (rc = launch_column_sum(sums, M > 0 ? slope_groups(M) : 0, N, 1, dbias, nullptr, stream)) != FB_OK) return rc;
+        if (dbias && (rc = launch_column_sum(sums, M > 0 ? slope_layout(M, N, type).down : 0, N, 1, dbias, nullptr, stream)) != FB_OK) return rc;
         const Factor d{make ? (const void *)dz : dy, make ? g.ldz : lddy, true};
         if (dx) {
             if (M > 0 && (rc = launch_pack(g.w, weight, ldw, N, K, type, wts, st)) != FB_OK) return rc;

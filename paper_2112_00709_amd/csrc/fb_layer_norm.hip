@@ -15,15 +15,21 @@ struct NormParams {
     float *part;                   // gradient: [workgroup][2][H], shares of dweight and dbias
 };
 
-// Vectors of EPL floats of [H], at the places a lane has of a row.
+// EPL elements of a vector of [H] as floats, at the places a lane has of a row; `none` where there is no vector.
 template <class W, int EPL, int VE>
 __device__ __forceinline__ void load_vector(const void *w, int H, int step, int lane, float none, float *v)
 {
+    constexpr int kN = Vec<W>::kN;
 #pragma unroll
     for (int i = 0; i < EPL / VE; ++i) {
         const int at = (i * step + lane) * VE;
 #pragma unroll
-        for (int j = 0; j < VE; ++j) v[i * VE + j] = w && at + j < H ? (float)((const W *)w)[at + j] : none;
+        for (int j = 0; j < VE; j += kN) {
+            float u[kN];
+            unpack<W>(w ? load_piece((const W *)w + at + j, H - at - j) : u32x4{}, u);
+#pragma unroll
+            for (int e = 0; e < kN; ++e) v[i * VE + j + e] = w ? u[e] : none;
+        }
     }
 }
 
@@ -166,11 +172,14 @@ __global__ __launch_bounds__(1024) void fb_layer_norm_long_kernel(NormParams p)
 }
 
 // dx of a row, and the row's share of dweight and dbias added to sums that the lane keeps in registers for its places of
-// the row over all rows it sees; they leave the kernel once, a row of sums a workgroup, for fb_column_sum_kernel.
+// the row over all rows it sees; they leave the kernel once, a row of sums a workgroup, for fb_column_sum_kernel.  The next row
+// is asked for before this one is worked on and the weight kept in registers, except where 16 elements a lane in 16 waves
+// leave no registers for either (65 to 94 of them would go to memory).
 template <class T, class W, int WAVES, int EPL>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void fb_layer_norm_grad_kernel(NormParams p)
 {
     constexpr int VE = Vec<T>::kN, NV = EPL / VE, kStep = WAVES * 64;
+    constexpr bool kLean = WAVES * EPL >= 256;
     __shared__ float slots[2][WAVES][2];
     __shared__ float joined[WAVES == 1 ? 4 : 1][WAVES == 1 ? EPL * 64 : 1];
     const int lane = WAVES == 1 ? (threadIdx.x & 63) : threadIdx.x;
@@ -178,8 +187,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void fb_layer_norm_g
     const int H = (int)p.H;
     const int64_t r0 = WAVES == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x;
     const int64_t rstep = WAVES == 1 ? (int64_t)gridDim.x * 4 : (int64_t)gridDim.x;
-    float w[EPL], dw[EPL], db[EPL];
-    load_vector<W, EPL, VE>(p.weight, H, kStep, lane, 1.0f, w);
+    float w[kLean ? 1 : EPL], dw[EPL], db[EPL];
+    if constexpr (!kLean) load_vector<W, EPL, VE>(p.weight, H, kStep, lane, 1.0f, w);
 #pragma unroll
     for (int i = 0; i < EPL; ++i) dw[i] = db[i] = 0.0f;
     const float inv = 1.0f / (float)H;
@@ -196,26 +205,32 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void fb_layer_norm_g
         mean = p.mean[r];
         rstd = p.rstd[r];
     };
-    if (r0 < p.R) ask(r0);
+    if (!kLean && r0 < p.R) ask(r0);
     int slot = 0;
     for (int64_t r = r0; r < p.R; r += rstep, slot ^= 1) {
         float xh[EPL], g[EPL];
+        if (kLean) ask(r);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             unpack<T>(rx[i], xh + i * VE);
             unpack<T>(rg[i], g + i * VE);
         }
         const float m = mean, s = rstd;
-        if (r + rstep < p.R) ask(r + rstep);
+        if (!kLean && r + rstep < p.R) ask(r + rstep);
         float t[2] = {0.0f, 0.0f};                      // (past the row's end dy is 0, and with it every share)
 #pragma unroll
-        for (int i = 0; i < EPL; ++i) {
-            xh[i] = (xh[i] - m) * s;
-            dw[i] = fmaf(g[i], xh[i], dw[i]);
-            db[i] += g[i];
-            g[i] *= w[i];
-            t[0] += g[i];
-            t[1] = fmaf(g[i], xh[i], t[1]);
+        for (int v = 0; v < NV; ++v) {
+            float wv[VE];
+            if constexpr (kLean) load_vector<W, VE, VE>(p.weight, H, 0, v * kStep + lane, 1.0f, wv);
+#pragma unroll
+            for (int i = v * VE; i < (v + 1) * VE; ++i) {
+                xh[i] = (xh[i] - m) * s;
+                dw[i] = fmaf(g[i], xh[i], dw[i]);
+                db[i] += g[i];
+                g[i] *= kLean ? wv[i - v * VE] : w[kLean ? 0 : i];
+                t[0] += g[i];
+                t[1] = fmaf(g[i], xh[i], t[1]);
+            }
         }
         if (p.y) {
             sum_row<WAVES, 2>(t, slots, slot);
@@ -366,15 +381,13 @@ int launch_column_sum(const float *part, int64_t P, int64_t C, int sets, float *
 
 namespace {
 
-// Longest rows that a workgroup holds in registers (the gradient of 16 elements a lane in 16 waves does not fit: 65 to 94 of
-// its registers would go to memory).
-constexpr int64_t kRowMax = 16384, kGradRowMax = 8192;
+constexpr int64_t kRowMax = 16384;       // longest row that a workgroup holds in registers
 constexpr int64_t kGradGroups = 512;     // workgroups of the gradient kernel: two a compute unit
-constexpr int64_t kLongRowGroups = 64;   // workgroups that share the rows of a piece of width
+constexpr int64_t kLongRowGroups = 128;  // workgroups that share the rows of a piece of width
 
 int64_t grad_groups(int64_t R, int64_t H)
 {
-    if (H > kGradRowMax) return std::min<int64_t>(R, kLongRowGroups);
+    if (H > kRowMax) return std::min<int64_t>(R, kLongRowGroups);
     return std::min<int64_t>(H <= 1024 ? (R + 3) / 4 : R, kGradGroups);
 }
 
@@ -384,8 +397,7 @@ int launch_norm(const NormParams &p, bool grad, hipStream_t stream)
     const int64_t groups = WAVES == 1 ? (p.R + 3) / 4 : p.R;
     const dim3 block(WAVES == 1 ? 256 : WAVES * 64);
     if (grad) {
-        if constexpr (WAVES * EPL < 256)
-            hipLaunchKernelGGL((fb_layer_norm_grad_kernel<T, W, WAVES, EPL>), dim3((unsigned)grad_groups(p.R, p.H)), block, 0, stream, p);
+        hipLaunchKernelGGL((fb_layer_norm_grad_kernel<T, W, WAVES, EPL>), dim3((unsigned)grad_groups(p.R, p.H)), block, 0, stream, p);
     } else {
         const int64_t most = (int64_t)kCUs * (WAVES == 16 ? 2 : 8);
         hipLaunchKernelGGL((fb_layer_norm_kernel<T, W, WAVES, EPL>), dim3((unsigned)std::min(groups, most)), block, 0, stream, p);
@@ -403,7 +415,7 @@ int launch_norm(const NormParams &p, bool grad, hipStream_t stream)
     if (H <= 2048) return launch_norm<T, W, 4, 8>(p, grad, stream);
     if (H <= 4096) return launch_norm<T, W, 4, 16>(p, grad, stream);
     if (H <= 8192) return launch_norm<T, W, 16, 8>(p, grad, stream);
-    if (H <= kRowMax && !grad) return launch_norm<T, W, 16, 16>(p, grad, stream);
+    if (H <= kRowMax) return launch_norm<T, W, 16, 16>(p, grad, stream);
     if (!grad) {
         hipLaunchKernelGGL((fb_layer_norm_long_kernel<T, W>), dim3((unsigned)std::min<int64_t>(p.R, 2 * kCUs)), dim3(1024), 0, stream, p);
         return launched("layer norm kernel launch: ");

@@ -110,32 +110,48 @@ __device__ __forceinline__ void merge_lists(const uint64_t *keys, int lists, int
 // The best `top` of the elements that a wave holds pieces of (in memory: piece i of a lane starts at element first + i * stride
 // of n), as keys, descending, to out[0 .. top) in LDS; peak[i] is the largest element of the lane's piece i.  The top-th
 // largest of the lanes' own maxima bounds the top-th best from below; what reaches it are few elements (about `top`) of few
-// pieces, which are read once more, put on a list and ranked there, one a lane.  Where ties, or rows of almost nothing but
-// -inf, make them more than 64 the elements are searched once per place.  (From memory: the pieces in registers, indexed at
-// run time, would take a copy of all this per element; up to four are chosen from by selects.)
+// pieces, which are read once more, put on a list and ranked there, one a lane.  Where fewer than `top` lanes have an element
+// above -inf, all such elements go to the list, and the places behind them to the first of the others.  Where ties make a
+// list longer than 64 the elements are searched once per place.  (From memory: the pieces in registers, indexed at
+// run time, would take a copy of all this per element; one of two is chosen by a select.)
 template <class T, int NV>
 __device__ __forceinline__ void best_of_wave(const T *row, const u32x4 (&raw)[NV], const float (&peak)[NV], float lane_max, int first, int stride, int n, int top, uint64_t *list, uint64_t *out)
 {
     constexpr int VE = Vec<T>::kN;
     const int lane = threadIdx.x & 63;
-    float cur = lane_max, bound = -kInf;
-    for (int found = 0; found < top;) {
-        bound = max_wave(cur);
-        const uint64_t hit = __ballot(cur == bound);
-        if (bound == -kInf || hit == 0) break;
-        found += __popcll(hit);
-        if (cur == bound) cur = -kInf;
+    // few are taken one after the other; for more their order's bits are found one by one, a comparison and a count each
+    float bound = -kInf;
+    if (top <= 6) {
+        float cur = lane_max;
+        for (int found = 0; found < top;) {
+            bound = max_wave(cur);
+            const uint64_t hit = __ballot(cur == bound);
+            if (bound == -kInf || hit == 0) break;
+            found += __popcll(hit);
+            if (cur == bound) cur = -kInf;
+        }
+    } else {
+        const uint32_t mine = order_of(lane_max);
+        uint32_t least = 0;
+#pragma unroll
+        for (int bit = 31; bit >= 0; --bit) {
+            const uint32_t with = least | 1u << bit;
+            least = __popcll(__ballot(mine >= with)) >= top ? with : least;
+        }
+        bound = value_of(least);
     }
+    const bool few = bound == -kInf;
+    auto reaches = [&](float x) { return few ? x > -kInf : x >= bound; };
     uint32_t pieces = 0;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) pieces |= peak[i] >= bound ? 1u << i : 0u;
+    for (int i = 0; i < NV; ++i) pieces |= reaches(peak[i]) ? 1u << i : 0u;
     int count = 0;
     while (count <= 64 && __ballot(pieces != 0) != 0) {
         const int at = first + (pieces ? __ffs(pieces) - 1 : 0) * stride;
         const int left = pieces ? n - at : 0;
         pieces &= pieces - 1;
         float v[VE];
-        if constexpr (NV <= 4) {
+        if constexpr (NV <= 2) {
             u32x4 piece = raw[0];
 #pragma unroll
             for (int i = 1; i < NV; ++i) piece = at == first + i * stride ? raw[i] : piece;
@@ -145,7 +161,7 @@ __device__ __forceinline__ void best_of_wave(const T *row, const u32x4 (&raw)[NV
         }
 #pragma unroll
         for (int j = 0; j < VE; ++j) {
-            const uint64_t hit = __ballot(j < left && v[j] >= bound);
+            const uint64_t hit = __ballot(j < left && reaches(v[j]));
             const int at_list = count + __popcll(hit & ((1ull << lane) - 1));
             if ((hit >> lane & 1) && at_list < 64) list[at_list] = key_of(v[j], (uint32_t)(at + j));
             count += __popcll(hit);
@@ -162,12 +178,24 @@ __device__ __forceinline__ void best_of_wave(const T *row, const u32x4 (&raw)[NV
         }
         if (lane < count && rank < top) out[rank] = mine;
         if (lane >= count && lane < top) out[lane] = 0;
+        if (few) {                                            // (a wave's first pieces lie side by side, 256 elements and more)
+            const int start = __builtin_amdgcn_readfirstlane(first);
+            int filled = count;
+            for (int i = 0; i < 128 && filled < top && start + i < n; i += 64) {
+                const int at = start + i + lane;
+                const bool low = at < n && !(load_one(row + (at < n ? at : 0)) > -kInf);
+                const uint64_t hit = __ballot(low);
+                const int to = filled + __popcll(hit & ((1ull << lane) - 1));
+                if (low && to < top) out[to] = key_of(-kInf, (uint32_t)at);
+                filled += __popcll(hit);
+            }
+        }
         return;
     }
     uint64_t last = ~0ull;
     for (int t = 0; t < top; ++t) {
         uint64_t best = 0;
-#pragma unroll 1
+#pragma unroll 4
         for (int i = 0; i < NV; ++i) {
             float v[VE];
             const int at = first + i * stride;
@@ -262,7 +290,7 @@ __device__ __forceinline__ Stats wave_stats(u32x4 (&raw)[NV], int first, int str
 
 // WAVES waves hold a row, or a workgroup's chunk of one (SPLIT); with one wave a row a workgroup has four rows at a time.
 template <class T, int WAVES, int NV, bool SPLIT>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64, NV * Vec<T>::kN <= 16 ? 8 : NV * Vec<T>::kN <= 32 ? 6 : 4) void fb_token_logprobs_kernel(TokenParams p)
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64, NV * Vec<T>::kN <= 16 ? 8 : 4) void fb_token_logprobs_kernel(TokenParams p)
 {
     constexpr int VE = Vec<T>::kN, kRows = WAVES == 1 ? 4 : 1, kW = WAVES == 1 ? 4 : WAVES;
     __shared__ uint64_t list[kW][64], best[kW][FB_TOP_MAX];
@@ -281,13 +309,14 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64, NV * Vec<T>::kN <= 1
     const int64_t at0 = SPLIT ? c * p.chunk : 0;
     const int n = (int)((SPLIT ? (p.V - at0 < p.chunk ? p.V - at0 : p.chunk) : p.V));
     const T *row = (const T *)p.logits + r * p.ld + at0;
-    const int first = ((WAVES == 1 ? 0 : wave) * NV * 64 + lane) * VE;   // a wave's pieces lie side by side
+    const int first = ((WAVES == 1 ? 0 : wave) * 64 + lane) * VE;
+    constexpr int kStride = WAVES * 64 * VE;                  // (waves take turns: all of them have a share of a short row)
     u32x4 raw[NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) raw[i] = load_piece(row + first + i * 64 * VE, n - (first + i * 64 * VE));
+    for (int i = 0; i < NV; ++i) raw[i] = load_piece(row + first + i * kStride, n - (first + i * kStride));
     float peak[NV], lane_max;
-    Stats st = wave_stats<T, NV>(raw, first, 64 * VE, n, peak, lane_max);
-    if (p.top) best_of_wave<T, NV>(row, raw, peak, lane_max, first, 64 * VE, n, p.top, list[wave], best[wave]);
+    Stats st = wave_stats<T, NV>(raw, first, kStride, n, peak, lane_max);
+    if (p.top) best_of_wave<T, NV>(row, raw, peak, lane_max, first, kStride, n, p.top, list[wave], best[wave]);
     lds_settled();
     const uint64_t *keys = best[wave];
     if constexpr (SPLIT) {
@@ -328,6 +357,74 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64, NV * Vec<T>::kN <= 1
         }
     }
     write_row<T>(p, r, token, st, keys, lane);
+}
+
+// Rows of up to 512 elements: a wave a row, element 64 j + lane in the lane's j-th register (narrow loads, but all lanes have
+// their share).  The top-th largest is found bit by bit of its order, exactly; what lies above it and as many of its equals
+// as there is room for, in ascending order of their numbers, are ranked one a lane.
+template <class T, int E>
+__global__ __launch_bounds__(256) void fb_token_short_kernel(TokenParams p)
+{
+    __shared__ uint64_t list[4][FB_TOP_MAX], best[4][FB_TOP_MAX];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t r = (int64_t)blockIdx.x * 4 + wave;
+    if (r >= p.R) return;                                     // (a whole wave)
+    const int32_t token = p.tokens[r];
+    if (token < 0) {
+        write_padding(p, r, lane);
+        return;
+    }
+    const int n = (int)p.V;
+    const T *row = (const T *)p.logits + r * p.ld;
+    float v[E], m = -kInf;
+#pragma unroll
+    for (int j = 0; j < E; ++j) v[j] = j * 64 + lane < n ? load_one(row + j * 64 + lane) : -kInf;
+#pragma unroll
+    for (int j = 0; j < E; ++j) m = fmaxf(m, v[j]);
+    m = max_wave(m);
+    const float base = m == -kInf ? 0.0f : m;
+    float S = 0.0f, U = 0.0f;
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+        const float d = v[j] - base, e = __builtin_amdgcn_exp2f(d * kLog2E);
+        S += e;
+        U = fmaf(e, fmaxf(d, -1e30f), U);                     // (e is 0 where d is -inf)
+    }
+    const Stats st = {m, sum_wave(S), sum_wave(U)};
+    if (p.top) {
+        uint32_t order[E], least = 0;
+#pragma unroll
+        for (int j = 0; j < E; ++j) order[j] = j * 64 + lane < n ? order_of(v[j]) : 0;   // (0: below every number)
+        for (int bit = 31; bit >= 0; --bit) {
+            const uint32_t with = least | 1u << bit;
+            int count = 0;
+#pragma unroll
+            for (int j = 0; j < E; ++j) count += __popcll(__ballot(order[j] >= with));
+            least = count >= p.top ? with : least;
+        }
+        int filled = 0;
+#pragma unroll
+        for (int equal = 0; equal < 2; ++equal)
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                const bool in = equal ? order[j] == least : order[j] > least;
+                const uint64_t hit = __ballot(in);
+                const int at = filled + __popcll(hit & ((1ull << lane) - 1));
+                if (in && at < p.top) list[wave][at] = (uint64_t)order[j] << 32 | (uint32_t)~(uint32_t)(j * 64 + lane);
+                filled += __popcll(hit);
+            }
+        lds_settled();
+        const uint64_t mine = lane < p.top ? list[wave][lane] : 0;
+        int rank = 0;
+        for (int c = 0; c < p.top; ++c) {
+            const uint64_t k = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(mine >> 32), c) << 32 |
+                               (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)mine, c);
+            rank += k > mine ? 1 : 0;
+        }
+        if (lane < p.top) best[wave][rank] = mine;
+        lds_settled();
+    }
+    write_row<T>(p, r, token, st, best[wave], lane);
 }
 
 // What the waves that share a row have found joined, one wave a row.
@@ -411,7 +508,7 @@ __global__ __launch_bounds__(256) void fb_token_logprobs_grad_kernel(TokenGradPa
     }
 }
 
-// How a call is laid out.  A wave holds up to 64 elements a lane: rows of up to 4096 elements go to a wave each where there
+// How a call is laid out.  Rows of up to 512 elements have a kernel of their own (waves = 0).  Otherwise a wave holds up to 64 elements a lane: rows of up to 4096 elements go to a wave each where there
 // are enough of them to fill the GPU, else to four waves; rows that four waves cannot hold are split over workgroups,
 // and so are long rows that are few.
 struct TokenPlan {
@@ -428,6 +525,7 @@ TokenPlan token_plan(int64_t R, int64_t V, int type)
     const int64_t vecs = (V + ve - 1) / ve, most = kMostElements / ve;
     TokenPlan t{};
     t.split = 1;
+    if (V <= 512) return t;
     const int64_t one = 64, four = 256;
     if (vecs <= one * 2 || (vecs <= one * most && R >= 4 * kCUs)) {
         t.waves = 1;
@@ -466,6 +564,18 @@ void launch_tokens(const TokenParams &p, hipStream_t stream)
 template <class T>
 int launch_tokens(const TokenParams &p, const TokenPlan &t, hipStream_t stream)
 {
+    if (t.waves == 0) {
+        const dim3 grid((unsigned)((p.R + 3) / 4)), block(256);
+        if (p.V <= 64)
+            hipLaunchKernelGGL((fb_token_short_kernel<T, 1>), grid, block, 0, stream, p);
+        else if (p.V <= 128)
+            hipLaunchKernelGGL((fb_token_short_kernel<T, 2>), grid, block, 0, stream, p);
+        else if (p.V <= 256)
+            hipLaunchKernelGGL((fb_token_short_kernel<T, 4>), grid, block, 0, stream, p);
+        else
+            hipLaunchKernelGGL((fb_token_short_kernel<T, 8>), grid, block, 0, stream, p);
+        return launched("token log probability kernel launch: ");
+    }
 #define FB_TOKENS(W, N) launch_tokens<T, W, N>(p, stream)
     if (t.waves == 1) {
         switch (t.nv) {

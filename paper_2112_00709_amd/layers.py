@@ -244,7 +244,7 @@ def fb_token_logprobs(logits, tokens, top: int = 0):
     if tokens.shape != lead:
         raise ValueError("tokens must have the leading shape of logits")
     pt = _vector(tokens, "tokens", R, (torch.int32,), dev)
-    lp, ent, z = (_out(logits, lead, torch.float32) for _ in range(3))
+    lp, ent, z = _out(logits, (3, *lead), torch.float32).unbind(0)
     ids, best = _out(logits, (*lead, max(top, 0)), torch.int32), _out(logits, (*lead, max(top, 0)), torch.float32)
     need = int(L.fb_token_logprobs_workspace_bytes(R, V, code, top))
     ws, pws = _workspace(need, logits)
