@@ -1,4 +1,4 @@
-"""LF-MMI objective as a differentiable PyTorch function on the GPU.
+"""LF-MMI objective and a network's last layers as differentiable PyTorch functions on the GPU.
 
 The network's output (pseudo-log-likelihoods, Sec. 3 of the paper) goes in, the
 objective of Eq. 16 comes out; its derivative with respect to every network
@@ -8,6 +8,11 @@ incoming gradient in the backward call.  Splitting a batch into sub-batches and
 calling ``backward`` once per sub-batch accumulates the parameter gradients of
 the whole batch (the B/F scheme of the paper's training recipe), since the
 objective is a sum over utterances.
+
+``layer_norm``, ``affine`` and ``token_logprobs`` are the operators of
+``paper_2112_00709_amd.layers`` with their gradients: what makes the network's
+output from hidden frames and takes the objective's derivative back into the
+weights, and the frame log probabilities that recipes use beside it.
 """
 from __future__ import annotations
 
@@ -62,3 +67,92 @@ def lfmmi_loss(emis, lengths, den: Graph, num: Graph, ws: Optional[object] = Non
 def workspace(den: Graph, num: Graph, B: int, N: int, D: int, device="cuda"):
     torch = _torch()
     return torch.empty((fb_lfmmi_workspace_bytes(den, num, B, N, D),), dtype=torch.uint8, device=device)
+
+
+# ----------------------------------------------------------------- a network's last layers
+
+_layer_fns = None
+
+
+def _layer_functions():
+    global _layer_fns
+    if _layer_fns is not None:
+        return _layer_fns
+    torch = _torch()
+    from torch.autograd.function import once_differentiable
+
+    from . import layers as fl
+
+    class _LayerNorm(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, weight, bias, eps):
+            y, mean, rstd = fl.fb_layer_norm(x, weight, bias, eps, want_stats=True)
+            ctx.save_for_backward(x, weight, mean, rstd)
+            ctx.bias_dtype = None if bias is None else bias.dtype
+            return y
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, dy):
+            x, weight, mean, rstd = ctx.saved_tensors
+            dx, dw, db = fl.fb_layer_norm_grad(dy.contiguous(), x, mean, rstd, weight, ctx.needs_input_grad[0], ctx.needs_input_grad[1],
+                                               ctx.needs_input_grad[2])
+            return dx, None if dw is None else dw.to(weight.dtype), None if db is None else db.to(ctx.bias_dtype), None
+
+    class _Affine(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, weight, bias, residual, activation, out_dtype):
+            keep = activation != "none" and any(ctx.needs_input_grad[:3])
+            out = fl.fb_affine(x, weight, bias, activation, residual, out_dtype, want_preact=keep)
+            y, preact = out if keep else (out, None)
+            ctx.save_for_backward(x, weight, preact)
+            ctx.activation = activation
+            return y
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, dy):
+            x, weight, preact = ctx.saved_tensors
+            dy = dy.contiguous()
+            dx = dw = db = None
+            if any(ctx.needs_input_grad[:3]):
+                dx, dw, db = fl.fb_affine_grad(dy, x, weight, ctx.activation, preact, *ctx.needs_input_grad[:3])
+            return dx, dw, db, dy if ctx.needs_input_grad[3] else None, None, None
+
+    class _TokenLogprobs(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, logits, tokens, top):
+            logprobs, entropy, logz, ids, best = fl.fb_token_logprobs(logits, tokens, top)
+            ctx.save_for_backward(logits, tokens, logz, entropy)
+            ctx.mark_non_differentiable(logz, ids, best)
+            ctx.set_materialize_grads(False)
+            return logprobs, entropy, logz, ids, best
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, g_logprobs, g_entropy, _g_logz, _g_ids, _g_best):
+            if g_logprobs is None and g_entropy is None:
+                return None, None, None
+            logits, tokens, logz, entropy = ctx.saved_tensors
+            g = [None if t is None else t.contiguous() for t in (g_logprobs, g_entropy)]
+            return fl.fb_token_logprobs_grad(logits, tokens, logz, entropy, *g), None, None
+
+    _layer_fns = _LayerNorm, _Affine, _TokenLogprobs
+    return _layer_fns
+
+
+def layer_norm(x, weight=None, bias=None, eps: float = 1e-5):
+    """``layers.fb_layer_norm`` with its gradient with respect to x, weight and bias."""
+    return _layer_functions()[0].apply(x, weight, bias, eps)
+
+
+def affine(x, weight, bias=None, activation: str = "none", residual=None, out_dtype=None):
+    """``layers.fb_affine`` with its gradient with respect to x, weight, bias and residual.  With an activation the forward
+    call keeps what it was applied to, rounded to x's type."""
+    return _layer_functions()[1].apply(x, weight, bias, residual, activation, out_dtype)
+
+
+def token_logprobs(logits, tokens, top: int = 0):
+    """``layers.fb_token_logprobs`` -> (logprobs, entropy, logz, top_ids, top_logprobs); the first two have gradients with
+    respect to the logits, the others do not."""
+    return _layer_functions()[2].apply(logits, tokens, top)
