@@ -14,8 +14,8 @@
  *
  * Rows are frames.  A matrix is given by its first element and the distance between rows in elements (`ld`); the elements of
  * a row are contiguous.  Rows may start at any element: no alignment beyond the element's own is asked for (workspaces: 256
- * bytes).  Row counts may be 0 (sums over no rows are 0); widths are at least 1; counts and distances are below 2^31 and
- * sizes in elements may exceed 2^32.
+ * bytes).  Row counts may be 0 (sums over no rows are 0) and are below 2^31, as are row distances; widths are at least 1 and
+ * below 2^28.  A matrix may have more than 2^32 elements.
  *
  * Types: FB_TYPE_F32, FB_TYPE_BF16, FB_TYPE_F16.  Sums, statistics and the products' accumulators are single precision
  * whatever the type, and a result is rounded once, when it is stored, unless a call says otherwise.
@@ -75,7 +75,8 @@ size_t fb_affine_workspace_bytes(const void *x, int64_t ldx, const void *weight,
  *   y         out, [M][N] of `out_type`, `type` or FB_TYPE_F32; may be residual
  *   preact    out, [M][N] of `type`, nullable: z, rounded (what fb_affine_grad takes)
  * FB_EINVAL: x, weight or y NULL, sizes or row distances out of range, an unknown type or activation, the workspace
- * missing or too small.
+ * missing or too small.  FB_EUNSUPPORTED: for M > 64, rows of x or weight longer than 4 MB or rows of y, residual or preact 2^27
+ * elements apart or more; for M <= 64, N of 2^26 and more.
  */
 int fb_affine(const void *x, int64_t ldx, const void *weight, int64_t ldw, const float *bias, const void *residual, int64_t ldr,
               int64_t M, int64_t N, int64_t K, int type, int act, void *y, int64_t ldy, int out_type, void *preact, int64_t ldp,
@@ -93,7 +94,7 @@ size_t fb_affine_grad_workspace_bytes(const void *dy, int64_t lddy, int dy_type,
  *   dx       out, [M][K] of `type`, nullable;  dweight out, [N][K] of `type`, contiguous, nullable;  dbias out, float [N], nullable
  * Where `type` has 16 bits the matrix units take dz in it: it is rounded to `type` before the two products if act or dy_type
  * makes it anything else (an error of the size of the outputs' own rounding); dbias is summed before that.
- * Errors as fb_affine; dy, x and weight must not be NULL.
+ * Errors as fb_affine (the limits for M > 64 hold for every M, dy among them); dy, x and weight must not be NULL.
  */
 int fb_affine_grad(const void *dy, int64_t lddy, int dy_type, const void *x, int64_t ldx, const void *weight, int64_t ldw,
                    const void *preact, int64_t ldp, int64_t M, int64_t N, int64_t K, int type, int act, void *dx, int64_t lddx,

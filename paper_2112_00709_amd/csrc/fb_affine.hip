@@ -207,6 +207,10 @@ int launch_pack(const Packed &k, const void *p, int64_t ld, int64_t rows, int64_
     return launch_slope(s, type, type, stream);
 }
 
+// What the matrix units' kernel addresses in 32 bits: 64 or 128 rows of a factor, 16 rows of what it stores or adds.
+bool too_long(int64_t width, int type) { return width * (int64_t)type_bytes(type) > (int64_t)1 << 22; }
+bool too_far(int64_t ld) { return ld >= (int64_t)1 << 27; }
+
 bool bad_sizes(int64_t M, int64_t N, int64_t K) { return bad_rows(M) || bad_width(N) || bad_width(K); }
 
 struct ForwardPlan {
@@ -292,6 +296,8 @@ int fb_affine(const void *x, int64_t ldx, const void *weight, int64_t ldw, const
         if (out_type != type && out_type != FB_TYPE_F32) return fail(FB_EINVAL, "fb_affine: the output's type is neither float nor the factors'");
         if (!y && M > 0) return fail(FB_EINVAL, "fb_affine: y is NULL");
         if (bad_ld(ldy, N) || (residual && bad_ld(ldr, N)) || (preact && bad_ld(ldp, N))) return fail(FB_EINVAL, "fb_affine: rows closer than N elements");
+        if (M > kFewRows ? too_long(K, type) || too_far(ldy) || (residual && too_far(ldr)) || (preact && too_far(ldp)) : N >= (int64_t)1 << 26)
+            return fail(FB_EUNSUPPORTED, "fb_affine: rows of x and weight longer than 4 MB, rows of y, residual or preact 2^27 elements apart, or (M <= 64) N of 2^26 and more");
         const ForwardPlan f = forward_plan(x, ldx, weight, ldw, M, N, K, type);
         if (f.bytes && (!ws || ws_bytes < f.bytes)) return fail(FB_EINVAL, "fb_affine: workspace missing or too small");
         hipStream_t st = (hipStream_t)stream;
@@ -333,6 +339,8 @@ int fb_affine_grad(const void *dy, int64_t lddy, int dy_type, const void *x, int
         if (act != FB_ACT_NONE && !preact && M > 0) return fail(FB_EINVAL, "fb_affine_grad: this activation needs preact");
         if (bad_ld(lddy, N) || (act != FB_ACT_NONE && bad_ld(ldp, N)) || (dx && bad_ld(lddx, K))) return fail(FB_EINVAL, "fb_affine_grad: rows closer than their width");
         if (!dx && !dweight && !dbias) return FB_OK;
+        if (too_long(K, type) || too_long(N, type) || (dx && too_far(lddx)))
+            return fail(FB_EUNSUPPORTED, "fb_affine_grad: rows of x, weight and dy longer than 4 MB, or rows of dx 2^27 elements apart");
         GradPlan g = grad_plan(dy, lddy, dy_type, x, ldx, weight, ldw, M, N, K, type, act);
         if (!ws || ws_bytes < g.bytes) return fail(FB_EINVAL, "fb_affine_grad: workspace missing or too small");
         hipStream_t st = (hipStream_t)stream;

@@ -171,9 +171,9 @@ __device__ __forceinline__ uint32_t min_wave_u(uint32_t v)
 // Host side: argument checks that the calls share.
 inline bool known_type(int t) { return t == FB_TYPE_F32 || t == FB_TYPE_BF16 || t == FB_TYPE_F16; }
 inline size_t type_bytes(int t) { return t == FB_TYPE_F32 ? 4 : 2; }
-constexpr int64_t kMostSize = (int64_t)1 << 31;
+constexpr int64_t kMostSize = (int64_t)1 << 31, kMostWidth = (int64_t)1 << 28;
 inline bool bad_rows(int64_t n) { return n < 0 || n >= kMostSize; }
-inline bool bad_width(int64_t n) { return n < 1 || n >= kMostSize; }
+inline bool bad_width(int64_t n) { return n < 1 || n >= kMostWidth; }
 inline bool bad_ld(int64_t ld, int64_t width) { return ld < width || ld >= kMostSize; }
 
 inline int launched(const char *what)

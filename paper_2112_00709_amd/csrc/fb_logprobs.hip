@@ -605,6 +605,19 @@ int launch_tokens(const TokenParams &p, const TokenPlan &t, hipStream_t stream)
     return rc;
 }
 
+// A launch has fewer than 2^32 threads: more rows than that leaves are worked on in several launches.
+constexpr int64_t kRowsALaunch = (int64_t)1 << 22, kPiecesALaunch = (int64_t)1 << 24;
+
+template <class T>
+T *from_row(T *p, int64_t elements) { return p ? p + elements : p; }
+inline const void *from_row(const void *p, int64_t elements, int type) { return (const char *)p + (size_t)elements * type_bytes(type); }
+
+int launch_tokens(const TokenParams &p, const TokenPlan &t, int type, hipStream_t stream)
+{
+    if (type == FB_TYPE_F32) return launch_tokens<float>(p, t, stream);
+    return type == FB_TYPE_BF16 ? launch_tokens<bf16>(p, t, stream) : launch_tokens<f16>(p, t, stream);
+}
+
 size_t stats_bytes(int64_t R, int split) { return ((size_t)R * split * kSplitWaves * 3 * sizeof(float) + 255) & ~(size_t)255; }
 
 int check_tokens(const char *who, const void *logits, int64_t ld, const int32_t *tokens, int64_t R, int64_t V, int type)
@@ -651,10 +664,20 @@ int fb_token_logprobs(const void *logits, int64_t ld, const int32_t *tokens, int
         p.split = t.split; p.chunk = t.chunk;
         p.part = (float *)ws;
         p.part_top = (uint64_t *)((char *)ws + (t.split > 1 ? stats_bytes(R, t.split) : 0));
-        if (R * t.split * kSplitWaves >= kMostSize) return fail(FB_EUNSUPPORTED, "fb_token_logprobs: more than 2^31 pieces of rows");
-        if (type == FB_TYPE_F32) return launch_tokens<float>(p, t, (hipStream_t)stream);
-        if (type == FB_TYPE_BF16) return launch_tokens<bf16>(p, t, (hipStream_t)stream);
-        return launch_tokens<f16>(p, t, (hipStream_t)stream);
+        if (t.split > 1 && R * t.split >= kPiecesALaunch) return fail(FB_EUNSUPPORTED, "fb_token_logprobs: more than 2^24 pieces of long rows");
+        for (int64_t r = 0; r < R; r += t.split > 1 ? R : kRowsALaunch) {
+            TokenParams q = p;
+            if (t.split == 1) {
+                q.R = std::min(R - r, kRowsALaunch);
+                q.logits = from_row(logits, r * ld, type);
+                q.tokens = from_row(tokens, r);
+                q.logprobs = from_row(logprobs, r); q.entropy = from_row(entropy, r); q.logz = from_row(logz, r);
+                q.top_ids = from_row(top_ids, r * top); q.top_logprobs = from_row(top_logprobs, r * top);
+            }
+            const int e = launch_tokens(q, t, type, (hipStream_t)stream);
+            if (e != FB_OK) return e;
+        }
+        return FB_OK;
     });
 }
 
@@ -674,15 +697,24 @@ int fb_token_logprobs_grad(const void *logits, int64_t ld, const int32_t *tokens
         p.g_logprobs = g_logprobs; p.g_entropy = g_entropy; p.dlogits = dlogits;
         const int64_t wide = 64 * kGradPieces * (16 / (int64_t)type_bytes(type));
         p.pieces = (V + wide - 1) / wide;
-        p.items = R * p.pieces;
-        if (p.items >= 4 * (kMostSize - 1)) return fail(FB_EUNSUPPORTED, "fb_token_logprobs_grad: more than 2^33 pieces of rows");
-        const dim3 grid((unsigned)((p.items + 3) / 4)), block(256);
-        if (type == FB_TYPE_F32)
-            hipLaunchKernelGGL(fb_token_logprobs_grad_kernel<float>, grid, block, 0, (hipStream_t)stream, p);
-        else if (type == FB_TYPE_BF16)
-            hipLaunchKernelGGL(fb_token_logprobs_grad_kernel<bf16>, grid, block, 0, (hipStream_t)stream, p);
-        else
-            hipLaunchKernelGGL(fb_token_logprobs_grad_kernel<f16>, grid, block, 0, (hipStream_t)stream, p);
+        const int64_t rows = std::max<int64_t>(1, kPiecesALaunch / p.pieces);
+        for (int64_t r = 0; r < R; r += rows) {
+            TokenGradParams q = p;
+            q.R = std::min(R - r, rows);
+            q.items = q.R * p.pieces;
+            q.logits = from_row(logits, r * ld, type);
+            q.dlogits = (void *)from_row((const void *)dlogits, r * ldd, type);
+            q.tokens = from_row(tokens, r);
+            q.logz = from_row(logz, r); q.entropy = from_row(entropy, r);
+            q.g_logprobs = from_row(g_logprobs, r); q.g_entropy = from_row(g_entropy, r);
+            const dim3 grid((unsigned)((q.items + 3) / 4)), block(256);
+            if (type == FB_TYPE_F32)
+                hipLaunchKernelGGL(fb_token_logprobs_grad_kernel<float>, grid, block, 0, (hipStream_t)stream, q);
+            else if (type == FB_TYPE_BF16)
+                hipLaunchKernelGGL(fb_token_logprobs_grad_kernel<bf16>, grid, block, 0, (hipStream_t)stream, q);
+            else
+                hipLaunchKernelGGL(fb_token_logprobs_grad_kernel<f16>, grid, block, 0, (hipStream_t)stream, q);
+        }
         return launched("token log probability gradient kernel launch: ");
     });
 }

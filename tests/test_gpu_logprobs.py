@@ -139,6 +139,24 @@ def test_one_lane_holds_all_the_best(fl):
         check(fl, x.bfloat16(), tokens, 12)
 
 
+@pytest.mark.parametrize("V", [40, 106, 300, 512, 513, 2000, 12544, 70001])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_rows_with_few_alternatives(fl, V, dtype):
+    """Fewer elements above -inf than alternatives are asked for (0, 1, 3, 30 of them, at the ends and in between): the others
+    follow in order of their numbers; and rows of a few values only, many times over."""
+    import torch
+    x = torch.full((7, V), -math.inf)
+    x[1, V - 1] = 2.0
+    x[2, [0, V // 2, V - 1]] = torch.tensor([1.0, 1.0, 3.0])
+    x[3, torch.arange(0, V, max(1, V // 30))[:30]] = torch.arange(30).float()[: len(torch.arange(0, V, max(1, V // 30))[:30])]
+    x[4] = 1.0
+    x[5] = torch.arange(V).remainder(3).float()
+    x[6, : V // 2] = -1.0
+    tokens = torch.full((7,), V - 1, dtype=torch.int32, device="cuda")
+    for top in (1, 5, 20, min(64, V)):
+        check(fl, x.to(getattr(torch, dtype)).cuda(), tokens, top)
+
+
 def test_lowest_value_and_large_values(fl):
     """Masks of the type's lowest value instead of -inf; logits near the type's largest."""
     import torch
@@ -244,6 +262,24 @@ def test_no_rows_leading_shapes_and_another_stream(fl):
     s.synchronize()
     for a, b in zip(flat, other):
         assert torch.equal(a, b.view(a.shape)) or (torch.isnan(a) == torch.isnan(b.view(a.shape))).all()
+
+
+def test_more_rows_than_a_launch_takes(fl):
+    """Rows beyond the first 2^22, and beyond 2^24 pieces of the gradient: the last ones are as the first."""
+    import torch
+    R = (1 << 24) + 77
+    g = torch.Generator().manual_seed(5)
+    few = torch.randn((64, 3), generator=g).cuda()
+    x = few.repeat((R + 63) // 64, 1)[:R].contiguous()
+    tokens = torch.arange(R, dtype=torch.int32, device="cuda") % 3
+    lp, ent, z, ids, _ = fl.fb_token_logprobs(x, tokens, top=2)
+    d = fl.fb_token_logprobs_grad(x, tokens, z, ent, torch.ones(R, device="cuda"), ent)
+    head = fl.fb_token_logprobs(x[-100:].contiguous(), tokens[-100:].contiguous(), top=2)
+    for a, b in zip((lp, ent, z, ids), head):
+        assert torch.equal(a[-100:], b)
+    dh = fl.fb_token_logprobs_grad(x[-100:].contiguous(), tokens[-100:].contiguous(), head[2], head[1], torch.ones(100, device="cuda"), head[1])
+    assert torch.equal(d[-100:], dh)
+    assert torch.isfinite(lp).all() and torch.isfinite(d).all()
 
 
 def test_recorded_into_a_graph(fl):

@@ -63,6 +63,16 @@ def test_malformed_arguments_are_codes(name, good, change):
     assert name.encode() in fb.lib().fb_last_error()
 
 
+def test_sizes_beyond_the_kernels_addresses_are_codes():
+    L = layers.lib()
+    far = 1 << 27
+    for change in [dict(M=65, ldy=far), dict(M=65, residual=_one(), ldr=far), dict(M=65, preact=_one(), ldp=far),
+                   dict(M=65, K=(1 << 20) + 1, ldx=1 << 21, ldw=1 << 21), dict(N=1 << 26, ldy=1 << 26)]:
+        assert L.fb_affine(*{**AFFINE, **change}.values()) == fb.FB_EUNSUPPORTED
+    for change in [dict(lddx=far), dict(K=(1 << 20) + 1, ldx=1 << 21, ldw=1 << 21, lddx=1 << 21)]:
+        assert L.fb_affine_grad(*{**AFFINE_GRAD, **change}.values()) == fb.FB_EUNSUPPORTED
+
+
 def test_workspaces():
     L = layers.lib()
     assert L.fb_layer_norm_grad_workspace_bytes(0, 10) > 0 and L.fb_layer_norm_grad_workspace_bytes(-1, 10) == 0
