@@ -100,7 +100,7 @@ SlopeLayout slope_layout(int64_t M, int64_t N, int type)
     for (s.lanes = 1; s.lanes < 64 && s.lanes < pieces;) s.lanes *= 2;
     s.wide = (pieces + s.lanes - 1) / s.lanes;
     const int64_t rows = 256 / s.lanes;      // at a time
-    s.down = std::max<int64_t>(1, std::min<int64_t>((M + rows - 1) / rows, std::max<int64_t>(64, 4 * kCUs / s.wide)));
+    s.down = std::max<int64_t>(1, std::min<int64_t>((M + rows * kRowsAhead - 1) / (rows * kRowsAhead), std::max<int64_t>(64, 4 * kCUs / s.wide)));
     return s;
 }
 

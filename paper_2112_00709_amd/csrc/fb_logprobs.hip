@@ -36,6 +36,10 @@ __device__ __forceinline__ uint32_t order_of(float x)
 __device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o ^ ((o & 0x80000000u) ? 0x80000000u : 0xffffffffu)); }
 __device__ __forceinline__ uint64_t key_of(float x, uint32_t j) { return (uint64_t)order_of(x) << 32 | (uint32_t)~j; }
 
+// What a wave's lanes have written to LDS, its other lanes read from here on (LDS serves a wave in order: only the compiler
+// is held).
+__device__ __forceinline__ void lds_settled() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+
 // Largest key of a wave; 0 stands for none.
 __device__ __forceinline__ uint64_t max_wave_key(uint64_t k)
 {
@@ -43,10 +47,6 @@ __device__ __forceinline__ uint64_t max_wave_key(uint64_t k)
     const uint32_t lo = max_wave_u((uint32_t)(k >> 32) == hi ? (uint32_t)k : 0u);
     return (uint64_t)hi << 32 | lo;
 }
-
-// What a wave's lanes have written to LDS, its other lanes read from here on (LDS serves a wave in order: only the compiler
-// is held).
-__device__ __forceinline__ void lds_settled() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
 struct Stats {
     float m, S, T;
@@ -61,40 +61,101 @@ __device__ __forceinline__ Stats join(const Stats &a, const Stats &b)
     return {M, fmaf(a.S, ea, b.S * eb), fmaf(fmaf(a.S, da, a.T), ea, fmaf(b.S, db, b.T) * eb)};
 }
 
-// The best `top` keys of `lists` descending lists of `top` keys each, descending, to `out`; missing ones are 0.  For one wave:
-// a lane keeps the heads of up to kHeads lists, the largest head of all is taken and its list moved on.  `keys` is read once
-// per key taken, so it may lie in memory.
-constexpr int kHeads = 8;
+// The rank of a key among `count` (at most 64) different ones, one a lane.
+__device__ __forceinline__ int rank_in_wave(uint64_t mine, int count)
+{
+    int rank = 0;
+    for (int c = 0; c < count; ++c) {
+        const uint64_t k = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(mine >> 32), c) << 32 |
+                           (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)mine, c);
+        rank += k > mine ? 1 : 0;
+    }
+    return rank;
+}
 
-__device__ __forceinline__ void merge_lists(const uint64_t *keys, int lists, int top, uint64_t *out)
+// The largest number that at least `top` lanes' `mine` reach, found bit by bit; 0 if there is none.
+__device__ __forceinline__ uint32_t reached_by(uint32_t mine, int top)
+{
+    uint32_t least = 0;
+#pragma unroll
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t with = least | 1u << bit;
+        least = __popcll(__ballot(mine >= with)) >= top ? with : least;
+    }
+    return least;
+}
+
+// The best `top` keys of `lists` descending lists of `top` keys each (at most 64 * HEADS of them), descending, to `out`;
+// missing ones are 0.  For one wave: a lane keeps the heads of up to HEADS lists.  What the lanes' largest heads bound from
+// below is put on a list and ranked there; where that is more than 64 keys, the largest head of all is taken and its list
+// moved on, once a place.  `keys` should lie in LDS: a list is moved on by a read that what follows waits for.
+constexpr int kKeysInLds = 4096;
+
+template <int HEADS>
+__device__ __forceinline__ void merge_heads(const uint64_t *keys, int lists, int top, uint64_t *list, uint64_t *out)
 {
     const int lane = threadIdx.x & 63;
-    if (lists <= 64 * kHeads) {
-        uint64_t head[kHeads], best = 0;
-        int at[kHeads];
+    uint64_t head[HEADS], best = 0;
+    int at[HEADS], end[HEADS];
+    auto start = [&]() {
+        best = 0;
 #pragma unroll
-        for (int h = 0; h < kHeads; ++h) {
+        for (int h = 0; h < HEADS; ++h) {
             at[h] = (h * 64 + lane) * top;
-            head[h] = h * 64 + lane < lists ? keys[at[h]] : 0;
+            end[h] = h * 64 + lane < lists ? at[h] + top : at[h];
+            head[h] = at[h] < end[h] ? keys[at[h]] : 0;
             best = head[h] > best ? head[h] : best;
         }
-        for (int t = 0; t < top; ++t) {
-            const uint64_t win = max_wave_key(best);
-            if (lane == 0) out[t] = win;
-            if (win != 0 && best == win) {                     // (keys are different: one lane)
-                best = 0;
+    };
+    auto move_on = [&](int h) {
+        ++at[h];
+        head[h] = at[h] < end[h] ? keys[at[h]] : 0;
+    };
+    start();
+    const uint32_t least = reached_by((uint32_t)(best >> 32), top);
+    int count = 0;
+    if (least != 0) {
 #pragma unroll
-                for (int h = 0; h < kHeads; ++h) {
-                    if (head[h] == win) {
-                        ++at[h];
-                        head[h] = at[h] < (h * 64 + lane + 1) * top ? keys[at[h]] : 0;
-                    }
-                    best = head[h] > best ? head[h] : best;
-                }
+        for (int h = 0; h < HEADS; ++h) {
+            for (;;) {
+                const bool in = (uint32_t)(head[h] >> 32) >= least;
+                const uint64_t hit = __ballot(in);
+                if (hit == 0 || count > 64) break;
+                const int to = count + __popcll(hit & ((1ull << lane) - 1));
+                if (in && to < 64) list[to] = head[h];
+                count += __popcll(hit);
+                if (in) move_on(h);
             }
         }
-        return;
+        lds_settled();
     }
+    if (least != 0 && count <= 64) {
+        const uint64_t mine = lane < count ? list[lane] : 0;
+        const int rank = rank_in_wave(mine, count);
+        if (lane < count && rank < top) out[rank] = mine;
+        return;                                                // (there are at least `top`)
+    }
+    start();
+    for (int t = 0; t < top; ++t) {
+        const uint64_t win = max_wave_key(best);
+        if (lane == 0) out[t] = win;
+        if (win != 0 && best == win) {                         // (keys are different: one lane)
+            best = 0;
+#pragma unroll
+            for (int h = 0; h < HEADS; ++h) {
+                if (head[h] == win) move_on(h);
+                best = head[h] > best ? head[h] : best;
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ void merge_lists(const uint64_t *keys, int lists, int top, uint64_t *list, uint64_t *out)
+{
+    if (lists <= 64) return merge_heads<1>(keys, lists, top, list, out);
+    if (lists <= 128) return merge_heads<2>(keys, lists, top, list, out);
+    if (lists <= 512) return merge_heads<8>(keys, lists, top, list, out);
+    const int lane = threadIdx.x & 63;
     uint64_t last = ~0ull;
     for (int t = 0; t < top; ++t) {
         uint64_t best = 0;
@@ -131,14 +192,7 @@ __device__ __forceinline__ void best_of_wave(const T *row, const u32x4 (&raw)[NV
             if (cur == bound) cur = -kInf;
         }
     } else {
-        const uint32_t mine = order_of(lane_max);
-        uint32_t least = 0;
-#pragma unroll
-        for (int bit = 31; bit >= 0; --bit) {
-            const uint32_t with = least | 1u << bit;
-            least = __popcll(__ballot(mine >= with)) >= top ? with : least;
-        }
-        bound = value_of(least);
+        bound = value_of(reached_by(order_of(lane_max), top));
     }
     const bool few = bound == -kInf;
     auto reaches = [&](float x) { return few ? x > -kInf : x >= bound; };
@@ -170,12 +224,7 @@ __device__ __forceinline__ void best_of_wave(const T *row, const u32x4 (&raw)[NV
     lds_settled();
     if (count <= 64) {
         const uint64_t mine = lane < count ? list[lane] : 0;
-        int rank = 0;
-        for (int c = 0; c < count; ++c) {
-            const uint64_t k = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(mine >> 32), c) << 32 |
-                               (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)mine, c);
-            rank += k > mine ? 1 : 0;
-        }
+        const int rank = rank_in_wave(mine, count);
         if (lane < count && rank < top) out[rank] = mine;
         if (lane >= count && lane < top) out[lane] = 0;
         if (few) {                                            // (a wave's first pieces lie side by side, 256 elements and more)
@@ -211,9 +260,15 @@ __device__ __forceinline__ void best_of_wave(const T *row, const u32x4 (&raw)[NV
     }
 }
 
-// A row's results from its statistics and the keys of its best elements (one lane a place).
 template <class T>
-__device__ __forceinline__ void write_row(const TokenParams &p, int64_t r, int32_t token, const Stats &st, const uint64_t *keys, int lane)
+__device__ __forceinline__ float given_logit(const TokenParams &p, int64_t r, int32_t token)
+{
+    return token >= 0 && token < p.V ? load_one((const T *)p.logits + r * p.ld + token) : __builtin_nanf("");
+}
+
+// A row's results from its statistics and the keys of its best elements (one lane a place); given: the token's logit, asked
+// for when the row is.
+__device__ __forceinline__ void write_row(const TokenParams &p, int64_t r, int32_t token, float given, const Stats &st, const uint64_t *keys, int lane)
 {
     const float ls = logf(st.S);
     const bool dead = st.m == -kInf && st.S == 0.0f;
@@ -222,8 +277,7 @@ __device__ __forceinline__ void write_row(const TokenParams &p, int64_t r, int32
         if (p.logz) p.logz[r] = logz;
         if (p.entropy) p.entropy[r] = dead ? 0.0f : ls - st.T / st.S;
         if (p.logprobs) {
-            const float x = token < p.V ? load_one((const T *)p.logits + r * p.ld + token) : __builtin_nanf("");
-            p.logprobs[r] = dead && token < p.V ? -kInf : x - logz;
+            p.logprobs[r] = dead && token < p.V ? -kInf : given - logz;
         }
     }
     if (lane < p.top) {
@@ -302,8 +356,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64, NV * Vec<T>::kN <= 1
     const int c = SPLIT ? (int)(item - r * p.split) : 0;
     if (r >= p.R) return;                                     // (a whole wave; with WAVES > 1 the whole workgroup)
     const int32_t token = p.tokens[r];
-    if (token < 0) {
-        if ((WAVES == 1 || wave == 0) && c == 0 && !SPLIT) write_padding(p, r, lane);
+    if (!SPLIT && token < 0) {
+        if (WAVES == 1 || wave == 0) write_padding(p, r, lane);
         return;
     }
     const int64_t at0 = SPLIT ? c * p.chunk : 0;
@@ -314,6 +368,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64, NV * Vec<T>::kN <= 1
     u32x4 raw[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) raw[i] = load_piece(row + first + i * kStride, n - (first + i * kStride));
+    if (SPLIT && token < 0) return;                           // (few rows: not waited for before the row is asked for)
+    const float given = SPLIT ? 0.0f : given_logit<T>(p, r, token);
     float peak[NV], lane_max;
     Stats st = wave_stats<T, NV>(raw, first, kStride, n, peak, lane_max);
     if (p.top) best_of_wave<T, NV>(row, raw, peak, lane_max, first, kStride, n, p.top, list[wave], best[wave]);
@@ -356,7 +412,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64, NV * Vec<T>::kN <= 1
             keys = row_best;
         }
     }
-    write_row<T>(p, r, token, st, keys, lane);
+    write_row(p, r, token, given, st, keys, lane);
 }
 
 // Rows of up to 512 elements: a wave a row, element 64 j + lane in the lane's j-th register (narrow loads, but all lanes have
@@ -376,6 +432,7 @@ __global__ __launch_bounds__(256) void fb_token_short_kernel(TokenParams p)
     }
     const int n = (int)p.V;
     const T *row = (const T *)p.logits + r * p.ld;
+    const float given = given_logit<T>(p, r, token);
     float v[E], m = -kInf;
 #pragma unroll
     for (int j = 0; j < E; ++j) v[j] = j * 64 + lane < n ? load_one(row + j * 64 + lane) : -kInf;
@@ -415,42 +472,52 @@ __global__ __launch_bounds__(256) void fb_token_short_kernel(TokenParams p)
             }
         lds_settled();
         const uint64_t mine = lane < p.top ? list[wave][lane] : 0;
-        int rank = 0;
-        for (int c = 0; c < p.top; ++c) {
-            const uint64_t k = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(mine >> 32), c) << 32 |
-                               (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)mine, c);
-            rank += k > mine ? 1 : 0;
-        }
+        const int rank = rank_in_wave(mine, p.top);
         if (lane < p.top) best[wave][rank] = mine;
         lds_settled();
     }
-    write_row<T>(p, r, token, st, best[wave], lane);
+    write_row(p, r, token, given, st, best[wave], lane);
 }
 
 // What the waves that share a row have found joined, one wave a row.
 template <class T, int WAVES>
 __global__ __launch_bounds__(64) void fb_token_join_kernel(TokenParams p)
 {
-    __shared__ uint64_t best[FB_TOP_MAX];
+    __shared__ uint64_t best[FB_TOP_MAX], list[64], near[kKeysInLds];
     const int lane = threadIdx.x;
     const int64_t r = blockIdx.x;
     const int32_t token = p.tokens[r];
+    const int lists = p.split * WAVES, n = lists * p.top;
+    const uint64_t *keys = p.part_top + (size_t)r * n;
+    const float *q = p.part + (size_t)r * lists * 3;
+    // (all that is needed is asked for before any of it is looked at, also for a padded row, where nothing was written)
+    Stats st = {-kInf, 0.0f, 0.0f};
+    if (lane < lists) st = {q[3 * lane], q[3 * lane + 1], q[3 * lane + 2]};
+    if (n <= kKeysInLds) {
+        for (int i = lane; i < n; i += 512) {
+            uint64_t k[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) k[u] = i + u * 64 < n ? keys[i + u * 64] : 0;
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (i + u * 64 < n) near[i + u * 64] = k[u];
+        }
+    }
     if (token < 0) {
         write_padding(p, r, lane);
         return;
     }
-    const int lists = p.split * WAVES;
-    const float *q = p.part + (size_t)r * lists * 3;
-    Stats st = {-kInf, 0.0f, 0.0f};
-    for (int c = lane; c < lists; c += 64) st = join(st, {q[3 * c], q[3 * c + 1], q[3 * c + 2]});
+    const float given = given_logit<T>(p, r, token);
+    for (int c = lane + 64; c < lists; c += 64) st = join(st, {q[3 * c], q[3 * c + 1], q[3 * c + 2]});
 #pragma unroll
     for (int step = 1; step < 64; step <<= 1) {
         const Stats o = {__shfl_xor(st.m, step), __shfl_xor(st.S, step), __shfl_xor(st.T, step)};
         st = join(st, o);
     }
-    if (p.top) merge_lists(p.part_top + (size_t)r * lists * p.top, lists, p.top, best);
     lds_settled();
-    write_row<T>(p, r, token, st, best, lane);
+    if (p.top) merge_lists(n <= kKeysInLds ? near : keys, lists, p.top, list, best);
+    lds_settled();
+    write_row(p, r, token, given, st, best, lane);
 }
 
 struct TokenGradParams {
