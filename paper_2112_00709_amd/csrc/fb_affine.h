@@ -40,6 +40,10 @@ struct Product {
 
 int launch_mfma_product(const Product &q, hipStream_t stream);   // factors as ready() wants them
 
+// Both products of a gradient in one launch, if their workgroups fit the GPU together.
+bool fits_as_pair(const Product &dx, const Product &dw);
+int launch_mfma_pair(const Product &dx, const Product &dw, hipStream_t stream);
+
 // Few rows of x (M <= kFewRows), both factors along k, at any address and distance.
 constexpr int64_t kFewRows = 64;
 int launch_few_rows(const Product &q, hipStream_t stream);

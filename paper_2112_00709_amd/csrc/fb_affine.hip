@@ -3,20 +3,53 @@
 
 namespace fb {
 
-int launch_column_sum(const float *part, int64_t P, int64_t C, int sets, float *out0, float *out1, void *stream);
-
 namespace {
 
-// The shares of a product added in their order and finished.
+// What is left behind the products: shares of up to two of them added in their order and finished, and the sums of columns
+// that fb_prepare_kernel has left a row a workgroup of (16 columns a workgroup, every sixteenth row a thread).
+struct JoinParams {
+    Product q[2];
+    int last[2];             // workgroups [0, last[0]) have q[0], [last[0], last[1]) q[1], the others columns
+    const float *sums;
+    int64_t rows, N;
+    float *out;
+};
+
 template <class T>
-__global__ __launch_bounds__(256) void fb_product_join_kernel(Product q)
+__global__ __launch_bounds__(256) void fb_join_kernel(JoinParams p)
 {
-    const int64_t n = q.M * q.N;
-    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < n; at += (int64_t)gridDim.x * 256) {
-        float s = 0.0f;
+    __shared__ float slots[16][16];
+    const int block = blockIdx.x;
+    if (block < p.last[1]) {
+        const int which = block < p.last[0] ? 0 : 1, first = which ? p.last[0] : 0;
+        const Product &q = p.q[which];
+        const int64_t n = q.M * q.N;
+        for (int64_t at = (int64_t)(block - first) * 256 + threadIdx.x; at < n; at += (int64_t)(p.last[which] - first) * 256) {
+            float s = 0.0f;
 #pragma unroll 8
-        for (int c = 0; c < q.split; ++c) s += q.part[(size_t)c * n + at];
-        finish_one<T>(q.f, at / q.N, at % q.N, s);
+            for (int c = 0; c < q.split; ++c) s += q.part[(size_t)c * n + at];
+            finish_one<T>(q.f, at / q.N, at % q.N, s);
+        }
+        return;
+    }
+    const int col = threadIdx.x & 15, g = threadIdx.x >> 4;
+    const int64_t c = (int64_t)(block - p.last[1]) * 16 + col;
+    float s[4] = {};
+    if (c < p.N) {
+        int64_t i = g;
+        for (; i + 48 < p.rows; i += 64) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) s[u] += p.sums[(i + 16 * u) * p.N + c];
+        }
+        for (; i < p.rows; i += 16) s[0] += p.sums[i * p.N + c];
+    }
+    slots[g][col] = (s[0] + s[1]) + (s[2] + s[3]);
+    __syncthreads();
+    if (g == 0 && c < p.N) {
+        float t = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) t += slots[i][col];
+        p.out[c] = t;
     }
 }
 
@@ -25,8 +58,9 @@ struct SlopeParams {
     int64_t lddy, ldz, M, N, ldo;
     int act;
     void *out;           // dz as the products take it, nullable
-    float *part;         // [gridDim.y][N]: shares of the sums over rows, nullable
+    float *part;         // [down][N]: shares of the sums over rows, nullable
     int lanes;           // a row: a power of two, 64 where the rows are wider than that many pieces
+    int wide, down;      // workgroups along the width and along the rows
 };
 
 // dz = dy act'(z) (or a copy of dy in rows of whole pieces), rounded to the factors' type, and the sums of its columns before
@@ -36,17 +70,17 @@ struct SlopeParams {
 constexpr int kRowsAhead = 4;
 
 template <class T, class D>
-__global__ __launch_bounds__(256) void fb_slope_kernel(SlopeParams p)
+__device__ __forceinline__ void make_rows(const SlopeParams &p, int block, float (*slots)[Vec<T>::kN + 1])
 {
     constexpr int VE = Vec<T>::kN, VD = Vec<D>::kN;
-    __shared__ float slots[256][VE + 1];
+    const int across = block % p.wide, down = block / p.wide;
     const int lane = threadIdx.x & (p.lanes - 1), sub = threadIdx.x / p.lanes, subs = 256 / p.lanes;
-    const int64_t at = ((int64_t)blockIdx.x * p.lanes + lane) * VE;
+    const int64_t at = ((int64_t)across * p.lanes + lane) * VE;
     const int n = at >= p.N ? 0 : (int)(p.N - at < VE ? p.N - at : VE);
     float sum[VE] = {};
     if (n > 0) {
-        const int64_t step = (int64_t)gridDim.y * subs;
-        for (int64_t r0 = (int64_t)blockIdx.y * subs + sub; r0 < p.M; r0 += kRowsAhead * step) {
+        const int64_t step = (int64_t)p.down * subs;
+        for (int64_t r0 = (int64_t)down * subs + sub; r0 < p.M; r0 += kRowsAhead * step) {
             u32x4 rg[kRowsAhead][VE / VD], rz[kRowsAhead];
 #pragma unroll
             for (int u = 0; u < kRowsAhead; ++u) {
@@ -79,29 +113,50 @@ __global__ __launch_bounds__(256) void fb_slope_kernel(SlopeParams p)
     for (int e = 0; e < VE; ++e) slots[threadIdx.x][e] = sum[e];
     __syncthreads();
     for (int c = threadIdx.x; c < p.lanes * VE; c += 256) {
-        const int64_t col = (int64_t)blockIdx.x * p.lanes * VE + c;
+        const int64_t col = (int64_t)across * p.lanes * VE + c;
         if (col >= p.N) continue;
         float s = 0.0f;
         for (int i = 0; i < subs; ++i) s += slots[i * p.lanes + c / VE][c % VE];
-        p.part[(size_t)blockIdx.y * p.N + col] = s;
+        p.part[(size_t)down * p.N + col] = s;
     }
 }
 
-// How that kernel is laid out: lanes a row, workgroups along the width and along the rows.
-struct SlopeLayout {
-    int lanes;
-    int64_t wide, down;
+// Up to three such jobs, the first with rows of type D.
+struct PrepareParams {
+    SlopeParams job[3];
+    int last[3];             // workgroups [last[i - 1], last[i]) have job i
 };
 
-SlopeLayout slope_layout(int64_t M, int64_t N, int type)
+template <class T, class D>
+__global__ __launch_bounds__(256) void fb_prepare_kernel(PrepareParams p)
 {
-    const int64_t ve = 16 / (int64_t)type_bytes(type), pieces = (N + ve - 1) / ve;
-    SlopeLayout s{};
-    for (s.lanes = 1; s.lanes < 64 && s.lanes < pieces;) s.lanes *= 2;
-    s.wide = (pieces + s.lanes - 1) / s.lanes;
-    const int64_t rows = 256 / s.lanes;      // at a time
-    s.down = std::max<int64_t>(1, std::min<int64_t>((M + rows * kRowsAhead - 1) / (rows * kRowsAhead), std::max<int64_t>(64, 4 * kCUs / s.wide)));
-    return s;
+    __shared__ float slots[256][Vec<T>::kN + 1];
+    const int block = blockIdx.x;
+    if (block < p.last[0])
+        make_rows<T, D>(p.job[0], block, slots);
+    else if (block < p.last[1])
+        make_rows<T, T>(p.job[1], block - p.last[0], slots);
+    else
+        make_rows<T, T>(p.job[2], block - p.last[1], slots);
+}
+
+void lay_out(SlopeParams &p, int type)
+{
+    const int64_t ve = 16 / (int64_t)type_bytes(type), pieces = (p.N + ve - 1) / ve;
+    for (p.lanes = 1; p.lanes < 64 && p.lanes < pieces;) p.lanes *= 2;
+    p.wide = (int)((pieces + p.lanes - 1) / p.lanes);
+    const int64_t rows = 256 / p.lanes * kRowsAhead;      // at a time
+    p.down = (int)std::max<int64_t>(1, std::min<int64_t>((p.M + rows - 1) / rows, std::max<int64_t>(64, 4 * kCUs / p.wide)));
+}
+
+// The shares of sums over M rows of N elements.
+int64_t sum_rows(int64_t M, int64_t N, int type)
+{
+    SlopeParams p{};
+    p.M = M;
+    p.N = N;
+    lay_out(p, type);
+    return p.down;
 }
 
 size_t aligned(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -109,10 +164,10 @@ size_t aligned(size_t n) { return (n + 255) & ~(size_t)255; }
 // Tiles and shares of k, by estimated clocks of the busiest compute unit: its tiles' work, for every round of workgroups that
 // it holds at a time (1, 2 or 4) a start, an end and the latency of every step, and, where k is shared, the sums' way through
 // memory and a launch to join them.  In single precision a share is at most 4096 long, so that roundings do not pile up.
-void plan(Product &q)
+void plan(Product &q, int only_tile = 0)
 {
     static constexpr int kSplits[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64, 96, 128};
-    struct Shape {
+    struct Shape {                          // (see fb_affine_mfma.hip)
         int tile, resident;
         double per_k16, per_k32;            // clocks of a compute unit on one k of a tile, measured
     };
@@ -122,6 +177,7 @@ void plan(Product &q)
     const int64_t deep = wide ? 32 : 64;
     double best = 0.0;
     for (const Shape &sh : kShapes) {
+        if (only_tile && sh.tile != only_tile) continue;
         const int64_t tiles = ((q.M + sh.tile - 1) / sh.tile) * ((q.N + sh.tile - 1) / sh.tile);
         for (const int64_t split : kSplits) {
             const int64_t share = std::max<int64_t>(deep, ((q.K + split - 1) / split + deep - 1) / deep * deep);
@@ -144,38 +200,65 @@ void plan(Product &q)
 
 size_t product_bytes(const Product &q) { return q.parts ? aligned((size_t)q.split * (size_t)q.M * (size_t)q.N * sizeof(float)) : 0; }
 
-template <class T>
-int launch_join(const Product &q, hipStream_t stream)
+// Products whose shares are to be joined (at most two) and columns to be added up (out), in one launch.
+int launch_join(const Product *a, const Product *b, int type, const float *sums, int64_t rows, int64_t N, float *out, hipStream_t stream)
 {
-    const int64_t groups = std::min<int64_t>((q.M * q.N + 255) / 256, 8 * kCUs);
-    hipLaunchKernelGGL(fb_product_join_kernel<T>, dim3((unsigned)groups), dim3(256), 0, stream, q);
+    JoinParams p{};
+    int blocks = 0, k = 0;
+    for (const Product *q : {a, b}) {
+        if (q && q->parts && q->M > 0) {
+            p.q[k] = *q;
+            blocks += (int)std::min<int64_t>((q->M * q->N + 255) / 256, 8 * kCUs);
+            p.last[k++] = blocks;
+        }
+    }
+    for (; k < 2; ++k) p.last[k] = blocks;
+    if (out) {
+        p.sums = sums;
+        p.rows = rows;
+        p.N = N;
+        p.out = out;
+        blocks += (int)((N + 15) / 16);
+    }
+    if (blocks == 0) return FB_OK;
+    if (type == FB_TYPE_F32)
+        hipLaunchKernelGGL(fb_join_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, stream, p);
+    else if (type == FB_TYPE_BF16)
+        hipLaunchKernelGGL(fb_join_kernel<bf16>, dim3((unsigned)blocks), dim3(256), 0, stream, p);
+    else
+        hipLaunchKernelGGL(fb_join_kernel<f16>, dim3((unsigned)blocks), dim3(256), 0, stream, p);
     return launched("product join kernel launch: ");
 }
 
-int launch_product(const Product &q, hipStream_t stream)
-{
-    if (q.M == 0) return FB_OK;
-    const int rc = launch_mfma_product(q, stream);
-    if (rc != FB_OK || !q.parts) return rc;
-    if (q.type == FB_TYPE_F32) return launch_join<float>(q, stream);
-    return q.type == FB_TYPE_BF16 ? launch_join<bf16>(q, stream) : launch_join<f16>(q, stream);
-}
+// Jobs that make rows, in one launch; the first has rows of dy_type.
+struct Prepare {
+    PrepareParams p{};
+    int n = 0, blocks = 0;
+    void add(SlopeParams s, int type)
+    {
+        lay_out(s, type);
+        p.job[n] = s;
+        blocks += s.wide * s.down;
+        p.last[n++] = blocks;
+    }
+};
 
-template <class T, class D>
-int launch_slope(const SlopeParams &p, const SlopeLayout &l, hipStream_t stream)
+int launch_prepare(Prepare &j, int type, int dy_type, hipStream_t stream)
 {
-    hipLaunchKernelGGL((fb_slope_kernel<T, D>), dim3((unsigned)l.wide, (unsigned)l.down), dim3(256), 0, stream, p);
-    return launched("activation slope kernel launch: ");
-}
-
-int launch_slope(SlopeParams p, int type, int dy_type, hipStream_t stream)
-{
-    const SlopeLayout l = slope_layout(p.M, p.N, type);
-    p.lanes = l.lanes;
-    if (type == FB_TYPE_F32) return launch_slope<float, float>(p, l, stream);
-    if (type == FB_TYPE_BF16)
-        return dy_type == type ? launch_slope<bf16, bf16>(p, l, stream) : launch_slope<bf16, float>(p, l, stream);
-    return dy_type == type ? launch_slope<f16, f16>(p, l, stream) : launch_slope<f16, float>(p, l, stream);
+    if (j.n == 0) return FB_OK;
+    for (int i = j.n; i < 3; ++i) j.p.last[i] = j.blocks;
+    const dim3 grid((unsigned)j.blocks), block(256);
+    if (type == FB_TYPE_F32)
+        hipLaunchKernelGGL((fb_prepare_kernel<float, float>), grid, block, 0, stream, j.p);
+    else if (type == FB_TYPE_BF16 && dy_type == type)
+        hipLaunchKernelGGL((fb_prepare_kernel<bf16, bf16>), grid, block, 0, stream, j.p);
+    else if (type == FB_TYPE_BF16)
+        hipLaunchKernelGGL((fb_prepare_kernel<bf16, float>), grid, block, 0, stream, j.p);
+    else if (dy_type == type)
+        hipLaunchKernelGGL((fb_prepare_kernel<f16, f16>), grid, block, 0, stream, j.p);
+    else
+        hipLaunchKernelGGL((fb_prepare_kernel<f16, float>), grid, block, 0, stream, j.p);
+    return launched("row preparation kernel launch: ");
 }
 
 int64_t whole_pieces(int64_t width, int type)
@@ -200,11 +283,10 @@ Packed packed(const void *p, int64_t ld, int64_t rows, int64_t width, int type)
     return k;
 }
 
-int launch_pack(const Packed &k, const void *p, int64_t ld, int64_t rows, int64_t width, int type, void *to, hipStream_t stream)
+// The job that makes the copy (nothing if none is needed).
+SlopeParams pack_job(const Packed &k, const void *p, int64_t ld, int64_t rows, int64_t width, void *to)
 {
-    if (!k.copy || rows == 0) return FB_OK;
-    const SlopeParams s{p, nullptr, ld, 0, rows, width, k.ld, FB_ACT_NONE, to, nullptr, 0};
-    return launch_slope(s, type, type, stream);
+    return SlopeParams{p, nullptr, ld, 0, rows, width, k.ld, FB_ACT_NONE, to, nullptr, 0, 0, 0};
 }
 
 // What the matrix units' kernel addresses in 32 bits: 64 or 128 rows of a factor, 16 rows of what it stores or adds.
@@ -236,6 +318,7 @@ ForwardPlan forward_plan(const void *x, int64_t ldx, const void *weight, int64_t
 // The two products of the gradient.
 struct GradPlan {
     Product dx, dw;
+    bool pair;            // in one launch
     bool slope;           // dz has to be made, or dy laid out anew
     int64_t ldz;
     Packed x, w;
@@ -250,14 +333,26 @@ GradPlan grad_plan(const void *dy, int64_t lddy, int dy_type, const void *x, int
     g.dw.M = N; g.dw.N = K; g.dw.K = M; g.dw.type = type;
     plan(g.dx);
     plan(g.dw);
+    // small products go together, by tiles of one size: each alone would start and end by itself
+    g.pair = fits_as_pair(g.dx, g.dw);
+    if (!g.pair && g.dx.tile <= 128 && g.dw.tile <= 128 && g.dx.tile != g.dw.tile) {
+        Product dx = g.dx, dw = g.dw;
+        plan(dx, 64);
+        plan(dw, 64);
+        g.pair = fits_as_pair(dx, dw);
+        if (g.pair) {
+            g.dx = dx;
+            g.dw = dw;
+        }
+    }
     g.slope = act != FB_ACT_NONE || dy_type != type || packed(dy, lddy, M, N, type).copy;
     g.ldz = whole_pieces(N, type);
     g.dz = g.slope ? aligned((size_t)M * (size_t)g.ldz * type_bytes(type)) : 0;
     g.x = packed(x, ldx, M, K, type);
     g.w = packed(weight, ldw, N, K, type);
-    g.sums = aligned((size_t)slope_layout(M, N, type).down * (size_t)N * sizeof(float));
-    g.part = std::max(product_bytes(g.dx), product_bytes(g.dw));
-    g.bytes = g.dz + g.x.bytes + g.w.bytes + g.sums + g.part;
+    g.sums = aligned((size_t)sum_rows(M, N, type) * (size_t)N * sizeof(float));
+    g.part = product_bytes(g.dx);
+    g.bytes = g.dz + g.x.bytes + g.w.bytes + g.sums + g.part + product_bytes(g.dw);
     return g;
 }
 
@@ -302,8 +397,6 @@ int fb_affine(const void *x, int64_t ldx, const void *weight, int64_t ldw, const
         if (f.bytes && (!ws || ws_bytes < f.bytes)) return fail(FB_EINVAL, "fb_affine: workspace missing or too small");
         hipStream_t st = (hipStream_t)stream;
         char *xs = (char *)ws, *wts = xs + f.x.bytes;
-        if ((rc = launch_pack(f.x, x, ldx, M, K, type, xs, st)) != FB_OK || (M > 0 && (rc = launch_pack(f.w, weight, ldw, N, K, type, wts, st)) != FB_OK))
-            return rc;
         Product q = f.q;
         q.f = {bias, residual, ldr, act, y, ldy, out_type, preact, ldp};
         if (f.few) {
@@ -311,10 +404,16 @@ int fb_affine(const void *x, int64_t ldx, const void *weight, int64_t ldw, const
             q.B = {weight, ldw, true};
             return M > 0 ? launch_few_rows(q, st) : FB_OK;
         }
+        if (M == 0) return FB_OK;
+        Prepare jobs;
+        if (f.x.copy) jobs.add(pack_job(f.x, x, ldx, M, K, xs), type);
+        if (f.w.copy) jobs.add(pack_job(f.w, weight, ldw, N, K, wts), type);
+        if ((rc = launch_prepare(jobs, type, type, st)) != FB_OK) return rc;
         q.A = {f.x.copy ? xs : x, f.x.ld, true};
         q.B = {f.w.copy ? wts : weight, f.w.ld, true};
         q.part = (float *)(wts + f.w.bytes);
-        return launch_product(q, st);
+        if ((rc = launch_mfma_product(q, st)) != FB_OK) return rc;
+        return launch_join(&q, nullptr, type, nullptr, 0, 0, nullptr, st);
     });
 }
 
@@ -347,29 +446,30 @@ int fb_affine_grad(const void *dy, int64_t lddy, int dy_type, const void *x, int
         char *dz = (char *)ws, *xs = dz + g.dz, *wts = xs + g.x.bytes;
         float *sums = (float *)(wts + g.w.bytes), *part = (float *)(wts + g.w.bytes + g.sums);
         const bool make = g.slope && (dx || dweight);
-        if (M > 0 && (make || dbias)) {
-            const SlopeParams p{dy, preact, lddy, ldp, M, N, g.ldz, act, make ? dz : nullptr, dbias ? sums : nullptr, 0};
-            if ((rc = launch_slope(p, type, dy_type, st)) != FB_OK) return rc;
-        }
-        if (dbias && (rc = launch_column_sum(sums, M > 0 ? slope_layout(M, N, type).down : 0, N, 1, dbias, nullptr, stream)) != FB_OK) return rc;
+        Prepare jobs;                                             // (the first may have rows of another type: dy's)
+        if (M > 0 && (make || dbias))
+            jobs.add(SlopeParams{dy, preact, lddy, ldp, M, N, g.ldz, act, make ? dz : nullptr, dbias ? sums : nullptr, 0, 0, 0}, type);
+        else
+            jobs.p.last[jobs.n++] = 0;
+        if (M > 0 && dx && g.w.copy) jobs.add(pack_job(g.w, weight, ldw, N, K, wts), type);
+        if (M > 0 && dweight && g.x.copy) jobs.add(pack_job(g.x, x, ldx, M, K, xs), type);
+        if (jobs.blocks > 0 && (rc = launch_prepare(jobs, type, dy_type, st)) != FB_OK) return rc;
         const Factor d{make ? (const void *)dz : dy, make ? g.ldz : lddy, true};
-        if (dx) {
-            if (M > 0 && (rc = launch_pack(g.w, weight, ldw, N, K, type, wts, st)) != FB_OK) return rc;
-            g.dx.A = d;
-            g.dx.B = {g.w.copy ? wts : weight, g.w.ld, false};
-            g.dx.f.y = dx; g.dx.f.ldy = lddx; g.dx.f.out_type = type;
-            g.dx.part = part;
-            if ((rc = launch_product(g.dx, st)) != FB_OK) return rc;
+        g.dx.A = d;
+        g.dx.B = {g.w.copy ? wts : weight, g.w.ld, false};
+        g.dx.f.y = dx; g.dx.f.ldy = lddx; g.dx.f.out_type = type;
+        g.dx.part = part;
+        g.dw.A = {d.p, d.ld, false};
+        g.dw.B = {g.x.copy ? xs : x, g.x.ld, false};
+        g.dw.f.y = dweight; g.dw.f.ldy = K; g.dw.f.out_type = type;
+        g.dw.part = (float *)((char *)part + g.part);
+        if (dx && dweight && g.pair) {
+            if ((rc = launch_mfma_pair(g.dx, g.dw, st)) != FB_OK) return rc;
+        } else {
+            if (dx && M > 0 && (rc = launch_mfma_product(g.dx, st)) != FB_OK) return rc;
+            if (dweight && (rc = launch_mfma_product(g.dw, st)) != FB_OK) return rc;
         }
-        if (dweight) {
-            if ((rc = launch_pack(g.x, x, ldx, M, K, type, xs, st)) != FB_OK) return rc;
-            g.dw.A = {d.p, d.ld, false};
-            g.dw.B = {g.x.copy ? xs : x, g.x.ld, false};
-            g.dw.f.y = dweight; g.dw.f.ldy = K; g.dw.f.out_type = type;
-            g.dw.part = part;
-            if ((rc = launch_product(g.dw, st)) != FB_OK) return rc;
-        }
-        return FB_OK;
+        return launch_join(dx ? &g.dx : nullptr, dweight ? &g.dw : nullptr, type, sums, M > 0 ? sum_rows(M, N, type) : 0, N, dbias, st);
     });
 }
 

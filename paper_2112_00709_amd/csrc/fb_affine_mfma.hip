@@ -239,11 +239,12 @@ constexpr int kPlain = -1;
 // The sums of a wave's part of a tile finished and stored.  They pass through LDS, 16 rows of C at a time and each wave in a
 // region of its own, so that whole runs of a row are stored: a lane's own are 4 neighbours, 8 apart in every 32 columns, of
 // one row in 32.  Piece c of a row lies at c ^ row, as eight lanes that write or read at once are to cover all banks.
+typedef const __attribute__((address_space(4))) Product *ProductArgs;
+
 template <class T, int FI, int FJ, int KIND>
-__device__ __forceinline__ void leave(const f32x16 (&acc)[FI][FJ], const f32x4 &bias, int share, int64_t i0, int64_t j0, float *mine)
+__device__ __forceinline__ void leave(ProductArgs args, const f32x16 (&acc)[FI][FJ], const f32x4 &bias, int share, int64_t i0, int64_t j0, float *mine)
 {
     // What is needed here alone is fetched and computed here: kept over the loops before it costs registers that they need.
-    const __attribute__((address_space(4))) Product *args = (const __attribute__((address_space(4))) Product *)__builtin_amdgcn_kernarg_segment_ptr();
     int lane = threadIdx.x & 63;
     asm volatile("" : "+s"(args), "+v"(lane));
     constexpr int kPer = FJ * 8, kRows = 64 / kPer, kR = 16 / kRows;
@@ -334,10 +335,19 @@ __device__ __forceinline__ void leave(const f32x16 (&acc)[FI][FJ], const f32x4 &
     }
 }
 
-// Workgroups stay and take tile after tile, so that the copies for the next tile are under way while this one's sums leave.
+// A product and its tiles, as a kernel gets it.
+struct Task {
+    Product q;
+    int tiles_i, tiles_j;
+};
+
+// Workgroup `block` of `blocks`: they stay and take tile after tile, so that the copies for the next tile are under way while
+// this one's sums leave.  `args`: where the kernel's argument with the product lies.
 template <class T, bool ALONG_A, bool ALONG_B, int WI, int WJ, int FI, int FJ, int KIND>
-__global__ __launch_bounds__(WI * WJ * 64) void fb_mfma_product_kernel(Product q, int tiles_i, int tiles_j)
+__device__ __forceinline__ void run_tiles(const Task &task, ProductArgs args, int block, int blocks)
 {
+    const Product &q = task.q;
+    const int tiles_i = task.tiles_i, tiles_j = task.tiles_j;
     constexpr int kI = WI * FI * 32, kJ = WJ * FJ * 32, kNW = WI * WJ;
     extern __shared__ char lds_raw[];
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds_raw;
@@ -346,7 +356,7 @@ __global__ __launch_bounds__(WI * WJ * 64) void fb_mfma_product_kernel(Product q
 
     // Workgroups go to the eight chiplets in turn: each chiplet has a run of neighbouring tiles, so that its L2 holds what
     // they share; within a run eight tiles down, then one across.
-    const int n = tiles_i * tiles_j * q.split, xcd = blockIdx.x % 8, run = n / 8 + (xcd < n % 8 ? 1 : 0);
+    const int n = tiles_i * tiles_j * q.split, xcd = block % 8, run = n / 8 + (xcd < n % 8 ? 1 : 0);
     const int run0 = xcd * (n / 8) + (xcd < n % 8 ? xcd : n % 8);
     struct Place {
         int share;
@@ -367,7 +377,7 @@ __global__ __launch_bounds__(WI * WJ * 64) void fb_mfma_product_kernel(Product q
     b.start(q.B, lds0 + 2 * a.kBytes, wave, wj * FJ * 32);
     // The copies run two steps ahead of the products, over the ends of tiles.
     constexpr int kCopies = a.kCopies + b.kCopies, kReads = FI + FJ, kSlots = FI * FJ;
-    int ahead = blockIdx.x / 8;                 // the tile that they are at, and what is left of its k
+    int ahead = block / 8;                 // the tile that they are at, and what is left of its k
     int64_t left = 0;
     auto enter = [&]() {
         if (ahead >= run) return;
@@ -382,7 +392,7 @@ __global__ __launch_bounds__(WI * WJ * 64) void fb_mfma_product_kernel(Product q
         if (left > 0) {
             left = left > kDeep ? left - kDeep : 0;
             if (left == 0) {
-                ahead += gridDim.x / 8;
+                ahead += blocks / 8;
                 enter();
             }
         }
@@ -414,7 +424,7 @@ __global__ __launch_bounds__(WI * WJ * 64) void fb_mfma_product_kernel(Product q
         }
     }
     int turn = 0;                               // the buffer that holds this step's share
-    for (int in_run = blockIdx.x / 8; in_run < run; in_run += gridDim.x / 8) {
+    for (int in_run = block / 8; in_run < run; in_run += blocks / 8) {
         const Place p = place(in_run);
         const int steps = (int)((p.length + kDeep - 1) / kDeep);
         f32x16 acc[FI][FJ] = {};
@@ -470,27 +480,86 @@ __global__ __launch_bounds__(WI * WJ * 64) void fb_mfma_product_kernel(Product q
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-        leave<T, FI, FJ, KIND>(acc, bias, p.share, p.i0 + wi * FI * 32, p.j0 + wj * FJ * 32,
+        leave<T, FI, FJ, KIND>(args, acc, bias, p.share, p.i0 + wi * FI * 32, p.j0 + wj * FJ * 32,
                                (float *)(lds_raw + 2 * (a.kBytes + b.kBytes)) + wave * 16 * FJ * 32);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (no copy into LDS outlives the workgroup)
 }
 
 template <class T, bool ALONG_A, bool ALONG_B, int WI, int WJ, int FI, int FJ, int KIND>
+__global__ __launch_bounds__(WI * WJ * 64) void fb_mfma_product_kernel(Task task)
+{
+    run_tiles<T, ALONG_A, ALONG_B, WI, WJ, FI, FJ, KIND>(task, (ProductArgs)__builtin_amdgcn_kernarg_segment_ptr(), blockIdx.x, gridDim.x);
+}
+
+// Both products of a gradient, dx by the first `blocks` workgroups and dW by the others: small ones fill the GPU together.
+template <class T, int WI, int WJ, int FI, int FJ>
+__global__ __launch_bounds__(WI * WJ * 64) void fb_mfma_pair_kernel(Task dx, Task dw, int blocks)
+{
+    const __attribute__((address_space(4))) char *args = (const __attribute__((address_space(4))) char *)__builtin_amdgcn_kernarg_segment_ptr();
+    if ((int)blockIdx.x < blocks)
+        run_tiles<T, true, false, WI, WJ, FI, FJ, kPlain>(dx, (ProductArgs)args, blockIdx.x, blocks);
+    else
+        run_tiles<T, false, false, WI, WJ, FI, FJ, kPlain>(dw, (ProductArgs)(args + sizeof(Task)), blockIdx.x - blocks, gridDim.x - blocks);
+}
+
+// A kernel's tile, on-chip memory and the workgroups that the GPU holds.
+template <int WI, int WJ, int FI, int FJ>
+struct Shape {
+    static constexpr int kI = WI * FI * 32, kJ = WJ * FJ * 32;
+    static constexpr size_t kBytes = (size_t)2 * (kI + kJ) * 128 + (size_t)WI * WJ * 16 * FJ * 32 * 4;
+    static constexpr int64_t kSlots = (int64_t)kCUs * (int64_t)(kLdsBytes / kBytes);
+};
+
+template <class S>
+Task task_of(const Product &q)
+{
+    return Task{q, (int)((q.M + S::kI - 1) / S::kI), (int)((q.N + S::kJ - 1) / S::kJ)};
+}
+template <class S>
+int64_t blocks_of(const Product &q)
+{
+    const int64_t n = ((q.M + S::kI - 1) / S::kI) * ((q.N + S::kJ - 1) / S::kJ) * q.split;
+    return n >= kMostSize ? n : std::min(S::kSlots, (n + 7) / 8 * 8);
+}
+
+template <class S, class K>
+int take_lds(K kernel)
+{
+    if (S::kBytes <= 64 * 1024) return FB_OK;
+    const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)S::kBytes);
+    return e == hipSuccess ? FB_OK : fail(FB_EHIP, std::string("hipFuncSetAttribute(LDS size): ") + hipGetErrorString(e));
+}
+
+template <class T, bool ALONG_A, bool ALONG_B, int WI, int WJ, int FI, int FJ, int KIND>
 int launch(const Product &q, hipStream_t stream)
 {
-    constexpr int kI = WI * FI * 32, kJ = WJ * FJ * 32;
-    const int64_t ti = (q.M + kI - 1) / kI, tj = (q.N + kJ - 1) / kJ;
-    if (ti * tj * q.split >= kMostSize) return fail(FB_EUNSUPPORTED, "affine product: more than 2^31 tiles");
-    constexpr size_t bytes = (size_t)2 * (kI + kJ) * 128 + (size_t)WI * WJ * 16 * FJ * 32 * 4;
-    constexpr int64_t slots = (int64_t)kCUs * (int64_t)(kLdsBytes / bytes);      // workgroups that the GPU holds
+    typedef Shape<WI, WJ, FI, FJ> S;
+    const int64_t blocks = blocks_of<S>(q);
+    if (blocks >= kMostSize) return fail(FB_EUNSUPPORTED, "affine product: more than 2^31 tiles");
     const auto kernel = fb_mfma_product_kernel<T, ALONG_A, ALONG_B, WI, WJ, FI, FJ, KIND>;
-    if (bytes > 64 * 1024) {
-        const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-        if (e != hipSuccess) return fail(FB_EHIP, std::string("hipFuncSetAttribute(LDS size): ") + hipGetErrorString(e));
-    }
-    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(slots, (ti * tj * q.split + 7) / 8 * 8)), dim3(WI * WJ * 64), bytes, stream, q, (int)ti, (int)tj);
+    const int rc = take_lds<S>(kernel);
+    if (rc != FB_OK) return rc;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(WI * WJ * 64), S::kBytes, stream, task_of<S>(q));
     return launched("matrix product kernel launch: ");
+}
+
+template <class T, int WI, int WJ, int FI, int FJ>
+int launch_pair(const Product &dx, const Product &dw, hipStream_t stream)
+{
+    typedef Shape<WI, WJ, FI, FJ> S;
+    const int64_t first = blocks_of<S>(dx);
+    const auto kernel = fb_mfma_pair_kernel<T, WI, WJ, FI, FJ>;
+    const int rc = take_lds<S>(kernel);
+    if (rc != FB_OK) return rc;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(first + blocks_of<S>(dw))), dim3(WI * WJ * 64), S::kBytes, stream, task_of<S>(dx), task_of<S>(dw), (int)first);
+    return launched("matrix product kernel launch: ");
+}
+
+template <class T>
+int launch_pair(const Product &dx, const Product &dw, hipStream_t stream)
+{
+    return dx.tile == 128 ? launch_pair<T, 2, 2, 2, 2>(dx, dw, stream) : launch_pair<T, 2, 2, 1, 1>(dx, dw, stream);
 }
 
 template <class T, bool ALONG_A, bool ALONG_B, int KIND>
@@ -515,6 +584,20 @@ int launch(const Product &q, hipStream_t stream)
 }
 
 }  // namespace
+
+bool fits_as_pair(const Product &dx, const Product &dw)
+{
+    // (beyond what the GPU holds at a time they are slower together: 9600 x 84 x 512 in single precision 50 instead of 39 us)
+    if (dx.tile != dw.tile || dx.tile > 128 || dx.M == 0 || dw.K == 0) return false;
+    if (dx.tile == 128) return blocks_of<Shape<2, 2, 2, 2>>(dx) + blocks_of<Shape<2, 2, 2, 2>>(dw) <= Shape<2, 2, 2, 2>::kSlots;
+    return blocks_of<Shape<2, 2, 1, 1>>(dx) + blocks_of<Shape<2, 2, 1, 1>>(dw) <= Shape<2, 2, 1, 1>::kSlots;
+}
+
+int launch_mfma_pair(const Product &dx, const Product &dw, hipStream_t stream)
+{
+    if (dx.type == FB_TYPE_F32) return launch_pair<float>(dx, dw, stream);
+    return dx.type == FB_TYPE_BF16 ? launch_pair<bf16>(dx, dw, stream) : launch_pair<f16>(dx, dw, stream);
+}
 
 int launch_mfma_product(const Product &q, hipStream_t stream)
 {

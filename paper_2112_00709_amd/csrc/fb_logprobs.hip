@@ -115,16 +115,17 @@ __device__ __forceinline__ void merge_heads(const uint64_t *keys, int lists, int
     const uint32_t least = reached_by((uint32_t)(best >> 32), top);
     int count = 0;
     if (least != 0) {
+        for (bool any = true; any && count <= 64;) {
+            any = false;
 #pragma unroll
-        for (int h = 0; h < HEADS; ++h) {
-            for (;;) {
+            for (int h = 0; h < HEADS; ++h) {
                 const bool in = (uint32_t)(head[h] >> 32) >= least;
                 const uint64_t hit = __ballot(in);
-                if (hit == 0 || count > 64) break;
                 const int to = count + __popcll(hit & ((1ull << lane) - 1));
                 if (in && to < 64) list[to] = head[h];
                 count += __popcll(hit);
                 if (in) move_on(h);
+                any = any || hit != 0;
             }
         }
         lds_settled();
@@ -244,7 +245,7 @@ __device__ __forceinline__ void best_of_wave(const T *row, const u32x4 (&raw)[NV
     uint64_t last = ~0ull;
     for (int t = 0; t < top; ++t) {
         uint64_t best = 0;
-#pragma unroll 4
+#pragma unroll
         for (int i = 0; i < NV; ++i) {
             float v[VE];
             const int at = first + i * stride;
