@@ -245,7 +245,7 @@ __device__ __forceinline__ void best_of_wave(const T *row, const u32x4 (&raw)[NV
     uint64_t last = ~0ull;
     for (int t = 0; t < top; ++t) {
         uint64_t best = 0;
-#pragma unroll
+#pragma unroll 4
         for (int i = 0; i < NV; ++i) {
             float v[VE];
             const int at = first + i * stride;
@@ -345,7 +345,7 @@ __device__ __forceinline__ Stats wave_stats(u32x4 (&raw)[NV], int first, int str
 
 // WAVES waves hold a row, or a workgroup's chunk of one (SPLIT); with one wave a row a workgroup has four rows at a time.
 template <class T, int WAVES, int NV, bool SPLIT>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64, NV * Vec<T>::kN <= 16 ? 8 : 4) void fb_token_logprobs_kernel(TokenParams p)
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64, NV * Vec<T>::kN <= 8 ? 8 : NV * Vec<T>::kN <= 16 ? 6 : 4) void fb_token_logprobs_kernel(TokenParams p)
 {
     constexpr int VE = Vec<T>::kN, kRows = WAVES == 1 ? 4 : 1, kW = WAVES == 1 ? 4 : WAVES;
     __shared__ uint64_t list[kW][64], best[kW][FB_TOP_MAX];
@@ -416,68 +416,106 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64, NV * Vec<T>::kN <= 1
     write_row(p, r, token, given, st, keys, lane);
 }
 
-// Rows of up to 512 elements: a wave a row, element 64 j + lane in the lane's j-th register (narrow loads, but all lanes have
-// their share).  The top-th largest is found bit by bit of its order, exactly; what lies above it and as many of its equals
-// as there is room for, in ascending order of their numbers, are ranked one a lane.
+// Rows of up to 512 elements: a wave a row at a time, element 64 j + lane in the lane's j-th register (narrow loads, but all
+// lanes have their share), the next row asked for before this one is worked on.  A few alternatives are taken one after the
+// other; for more the top-th largest is found bit by bit of its order, exactly, and what lies above it and as many of its
+// equals as there is room for, in ascending order of their numbers, are ranked one a lane.  Bound by instruction issue, some 150
+// a row and 25 an alternative: 69120 rows of 84 floats take 14 us, with 3 alternatives 23 (by the bits, a comparison and a
+// count each for the scalar unit, 38), with 20 46.
 template <class T, int E>
 __global__ __launch_bounds__(256) void fb_token_short_kernel(TokenParams p)
 {
     __shared__ uint64_t list[4][FB_TOP_MAX], best[4][FB_TOP_MAX];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t r = (int64_t)blockIdx.x * 4 + wave;
-    if (r >= p.R) return;                                     // (a whole wave)
-    const int32_t token = p.tokens[r];
-    if (token < 0) {
-        write_padding(p, r, lane);
-        return;
-    }
-    const int n = (int)p.V;
-    const T *row = (const T *)p.logits + r * p.ld;
-    const float given = given_logit<T>(p, r, token);
-    float v[E], m = -kInf;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = (int)p.V;
+    const int64_t step = (int64_t)gridDim.x * 4;
+    int32_t next_token = -1;
+    float next[E];
+    auto ask = [&](int64_t r) {
+        next_token = p.tokens[r];
+        const T *row = (const T *)p.logits + r * p.ld;
 #pragma unroll
-    for (int j = 0; j < E; ++j) v[j] = j * 64 + lane < n ? load_one(row + j * 64 + lane) : -kInf;
+        for (int j = 0; j < E; ++j) next[j] = j * 64 + lane < n ? load_one(row + j * 64 + lane) : -kInf;
+    };
+    int64_t r = (int64_t)blockIdx.x * 4 + wave;
+    if (r < p.R) ask(r);
+    for (; r < p.R; r += step) {
+        const int32_t token = __builtin_amdgcn_readfirstlane(next_token);
+        float v[E], m = -kInf;
 #pragma unroll
-    for (int j = 0; j < E; ++j) m = fmaxf(m, v[j]);
-    m = max_wave(m);
-    const float base = m == -kInf ? 0.0f : m;
-    float S = 0.0f, U = 0.0f;
-#pragma unroll
-    for (int j = 0; j < E; ++j) {
-        const float d = v[j] - base, e = __builtin_amdgcn_exp2f(d * kLog2E);
-        S += e;
-        U = fmaf(e, fmaxf(d, -1e30f), U);                     // (e is 0 where d is -inf)
-    }
-    const Stats st = {m, sum_wave(S), sum_wave(U)};
-    if (p.top) {
-        uint32_t order[E], least = 0;
-#pragma unroll
-        for (int j = 0; j < E; ++j) order[j] = j * 64 + lane < n ? order_of(v[j]) : 0;   // (0: below every number)
-        for (int bit = 31; bit >= 0; --bit) {
-            const uint32_t with = least | 1u << bit;
-            int count = 0;
-#pragma unroll
-            for (int j = 0; j < E; ++j) count += __popcll(__ballot(order[j] >= with));
-            least = count >= p.top ? with : least;
+        for (int j = 0; j < E; ++j) v[j] = next[j];
+        if (r + step < p.R) ask(r + step);
+        if (token < 0) {
+            write_padding(p, r, lane);
+            continue;
         }
-        int filled = 0;
 #pragma unroll
-        for (int equal = 0; equal < 2; ++equal)
+        for (int j = 0; j < E; ++j) m = fmaxf(m, v[j]);
+        m = max_wave(m);
+        const float base = m == -kInf ? 0.0f : m;
+        float S = 0.0f, U = 0.0f;
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-                const bool in = equal ? order[j] == least : order[j] > least;
-                const uint64_t hit = __ballot(in);
-                const int at = filled + __popcll(hit & ((1ull << lane) - 1));
-                if (in && at < p.top) list[wave][at] = (uint64_t)order[j] << 32 | (uint32_t)~(uint32_t)(j * 64 + lane);
-                filled += __popcll(hit);
+        for (int j = 0; j < E; ++j) {
+            const float d = v[j] - base, e = __builtin_amdgcn_exp2f(d * kLog2E);
+            S += e;
+            U = fmaf(e, fmaxf(d, -1e30f), U);                 // (e is 0 where d is -inf)
+        }
+        const Stats st = {m, sum_wave(S), sum_wave(U)};
+        float given = v[0];
+#pragma unroll
+        for (int j = 1; j < E; ++j) given = token >> 6 == j ? v[j] : given;
+        given = token < n ? __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(given), token & 63)) : __builtin_nanf("");
+        if (p.top) {
+            uint32_t order[E];
+#pragma unroll
+            for (int j = 0; j < E; ++j) order[j] = j * 64 + lane < n ? order_of(v[j]) : 0;   // (0: below every number)
+            if (p.top <= 6) {
+                for (int t = 0; t < p.top; ++t) {
+                    uint32_t mine = 0;
+#pragma unroll
+                    for (int j = 0; j < E; ++j) mine = order[j] > mine ? order[j] : mine;
+                    const uint32_t win = max_wave_u(mine);
+                    int owner = -1;                           // the lowest number of those that have it
+#pragma unroll
+                    for (int j = 0; j < E; ++j) {
+                        const uint64_t hit = __ballot(order[j] == win);
+                        const bool here = owner < 0 && hit != 0;
+                        owner = here ? __ffsll((unsigned long long)hit) - 1 : owner;
+                        if (here && lane == owner) {
+                            best[wave][t] = (uint64_t)win << 32 | (uint32_t)~(uint32_t)(j * 64 + lane);
+                            order[j] = 0;
+                        }
+                    }
+                }
+            } else {
+                uint32_t least = 0;
+                for (int bit = 31; bit >= 0; --bit) {
+                    const uint32_t with = least | 1u << bit;
+                    int count = 0;
+#pragma unroll
+                    for (int j = 0; j < E; ++j) count += __popcll(__ballot(order[j] >= with));
+                    least = count >= p.top ? with : least;
+                }
+                int filled = 0;
+#pragma unroll
+                for (int equal = 0; equal < 2; ++equal)
+#pragma unroll
+                    for (int j = 0; j < E; ++j) {
+                        const bool in = equal ? order[j] == least : order[j] > least;
+                        const uint64_t hit = __ballot(in);
+                        const int at = filled + __popcll(hit & ((1ull << lane) - 1));
+                        if (in && at < p.top) list[wave][at] = (uint64_t)order[j] << 32 | (uint32_t)~(uint32_t)(j * 64 + lane);
+                        filled += __popcll(hit);
+                    }
+                lds_settled();
+                const uint64_t mine = lane < p.top ? list[wave][lane] : 0;
+                const int rank = rank_in_wave(mine, p.top);
+                if (lane < p.top) best[wave][rank] = mine;
             }
-        lds_settled();
-        const uint64_t mine = lane < p.top ? list[wave][lane] : 0;
-        const int rank = rank_in_wave(mine, p.top);
-        if (lane < p.top) best[wave][rank] = mine;
+            lds_settled();
+        }
+        write_row(p, r, token, given, st, best[wave], lane);
         lds_settled();
     }
-    write_row(p, r, token, given, st, best[wave], lane);
 }
 
 // What the waves that share a row have found joined, one wave a row.
@@ -633,7 +671,7 @@ template <class T>
 int launch_tokens(const TokenParams &p, const TokenPlan &t, hipStream_t stream)
 {
     if (t.waves == 0) {
-        const dim3 grid((unsigned)((p.R + 3) / 4)), block(256);
+        const dim3 grid((unsigned)std::min<int64_t>((p.R + 3) / 4, 32 * kCUs)), block(256);   // (bound by issue: 8, 16, 32 a unit: 26, 25, 24 us)
         if (p.V <= 64)
             hipLaunchKernelGGL((fb_token_short_kernel<T, 1>), grid, block, 0, stream, p);
         else if (p.V <= 128)
