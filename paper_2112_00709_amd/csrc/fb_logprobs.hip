@@ -3,7 +3,11 @@
 // One pass over the logits.  A wave holds a piece of a row in registers (as stored, 16 bytes a piece and lane), takes its
 // maximum m and with d = x - m the sums S = sum e^d and T = sum e^d d; then log Z = m + log S and H = log S - T / S.  Pieces
 // of a row are joined by (m, S, T) -> (M, S e^(m-M), (T + S (m - M)) e^(m-M)), so a long row is split over as many waves
-// and workgroups as it takes, and the logits are never read twice.
+// and workgroups as it takes; of the logits only the few pieces that hold alternatives are read again.
+//
+// Many rows are bound by memory: 69120 rows of 3000 floats with 3 alternatives take 134 us (6.2 TB/s of the bytes of the rows
+// that count).  Few rows are a chain of latencies: one row of 128000 in bfloat16 takes 6 us in 32 workgroups and 5.5 to join
+// them with 10 alternatives (5.5 in all without alternatives).
 #include "fb_layers_device.h"
 
 namespace fb {
@@ -570,7 +574,8 @@ struct TokenGradParams {
 
 constexpr int kGradPieces = 4;
 
-// One element at a time is all there is to it: bound by memory.  A wave has 4 KB of a row.
+// One element at a time is all there is to it: bound by memory.  A wave has 4 KB of a row.  4095 rows of 32001 in bfloat16
+// (rows at odd addresses) take 103 us, 5.1 TB/s.
 template <class T>
 __global__ __launch_bounds__(256) void fb_token_logprobs_grad_kernel(TokenGradParams p)
 {
