@@ -341,8 +341,6 @@ __global__ __launch_bounds__(256) void fb_layer_norm_long_dw_kernel(NormParams p
     }
 }
 
-}  // namespace
-
 // out[k][c] = sum over i < P of part[i][k][c], in a fixed order: 16 threads share a column, each adding every 16th row.
 __global__ __launch_bounds__(1024) void fb_column_sum_kernel(const float *part, int64_t P, int64_t C, float *out0, float *out1)
 {
@@ -374,14 +372,11 @@ __global__ __launch_bounds__(1024) void fb_column_sum_kernel(const float *part, 
     }
 }
 
-int launch_column_sum(const float *part, int64_t P, int64_t C, int sets, float *out0, float *out1, void *stream)
+int launch_column_sum(const float *part, int64_t P, int64_t C, float *out0, float *out1, void *stream)
 {
-    hipLaunchKernelGGL(fb_column_sum_kernel, dim3((unsigned)((C + 63) / 64), (unsigned)sets), dim3(1024), 0, (hipStream_t)stream, part, P, C,
-                       out0, out1);
+    hipLaunchKernelGGL(fb_column_sum_kernel, dim3((unsigned)((C + 63) / 64), 2), dim3(1024), 0, (hipStream_t)stream, part, P, C, out0, out1);
     return launched("column sum kernel launch: ");
 }
-
-namespace {
 
 constexpr int64_t kRowMax = 16384;       // longest row that a workgroup holds in registers
 // Workgroups of the gradient kernel: two a compute unit, one where it has 16 waves.  (Each leaves a row of sums to be added up:
@@ -508,7 +503,7 @@ int fb_layer_norm_grad(const void *dy, int64_t lddy, const void *x, int64_t ldx,
             rc = dispatch_norm(p, type, wtype, true, (hipStream_t)stream);
             if (rc != FB_OK) return rc;
         }
-        return sums ? launch_column_sum((const float *)ws, R > 0 ? grad_groups(R, H) : 0, H, 2, dweight, dbias, stream) : FB_OK;
+        return sums ? launch_column_sum((const float *)ws, R > 0 ? grad_groups(R, H) : 0, H, dweight, dbias, stream) : FB_OK;
     });
 }
 

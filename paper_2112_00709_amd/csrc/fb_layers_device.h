@@ -148,6 +148,23 @@ __device__ __forceinline__ uint32_t over_wave(uint32_t v, Op op)
     const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
     return op(b[0], b[1]);
 }
+// op over the lane's row of 16 lanes, in each of them.
+template <class Op>
+__device__ __forceinline__ uint32_t over_row(uint32_t v, Op op)
+{
+    v = op(v, lane_move<0xB1>(v));
+    v = op(v, lane_move<0x4E>(v));
+    v = op(v, lane_move<0x141>(v));
+    return op(v, lane_move<0x140>(v));
+}
+__device__ __forceinline__ float sum_row16(float v)
+{
+    return __uint_as_float(over_row(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
+}
+__device__ __forceinline__ float max_row16(float v)
+{
+    return __uint_as_float(over_row(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }));
+}
 __device__ __forceinline__ float sum_wave(float v)
 {
     return __uint_as_float(over_wave(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
@@ -160,10 +177,6 @@ __device__ __forceinline__ float max_wave(float v)
 __device__ __forceinline__ uint32_t max_wave_u(uint32_t v)
 {
     return over_wave(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
-}
-__device__ __forceinline__ uint32_t min_wave_u(uint32_t v)
-{
-    return over_wave(v, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
 }
 
 }  // namespace

@@ -420,12 +420,10 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64, NV * Vec<T>::kN <= 8
     write_row(p, r, token, given, st, keys, lane);
 }
 
-// Rows of up to 512 elements: a wave a row at a time, element 64 j + lane in the lane's j-th register (narrow loads, but all
-// lanes have their share), the next row asked for before this one is worked on.  A few alternatives are taken one after the
-// other; for more the top-th largest is found bit by bit of its order, exactly, and what lies above it and as many of its
-// equals as there is room for, in ascending order of their numbers, are ranked one a lane.  Bound by instruction issue, some 150
-// a row and 25 an alternative: 69120 rows of 84 floats take 14 us, with 3 alternatives 23 (by the bits, a comparison and a
-// count each for the scalar unit, 38), with 20 46.
+// Rows of up to 512 elements with more than kTakenInTurn alternatives: a wave a row at a time, element 64 j + lane in the lane's
+// j-th register, the next row asked for before this one is worked on.  The top-th largest is found bit by bit of its order,
+// exactly, and what lies above it and as many of its equals as there is room for, in ascending order of their numbers, are
+// ranked one a lane.  Bound by instruction issue, the bits for the most part: a comparison and a count each and register.
 template <class T, int E>
 __global__ __launch_bounds__(256) void fb_token_short_kernel(TokenParams p)
 {
@@ -468,57 +466,115 @@ __global__ __launch_bounds__(256) void fb_token_short_kernel(TokenParams p)
 #pragma unroll
         for (int j = 1; j < E; ++j) given = token >> 6 == j ? v[j] : given;
         given = token < n ? __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(given), token & 63)) : __builtin_nanf("");
-        if (p.top) {
-            uint32_t order[E];
+        uint32_t order[E];
 #pragma unroll
-            for (int j = 0; j < E; ++j) order[j] = j * 64 + lane < n ? order_of(v[j]) : 0;   // (0: below every number)
-            if (p.top <= 6) {
-                for (int t = 0; t < p.top; ++t) {
-                    uint32_t mine = 0;
+        for (int j = 0; j < E; ++j) order[j] = j * 64 + lane < n ? order_of(v[j]) : 0;   // (0: below every number)
+        uint32_t least = 0;
+        for (int bit = 31; bit >= 0; --bit) {
+            const uint32_t with = least | 1u << bit;
+            int count = 0;
 #pragma unroll
-                    for (int j = 0; j < E; ++j) mine = order[j] > mine ? order[j] : mine;
-                    const uint32_t win = max_wave_u(mine);
-                    int owner = -1;                           // the lowest number of those that have it
-#pragma unroll
-                    for (int j = 0; j < E; ++j) {
-                        const uint64_t hit = __ballot(order[j] == win);
-                        const bool here = owner < 0 && hit != 0;
-                        owner = here ? __ffsll((unsigned long long)hit) - 1 : owner;
-                        if (here && lane == owner) {
-                            best[wave][t] = (uint64_t)win << 32 | (uint32_t)~(uint32_t)(j * 64 + lane);
-                            order[j] = 0;
-                        }
-                    }
-                }
-            } else {
-                uint32_t least = 0;
-                for (int bit = 31; bit >= 0; --bit) {
-                    const uint32_t with = least | 1u << bit;
-                    int count = 0;
-#pragma unroll
-                    for (int j = 0; j < E; ++j) count += __popcll(__ballot(order[j] >= with));
-                    least = count >= p.top ? with : least;
-                }
-                int filled = 0;
-#pragma unroll
-                for (int equal = 0; equal < 2; ++equal)
-#pragma unroll
-                    for (int j = 0; j < E; ++j) {
-                        const bool in = equal ? order[j] == least : order[j] > least;
-                        const uint64_t hit = __ballot(in);
-                        const int at = filled + __popcll(hit & ((1ull << lane) - 1));
-                        if (in && at < p.top) list[wave][at] = (uint64_t)order[j] << 32 | (uint32_t)~(uint32_t)(j * 64 + lane);
-                        filled += __popcll(hit);
-                    }
-                lds_settled();
-                const uint64_t mine = lane < p.top ? list[wave][lane] : 0;
-                const int rank = rank_in_wave(mine, p.top);
-                if (lane < p.top) best[wave][rank] = mine;
-            }
-            lds_settled();
+            for (int j = 0; j < E; ++j) count += __popcll(__ballot(order[j] >= with));
+            least = count >= p.top ? with : least;
         }
+        int filled = 0;
+#pragma unroll
+        for (int equal = 0; equal < 2; ++equal)
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                const bool in = equal ? order[j] == least : order[j] > least;
+                const uint64_t hit = __ballot(in);
+                const int at = filled + __popcll(hit & ((1ull << lane) - 1));
+                if (in && at < p.top) list[wave][at] = (uint64_t)order[j] << 32 | (uint32_t)~(uint32_t)(j * 64 + lane);
+                filled += __popcll(hit);
+            }
+        lds_settled();
+        const uint64_t mine = lane < p.top ? list[wave][lane] : 0;
+        const int rank = rank_in_wave(mine, p.top);
+        if (lane < p.top) best[wave][rank] = mine;
+        lds_settled();
         write_row(p, r, token, given, st, best[wave], lane);
         lds_settled();
+    }
+}
+
+// Rows of up to 512 elements otherwise: four rows a wave, 16 lanes a row, so that a reduction takes 4 steps for four rows instead
+// of 6 for one.  Alternatives are taken one after the other: the largest order left, and among those that have it the lowest
+// number.  Bound by issue still: 69120 rows of 84 floats take 6.5 us, 1.4 us more for each alternative (a row a wave at a time:
+// 14.5 us, with 3 alternatives 23 where they are taken in turn).  In turn and by the bits, 40000 rows: of 84, 20 alternatives
+// 24 and 27 us; of 140, 37 and 40; of 300, 63 and 68: kTakenInTurn.
+constexpr int kTakenInTurn = 24;
+
+// Without PIECES element 16 j + l is in lane l's j-th register.  With them a lane has 16 bytes of the row at a time, the
+// 16 i + l-th; the last, where it is not whole, ends at the row's end, and what it has in common with the one before counts
+// there.  (16-bit rows of 500, 40000 of them: 12 us, one element at a time 24.  Up to 128 elements both are alike.)
+template <class T, int E, bool PIECES>
+__global__ __launch_bounds__(256) void fb_token_tiny_kernel(TokenParams p)
+{
+    const int lane = threadIdx.x & 63, l = lane & 15, n = (int)p.V;
+    const int64_t at = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * 4 + (lane >> 4);
+    const bool real = at < p.R;                               // (a row past the end: the last one again, not stored)
+    const int64_t r = real ? at : p.R - 1;
+    const int32_t token = p.tokens[r];
+    const T *row = (const T *)p.logits + r * p.ld;
+    constexpr int VE = PIECES ? Vec<T>::kN : 1;
+    auto piece = [&](int e) { return (e / VE * 16 + l) * VE; };
+    auto number = [&](int e) { return !PIECES || piece(e) < n - VE ? piece(e) + e % VE : n - VE + e % VE; };
+    auto there = [&](int e) { return piece(e) < n && (!PIECES || number(e) >= piece(e)); };
+    float v[E], m = -kInf;
+    if constexpr (PIECES) {
+#pragma unroll
+        for (int e = 0; e < E; e += VE) unpack<T>(piece(e) < n ? *(const u32x4_any *)(row + number(e)) : u32x4{0, 0, 0, 0}, v + e);
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = there(e) ? load_one(row + number(e)) : -kInf;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = there(e) ? v[e] : -kInf;
+#pragma unroll
+    for (int j = 0; j < E; ++j) m = fmaxf(m, v[j]);
+    m = max_row16(m);
+    const float base = m == -kInf ? 0.0f : m;
+    float S = 0.0f, U = 0.0f, pick = v[0];
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+        const float d = v[j] - base, e = __builtin_amdgcn_exp2f(d * kLog2E);
+        S += e;
+        U = fmaf(e, fmaxf(d, -1e30f), U);                     // (e is 0 where d is -inf)
+        pick = there(j) && number(j) == token ? v[j] : pick;
+    }
+    S = sum_row16(S);
+    U = sum_row16(U);
+    const bool live = token >= 0, dead = m == -kInf && S == 0.0f, known = token < n;
+    const float given = __shfl(pick, (lane & 48) | (token / VE & 15));
+    const float ls = logf(S), logz = dead ? -kInf : m + ls;
+    if (real && l == 0) {
+        if (p.logz) p.logz[r] = live ? logz : 0.0f;
+        if (p.entropy) p.entropy[r] = live && !dead ? ls - U / S : 0.0f;
+        if (p.logprobs) p.logprobs[r] = !live ? 0.0f : !known ? __builtin_nanf("") : dead ? -kInf : given - logz;
+    }
+    if (p.top == 0) return;
+    uint32_t order[E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) order[j] = there(j) ? order_of(v[j]) : 0;   // (0: below every number)
+    for (int t = 0; t < p.top; ++t) {
+        uint32_t mine = 0;
+#pragma unroll
+        for (int j = 0; j < E; ++j) mine = order[j] > mine ? order[j] : mine;
+        const uint32_t win = over_row(mine, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+        uint32_t lowest = ~0u;
+#pragma unroll
+        for (int j = E - 1; j >= 0; --j) lowest = order[j] == win ? (uint32_t)number(j) : lowest;
+        const uint32_t first = over_row(lowest, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+        if (lowest == first) {                                // one lane of the row
+#pragma unroll
+            for (int j = 0; j < E; ++j) order[j] = (uint32_t)number(j) == first ? 0 : order[j];
+            if (real) {
+                const float x = value_of(win);
+                p.top_ids[r * p.top + t] = live ? (int32_t)first : -1;
+                p.top_logprobs[r * p.top + t] = !live ? 0.0f : x == -kInf ? -kInf : x - logz;
+            }
+        }
     }
 }
 
@@ -619,8 +675,34 @@ __global__ __launch_bounds__(256) void fb_token_logprobs_grad_kernel(TokenGradPa
     }
 }
 
-// How a call is laid out.  Rows of up to 512 elements have a kernel of their own (waves = 0).  Otherwise a wave holds up to 64 elements a lane: rows of up to 4096 elements go to a wave each where there
-// are enough of them to fill the GPU, else to four waves; rows that four waves cannot hold are split over workgroups,
+// The same for rows of up to 128 pieces, a piece a lane: `lanes` lanes, a power of two, have a row, so short ones fill the waves
+// too.  (69120 rows of 84 in bfloat16: 10 us, by the kernel above 64; 20000 of 1000: 16 and 22; of 2000, 250 pieces: 27 and 28.)
+template <class T>
+__global__ __launch_bounds__(256) void fb_token_short_grad_kernel(TokenGradParams p, int lanes)
+{
+    constexpr int VE = Vec<T>::kN;
+    const int l = threadIdx.x & (lanes - 1);
+    const int64_t r = (int64_t)blockIdx.x * (256 / lanes) + threadIdx.x / lanes;
+    const int at = l * VE, n = (int)p.V - at;
+    if (r >= p.R || n <= 0) return;
+    const int32_t token = p.tokens[r];
+    const float logz = p.logz[r];
+    const bool live = token >= 0 && logz != -kInf;
+    const float g = p.g_logprobs ? p.g_logprobs[r] : 0.0f, h = p.g_entropy ? p.g_entropy[r] : 0.0f, ent = p.g_entropy ? p.entropy[r] : 0.0f;
+    const float a = fmaf(h, ent, g);
+    float v[VE];
+    unpack<T>(load_piece((const T *)p.logits + r * p.ld + at, n), v);
+#pragma unroll
+    for (int j = 0; j < VE; ++j) {
+        const float lp = v[j] - logz, q = __builtin_amdgcn_exp2f(lp * kLog2E);
+        const float d = -q * fmaf(h, fmaxf(lp, -1e30f), a) + (at + j == token ? g : 0.0f);
+        v[j] = live ? d : 0.0f;
+    }
+    store_piece((T *)p.dlogits + r * p.ldd + at, n, pack<T>(v));
+}
+
+// How a call is laid out.  Rows of up to 512 elements have kernels of their own (waves = 0).  Otherwise a wave holds up to 64
+// elements a lane: rows of up to 4096 elements go to a wave each where there are enough of them to fill the GPU, else to four; rows that four waves cannot hold are split over workgroups,
 // and so are long rows that are few.
 struct TokenPlan {
     int waves, nv, split;
@@ -677,14 +759,27 @@ int launch_tokens(const TokenParams &p, const TokenPlan &t, hipStream_t stream)
 {
     if (t.waves == 0) {
         const dim3 grid((unsigned)std::min<int64_t>((p.R + 3) / 4, 32 * kCUs)), block(256);   // (bound by issue: 8, 16, 32 a unit: 26, 25, 24 us)
-        if (p.V <= 64)
-            hipLaunchKernelGGL((fb_token_short_kernel<T, 1>), grid, block, 0, stream, p);
-        else if (p.V <= 128)
-            hipLaunchKernelGGL((fb_token_short_kernel<T, 2>), grid, block, 0, stream, p);
-        else if (p.V <= 256)
-            hipLaunchKernelGGL((fb_token_short_kernel<T, 4>), grid, block, 0, stream, p);
-        else
-            hipLaunchKernelGGL((fb_token_short_kernel<T, 8>), grid, block, 0, stream, p);
+        const dim3 tiny((unsigned)((p.R + 15) / 16));
+        if (p.top > kTakenInTurn) {
+            if (p.V <= 64)
+                hipLaunchKernelGGL((fb_token_short_kernel<T, 1>), grid, block, 0, stream, p);
+            else if (p.V <= 128)
+                hipLaunchKernelGGL((fb_token_short_kernel<T, 2>), grid, block, 0, stream, p);
+            else if (p.V <= 256)
+                hipLaunchKernelGGL((fb_token_short_kernel<T, 4>), grid, block, 0, stream, p);
+            else
+                hipLaunchKernelGGL((fb_token_short_kernel<T, 8>), grid, block, 0, stream, p);
+        } else if (p.V <= 32) {
+            hipLaunchKernelGGL((fb_token_tiny_kernel<T, 2, false>), tiny, block, 0, stream, p);
+        } else if (p.V <= 64) {
+            hipLaunchKernelGGL((fb_token_tiny_kernel<T, 4, false>), tiny, block, 0, stream, p);
+        } else if (p.V <= 128) {
+            hipLaunchKernelGGL((fb_token_tiny_kernel<T, 8, false>), tiny, block, 0, stream, p);
+        } else if (p.V <= 256) {
+            hipLaunchKernelGGL((fb_token_tiny_kernel<T, 16, true>), tiny, block, 0, stream, p);
+        } else {
+            hipLaunchKernelGGL((fb_token_tiny_kernel<T, 32, true>), tiny, block, 0, stream, p);
+        }
         return launched("token log probability kernel launch: ");
     }
 #define FB_TOKENS(W, N) launch_tokens<T, W, N>(p, stream)
@@ -806,7 +901,7 @@ int fb_token_logprobs_grad(const void *logits, int64_t ld, const int32_t *tokens
         TokenGradParams p{};
         p.logits = logits; p.ld = ld; p.R = R; p.V = V; p.ldd = ldd; p.tokens = tokens; p.logz = logz; p.entropy = entropy;
         p.g_logprobs = g_logprobs; p.g_entropy = g_entropy; p.dlogits = dlogits;
-        const int64_t wide = 64 * kGradPieces * (16 / (int64_t)type_bytes(type));
+        const int64_t ve = 16 / (int64_t)type_bytes(type), wide = 64 * kGradPieces * ve;
         p.pieces = (V + wide - 1) / wide;
         const int64_t rows = std::max<int64_t>(1, kPiecesALaunch / p.pieces);
         for (int64_t r = 0; r < R; r += rows) {
@@ -819,7 +914,18 @@ int fb_token_logprobs_grad(const void *logits, int64_t ld, const int32_t *tokens
             q.logz = from_row(logz, r); q.entropy = from_row(entropy, r);
             q.g_logprobs = from_row(g_logprobs, r); q.g_entropy = from_row(g_entropy, r);
             const dim3 grid((unsigned)((q.items + 3) / 4)), block(256);
-            if (type == FB_TYPE_F32)
+            const int64_t row_pieces = (V + ve - 1) / ve;
+            if (row_pieces <= 128) {
+                int lanes = 1;
+                while (lanes < row_pieces) lanes *= 2;
+                const dim3 few((unsigned)((q.R * lanes + 255) / 256));
+                if (type == FB_TYPE_F32)
+                    hipLaunchKernelGGL(fb_token_short_grad_kernel<float>, few, block, 0, (hipStream_t)stream, q, lanes);
+                else if (type == FB_TYPE_BF16)
+                    hipLaunchKernelGGL(fb_token_short_grad_kernel<bf16>, few, block, 0, (hipStream_t)stream, q, lanes);
+                else
+                    hipLaunchKernelGGL(fb_token_short_grad_kernel<f16>, few, block, 0, (hipStream_t)stream, q, lanes);
+            } else if (type == FB_TYPE_F32)
                 hipLaunchKernelGGL(fb_token_logprobs_grad_kernel<float>, grid, block, 0, (hipStream_t)stream, q);
             else if (type == FB_TYPE_BF16)
                 hipLaunchKernelGGL(fb_token_logprobs_grad_kernel<bf16>, grid, block, 0, (hipStream_t)stream, q);

@@ -220,6 +220,26 @@ def test_gradient_against_the_formula(fl, R, V, dtype, gap):
         assert d.dtype == x.dtype
 
 
+@pytest.mark.parametrize("V", [5, 31, 32, 33, 64, 65, 127, 128, 129, 136, 137, 200, 255, 256, 257, 263, 383, 511, 512, 1000, 1025])
+@pytest.mark.parametrize("dtype,gap", [("float32", 1), ("bfloat16", 0), ("float16", 3)])
+def test_short_rows_of_every_kind_of_end(fl, V, dtype, gap):
+    """Rows that end inside, at and after a piece of 16 bytes, as many as do not fill a workgroup; few and many alternatives."""
+    import torch
+    R = 37
+    x, tokens = make(R, V, dtype, gap, V)
+    tokens[5], tokens[6] = V - 1, 0
+    for top in sorted({min(t, V) for t in (0, 3, 24, 25)}):
+        check(fl, x, tokens, top)
+    gen = torch.Generator().manual_seed(V)
+    g, h = torch.randn(R, generator=gen).cuda(), torch.randn(R, generator=gen).cuda()
+    lp, ent, z, _, _ = fl.fb_token_logprobs(x, tokens)
+    d = fl.fb_token_logprobs_grad(x, tokens, z, ent, g, h)
+    want = grad_definition(x, tokens, z, ent, g, h)
+    size = g.abs().cpu().double() + h.abs().cpu().double() * (2 + 2 * math.log(V + 1))
+    tol = 60 * U * size[:, None] + H_OF[dtype] * want.abs() + (2.0 ** -24 if dtype == "float16" else 0)
+    assert ((d.double().cpu() - want).abs() <= tol).all()
+
+
 def test_gradient_against_differences(fl):
     import torch
     gen = torch.Generator().manual_seed(3)
