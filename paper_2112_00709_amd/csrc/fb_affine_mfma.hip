@@ -8,10 +8,12 @@
 // first 16 and a lane of the upper half the others: in single precision, whose instruction takes 2 k, the four k of the one
 // are multiplied beside those of the other.
 //
-// LDS banks.  [row][k]: the 16-byte piece c of a row lies at piece c ^ (row & 7), so eight rows read at one c cover all
-// banks.  [k][rows] of 16 bits: piece c of a k lies at c ^ ((k & 3) << 1): the four k that a transposing read takes at once
-// lie in different quarters of the banks.  The copies write LDS in order of lanes, so the exchange is in the address a lane
-// reads.
+// LDS banks.  [row][k]: the 16-byte piece c of a row lies at piece c ^ (row & 7), so eight rows read at one c share no bank
+// of 32.  [k][rows] of 16 bits: piece c of a k lies at c ^ ((k & 3) << 1): the four k that a transposing read takes at once
+// lie in different quarters of those.  The copies write LDS in order of lanes, so the exchange is in the address a lane reads.
+// There are 64 banks, and the counters say that half of the passes are conflicts.  An exchange over all 64 (row >> 1 instead of
+// row, k << 2 instead of k << 1) has none, and LDS is busy 26 % of the time instead of 43 %; the times stayed what they are
+// (8192 cubed 875 and 875 us, 69120 x 3000 x 1024 446 and 446), for two more registers: LDS is not what bounds this.
 //
 // Measured, bfloat16: 8192 cubed 840 us forward (1310 TFLOP/s; the library's product on the same card 1376), 836 for dx, 816
 // for dW (the library 1211 and 1069).  69120 x 3000 x 1024: 435 us, 497 with single-precision output (library, bfloat16 output:
