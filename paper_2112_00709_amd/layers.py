@@ -116,6 +116,13 @@ def _out(like, shape, dtype):
     return t
 
 
+def _out_like(t):
+    """An output of t's shape and type, contiguous (where t is too by the shorter way: a third of a small call is allocations)."""
+    if _base.POISON_NEW_BUFFERS or not t.is_contiguous():
+        return _out(t, t.shape, t.dtype)
+    return torch.empty_like(t)
+
+
 def _workspace(n: int, like):
     if n == 0:
         return None, None
@@ -135,10 +142,10 @@ def fb_layer_norm(x, weight=None, bias=None, eps: float = 1e-5, want_stats: bool
     if weight is not None and bias is not None and weight.dtype != bias.dtype:
         raise ValueError("weight and bias must have one type")
     pw, pb = _vector(weight, "weight", H, (torch.float32, x.dtype), dev), _vector(bias, "bias", H, (torch.float32, x.dtype), dev)
-    y = _out(x, x.shape, x.dtype)
+    y = _out_like(x)
     mean = rstd = pm = pr = None
     if want_stats:
-        mean, rstd = _out(x, x.shape[:-1], torch.float32), _out(x, x.shape[:-1], torch.float32)
+        mean, rstd = _out(x, (2, *x.shape[:-1]), torch.float32).unbind(0)
         pm, pr = mean.data_ptr(), rstd.data_ptr()
     _check(L.fb_layer_norm(px, ldx, pw, pb, wtype, R, H, code, eps, y.data_ptr(), H, pm, pr, _raw_stream(dev)))
     return (y, mean, rstd) if want_stats else y
@@ -155,7 +162,7 @@ def fb_layer_norm_grad(dy, x, mean, rstd, weight=None, want_dx: bool = True, wan
     pm, pr = _vector(mean, "mean", R, (torch.float32,), dev), _vector(rstd, "rstd", R, (torch.float32,), dev)
     wtype = F32 if weight is None else _type(weight, "weight")
     pw = _vector(weight, "weight", H, (torch.float32, x.dtype), dev)
-    dx = _out(x, x.shape, x.dtype) if want_dx else None
+    dx = _out_like(x) if want_dx else None
     dw = _out(x, (H,), torch.float32) if want_dweight else None
     db = _out(x, (H,), torch.float32) if want_dbias else None
     need = int(L.fb_layer_norm_grad_workspace_bytes(R, H)) if want_dweight or want_dbias else 0
@@ -221,7 +228,7 @@ def fb_affine_grad(dy, x, weight, activation: str = "none", preact=None, want_dx
         if preact is None:
             raise ValueError("preact is needed for this activation")
         pz, ldz, _, _, _ = _rows(preact, "preact", N, x.dtype, x.shape[:-1], dev)
-    dx = _out(x, x.shape, x.dtype) if want_dx else None
+    dx = _out_like(x) if want_dx else None
     dw = _out(x, (N, K), x.dtype) if want_dweight else None
     db = _out(x, (N,), torch.float32) if want_dbias else None
     dtype = _types[dy.dtype]
@@ -264,6 +271,6 @@ def fb_token_logprobs_grad(logits, tokens, logz, entropy, g_logprobs, g_entropy=
     pt, pz = _vector(tokens, "tokens", R, (torch.int32,), dev), _vector(logz, "logz", R, f, dev)
     pe = _vector(entropy, "entropy", R, f, dev)
     pg, ph = _vector(g_logprobs, "g_logprobs", R, f, dev), _vector(g_entropy, "g_entropy", R, f, dev)
-    d = _out(logits, logits.shape, logits.dtype)
+    d = _out_like(logits)
     _check(L.fb_token_logprobs_grad(p, ld, pt, pz, pe, pg, ph, R, V, code, d.data_ptr(), V, _raw_stream(dev)))
     return d
