@@ -36,6 +36,7 @@ struct Product {
     int split;
     int64_t share;       // length of a share
     int tile;            // 256, 128 or 64, the side of the tiles
+    bool past;           // y goes past the caches (never parts: they are joined at once)
 };
 
 int launch_mfma_product(const Product &q, hipStream_t stream);   // factors as ready() wants them

@@ -16,7 +16,7 @@
 // (8192 cubed 875 and 875 us, 69120 x 3000 x 1024 446 and 446), for two more registers: LDS is not what bounds this.
 //
 // Measured, bfloat16: 8192 cubed 840 us forward (1310 TFLOP/s; the library's product on the same card 1376), 836 for dx, 816
-// for dW (the library 1211 and 1069).  69120 x 3000 x 1024: 435 us, 497 with single-precision output (library, bfloat16 output:
+// for dW (the library 1211 and 1069).  69120 x 3000 x 1024: 435 us, 471 with single-precision output (library, bfloat16 output:
 // 483); of these some 370 are the products and the rest the sums' way out, which nothing overlaps: workgroups do it at the
 // same time, and with one workgroup a compute unit (128 of 160 KB of LDS) a unit's matrix cores wait meanwhile.  Tiles of 128
 // in two workgroups a unit overlap it but read LDS more: 534 us.  Four waves of 128 x 128 instead of eight of 128 x 64: the
@@ -173,12 +173,26 @@ __device__ __forceinline__ f32x4 load_four(const T *p)
     }
 }
 template <class T>
-__device__ __forceinline__ void store_four(T *p, const f32x4 &v)
+__device__ __forceinline__ void store_four(T *p, const f32x4 &v, bool past)
 {
-    if constexpr (sizeof(T) == 4)
-        *(f32x4_any *)p = v;
-    else
-        *(u32x2_any *)p = u32x2{pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3])};
+    if constexpr (sizeof(T) == 4) {
+        if (past) {
+            apart();
+            __builtin_nontemporal_store(v, (f32x4_any *)p);
+            apart();
+        } else {
+            *(f32x4_any *)p = v;
+        }
+    } else {
+        const u32x2 four = {pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3])};
+        if (past) {
+            apart();
+            __builtin_nontemporal_store(four, (u32x2_any *)p);
+            apart();
+        } else {
+            *(u32x2_any *)p = four;
+        }
+    }
 }
 
 // R times four neighbouring sums, `step` rows apart: those of a lane's row `row`, row + step, .. below `rows`, n of the four
@@ -190,14 +204,18 @@ struct Spot {
 };
 
 template <class T, class O, int R, int STEP>
-__device__ __forceinline__ void store_rows(O *p, int64_t ld, const Spot &at, const f32x4 (&w)[R])
+__device__ __forceinline__ void store_rows(O *p, int64_t ld, const Spot &at, const f32x4 (&w)[R], bool past)
 {
     O *base = p + at.i * ld + at.j;
     const uint32_t off = (uint32_t)at.row * (uint32_t)ld + (uint32_t)at.col;
-    if (at.n == 4) {
+    if (at.n == 4 && past) {
 #pragma unroll
         for (int r = 0; r < R; ++r, base += STEP * ld)
-            if (at.row + r * STEP < at.rows) store_four(base + off, w[r]);
+            if (at.row + r * STEP < at.rows) store_four(base + off, w[r], true);
+    } else if (at.n == 4) {
+#pragma unroll
+        for (int r = 0; r < R; ++r, base += STEP * ld)
+            if (at.row + r * STEP < at.rows) store_four(base + off, w[r], false);
     } else {
 #pragma unroll 1
         for (int e = 0; e < at.n; ++e) {
@@ -265,6 +283,7 @@ __device__ __forceinline__ void leave(ProductArgs args, const f32x16 (&acc)[FI][
     const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)mine + (lane & 15) * FJ * 128;
     const bool split = KIND == kPlain && args->parts, relu = KIND == FB_ACT_RELU || (KIND == kPlain && !split && args->f.act == FB_ACT_RELU);
     const int out_type = split ? FB_TYPE_F32 : args->f.out_type;
+    const bool past = args->past;
     const int64_t ld = split ? N : args->f.ldy;
     void *y = split ? (void *)(args->part + (size_t)share * M * N) : args->f.y;
     const void *residual = KIND == kPlain ? nullptr : args->f.residual;
@@ -299,9 +318,9 @@ __device__ __forceinline__ void leave(ProductArgs args, const f32x16 (&acc)[FI][
     };
     auto store = [&](const Spot &at, const f32x4 (&w)[kR]) {
         if (out_type == FB_TYPE_F32)
-            store_rows<T, float, kR, kRows>((float *)y, ld, at, w);
+            store_rows<T, float, kR, kRows>((float *)y, ld, at, w, past);
         else
-            store_rows<T, T, kR, kRows>((T *)y, ld, at, w);
+            store_rows<T, T, kR, kRows>((T *)y, ld, at, w, past);
     };
     if constexpr (KIND == kPlain) {
 #pragma unroll
@@ -337,7 +356,7 @@ __device__ __forceinline__ void leave(ProductArgs args, const f32x16 (&acc)[FI][
             get(w);
             const Spot at = spot(pass);
             if (at.rows > in_row && nj > 0) {
-                if (args->f.preact) store_rows<T, T, kR, kRows>((T *)args->f.preact, args->f.ldp, at, w);
+                if (args->f.preact) store_rows<T, T, kR, kRows>((T *)args->f.preact, args->f.ldp, at, w, past);
                 act(w, KIND);
                 if (res16) add_rows<T, kR>(at, raw, w);
                 if (res32) add_rows<kR, kRows>(res32, args->f.ldr, at, w);
@@ -526,7 +545,9 @@ struct Shape {
 template <class S>
 Task task_of(const Product &q)
 {
-    return Task{q, (int)((q.M + S::kI - 1) / S::kI), (int)((q.N + S::kJ - 1) / S::kJ)};
+    Task t{q, (int)((q.M + S::kI - 1) / S::kI), (int)((q.N + S::kJ - 1) / S::kJ)};
+    t.q.past = !q.parts && goes_past(q.M, q.N, q.f.out_type);
+    return t;
 }
 template <class S>
 int64_t blocks_of(const Product &q)

@@ -15,6 +15,7 @@ struct NormParams {
     float eps;
     float *mean, *rstd;            // out; in for the gradient
     float *part;                   // gradient: [workgroup][2][H], shares of dweight and dbias
+    bool past;                     // y goes past the caches
 };
 
 // EPL elements of a vector of [H] as floats, at the places a lane has of a row; `none` where there is no vector.
@@ -119,7 +120,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void fb_layer_norm_k
             float o[VE];
 #pragma unroll
             for (int j = 0; j < VE; ++j) o[j] = fmaf(v[i * VE + j] * rstd, w[i * VE + j], b[i * VE + j]);
-            store_piece(y + at, H - at, pack<T>(o));
+            store_piece(y + at, H - at, pack<T>(o), p.past);
         }
     }
 }
@@ -168,7 +169,7 @@ __global__ __launch_bounds__(1024) void fb_layer_norm_long_kernel(NormParams p)
                 const float b = p.bias && in ? (float)((const W *)p.bias)[at + j] : 0.0f;
                 o[j] = fmaf((v[j] - mean) * rstd, w, b);
             }
-            store_piece(y + at, H - at, pack<T>(o));
+            store_piece(y + at, H - at, pack<T>(o), p.past);
         }
     }
 }
@@ -244,7 +245,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void fb_layer_norm_g
                 float o[VE];
 #pragma unroll
                 for (int j = 0; j < VE; ++j) o[j] = s * (g[i * VE + j] - c0 - xh[i * VE + j] * c1);
-                store_piece(dx + at, H - at, pack<T>(o));
+                store_piece(dx + at, H - at, pack<T>(o), p.past);
             }
         }
     }
@@ -306,7 +307,7 @@ __global__ __launch_bounds__(1024) void fb_layer_norm_long_dx_kernel(NormParams 
                 const float w = p.weight && at + j < H ? (float)((const W *)p.weight)[at + j] : 1.0f;
                 o[j] = s * (g[j] * w - c0 - (v[j] - m) * s * c1);
             }
-            store_piece(dx + at, H - at, pack<T>(o));
+            store_piece(dx + at, H - at, pack<T>(o), p.past);
         }
     }
 }
@@ -470,6 +471,7 @@ int fb_layer_norm(const void *x, int64_t ldx, const void *weight, const void *bi
         if (R == 0) return FB_OK;
         NormParams p{};
         p.x = x; p.ldx = ldx; p.weight = weight; p.bias = bias; p.R = R; p.H = H; p.eps = eps; p.y = y; p.ldy = ldy;
+        p.past = goes_past(R, H, type);
         p.mean = mean; p.rstd = rstd;
         return dispatch_norm(p, type, wtype, false, (hipStream_t)stream);
     });
@@ -497,6 +499,7 @@ int fb_layer_norm_grad(const void *dy, int64_t lddy, const void *x, int64_t ldx,
             return fail(FB_EINVAL, "fb_layer_norm_grad: workspace missing or too small");
         NormParams p{};
         p.x = x; p.ldx = ldx; p.dy = dy; p.lddy = lddy; p.weight = weight; p.R = R; p.H = H; p.y = dx; p.ldy = lddx;
+        p.past = goes_past(R, H, type);
         p.mean = const_cast<float *>(mean); p.rstd = const_cast<float *>(rstd);
         p.part = sums ? (float *)ws : nullptr;
         if (R > 0 && (dx || sums)) {

@@ -625,6 +625,7 @@ struct TokenGradParams {
     const int32_t *tokens;
     const float *logz, *entropy, *g_logprobs, *g_entropy;
     void *dlogits;
+    bool past;                 // dlogits goes past the caches
     int64_t pieces, items;     // pieces of 64 * kGradPieces vectors a row, and of all rows
 };
 
@@ -671,7 +672,7 @@ __global__ __launch_bounds__(256) void fb_token_logprobs_grad_kernel(TokenGradPa
 #pragma unroll
             for (int j = 0; j < VE; ++j) v[j] = 0.0f;
         }
-        store_piece(out + at, n - at, pack<T>(v));
+        store_piece(out + at, n - at, pack<T>(v), p.past);
     }
 }
 
@@ -901,6 +902,7 @@ int fb_token_logprobs_grad(const void *logits, int64_t ld, const int32_t *tokens
         TokenGradParams p{};
         p.logits = logits; p.ld = ld; p.R = R; p.V = V; p.ldd = ldd; p.tokens = tokens; p.logz = logz; p.entropy = entropy;
         p.g_logprobs = g_logprobs; p.g_entropy = g_entropy; p.dlogits = dlogits;
+        p.past = goes_past(R, V, type);
         const int64_t ve = 16 / (int64_t)type_bytes(type), wide = 64 * kGradPieces * ve;
         p.pieces = (V + wide - 1) / wide;
         const int64_t rows = std::max<int64_t>(1, kPiecesALaunch / p.pieces);
