@@ -1,6 +1,6 @@
 // Layer norm and its gradient (fb_layers.h).  Both are bound by memory: a row is read once into registers, everything that
-// needs it whole is formed there, and it is written once.  69120 rows of 1024 in bfloat16 take 51 us forward (5.5 TB/s of the
-// bytes that have to be moved; a large copy reaches 4.8) and 84 us backward (5.1 TB/s, 5 us of them the reduction of the
+// needs it whole is formed there, and it is written once.  69120 rows of 1024 in bfloat16 take 53 us forward (5.3 TB/s of the
+// bytes that have to be moved; a large copy reaches 4.8) and 81 us backward (5.3 TB/s, 5 us of them the reduction of the
 // weight's gradient), 8000 rows of 4096 floats 43 and 84; single rows 3 us of latency.
 #include "fb_layers_device.h"
 
