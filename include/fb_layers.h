@@ -93,7 +93,9 @@ size_t fb_affine_grad_workspace_bytes(const void *dy, int64_t lddy, int dy_type,
  *   dy       [M][N] of `dy_type`, `type` or FB_TYPE_F32;  preact [M][N] of `type`, needed unless act is FB_ACT_NONE
  *   dx       out, [M][K] of `type`, nullable;  dweight out, [N][K] of `type`, contiguous, nullable;  dbias out, float [N], nullable
  * Where `type` has 16 bits the matrix units take dz in it: it is rounded to `type` before the two products if act or dy_type
- * makes it anything else (an error of the size of the outputs' own rounding); dbias is summed before that.
+ * makes it anything else (an error of the size of the outputs' own rounding); dbias is summed before that.  To FB_TYPE_F16 it is
+ * rounded times a power of two that brings the largest finite |dy| into [2^14, 2^15), and the products are taken times its inverse, so
+ * dy may be of any size; a dz below 2^-29 of the largest |dy| is off by up to 2^-39 of that.
  * Errors as fb_affine (the limits for M > 64 hold for every M, dy among them); dy, x and weight must not be NULL.
  */
 int fb_affine_grad(const void *dy, int64_t lddy, int dy_type, const void *x, int64_t ldx, const void *weight, int64_t ldw,

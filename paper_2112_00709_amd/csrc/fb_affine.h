@@ -13,7 +13,8 @@ struct Factor {
     bool along;
 };
 
-// What becomes of the sums: y = act(sum + bias[j]) + residual, preact = sum + bias[j].
+// What becomes of the sums: y = act(sum + bias[j]) + residual, preact = sum + bias[j].  Sums of half-precision products whose first
+// factor is dz are taken times *undo before that (see fb_peak_kernel).
 struct Finish {
     const float *bias;
     const void *residual;
@@ -24,6 +25,7 @@ struct Finish {
     int out_type;
     void *preact;        // of the factors' type
     int64_t ldp;
+    const float *undo;   // nullable
 };
 
 struct Product {

@@ -272,7 +272,7 @@ constexpr int kPlain = -1;
 typedef const __attribute__((address_space(4))) Product *ProductArgs;
 
 template <class T, int FI, int FJ, int KIND>
-__device__ __forceinline__ void leave(ProductArgs args, const f32x16 (&acc)[FI][FJ], const f32x4 &bias, int share, int64_t i0, int64_t j0, float *mine)
+__device__ __forceinline__ void leave(ProductArgs args, const f32x16 (&acc)[FI][FJ], const f32x4 &bias, float undo, int share, int64_t i0, int64_t j0, float *mine)
 {
     // What is needed here alone is fetched and computed here: kept over the loops before it costs registers that they need.
     int lane = threadIdx.x & 63;
@@ -306,7 +306,9 @@ __device__ __forceinline__ void leave(ProductArgs args, const f32x16 (&acc)[FI][
 #pragma unroll
         for (int r = 0; r < kR; ++r) {
             const int row = r * kRows + in_row;
-            w[r] = *(const f32x4 *)(mine + row * FJ * 32 + ((lane % kPer) ^ (row & (kPer - 1))) * 4) + bias;
+            const f32x4 s = *(const f32x4 *)(mine + row * FJ * 32 + ((lane % kPer) ^ (row & (kPer - 1))) * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[r][e] = fmaf(s[e], undo, bias[e]);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     };
@@ -400,6 +402,11 @@ __device__ __forceinline__ void run_tiles(const Task &task, ProductArgs args, in
         const int64_t k0 = (int64_t)share * q.share;
         return Place{share, (int64_t)(first + v % down) * kI, (int64_t)(v / down) * kJ, k0 + q.share < q.K ? q.share : q.K - k0};
     };
+
+    float undo = 1.0f;                     // (products of a half-precision gradient; shares of k leave as they are)
+    if constexpr (std::is_same<T, f16>::value && !ALONG_B) {
+        if (q.f.undo && !q.parts) undo = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(*q.f.undo)));
+    }
 
     constexpr int kDeep = kDeepOf<T>;
     Side<T, ALONG_A, kI, kNW, FI> a;
@@ -511,7 +518,7 @@ __device__ __forceinline__ void run_tiles(const Task &task, ProductArgs args, in
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-        leave<T, FI, FJ, KIND>(args, acc, bias, p.share, p.i0 + wi * FI * 32, p.j0 + wj * FJ * 32,
+        leave<T, FI, FJ, KIND>(args, acc, bias, undo, p.share, p.i0 + wi * FI * 32, p.j0 + wj * FJ * 32,
                                (float *)(lds_raw + 2 * (a.kBytes + b.kBytes)) + wave * 16 * FJ * 32);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (no copy into LDS outlives the workgroup)
