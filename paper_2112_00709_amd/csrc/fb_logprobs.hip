@@ -631,6 +631,10 @@ struct TokenGradParams {
 
 constexpr int kGradPieces = 4;
 
+// p = e^lp is 0 in single precision below this, and p (g + h (lp + H)) then too: with lp held here the bracket is finite for every h
+// below 10^36, also where lp is -inf.
+constexpr float kLeastLog = -128.0f;
+
 // One element at a time is all there is to it: bound by memory.  A wave has 4 KB of a row.  4095 rows of 32001 in bfloat16
 // (rows at odd addresses) take 103 us, 5.1 TB/s.
 template <class T>
@@ -665,7 +669,7 @@ __global__ __launch_bounds__(256) void fb_token_logprobs_grad_kernel(TokenGradPa
 #pragma unroll
             for (int j = 0; j < VE; ++j) {
                 const float lp = v[j] - logz, q = __builtin_amdgcn_exp2f(lp * kLog2E);
-                v[j] = -q * fmaf(h, fmaxf(lp, -1e30f), a);
+                v[j] = -q * fmaf(h, fmaxf(lp, kLeastLog), a);
                 if (at + j == hit) v[j] += g;
             }
         } else {
@@ -696,7 +700,7 @@ __global__ __launch_bounds__(256) void fb_token_short_grad_kernel(TokenGradParam
 #pragma unroll
     for (int j = 0; j < VE; ++j) {
         const float lp = v[j] - logz, q = __builtin_amdgcn_exp2f(lp * kLog2E);
-        const float d = -q * fmaf(h, fmaxf(lp, -1e30f), a) + (at + j == token ? g : 0.0f);
+        const float d = -q * fmaf(h, fmaxf(lp, kLeastLog), a) + (at + j == token ? g : 0.0f);
         v[j] = live ? d : 0.0f;
     }
     store_piece((T *)p.dlogits + r * p.ldd + at, n, pack<T>(v));
