@@ -123,7 +123,8 @@ def _layer_functions():
         @staticmethod
         def forward(ctx, logits, tokens, top):
             logprobs, entropy, logz, ids, best = fl.fb_token_logprobs(logits, tokens, top)
-            ctx.save_for_backward(logits, tokens, logz, entropy)
+            if ctx.needs_input_grad[0]:                    # (copies: the caller may change its results in place)
+                ctx.save_for_backward(logits, tokens, logz.clone(), entropy.clone())
             ctx.mark_non_differentiable(logz, ids, best)
             ctx.set_materialize_grads(False)
             return logprobs, entropy, logz, ids, best

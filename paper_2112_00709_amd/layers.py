@@ -30,11 +30,12 @@ _lib = None
 torch = None                     # loaded with the library, see lib()
 _types = {}
 _raw_stream = None               # device index -> address of its current stream
+_current_device = None
 
 
 def lib() -> ctypes.CDLL:
     """The built library with these calls' signatures (fails loudly when it has not been built)."""
-    global _lib, torch, _raw_stream
+    global _lib, torch, _raw_stream, _current_device
     if _lib is None:
         L = _base.lib()
         vp, i32, i64, f32, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
@@ -55,6 +56,8 @@ def lib() -> ctypes.CDLL:
         _types.update({t.float32: F32, t.bfloat16: BF16, t.float16: F16})
         # the stream's address without the object around it, which takes as long to make as a kernel launch
         _raw_stream = getattr(t._C, "_cuda_getCurrentRawStream", None) or (lambda device: t.cuda.current_stream(device).cuda_stream)
+        # (asked for beside a tensor on a GPU only: the runtime has been set up)
+        _current_device = getattr(t._C, "_cuda_getDevice", None) or t.cuda.current_device
         _lib = L
     return _lib
 
@@ -69,7 +72,7 @@ def _type(t, what: str) -> int:
 def _rows(t, what: str, width: Optional[int] = None, dtype=None, lead=None, device: Optional[int] = None):
     """-> (address, row distance, rows, width, device) of [..., width] as rows; device None: it has to be the current one."""
     on = t.get_device()
-    if on < 0 or on != (torch.cuda.current_device() if device is None else device) or t.dim() < 1:
+    if on < 0 or on != (_current_device() if device is None else device) or t.dim() < 1:
         raise ValueError(f"{what} must be a tensor of at least one dimension on the current CUDA device")
     shape = t.shape
     w = shape[-1]
@@ -116,11 +119,17 @@ def _out(like, shape, dtype):
     return t
 
 
-def _out_like(t):
+def _out_like(t, dtype=None):
     """An output of t's shape and type, contiguous (where t is too by the shorter way: a third of a small call is allocations)."""
     if _base.POISON_NEW_BUFFERS or not t.is_contiguous():
-        return _out(t, t.shape, t.dtype)
-    return torch.empty_like(t)
+        return _out(t, t.shape, dtype or t.dtype)
+    return torch.empty_like(t, dtype=dtype)
+
+
+def _floats(n: int, like, shape):
+    """n float32 outputs of one shape in one allocation, as tensors of their own (.data): as views of one tensor they could not be
+    changed in place where gradients are recorded."""
+    return [t.data for t in _out(like, (n, *shape), torch.float32).unbind(0)]
 
 
 def _workspace(n: int, like):
@@ -141,11 +150,12 @@ def fb_layer_norm(x, weight=None, bias=None, eps: float = 1e-5, want_stats: bool
     wtype = F32 if wt is None else _type(wt, "weight")
     if weight is not None and bias is not None and weight.dtype != bias.dtype:
         raise ValueError("weight and bias must have one type")
-    pw, pb = _vector(weight, "weight", H, (torch.float32, x.dtype), dev), _vector(bias, "bias", H, (torch.float32, x.dtype), dev)
+    types = torch.float32, x.dtype
+    pw, pb = _vector(weight, "weight", H, types, dev), _vector(bias, "bias", H, types, dev)
     y = _out_like(x)
     mean = rstd = pm = pr = None
     if want_stats:
-        mean, rstd = _out(x, (2, *x.shape[:-1]), torch.float32).unbind(0)
+        mean, rstd = _floats(2, x, x.shape[:-1])
         pm, pr = mean.data_ptr(), rstd.data_ptr()
     _check(L.fb_layer_norm(px, ldx, pw, pb, wtype, R, H, code, eps, y.data_ptr(), H, pm, pr, _raw_stream(dev)))
     return (y, mean, rstd) if want_stats else y
@@ -251,8 +261,9 @@ def fb_token_logprobs(logits, tokens, top: int = 0):
     if tokens.shape != lead:
         raise ValueError("tokens must have the leading shape of logits")
     pt = _vector(tokens, "tokens", R, (torch.int32,), dev)
-    lp, ent, z = _out(logits, (3, *lead), torch.float32).unbind(0)
-    ids, best = _out(logits, (*lead, max(top, 0)), torch.int32), _out(logits, (*lead, max(top, 0)), torch.float32)
+    lp, ent, z = _floats(3, logits, lead)
+    best = _out(logits, (*lead, max(top, 0)), torch.float32)
+    ids = _out_like(best, torch.int32)
     need = int(L.fb_token_logprobs_workspace_bytes(R, V, code, top))
     ws, pws = _workspace(need, logits)
     _check(L.fb_token_logprobs(p, ld, pt, R, V, code, top, lp.data_ptr(), ent.data_ptr(), z.data_ptr(), ids.data_ptr(),
