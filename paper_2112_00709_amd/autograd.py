@@ -83,9 +83,13 @@ def _layer_functions():
 
     from . import layers as fl
 
+    # `recording`: whether gradients are recorded where the function is called (inside of forward they never are, and
+    # needs_input_grad does not look at it).  What only a backward pass reads is formed if one can follow.
     class _LayerNorm(torch.autograd.Function):
         @staticmethod
-        def forward(ctx, x, weight, bias, eps):
+        def forward(ctx, x, weight, bias, eps, recording):
+            if not (recording and any(ctx.needs_input_grad[:3])):
+                return fl.fb_layer_norm(x, weight, bias, eps)
             y, mean, rstd = fl.fb_layer_norm(x, weight, bias, eps, want_stats=True)
             ctx.save_for_backward(x, weight, mean, rstd)
             ctx.bias_dtype = None if bias is None else bias.dtype
@@ -97,12 +101,12 @@ def _layer_functions():
             x, weight, mean, rstd = ctx.saved_tensors
             dx, dw, db = fl.fb_layer_norm_grad(dy.contiguous(), x, mean, rstd, weight, ctx.needs_input_grad[0], ctx.needs_input_grad[1],
                                                ctx.needs_input_grad[2])
-            return dx, None if dw is None else dw.to(weight.dtype), None if db is None else db.to(ctx.bias_dtype), None
+            return dx, None if dw is None else dw.to(weight.dtype), None if db is None else db.to(ctx.bias_dtype), None, None
 
     class _Affine(torch.autograd.Function):
         @staticmethod
-        def forward(ctx, x, weight, bias, residual, activation, out_dtype):
-            keep = activation != "none" and any(ctx.needs_input_grad[:3])
+        def forward(ctx, x, weight, bias, residual, activation, out_dtype, recording):
+            keep = recording and activation != "none" and any(ctx.needs_input_grad[:3])
             out = fl.fb_affine(x, weight, bias, activation, residual, out_dtype, want_preact=keep)
             y, preact = out if keep else (out, None)
             ctx.save_for_backward(x, weight, preact)
@@ -117,13 +121,13 @@ def _layer_functions():
             dx = dw = db = None
             if any(ctx.needs_input_grad[:3]):
                 dx, dw, db = fl.fb_affine_grad(dy, x, weight, ctx.activation, preact, *ctx.needs_input_grad[:3])
-            return dx, dw, db, dy if ctx.needs_input_grad[3] else None, None, None
+            return dx, dw, db, dy if ctx.needs_input_grad[3] else None, None, None, None
 
     class _TokenLogprobs(torch.autograd.Function):
         @staticmethod
-        def forward(ctx, logits, tokens, top):
+        def forward(ctx, logits, tokens, top, recording):
             logprobs, entropy, logz, ids, best = fl.fb_token_logprobs(logits, tokens, top)
-            if ctx.needs_input_grad[0]:                    # (copies: the caller may change its results in place)
+            if recording and ctx.needs_input_grad[0]:      # (copies: the caller may change its results in place)
                 ctx.save_for_backward(logits, tokens, logz.clone(), entropy.clone())
             ctx.mark_non_differentiable(logz, ids, best)
             ctx.set_materialize_grads(False)
@@ -133,10 +137,10 @@ def _layer_functions():
         @once_differentiable
         def backward(ctx, g_logprobs, g_entropy, _g_logz, _g_ids, _g_best):
             if g_logprobs is None and g_entropy is None:
-                return None, None, None
+                return None, None, None, None
             logits, tokens, logz, entropy = ctx.saved_tensors
             g = [None if t is None else t.contiguous() for t in (g_logprobs, g_entropy)]
-            return fl.fb_token_logprobs_grad(logits, tokens, logz, entropy, *g), None, None
+            return fl.fb_token_logprobs_grad(logits, tokens, logz, entropy, *g), None, None, None
 
     _layer_fns = _LayerNorm, _Affine, _TokenLogprobs
     return _layer_fns
@@ -144,16 +148,16 @@ def _layer_functions():
 
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5):
     """``layers.fb_layer_norm`` with its gradient with respect to x, weight and bias."""
-    return _layer_functions()[0].apply(x, weight, bias, eps)
+    return _layer_functions()[0].apply(x, weight, bias, eps, _torch().is_grad_enabled())
 
 
 def affine(x, weight, bias=None, activation: str = "none", residual=None, out_dtype=None):
-    """``layers.fb_affine`` with its gradient with respect to x, weight, bias and residual.  With an activation the forward
-    call keeps what it was applied to, rounded to x's type."""
-    return _layer_functions()[1].apply(x, weight, bias, residual, activation, out_dtype)
+    """``layers.fb_affine`` with its gradient with respect to x, weight, bias and residual.  Where a gradient can
+    follow, the forward call of an activation keeps what that was applied to, rounded to x's type."""
+    return _layer_functions()[1].apply(x, weight, bias, residual, activation, out_dtype, _torch().is_grad_enabled())
 
 
 def token_logprobs(logits, tokens, top: int = 0):
     """``layers.fb_token_logprobs`` -> (logprobs, entropy, logz, top_ids, top_logprobs); the first two have gradients with
     respect to the logits, the others do not."""
-    return _layer_functions()[2].apply(logits, tokens, top)
+    return _layer_functions()[2].apply(logits, tokens, top, _torch().is_grad_enabled())
