@@ -347,35 +347,41 @@ __global__ __launch_bounds__(1024) void fb_column_sum_kernel(const float *part, 
 {
     __shared__ float slots[16][64];
     const int col = threadIdx.x & 63, g = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + col;
     const int k = blockIdx.y;
     float *out = k ? out1 : out0;
-    float s0 = 0.0f, s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
-    if (out && c < C) {
-        const float *q = part + (size_t)k * C + c;
-        const int64_t step = (int64_t)gridDim.y * C;
-        int64_t i = g;
-        for (; i + 48 < P; i += 64) {
-            s0 += q[i * step];
-            s1 += q[(i + 16) * step];
-            s2 += q[(i + 32) * step];
-            s3 += q[(i + 48) * step];
+    if (!out) return;
+    for (int64_t c0 = (int64_t)blockIdx.x * 64; c0 < C; c0 += (int64_t)gridDim.x * 64) {
+        const int64_t c = c0 + col;
+        float s0 = 0.0f, s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
+        if (c < C) {
+            const float *q = part + (size_t)k * C + c;
+            const int64_t step = (int64_t)gridDim.y * C;
+            int64_t i = g;
+            for (; i + 48 < P; i += 64) {
+                s0 += q[i * step];
+                s1 += q[(i + 16) * step];
+                s2 += q[(i + 32) * step];
+                s3 += q[(i + 48) * step];
+            }
+            for (; i < P; i += 16) s0 += q[i * step];
         }
-        for (; i < P; i += 16) s0 += q[i * step];
-    }
-    slots[g][col] = (s0 + s1) + (s2 + s3);
-    __syncthreads();
-    if (g == 0 && out && c < C) {
-        float s = 0.0f;
+        slots[g][col] = (s0 + s1) + (s2 + s3);
+        __syncthreads();
+        if (g == 0 && c < C) {
+            float s = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s += slots[i][col];
-        out[c] = s;
+            for (int i = 0; i < 16; ++i) s += slots[i][col];
+            out[c] = s;
+        }
+        __syncthreads();
     }
 }
 
 int launch_column_sum(const float *part, int64_t P, int64_t C, float *out0, float *out1, void *stream)
 {
-    hipLaunchKernelGGL(fb_column_sum_kernel, dim3((unsigned)((C + 63) / 64), 2), dim3(1024), 0, (hipStream_t)stream, part, P, C, out0, out1);
+    // (2^22 workgroups of 1024 threads, those of the widest rows, are more threads than a launch may have)
+    const int64_t groups = std::min<int64_t>((C + 63) / 64, (int64_t)1 << 21);
+    hipLaunchKernelGGL(fb_column_sum_kernel, dim3((unsigned)groups, 2), dim3(1024), 0, (hipStream_t)stream, part, P, C, out0, out1);
     return launched("column sum kernel launch: ");
 }
 
