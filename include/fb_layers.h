@@ -64,7 +64,9 @@ int fb_layer_norm_grad(const void *dy, int64_t lddy, const void *x, int64_t ldx,
                        float *dbias, void *ws, size_t ws_bytes, fb_stream stream);
 
 /* Bytes of workspace fb_affine needs for these arguments (0: none, or bad arguments).  Of x and weight only the address counts:
- * matrices whose rows are not whole 16-byte pieces at multiples of 16 bytes are copied to such rows first (unless M <= 64). */
+ * matrices whose rows are not whole 16-byte pieces at multiples of 16 bytes are copied to such rows first (unless M <= 64).  Where
+ * K is shared between workgroups the sums of each share go there too, 4 M N bytes a share: K above 4096 in FB_TYPE_F32 is always
+ * shared (4096 x 4096 x 4160: 134 MB, 69120 x 3000 x 5120: 1.7 GB), otherwise products of few tiles are. */
 size_t fb_affine_workspace_bytes(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t N, int64_t K, int type);
 
 /*
@@ -82,8 +84,8 @@ int fb_affine(const void *x, int64_t ldx, const void *weight, int64_t ldw, const
               int64_t M, int64_t N, int64_t K, int type, int act, void *y, int64_t ldy, int out_type, void *preact, int64_t ldp,
               void *ws, size_t ws_bytes, fb_stream stream);
 
-/* Bytes of workspace fb_affine_grad needs for these arguments (0: bad arguments); addresses count as in
- * fb_affine_workspace_bytes. */
+/* Bytes of workspace fb_affine_grad needs for these arguments (0: bad arguments); addresses count, and products are shared, as in
+ * fb_affine_workspace_bytes (dx along N, dweight along M). */
 size_t fb_affine_grad_workspace_bytes(const void *dy, int64_t lddy, int dy_type, const void *x, int64_t ldx, const void *weight, int64_t ldw,
                                       int64_t M, int64_t N, int64_t K, int type, int act);
 
@@ -122,7 +124,8 @@ size_t fb_token_logprobs_workspace_bytes(int64_t R, int64_t V, int type, int top
  * and entropy 0.  A row with NaN or +inf has NaN for logz, logprobs and entropy and unspecified alternatives; so has a row
  * whose token is V or more for logprobs alone.
  * FB_EINVAL: logits or tokens NULL, R < 0, V < 1, a row distance below V, top < 0 or above FB_TOP_MAX or V, an unknown type,
- * the workspace missing or too small.
+ * the workspace missing or too small.  FB_EUNSUPPORTED: rows so long and so many that their pieces of up to 16384 elements are 2^24
+ * or more.
  */
 int fb_token_logprobs(const void *logits, int64_t ld, const int32_t *tokens, int64_t R, int64_t V, int type, int top,
                       float *logprobs, float *entropy, float *logz, int32_t *top_ids, float *top_logprobs, void *ws,

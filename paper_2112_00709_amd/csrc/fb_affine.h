@@ -65,8 +65,9 @@ constexpr float kLog2E = 1.44269504088896340736f;
 
 // Phi(-|z|) and e^(-z^2/2).  Phi(-|z|) = e^(-z^2/2) P(t) / 2 with t = 1 / (1 + 0.4375 |z| / sqrt 2): P, of degree 8 and without a
 // constant, is fitted to e^(x^2) erfc(x) over t in [1 / (1 + 0.4375 * 11), 1] by least squares with weights moved towards equal
-// relative errors: 1.6e-7, with the roundings 4.6e-7 (a library erf takes three times the instructions, and its difference
-// from 1 has no digits left in the tail).
+// relative errors: 1.6e-7, with the roundings 5.6e-7 for |z| up to 2.  Further out the exponent's rounding counts, which grows as
+// the exponent does: 1.5e-6 at 5.5, 7.4e-6 at 12.5, of values of 2e-8 and 4e-36.  (A library erf takes three times the
+// instructions, and its difference from 1 has no digits left in the tail.)
 __device__ __forceinline__ float normal_tail(float z, float &e)
 {
     const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.4375f * 0.70710678118654752440f, 1.0f));

@@ -62,7 +62,8 @@ __global__ __launch_bounds__(256) void fb_join_kernel(JoinParams p)
 // that brings the largest |dy| into [2^14, 2^15) (slopes are at most 1.13), and the sums are taken times its inverse when they leave.
 // What the largest exceeds by 2^29 and more loses digits, an error of at most 2^-39 of the largest; infinities and NaN do not
 // count.  One more pass over dy, bound by memory, for half precision alone and only where dz has to be rounded: 36 of 529 us for the
-// gradient of 44160 x 2048 x 1024 behind a gelu (5 TB/s), 65 of 543 with dy in single precision; 2 to 5 us in small ones.
+// gradient of 44160 x 2048 x 1024 behind a gelu, 65 of 543 with dy in single precision (5 TB/s; 48 and 92 us where dy is new each
+// time: with twice or four times the workgroups or the loads asked for ahead 50 and 80 to 92); 2 to 5 us in small ones.
 struct PeakParams {
     const void *dy;
     int64_t ld, M, N;
@@ -268,7 +269,8 @@ size_t aligned(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Tiles and shares of k, by estimated clocks of the busiest compute unit: its tiles' work, for every round of workgroups that
 // it holds at a time (1, 2 or 4) a start, an end and the latency of every step, and, where k is shared, the sums' way through
-// memory and a launch to join them.  In single precision a share is at most 4096 long, so that roundings do not pile up.
+// memory and a launch to join them.  In single precision a share is at most 4096 long, so that roundings do not pile up, as long as
+// 128 shares are enough for that (k up to 524288); with k above 4096 the sums always go through memory then, split M N floats of it.
 void plan(Product &q, int only_tile = 0)
 {
     static constexpr int kSplits[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64, 96, 128};

@@ -3,8 +3,9 @@
 // A workgroup has 16 rows of the weight and all rows of x, up to 64; its waves share k, each taking every WAVES-th step of it, so
 // that together they read runs of 256 bytes and more of a row.  What a lane loads (16 bytes of a row) is what the matrix
 // instruction takes, rows of the weight against rows of x, so nothing passes through LDS but the waves' sums at the end, where
-// they are added in the waves' order.  With 16 rows a workgroup even N of some thousands reaches all compute units.
-// One row by 2048 x 2048 in bfloat16 takes 6 us (8.4 MB: 1.7 at a copy's rate; the rest is a launch and one trip to memory),
+// they are added in the waves' order.  With 16 rows a workgroup all compute units have work from N = 4081 on.
+// One row by 2048 x 2048 in bfloat16 takes 6 us (8.4 MB: 1.7 at a copy's rate; the rest is a launch and one trip to memory, with
+// half of the compute units at work),
 // 16 rows by 4096 x 4096 11 us, 64 rows by 2048 x 2048 12 us; 65 rows take 15 in the tiled kernel.
 #include "fb_affine.h"
 

@@ -161,18 +161,6 @@ typedef u32x2 u32x2_any __attribute__((aligned(2)));
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
 
 template <class T>
-__device__ __forceinline__ f32x4 load_four(const T *p)
-{
-    if constexpr (sizeof(T) == 4) {
-        return *(const f32x4_any *)p;
-    } else {
-        const u32x2 r = *(const u32x2_any *)p;
-        float v[8];
-        unpack<T>(u32x4{r[0], r[1], 0, 0}, v);
-        return f32x4{v[0], v[1], v[2], v[3]};
-    }
-}
-template <class T>
 __device__ __forceinline__ void store_four(T *p, const f32x4 &v, bool past)
 {
     if constexpr (sizeof(T) == 4) {
