@@ -5,6 +5,7 @@
  * on the network's side of it, forward and backward:
  *
  *   fb_layer_norm, fb_layer_norm_grad             normalisation of hidden frames
+ *   fb_residual_norm, fb_residual_norm_grad       from one block into the next: norm, gate, scale, residual, norm
  *   fb_affine, fb_affine_grad                     y = act(x W^T + b) + residual
  *   fb_token_logprobs, fb_token_logprobs_grad     log probabilities of given tokens, entropy, best alternatives
  *
@@ -62,6 +63,48 @@ size_t fb_layer_norm_grad_workspace_bytes(int64_t R, int64_t H);
 int fb_layer_norm_grad(const void *dy, int64_t lddy, const void *x, int64_t ldx, const float *mean, const float *rstd,
                        const void *weight, int wtype, int64_t R, int64_t H, int type, void *dx, int64_t lddx, float *dweight,
                        float *dbias, void *ws, size_t ws_bytes, fb_stream stream);
+
+enum { FB_NORM_NONE = 0, FB_NORM_LAYER = 1, FB_NORM_RMS = 2 };
+
+/*
+ * From one block into the next, R rows of H elements, H at most 8192:
+ *   u = norm_inner(h),  s = residual + scale gate u,  y = norm_outer(s)
+ * where a norm is (FB_NORM_LAYER)  (x - mean) rstd weight + bias,  mean = sum x / H,  rstd = 1 / sqrt(sum (x - mean)^2 / H + eps),
+ * (FB_NORM_RMS) the same with mean = 0, or (FB_NORM_NONE) x itself.
+ *   h, residual, s, y   [R][H] of `type`; residual nullable (0), y needed unless outer is FB_NORM_NONE
+ *   gate                [R][H] of `type`, or with ldg = 0 [H] of `wtype` for all rows; nullable (1)
+ *   inner_weight, inner_bias, weight, bias   [H] of `wtype` (FB_TYPE_F32 or `type`), nullable (1 and 0), only with their norm
+ *   stats               out, float [4][R]: inner mean and rstd, outer mean and rstd (0 and 1 where there is no norm, mean 0 of
+ *                       FB_NORM_RMS), nullable (what fb_residual_norm_grad takes)
+ * y and the outer statistics are of s before its rounding.  s and y may each be h, residual or gate of rows, at the same distances.
+ * FB_EINVAL: h, s or a needed y NULL, R < 0, H < 1, a row distance below H, an unknown type or norm, a weight or bias without its
+ * norm, eps negative or not finite, scale not finite.  FB_EUNSUPPORTED: H above 8192.
+ */
+int fb_residual_norm(const void *h, int64_t ldh, const void *residual, int64_t ldr, const void *gate, int64_t ldg, float scale, int inner,
+                     const void *inner_weight, const void *inner_bias, int outer, const void *weight, const void *bias, int wtype, int64_t R,
+                     int64_t H, int type, float eps, void *s, int64_t lds, void *y, int64_t ldy, float *stats, fb_stream stream);
+
+/* Bytes of workspace fb_residual_norm_grad needs (0 on bad arguments). */
+size_t fb_residual_norm_grad_workspace_bytes(int64_t R, int64_t H);
+
+/*
+ * Its gradient, from those of s and y:
+ *   dresidual = ds + (dy through the outer norm at s),  du = scale gate dresidual,  dh = du through the inner norm at h,
+ *   dgate = scale dresidual u,  and for each norm dweight = sum over rows of dy xh,  dbias = sum over rows of dy
+ *   ds           [R][H] of `type`, nullable (0) if there is an outer norm;  dy, s  [R][H] of `type`, needed if there is one
+ *   h            [R][H], needed if there is an inner norm or dgate is wanted;  stats, if there is any norm, as the forward call left them
+ *   dh, dresidual  out, [R][H] of `type`, nullable
+ *   dgate        out, like gate: [R][H] of `type`, or with ldg = 0 float [H], the sum over rows; nullable
+ *   dinner_weight, dinner_bias, dweight, dbias   out, float [H], nullable, only with their norm
+ *   ws           fb_residual_norm_grad_workspace_bytes(), needed if a sum over rows is wanted
+ * Outputs of rows may each be one of the inputs of rows, at the same distances.  Errors as fb_residual_norm; what is needed must not be NULL, the
+ * workspace not too small.
+ */
+int fb_residual_norm_grad(const void *ds, int64_t ldds, const void *dy, int64_t lddy, const void *h, int64_t ldh, const void *s, int64_t lds,
+                          const float *stats, const void *gate, int64_t ldg, float scale, int inner, const void *inner_weight, const void *inner_bias,
+                          int outer, const void *weight, int wtype, int64_t R, int64_t H, int type, void *dh, int64_t lddh, void *dresidual,
+                          int64_t lddr, void *dgate, int64_t lddg, float *dinner_weight, float *dinner_bias, float *dweight, float *dbias, void *ws,
+                          size_t ws_bytes, fb_stream stream);
 
 /* Bytes of workspace fb_affine needs for these arguments (0: none, or bad arguments).  Of x and weight only the address counts:
  * matrices whose rows are not whole 16-byte pieces at multiples of 16 bytes are copied to such rows first (unless M <= 64).  Where

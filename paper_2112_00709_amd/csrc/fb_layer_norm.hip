@@ -18,48 +18,6 @@ struct NormParams {
     bool past;                     // y goes past the caches
 };
 
-// EPL elements of a vector of [H] as floats, at the places a lane has of a row; `none` where there is no vector.
-template <class W, int EPL, int VE>
-__device__ __forceinline__ void load_vector(const void *w, int H, int step, int lane, float none, float *v)
-{
-    constexpr int kN = Vec<W>::kN;
-#pragma unroll
-    for (int i = 0; i < EPL / VE; ++i) {
-        const int at = (i * step + lane) * VE;
-#pragma unroll
-        for (int j = 0; j < VE; j += kN) {
-            float u[kN];
-            unpack<W>(w ? load_piece((const W *)w + at + j, H - at - j) : u32x4{}, u);
-#pragma unroll
-            for (int e = 0; e < kN; ++e) v[i * VE + j + e] = w ? u[e] : none;
-        }
-    }
-}
-
-// Sums of N numbers a thread over the WAVES waves of a workgroup that share a row.  `slot` alternates, so that one barrier
-// a call is enough: a wave writes a slot again only behind the next barrier, which every wave reaches when it has read it.
-template <int WAVES, int N>
-__device__ __forceinline__ void sum_row(float (&v)[N], float (*slots)[WAVES][N], int slot)
-{
-#pragma unroll
-    for (int n = 0; n < N; ++n) v[n] = sum_wave(v[n]);
-    if constexpr (WAVES > 1) {
-        const int wave = threadIdx.x >> 6;
-        if ((threadIdx.x & 63) == 0) {
-#pragma unroll
-            for (int n = 0; n < N; ++n) slots[slot][wave][n] = v[n];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            float s = 0.0f;
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) s += slots[slot][w][n];
-            v[n] = s;
-        }
-    }
-}
-
 // y = (x - mean) rstd weight + bias.  WAVES waves of 64 lanes hold a row, EPL elements a lane; with one wave a row a
 // workgroup has four rows at a time.  The next row is asked for before this one is worked on.  The variance is the mean of
 // the squared distances from the mean, of the values in registers: no difference of large sums.

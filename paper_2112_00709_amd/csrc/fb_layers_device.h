@@ -189,6 +189,48 @@ __device__ __forceinline__ uint32_t max_wave_u(uint32_t v)
     return over_wave(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
 }
 
+// EPL elements of a vector of [H] as floats, at the places a lane has of a row; `none` where there is no vector.
+template <class W, int EPL, int VE>
+__device__ __forceinline__ void load_vector(const void *w, int H, int step, int lane, float none, float *v)
+{
+    constexpr int kN = Vec<W>::kN;
+#pragma unroll
+    for (int i = 0; i < EPL / VE; ++i) {
+        const int at = (i * step + lane) * VE;
+#pragma unroll
+        for (int j = 0; j < VE; j += kN) {
+            float u[kN];
+            unpack<W>(w ? load_piece((const W *)w + at + j, H - at - j) : u32x4{}, u);
+#pragma unroll
+            for (int e = 0; e < kN; ++e) v[i * VE + j + e] = w ? u[e] : none;
+        }
+    }
+}
+
+// Sums of N numbers a thread over the WAVES neighbouring waves of a workgroup that share a row.  `slot` alternates, so that one barrier
+// a call is enough: a wave writes a slot again only behind the next barrier, which every wave reaches when it has read it.
+template <int WAVES, int N>
+__device__ __forceinline__ void sum_row(float (&v)[N], float (*slots)[WAVES][N], int slot)
+{
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] = sum_wave(v[n]);
+    if constexpr (WAVES > 1) {
+        const int wave = (threadIdx.x >> 6) % WAVES;
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) slots[slot][wave][n] = v[n];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            float s = 0.0f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) s += slots[slot][w][n];
+            v[n] = s;
+        }
+    }
+}
+
 }  // namespace
 
 // Host side: argument checks that the calls share.

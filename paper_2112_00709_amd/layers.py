@@ -19,10 +19,12 @@ from . import FBError, _check  # noqa: F401  (FBError: what a failing call raise
 
 F32, BF16, F16 = 0, 1, 2
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+NORMS = {"none": 0, "layer": 1, "rms": 2}
 TOP_MAX = 64
 
 # every symbol include/fb_layers.h declares
-SYMBOLS = ["fb_layer_norm", "fb_layer_norm_grad_workspace_bytes", "fb_layer_norm_grad", "fb_affine_workspace_bytes", "fb_affine",
+SYMBOLS = ["fb_layer_norm", "fb_layer_norm_grad_workspace_bytes", "fb_layer_norm_grad", "fb_residual_norm",
+           "fb_residual_norm_grad_workspace_bytes", "fb_residual_norm_grad", "fb_affine_workspace_bytes", "fb_affine",
            "fb_affine_grad_workspace_bytes", "fb_affine_grad", "fb_token_logprobs_workspace_bytes", "fb_token_logprobs",
            "fb_token_logprobs_grad"]
 
@@ -42,6 +44,10 @@ def lib() -> ctypes.CDLL:
         L.fb_layer_norm.argtypes = [vp, i64, vp, vp, i32, i64, i64, i32, f32, vp, i64, vp, vp, vp]
         L.fb_layer_norm_grad_workspace_bytes.argtypes = [i64, i64]
         L.fb_layer_norm_grad.argtypes = [vp, i64, vp, i64, vp, vp, vp, i32, i64, i64, i32, vp, i64, vp, vp, vp, sz, vp]
+        L.fb_residual_norm.argtypes = [vp, i64, vp, i64, vp, i64, f32, i32, vp, vp, i32, vp, vp, i32, i64, i64, i32, f32, vp, i64, vp, i64, vp, vp]
+        L.fb_residual_norm_grad_workspace_bytes.argtypes = [i64, i64]
+        L.fb_residual_norm_grad.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i64, f32, i32, vp, vp, i32, vp, i32, i64, i64, i32,
+                                            vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, sz, vp]
         L.fb_affine_workspace_bytes.argtypes = [vp, i64, vp, i64, i64, i64, i64, i32]
         L.fb_affine.argtypes = [vp, i64, vp, i64, vp, vp, i64, i64, i64, i64, i32, i32, vp, i64, i32, vp, i64, vp, sz, vp]
         L.fb_affine_grad_workspace_bytes.argtypes = [vp, i64, i32, vp, i64, vp, i64, i64, i64, i64, i32, i32]
@@ -180,6 +186,103 @@ def fb_layer_norm_grad(dy, x, mean, rstd, weight=None, want_dx: bool = True, wan
     _check(L.fb_layer_norm_grad(pdy, lddy, px, ldx, pm, pr, pw, wtype, R, H, code, dx.data_ptr() if want_dx else None, H,
                                 dw.data_ptr() if want_dweight else None, db.data_ptr() if want_dbias else None, pws, need, _raw_stream(dev)))
     return dx, dw, db
+
+
+def _norm_kind(kind: str, what: str, weight, bias=None) -> int:
+    if kind not in NORMS:
+        raise ValueError(f"{what} must be one of {', '.join(NORMS)}")
+    if kind == "none" and (weight is not None or bias is not None):
+        raise ValueError(f"weight or bias without {what} norm")
+    return NORMS[kind]
+
+
+def _one_type(x, vectors) -> int:
+    """The type of vectors of [H], float32 or x's, one of all of them."""
+    seen = {v.dtype for v in vectors if v is not None}
+    if len(seen) > 1:
+        raise ValueError("weights, biases and a gate of one row must have one type")
+    for dtype in seen:
+        if dtype not in (torch.float32, x.dtype):
+            raise ValueError(f"weights, biases and a gate of one row must be float32 or {x.dtype}")
+        return _types[dtype]
+    return F32
+
+
+def _gate(gate, H: int, lead, x, dev: int):
+    """-> (address, row distance: 0 for one row, whether it is one row)."""
+    if gate is None:
+        return None, 0, False
+    if gate.dim() == 1:
+        return _vector(gate, "gate", H, (torch.float32, x.dtype), dev), 0, True
+    p, ld, _, _, _ = _rows(gate, "gate", H, x.dtype, lead, dev)
+    return p, ld, False
+
+
+def fb_residual_norm(h, residual=None, gate=None, scale: float = 1.0, inner: str = "none", inner_weight=None, inner_bias=None,
+                     outer: str = "layer", weight=None, bias=None, eps: float = 1e-5, want_stats: bool = False):
+    """From one block into the next: s = residual + scale gate norm_inner(h), y = norm_outer(s).
+    -> (s, y) like h, y None with outer "none"; with want_stats (s, y, stats), stats float32 [4, ...] of h's leading shape: inner
+    mean and rstd, outer mean and rstd.
+
+    ``inner``, ``outer``: "none", "layer" or "rms" (no mean); ``h``, ``residual`` [..., H], H up to 8192; ``gate`` like h, or [H] for all
+    rows; weights, biases and a gate of [H] float32 or of h's type (all of one)."""
+    L = lib()
+    code = _type(h, "h")
+    ph, ldh, R, H, dev = _rows(h, "h")
+    lead = h.shape[:-1]
+    pr, ldr = None, H
+    if residual is not None:
+        pr, ldr, _, _, _ = _rows(residual, "residual", H, h.dtype, lead, dev)
+    kin, kout = _norm_kind(inner, "inner", inner_weight, inner_bias), _norm_kind(outer, "outer", weight, bias)
+    pg, ldg, one = _gate(gate, H, lead, h, dev)
+    wtype = _one_type(h, (inner_weight, inner_bias, weight, bias, gate if one else None))
+    f = torch.float32, h.dtype
+    vectors = [_vector(v, what, H, f, dev) for v, what in ((inner_weight, "inner_weight"), (inner_bias, "inner_bias"), (weight, "weight"), (bias, "bias"))]
+    s = _out_like(h)
+    y = _out_like(h) if kout else None
+    stats = _out(h, (4, *lead), torch.float32) if want_stats else None
+    _check(L.fb_residual_norm(ph, ldh, pr, ldr, pg, ldg, scale, kin, vectors[0], vectors[1], kout, vectors[2], vectors[3], wtype, R, H, code, eps,
+                              s.data_ptr(), H, y.data_ptr() if kout else None, H, stats.data_ptr() if want_stats else None, _raw_stream(dev)))
+    return (s, y, stats) if want_stats else (s, y)
+
+
+def fb_residual_norm_grad(ds, dy, h, s, stats, gate=None, scale: float = 1.0, inner: str = "none", inner_weight=None, inner_bias=None,
+                          outer: str = "layer", weight=None, want_dh: bool = True, want_dresidual: bool = True, want_dgate: bool = True,
+                          want_dinner: bool = True, want_douter: bool = True):
+    """-> (dh, dresidual like h, dgate like gate (float32 for a gate of [H]), dinner_weight, dinner_bias, dweight, dbias [H] float32), None
+    in the place of one that is not wanted or has nothing to be the gradient of.
+
+    ``ds`` (None: 0), ``dy`` (None with outer "none") like h; ``s``, ``stats``: as fb_residual_norm returned them; want_dinner and
+    want_douter: both gradients of a norm's weight and bias."""
+    L = lib()
+    code = _type(h, "h")
+    ph, ldh, R, H, dev = _rows(h, "h")
+    lead = h.shape[:-1]
+    kin, kout = _norm_kind(inner, "inner", inner_weight, inner_bias), _norm_kind(outer, "outer", weight)
+    if dy is None and kout:
+        raise ValueError("dy is needed with an outer norm")
+    if ds is None and not kout:
+        raise ValueError("ds is needed without an outer norm")
+    (pds, ldds), (pdy, lddy), (ps, lds) = [(None, H) if t is None else _rows(t, what, H, h.dtype, lead, dev)[:2]
+                                           for t, what in ((ds, "ds"), (dy if kout else None, "dy"), (s if kout else None, "s"))]
+    pstats = _vector(stats, "stats", 4 * R, (torch.float32,), dev)
+    pg, ldg, one = _gate(gate, H, lead, h, dev)
+    wtype = _one_type(h, (inner_weight, inner_bias, weight, gate if one else None))
+    f = torch.float32, h.dtype
+    vectors = [_vector(v, what, H, f, dev) for v, what in ((inner_weight, "inner_weight"), (inner_bias, "inner_bias"), (weight, "weight"))]
+    dh = _out_like(h) if want_dh else None
+    dr = _out_like(h) if want_dresidual else None
+    dg = None
+    if want_dgate and gate is not None:
+        dg = _out(h, (H,), torch.float32) if one else _out_like(h)
+    sums = [_out(h, (H,), torch.float32) if kind and want else None
+            for kind, want in ((kin, want_dinner), (kin, want_dinner), (kout, want_douter), (kout, want_douter))]
+    need = int(L.fb_residual_norm_grad_workspace_bytes(R, H)) if (one and dg is not None) or any(t is not None for t in sums) else 0
+    ws, pws = _workspace(need, h)
+    address = [None if t is None else t.data_ptr() for t in (dh, dr, dg, *sums)]
+    _check(L.fb_residual_norm_grad(pds, ldds, pdy, lddy, ph, ldh, ps, lds, pstats, pg, ldg, scale, kin, vectors[0], vectors[1], kout, vectors[2], wtype,
+                                   R, H, code, address[0], H, address[1], H, address[2], H, *address[3:], pws, need, _raw_stream(dev)))
+    return (dh, dr, dg, *sums)
 
 
 def _activation(name: str) -> int:
