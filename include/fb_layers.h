@@ -7,6 +7,7 @@
  *   fb_layer_norm, fb_layer_norm_grad             normalisation of hidden frames
  *   fb_residual_norm, fb_residual_norm_grad       from one block into the next: norm, gate, scale, residual, norm
  *   fb_affine, fb_affine_grad                     y = act(x W^T + b) + residual
+ *   fb_gated_affine, fb_gated_affine_grad         y = act(x G^T + a) (x U^T + b), elementwise
  *   fb_token_logprobs, fb_token_logprobs_grad     log probabilities of given tokens, entropy, best alternatives
  *
  * Conventions are those of fb.h: device pointers owned by the caller, kernels enqueued on `stream`, nothing allocated, freed
@@ -35,7 +36,8 @@ enum {
     FB_ACT_NONE = 0,
     FB_ACT_RELU = 1,  /* max(z, 0), slope 0 at 0              */
     FB_ACT_GELU = 2,  /* z Phi(z), Phi the normal distribution */
-    FB_ACT_SILU = 3   /* z / (1 + e^-z)                        */
+    FB_ACT_SILU = 3,  /* z / (1 + e^-z)                        */
+    FB_ACT_SIGMOID = 4 /* 1 / (1 + e^-z), of gated layers alone */
 };
 
 /*
@@ -146,6 +148,35 @@ size_t fb_affine_grad_workspace_bytes(const void *dy, int64_t lddy, int dy_type,
 int fb_affine_grad(const void *dy, int64_t lddy, int dy_type, const void *x, int64_t ldx, const void *weight, int64_t ldw,
                    const void *preact, int64_t ldp, int64_t M, int64_t N, int64_t K, int type, int act, void *dx, int64_t lddx,
                    void *dweight, float *dbias, void *ws, size_t ws_bytes, fb_stream stream);
+
+/* Bytes of workspace fb_gated_affine needs for these arguments (0: none, or bad arguments); as fb_affine_workspace_bytes, the weight
+ * having 2 N rows. */
+size_t fb_gated_affine_workspace_bytes(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t N, int64_t K, int type);
+
+/*
+ * Gated layer:  g = x G^T + bias[0 .. N),  u = x U^T + bias[N .. 2N),  y = act(g) u, element by element
+ *   x        [M][K] of `type`;  weight [2 N][K] of `type`: G's rows, then U's;  bias float [2 N], nullable
+ *   act      any activation, FB_ACT_SIGMOID among them
+ *   y        out, [M][N] of `type`;  preact  out, [M][2 N] of `type`, nullable: g, then u, rounded (what fb_gated_affine_grad takes)
+ * y is of g and u before their rounding.  N is below 2^27.  Errors as fb_affine (FB_EUNSUPPORTED for M <= 64: N of 2^25 and more).
+ */
+int fb_gated_affine(const void *x, int64_t ldx, const void *weight, int64_t ldw, const float *bias, int64_t M, int64_t N, int64_t K, int type, int act,
+                    void *y, int64_t ldy, void *preact, int64_t ldp, void *ws, size_t ws_bytes, fb_stream stream);
+
+/* Bytes of workspace fb_gated_affine_grad needs for these arguments (0: bad arguments). */
+size_t fb_gated_affine_grad_workspace_bytes(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t N, int64_t K, int type);
+
+/*
+ * Its gradient:  dz = [dy u act'(g), dy act(g)],  dx = dz W,  dweight = dz^T x,  dbias = sum over rows of dz
+ *   dy      [M][N] of `type`;  preact [M][2 N] of `type`
+ *   dx      out, [M][K] of `type`, nullable;  dweight out, [2 N][K] of `type`, contiguous, nullable;  dbias out, float [2 N], nullable
+ * Where `type` has 16 bits dz is rounded to it before the two products, to FB_TYPE_F16 times a power of two that brings the largest
+ * finite |dz| into [2^14, 2^15) (as in fb_affine_grad); dbias is summed before that.
+ * Errors as fb_affine_grad; dy, x, weight and preact must not be NULL.
+ */
+int fb_gated_affine_grad(const void *dy, int64_t lddy, const void *x, int64_t ldx, const void *weight, int64_t ldw, const void *preact, int64_t ldp,
+                         int64_t M, int64_t N, int64_t K, int type, int act, void *dx, int64_t lddx, void *dweight, float *dbias, void *ws,
+                         size_t ws_bytes, fb_stream stream);
 
 /* The most alternatives fb_token_logprobs returns a row. */
 enum { FB_TOP_MAX = 64 };

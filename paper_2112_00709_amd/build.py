@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfb_amd.so")
 SOURCES = ["fb_kernels.hip", "fb_graph.cpp", "fb_sell.cpp", "fb_stream.cpp", "fb_pstream.cpp", "fb_small.cpp", "fb_api.cpp", "fb_leaky.hip",
            "fb_small.hip", "fb_small_linear.hip", "fb_post_small.hip", "fb_layer_norm.hip", "fb_residual_norm.hip", "fb_logprobs.hip",
-           "fb_affine.hip", "fb_affine_mfma.hip", "fb_affine_few.hip"]
+           "fb_affine.hip", "fb_affine_mfma.hip", "fb_affine_few.hip", "fb_gated.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",
@@ -27,7 +27,7 @@ def is_stale() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    deps = sources() + [os.path.join(CSRC, h) for h in ("fb_internal.h", "fb_device.h", "fb_small_run.h", "fb_layers_device.h", "fb_affine.h")] + [
+    deps = sources() + [os.path.join(CSRC, h) for h in ("fb_internal.h", "fb_device.h", "fb_small_run.h", "fb_layers_device.h", "fb_affine.h", "fb_mfma.h")] + [
         os.path.join(HERE, "..", "include", h) for h in ("fb.h", "fb_layers.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 

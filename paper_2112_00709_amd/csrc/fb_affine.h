@@ -51,6 +51,9 @@ int launch_mfma_pair(const Product &dx, const Product &dw, hipStream_t stream);
 constexpr int64_t kFewRows = 64;
 int launch_few_rows(const Product &q, hipStream_t stream);
 
+// Gated layers: B is the gate's N rows and the other factor's N behind them, N the outputs' width.
+int launch_few_pairs(const Product &q, hipStream_t stream);
+
 // Whether the matrix units' kernel can take a factor as it is: whole 16-byte pieces, at addresses and distances that are
 // multiples of 16 bytes, and a tile's rows within the 2^31 bytes of a buffer.  `width`: the length of its rows in memory.
 inline bool ready(const void *p, int64_t ld, int64_t width, int type)
@@ -58,6 +61,103 @@ inline bool ready(const void *p, int64_t ld, int64_t width, int type)
     const int64_t piece = 16 / (int64_t)type_bytes(type);
     return ((uintptr_t)p & 15) == 0 && ld % piece == 0 && width % piece == 0 && ld * (int64_t)type_bytes(type) < (int64_t)1 << 22;
 }
+
+// Rows made before the products: dz = dy act'(z), or a copy in rows of whole pieces, and shares of the sums of their columns.
+struct SlopeParams {
+    const void *dy, *z;
+    int64_t lddy, ldz, M, N, ldo;
+    int act;
+    void *out;           // dz as the products take it, nullable
+    float *part;         // [down][N]: shares of the sums over rows, nullable
+    int lanes;           // a row: a power of two, 64 where the rows are wider than that many pieces
+    int wide, down;      // workgroups along the width and along the rows
+    const uint32_t *peaks;   // half precision: shares of the largest |dy| that sets the power of two out is taken times, nullable
+    int n_peaks;
+    float *undo;         // its inverse, out
+    const int32_t *counts;   // rows of out whose number here is negative are zeros, nullable
+};
+
+void lay_out(SlopeParams &p, int type);
+int64_t sum_rows(int64_t M, int64_t N, int type);   // the shares of sums over M rows of N elements
+
+// Up to three jobs that make rows, the first from rows of another type.
+struct PrepareParams {
+    SlopeParams job[3];
+    int last[3];             // workgroups [last[i - 1], last[i]) have job i
+};
+
+// Jobs that make rows, in one launch; the first has rows of dy_type.
+struct Prepare {
+    PrepareParams p{};
+    int n = 0, blocks = 0;
+    void add(SlopeParams s, int type)
+    {
+        lay_out(s, type);
+        p.job[n] = s;
+        blocks += s.wide * s.down;
+        p.last[n++] = blocks;
+    }
+};
+
+int launch_prepare(Prepare &j, int type, int dy_type, hipStream_t stream);
+
+inline size_t aligned(size_t n) { return (n + 255) & ~(size_t)255; }
+
+void plan(Product &q, int only_tile = 0);           // tiles and shares of k
+inline size_t product_bytes(const Product &q) { return q.parts ? aligned((size_t)q.split * (size_t)q.M * (size_t)q.N * sizeof(float)) : 0; }
+int launch_join(const Product *a, const Product *b, int type, const float *sums, int64_t rows, int64_t N, float *out, hipStream_t stream);
+
+inline int64_t whole_pieces(int64_t width, int type)
+{
+    const int64_t piece = 16 / (int64_t)type_bytes(type);
+    return (width + piece - 1) / piece * piece;
+}
+
+// A matrix that the matrix units' kernel cannot take as it is, copied to rows of whole pieces (padded with zeros).
+struct Packed {
+    bool copy;
+    int64_t ld;
+    size_t bytes;
+};
+
+inline Packed packed(const void *p, int64_t ld, int64_t rows, int64_t width, int type)
+{
+    Packed k{};
+    k.copy = !ready(p, ld, width, type);
+    k.ld = k.copy ? whole_pieces(width, type) : ld;
+    k.bytes = k.copy ? aligned((size_t)rows * (size_t)k.ld * type_bytes(type)) : 0;
+    return k;
+}
+
+// The job that makes the copy (nothing if none is needed).
+inline SlopeParams pack_job(const Packed &k, const void *p, int64_t ld, int64_t rows, int64_t width, void *to)
+{
+    return SlopeParams{p, nullptr, ld, 0, rows, width, k.ld, FB_ACT_NONE, to, nullptr, 0, 0, 0, nullptr, 0, nullptr, nullptr};
+}
+
+// What the matrix units' kernel addresses in 32 bits: 64 or 128 rows of a factor, 16 rows of what it stores or adds.
+inline bool too_long(int64_t width, int type) { return width * (int64_t)type_bytes(type) > (int64_t)1 << 22; }
+inline bool too_far(int64_t ld) { return ld >= (int64_t)1 << 27; }
+
+inline bool bad_sizes(int64_t M, int64_t N, int64_t K) { return bad_rows(M) || bad_width(N) || bad_width(K); }
+
+// The two products of the gradient.
+struct GradPlan {
+    Product dx, dw;
+    bool pair;            // in one launch
+    bool slope;           // dz has to be made, or dy laid out anew
+    bool scale;           // and is rounded to half precision: times a power of two
+    int64_t ldz;
+    Packed x, w;
+    size_t dz, sums, range, part, bytes;
+};
+
+GradPlan grad_plan(const void *dy, int64_t lddy, int dy_type, const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t N, int64_t K, int type,
+                   int act);
+int launch_grad(GradPlan &g, const Factor &d, const float *undo, void *dx, int64_t lddx, void *dweight, float *part, const float *sums, int64_t rows, float *dbias,
+                hipStream_t stream);
+
+constexpr int kPeakGroups = kCUs;    // four peaks a lane for those who need the largest
 
 namespace {
 
@@ -92,6 +192,7 @@ __device__ __forceinline__ float act_of(float z, int act)
         return z * (z > 0.0f ? 1.0f - h : h);
     }
     if (act == FB_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -kLog2E));
+    if (act == FB_ACT_SIGMOID) return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -kLog2E));
     return z;
 }
 
@@ -107,7 +208,27 @@ __device__ __forceinline__ float act_slope(float z, int act)
         const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -kLog2E));
         return s * fmaf(z, 1.0f - s, 1.0f);
     }
+    if (act == FB_ACT_SIGMOID) {                                 // s(z) s(-z), in which no digits cancel
+        const float e = __builtin_amdgcn_exp2f(-fabsf(z) * kLog2E), s = __builtin_amdgcn_rcpf(1.0f + e);
+        return e * s * s;
+    }
     return 1.0f;
+}
+
+// The power of two for a largest |dy|, and its inverse; both are normal numbers whatever the largest is.
+__device__ __forceinline__ void range_of(const uint32_t *peaks, int n, float &scale, float &undo)
+{
+    const int lane = threadIdx.x & 63;
+    uint32_t peak = 0;
+#pragma unroll
+    for (int i = 0; i < kPeakGroups; i += 64) {
+        const uint32_t one = i + lane < n ? peaks[i + lane] : 0;
+        peak = one > peak ? one : peak;
+    }
+    peak = max_wave_u(peak);
+    const uint32_t e = peak >> 23, up = peak == 0 ? 127 : e < 15 ? 253 : 268 - e;      // 2^(14 - (e - 127))
+    scale = __uint_as_float(up << 23);
+    undo = __uint_as_float((254 - up) << 23);
 }
 
 // One sum finished and stored.  T: the factors' type.
@@ -124,6 +245,22 @@ __device__ __forceinline__ void finish_one(const Finish &f, int64_t i, int64_t j
         if (f.residual) s += (float)((const T *)f.residual)[i * f.ldr + j];
         ((T *)f.y)[i * f.ldy + j] = (T)s;
     }
+}
+
+// A pair of sums of a gated layer finished and stored: y = act(g + bias[j]) (u + bias[N + j]), preact both before that.
+template <class T>
+__device__ __forceinline__ void finish_pair(const Finish &f, int64_t N, int64_t i, int64_t j, float g, float u)
+{
+    if (f.bias) {
+        g += f.bias[j];
+        u += f.bias[N + j];
+    }
+    if (f.preact) {
+        T *z = (T *)f.preact + i * f.ldp + j;
+        z[0] = (T)g;
+        z[N] = (T)u;
+    }
+    ((T *)f.y)[i * f.ldy + j] = (T)(act_of(g, f.act) * u);
 }
 
 }  // namespace

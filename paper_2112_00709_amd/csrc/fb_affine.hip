@@ -70,8 +70,6 @@ struct PeakParams {
     uint32_t *peaks;
 };
 
-constexpr int kPeakGroups = kCUs;    // four peaks a lane for those who need the largest
-
 template <class D>
 __global__ __launch_bounds__(1024) void fb_peak_kernel(PeakParams p)
 {
@@ -129,35 +127,6 @@ int launch_peak(const PeakParams &p, int dy_type, hipStream_t stream)
     return launched("peak kernel launch: ");
 }
 
-// The power of two for a largest |dy|, and its inverse; both are normal numbers whatever the largest is.
-__device__ __forceinline__ void range_of(const uint32_t *peaks, int n, float &scale, float &undo)
-{
-    const int lane = threadIdx.x & 63;
-    uint32_t peak = 0;
-#pragma unroll
-    for (int i = 0; i < kPeakGroups; i += 64) {
-        const uint32_t one = i + lane < n ? peaks[i + lane] : 0;
-        peak = one > peak ? one : peak;
-    }
-    peak = max_wave_u(peak);
-    const uint32_t e = peak >> 23, up = peak == 0 ? 127 : e < 15 ? 253 : 268 - e;      // 2^(14 - (e - 127))
-    scale = __uint_as_float(up << 23);
-    undo = __uint_as_float((254 - up) << 23);
-}
-
-struct SlopeParams {
-    const void *dy, *z;
-    int64_t lddy, ldz, M, N, ldo;
-    int act;
-    void *out;           // dz as the products take it, nullable
-    float *part;         // [down][N]: shares of the sums over rows, nullable
-    int lanes;           // a row: a power of two, 64 where the rows are wider than that many pieces
-    int wide, down;      // workgroups along the width and along the rows
-    const uint32_t *peaks;   // half precision: shares of the largest |dy| that sets the power of two out is taken times, nullable
-    int n_peaks;
-    float *undo;         // its inverse, out
-};
-
 // dz = dy act'(z) (or a copy of dy in rows of whole pieces), rounded to the factors' type, and the sums of its columns before
 // the rounding.  Bound by memory: 44160 x 2048 in bfloat16 with max(z, 0) take 100 us, 5.4 TB/s.  A thread has one piece of the
 // width; `lanes` threads have a row side by side, so narrow rows fill the waves too, and kRowsAhead rows are asked for before the
@@ -210,6 +179,10 @@ __device__ __forceinline__ void make_rows(const SlopeParams &p, int block, float
 #pragma unroll
                     for (int e = 0; e < VE; ++e) g[e] *= scale;
                 }
+                if (p.out && p.counts && r < p.M && p.counts[r] < 0) {
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) g[e] = 0.0f;
+                }
                 if (p.out && r < p.M) store_piece((T *)p.out + r * p.ldo + at, VE, pack<T>(g));   // (rows of whole pieces)
             }
         }
@@ -227,12 +200,6 @@ __device__ __forceinline__ void make_rows(const SlopeParams &p, int block, float
     }
 }
 
-// Up to three such jobs, the first with rows of type D.
-struct PrepareParams {
-    SlopeParams job[3];
-    int last[3];             // workgroups [last[i - 1], last[i]) have job i
-};
-
 template <class T, class D>
 __global__ __launch_bounds__(256) void fb_prepare_kernel(PrepareParams p)
 {
@@ -245,6 +212,8 @@ __global__ __launch_bounds__(256) void fb_prepare_kernel(PrepareParams p)
     else
         make_rows<T, T>(p.job[2], block - p.last[1], slots);
 }
+
+}  // namespace
 
 void lay_out(SlopeParams &p, int type)
 {
@@ -265,13 +234,11 @@ int64_t sum_rows(int64_t M, int64_t N, int type)
     return p.down;
 }
 
-size_t aligned(size_t n) { return (n + 255) & ~(size_t)255; }
-
 // Tiles and shares of k, by estimated clocks of the busiest compute unit: its tiles' work, for every round of workgroups that
 // it holds at a time (1, 2 or 4) a start, an end and the latency of every step, and, where k is shared, the sums' way through
 // memory and a launch to join them.  In single precision a share is at most 4096 long, so that roundings do not pile up, as long as
 // 128 shares are enough for that (k up to 524288); with k above 4096 the sums always go through memory then, split M N floats of it.
-void plan(Product &q, int only_tile = 0)
+void plan(Product &q, int only_tile)
 {
     static constexpr int kSplits[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64, 96, 128};
     struct Shape {                          // (see fb_affine_mfma.hip)
@@ -305,8 +272,6 @@ void plan(Product &q, int only_tile = 0)
     q.parts = q.split > 1 || q.N < 4;       // (the kernel takes a residual by fours)
 }
 
-size_t product_bytes(const Product &q) { return q.parts ? aligned((size_t)q.split * (size_t)q.M * (size_t)q.N * sizeof(float)) : 0; }
-
 // Products whose shares are to be joined (at most two) and columns to be added up (out), in one launch.
 int launch_join(const Product *a, const Product *b, int type, const float *sums, int64_t rows, int64_t N, float *out, hipStream_t stream)
 {
@@ -337,19 +302,6 @@ int launch_join(const Product *a, const Product *b, int type, const float *sums,
     return launched("product join kernel launch: ");
 }
 
-// Jobs that make rows, in one launch; the first has rows of dy_type.
-struct Prepare {
-    PrepareParams p{};
-    int n = 0, blocks = 0;
-    void add(SlopeParams s, int type)
-    {
-        lay_out(s, type);
-        p.job[n] = s;
-        blocks += s.wide * s.down;
-        p.last[n++] = blocks;
-    }
-};
-
 int launch_prepare(Prepare &j, int type, int dy_type, hipStream_t stream)
 {
     if (j.n == 0) return FB_OK;
@@ -368,39 +320,7 @@ int launch_prepare(Prepare &j, int type, int dy_type, hipStream_t stream)
     return launched("row preparation kernel launch: ");
 }
 
-int64_t whole_pieces(int64_t width, int type)
-{
-    const int64_t piece = 16 / (int64_t)type_bytes(type);
-    return (width + piece - 1) / piece * piece;
-}
-
-// A matrix that the matrix units' kernel cannot take as it is, copied to rows of whole pieces (padded with zeros).
-struct Packed {
-    bool copy;
-    int64_t ld;
-    size_t bytes;
-};
-
-Packed packed(const void *p, int64_t ld, int64_t rows, int64_t width, int type)
-{
-    Packed k{};
-    k.copy = !ready(p, ld, width, type);
-    k.ld = k.copy ? whole_pieces(width, type) : ld;
-    k.bytes = k.copy ? aligned((size_t)rows * (size_t)k.ld * type_bytes(type)) : 0;
-    return k;
-}
-
-// The job that makes the copy (nothing if none is needed).
-SlopeParams pack_job(const Packed &k, const void *p, int64_t ld, int64_t rows, int64_t width, void *to)
-{
-    return SlopeParams{p, nullptr, ld, 0, rows, width, k.ld, FB_ACT_NONE, to, nullptr, 0, 0, 0, nullptr, 0, nullptr};
-}
-
-// What the matrix units' kernel addresses in 32 bits: 64 or 128 rows of a factor, 16 rows of what it stores or adds.
-bool too_long(int64_t width, int type) { return width * (int64_t)type_bytes(type) > (int64_t)1 << 22; }
-bool too_far(int64_t ld) { return ld >= (int64_t)1 << 27; }
-
-bool bad_sizes(int64_t M, int64_t N, int64_t K) { return bad_rows(M) || bad_width(N) || bad_width(K); }
+namespace {
 
 struct ForwardPlan {
     Product q;
@@ -422,16 +342,7 @@ ForwardPlan forward_plan(const void *x, int64_t ldx, const void *weight, int64_t
     return f;
 }
 
-// The two products of the gradient.
-struct GradPlan {
-    Product dx, dw;
-    bool pair;            // in one launch
-    bool slope;           // dz has to be made, or dy laid out anew
-    bool scale;           // and is rounded to half precision: times a power of two
-    int64_t ldz;
-    Packed x, w;
-    size_t dz, sums, range, part, bytes;
-};
+}  // namespace
 
 GradPlan grad_plan(const void *dy, int64_t lddy, int dy_type, const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t N,
                    int64_t K, int type, int act)
@@ -465,6 +376,31 @@ GradPlan grad_plan(const void *dy, int64_t lddy, int dy_type, const void *x, int
     g.bytes = g.dz + g.x.bytes + g.w.bytes + g.sums + g.range + g.part + product_bytes(g.dw);
     return g;
 }
+
+// dx = dz W and dweight = dz^T x, whose second factors are set, and what is left behind them; the sums of dz's columns are in `sums`.
+int launch_grad(GradPlan &g, const Factor &d, const float *undo, void *dx, int64_t lddx, void *dweight, float *part, const float *sums, int64_t rows, float *dbias,
+                hipStream_t st)
+{
+    const int64_t M = g.dx.M, N = g.dw.M, K = g.dx.N;
+    const int type = g.dx.type;
+    int rc;
+    g.dx.A = d;
+    g.dx.f.y = dx; g.dx.f.ldy = lddx; g.dx.f.out_type = type;
+    g.dx.f.undo = g.dw.f.undo = undo;
+    g.dx.part = part;
+    g.dw.A = {d.p, d.ld, false};
+    g.dw.f.y = dweight; g.dw.f.ldy = K; g.dw.f.out_type = type;
+    g.dw.part = (float *)((char *)part + g.part);
+    if (dx && dweight && g.pair) {
+        if ((rc = launch_mfma_pair(g.dx, g.dw, st)) != FB_OK) return rc;
+    } else {
+        if (dx && M > 0 && (rc = launch_mfma_product(g.dx, st)) != FB_OK) return rc;
+        if (dweight && (rc = launch_mfma_product(g.dw, st)) != FB_OK) return rc;
+    }
+    return launch_join(dx ? &g.dx : nullptr, dweight ? &g.dw : nullptr, type, sums, rows, N, dbias, st);
+}
+
+namespace {
 
 int check_affine(const char *who, const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t N, int64_t K, int type, int act)
 {
@@ -570,22 +506,9 @@ int fb_affine_grad(const void *dy, int64_t lddy, int dy_type, const void *x, int
         if (M > 0 && dweight && g.x.copy) jobs.add(pack_job(g.x, x, ldx, M, K, xs), type);
         if (jobs.blocks > 0 && (rc = launch_prepare(jobs, type, dy_type, st)) != FB_OK) return rc;
         const Factor d{make ? (const void *)dz : dy, make ? g.ldz : lddy, true};
-        g.dx.A = d;
         g.dx.B = {g.w.copy ? wts : weight, g.w.ld, false};
-        g.dx.f.y = dx; g.dx.f.ldy = lddx; g.dx.f.out_type = type;
-        g.dx.f.undo = g.dw.f.undo = scale ? undo : nullptr;
-        g.dx.part = part;
-        g.dw.A = {d.p, d.ld, false};
         g.dw.B = {g.x.copy ? xs : x, g.x.ld, false};
-        g.dw.f.y = dweight; g.dw.f.ldy = K; g.dw.f.out_type = type;
-        g.dw.part = (float *)((char *)part + g.part);
-        if (dx && dweight && g.pair) {
-            if ((rc = launch_mfma_pair(g.dx, g.dw, st)) != FB_OK) return rc;
-        } else {
-            if (dx && M > 0 && (rc = launch_mfma_product(g.dx, st)) != FB_OK) return rc;
-            if (dweight && (rc = launch_mfma_product(g.dw, st)) != FB_OK) return rc;
-        }
-        return launch_join(dx ? &g.dx : nullptr, dweight ? &g.dw : nullptr, type, sums, M > 0 ? sum_rows(M, N, type) : 0, N, dbias, st);
+        return launch_grad(g, d, scale ? undo : nullptr, dx, lddx, dweight, part, sums, M > 0 ? sum_rows(M, N, type) : 0, dbias, st);
     });
 }
 

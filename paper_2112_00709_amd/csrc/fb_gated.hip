@@ -1,0 +1,444 @@
+// Gated layer and its gradient (fb_layers.h): y = act(x G^T + a) (x U^T + b).
+//
+// Forward, both products are one, of x with G and U in turn 32 rows of each (see Side in fb_mfma.h): a wave's two fragments of the
+// weight are the same rows of both, so that g and u of an output meet in one wave and y leaves alone.
+#include "fb_mfma.h"
+
+namespace fb {
+
+namespace {
+
+// Sums of a wave leave as y = act(g) u: 16 rows of C at a time through LDS, as in Finished, the gate's 32 columns and behind
+// them the other factor's.
+struct Gated {
+    static constexpr bool kPaired = true;
+    static constexpr int kEarly = 2;
+
+    template <int FJ>
+    static __device__ __forceinline__ void early(const Product &q, int64_t j0, int wj, int lane, f32x4 (&four)[2])
+    {
+        const int64_t j = j0 + wj * 32 + lane % 8 * 4;
+        bias_of(q.f.bias, q.N, j, four[0]);
+        bias_of(q.f.bias + q.N, q.N, j, four[1]);
+    }
+
+    template <class T, int FI, int FJ>
+    static __device__ __forceinline__ void leave(ProductArgs args, const f32x16 (&acc)[FI][FJ], const f32x4 (&bias)[2], float, const Where &where)
+    {
+        static_assert(FJ == 2, "a fragment of either factor");
+        int lane = threadIdx.x & 63;
+        asm volatile("" : "+s"(args), "+v"(lane));
+        constexpr int kR = 2, kRows = 8;
+        const int64_t M = args->M, N = args->N, i0 = where.i0 + where.wi * FI * 32, j0 = where.j0 + where.wj * 32, j = j0 + lane % 8 * 4;
+        const int nj = (int)(N - j < 4 ? (N - j < 0 ? 0 : N - j) : 4), in_row = lane / 8, act = args->f.act;
+        const bool past = args->past;
+        float *mine = where.room + where.wave * 16 * FJ * 32;
+        const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)mine + (lane & 15) * FJ * 128;
+#pragma unroll 1
+        for (int pass = 0; pass < 2 * FI; ++pass) {
+            if ((lane >> 4 & 1) == (pass & 1)) {
+                auto put = [&](const f32x16 (&sums)[FJ]) {
+#pragma unroll
+                    for (int y = 0; y < FJ; ++y)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const f32x4 w = {sums[y][4 * e], sums[y][4 * e + 1], sums[y][4 * e + 2], sums[y][4 * e + 3]};
+                            *(__attribute__((address_space(3))) f32x4 *)(uintptr_t)(to + ((y * 8 + 2 * e + (lane >> 5)) ^ (lane & 15)) * 16) = w;
+                        }
+                };
+                if (pass < 2) put(acc[0]);
+                else if (FI <= 2 || pass < 4) put(acc[1 % FI]);
+                else if (pass < 6) put(acc[2 % FI]);
+                else put(acc[3 % FI]);
+            }
+            f32x4 g[kR], u[kR];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+            for (int r = 0; r < kR; ++r) {
+                const int row = r * kRows + in_row;
+                g[r] = *(const f32x4 *)(mine + row * FJ * 32 + ((lane % 8) ^ row) * 4) + bias[0];
+                u[r] = *(const f32x4 *)(mine + row * FJ * 32 + ((lane % 8 + 8) ^ row) * 4) + bias[1];
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            const int64_t i = i0 + pass * 16;
+            const Spot at{i, j0, in_row, (lane % 8) * 4, (int)(M - i < 16 ? M - i : 16), nj};
+            if (at.rows > in_row && nj > 0) {
+                if (args->f.preact) {
+                    store_rows<T, T, kR, kRows>((T *)args->f.preact, args->f.ldp, at, g, past);
+                    store_rows<T, T, kR, kRows>((T *)args->f.preact + N, args->f.ldp, at, u, past);
+                }
+                auto gate = [&](int which) {
+#pragma unroll
+                    for (int r = 0; r < kR; ++r)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) u[r][e] *= act_of(g[r][e], which);
+                };
+                if (act == FB_ACT_SILU) gate(FB_ACT_SILU);
+                else if (act == FB_ACT_GELU) gate(FB_ACT_GELU);
+                else if (act == FB_ACT_SIGMOID) gate(FB_ACT_SIGMOID);
+                else if (act == FB_ACT_RELU) gate(FB_ACT_RELU);
+                else gate(FB_ACT_NONE);
+                store_rows<T, T, kR, kRows>((T *)args->f.y, args->f.ldy, at, u, past);
+            }
+        }
+    }
+};
+
+template <class T>
+int launch_gated(const Product &q, hipStream_t stream)
+{
+    return q.tile == 256 ? launch<T, true, true, 2, 4, 4, 2, Gated>(q, stream) : launch<T, true, true, 2, 2, 2, 2, Gated>(q, stream);
+}
+
+// Shares of k added in their order, pair by pair, and finished.
+template <class T>
+__global__ __launch_bounds__(256) void fb_gated_join_kernel(Product q)
+{
+    const int64_t N = q.N / 2, n = q.M * N;
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < n; at += (int64_t)gridDim.x * 256) {
+        const int64_t i = at / N, j = at - i * N;
+        float g = 0.0f, u = 0.0f;
+#pragma unroll 4
+        for (int c = 0; c < q.split; ++c) {
+            const float *part = q.part + ((size_t)c * q.M + i) * q.N + j;
+            g += part[0];
+            u += part[N];
+        }
+        finish_pair<T>(q.f, N, i, j, g, u);
+    }
+}
+
+int launch_gated_join(const Product &q, hipStream_t stream)
+{
+    const dim3 grid((unsigned)std::min<int64_t>((q.M * (q.N / 2) + 255) / 256, 8 * kCUs)), block(256);
+    if (q.type == FB_TYPE_F32)
+        hipLaunchKernelGGL(fb_gated_join_kernel<float>, grid, block, 0, stream, q);
+    else if (q.type == FB_TYPE_BF16)
+        hipLaunchKernelGGL(fb_gated_join_kernel<bf16>, grid, block, 0, stream, q);
+    else
+        hipLaunchKernelGGL(fb_gated_join_kernel<f16>, grid, block, 0, stream, q);
+    return launched("gated join kernel launch: ");
+}
+
+// dz = [dy u act'(g), dy act(g)], rounded to the factors' type, and the sums of its columns before the rounding.  Bound by memory.
+// A thread has one piece of the width, of both halves; the layout of threads is that of rows of N (lay_out).
+struct GatedSlopeParams {
+    const void *dy, *z;
+    int64_t lddy, ldz, M, N, ldo;
+    int act;
+    void *out;               // nullable
+    float *part;             // [down][2 N], nullable
+    int lanes, wide, down;
+    uint32_t *peaks;         // half precision: of the largest finite |dz|, see fb_affine_grad; nullable
+    int n_peaks;
+    float *undo;
+};
+
+constexpr int kPairsAhead = 2;
+
+template <class T>
+__device__ __forceinline__ void slopes_of(const u32x4 &rd, const u32x4 &rg, const u32x4 &ru, int act, float *dg, float *du)
+{
+    constexpr int VE = Vec<T>::kN;
+    float d[VE], g[VE], u[VE];
+    unpack<T>(rd, d);
+    unpack<T>(rg, g);
+    unpack<T>(ru, u);
+    auto by = [&](int which) {
+#pragma unroll
+        for (int e = 0; e < VE; ++e) {
+            dg[e] = d[e] * u[e] * act_slope(g[e], which);
+            du[e] = d[e] * act_of(g[e], which);
+        }
+    };
+    if (act == FB_ACT_SILU) by(FB_ACT_SILU);
+    else if (act == FB_ACT_GELU) by(FB_ACT_GELU);
+    else if (act == FB_ACT_SIGMOID) by(FB_ACT_SIGMOID);
+    else if (act == FB_ACT_RELU) by(FB_ACT_RELU);
+    else by(FB_ACT_NONE);
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void fb_gated_slope_kernel(GatedSlopeParams p)
+{
+    constexpr int VE = Vec<T>::kN;
+    __shared__ float slots[256][2 * VE + 1];
+    const int across = blockIdx.x % p.wide, down = blockIdx.x / p.wide;
+    const int lane = threadIdx.x & (p.lanes - 1), sub = threadIdx.x / p.lanes, subs = 256 / p.lanes;
+    const int64_t at = ((int64_t)across * p.lanes + lane) * VE;
+    const int n = at >= p.N ? 0 : (int)(p.N - at < VE ? p.N - at : VE);
+    float sum[2 * VE] = {}, scale = 1.0f;
+    if constexpr (std::is_same<T, f16>::value) {
+        if (p.peaks) {
+            float undo;
+            range_of(p.peaks, p.n_peaks, scale, undo);
+            if (blockIdx.x == 0 && threadIdx.x == 0) *p.undo = undo;
+        }
+    }
+    if (n > 0) {
+        const int64_t step = (int64_t)p.down * subs;
+        const int zeros = at + VE >= p.N ? (int)(p.ldo - 2 * p.N) : 0;       // the row's last columns, that the products read
+        for (int64_t r0 = (int64_t)down * subs + sub; r0 < p.M; r0 += kPairsAhead * step) {
+            u32x4 rd[kPairsAhead], rg[kPairsAhead], ru[kPairsAhead];
+#pragma unroll
+            for (int a = 0; a < kPairsAhead; ++a) {
+                const int64_t r = r0 + a * step;
+                const int here = r < p.M ? n : 0;
+                rd[a] = load_piece((const T *)p.dy + r * p.lddy + at, here);
+                rg[a] = load_piece((const T *)p.z + r * p.ldz + at, here);
+                ru[a] = load_piece((const T *)p.z + r * p.ldz + p.N + at, here);
+            }
+#pragma unroll
+            for (int a = 0; a < kPairsAhead; ++a) {
+                const int64_t r = r0 + a * step;
+                if (r >= p.M) break;
+                float d[2 * VE];
+                slopes_of<T>(rd[a], rg[a], ru[a], p.act, d, d + VE);
+#pragma unroll
+                for (int e = 0; e < 2 * VE; ++e) {
+                    sum[e] += d[e];
+                    d[e] *= scale;
+                }
+                if (!p.out) continue;
+                T *out = (T *)p.out + r * p.ldo;
+                store_piece(out + at, n, pack<T>(d));
+                store_piece(out + p.N + at, n, pack<T>(d + VE));
+                for (int c = 0; c < zeros; ++c) out[2 * p.N + c] = (T)0.0f;
+            }
+        }
+    }
+    if (!p.part) return;
+#pragma unroll
+    for (int e = 0; e < 2 * VE; ++e) slots[threadIdx.x][e] = sum[e];
+    __syncthreads();
+    for (int c = threadIdx.x; c < p.lanes * VE * 2; c += 256) {
+        const int half = c / (p.lanes * VE), k = c % (p.lanes * VE);
+        const int64_t col = (int64_t)across * p.lanes * VE + k;
+        if (col >= p.N) continue;
+        float s = 0.0f;
+        for (int i = 0; i < subs; ++i) s += slots[i * p.lanes + k / VE][half * VE + k % VE];
+        p.part[(size_t)down * 2 * p.N + half * p.N + col] = s;
+    }
+}
+
+// The largest finite |dz|, a share a workgroup (half precision: what fb_affine_grad finds of dy, here of dz itself, as u and act(g) are
+// not bounded).
+__global__ __launch_bounds__(1024) void fb_gated_peak_kernel(GatedSlopeParams p)
+{
+    constexpr int VE = Vec<f16>::kN, kAhead = 2;
+    __shared__ uint32_t slots[16];
+    const int64_t pieces = (p.N + VE - 1) / VE, step = (int64_t)gridDim.x * 1024, down = step / pieces, across = step - down * pieces;
+    const int64_t at = (int64_t)blockIdx.x * 1024 + threadIdx.x;
+    int64_t r = at / pieces, c = at - r * pieces;
+    uint32_t peak = 0;
+    while (r < p.M) {
+        u32x4 rd[kAhead], rg[kAhead], ru[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int n = r < p.M ? (int)(p.N - c * VE) : 0;
+            rd[u] = load_piece((const f16 *)p.dy + r * p.lddy + c * VE, n);
+            rg[u] = load_piece((const f16 *)p.z + r * p.ldz + c * VE, n);
+            ru[u] = load_piece((const f16 *)p.z + r * p.ldz + p.N + c * VE, n);
+            r += down;
+            c += across;
+            if (c >= pieces) {
+                c -= pieces;
+                ++r;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            float d[2 * VE];
+            slopes_of<f16>(rd[u], rg[u], ru[u], p.act, d, d + VE);
+#pragma unroll
+            for (int e = 0; e < 2 * VE; ++e) {
+                const uint32_t a = __float_as_uint(d[e]) & 0x7fffffffu;
+                peak = a < 0x7f800000u && a > peak ? a : peak;
+            }
+        }
+    }
+    peak = max_wave_u(peak);
+    if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = peak;
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        peak = max_wave_u(threadIdx.x < 16 ? slots[threadIdx.x] : 0u);
+        if (threadIdx.x == 0) p.peaks[blockIdx.x] = peak;
+    }
+}
+
+void lay_out_pairs(GatedSlopeParams &p, int type)
+{
+    const int64_t ve = 16 / (int64_t)type_bytes(type), pieces = (p.N + ve - 1) / ve;
+    for (p.lanes = 1; p.lanes < 64 && p.lanes < pieces;) p.lanes *= 2;
+    p.wide = (int)((pieces + p.lanes - 1) / p.lanes);
+    const int64_t rows = 256 / p.lanes * kPairsAhead;      // at a time
+    p.down = (int)std::max<int64_t>(1, std::min<int64_t>((p.M + rows - 1) / rows, std::max<int64_t>(64, 8 * kCUs / p.wide)));
+    p.n_peaks = (int)std::min<int64_t>(kPeakGroups, (p.M * pieces + 1023) / 1024);
+}
+
+struct GatedPlan {
+    Product q;               // N: both factors' rows if the sums go through memory, else the outputs'
+    bool few;
+    Packed x, w;
+    size_t bytes;
+};
+
+GatedPlan gated_plan(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t N, int64_t K, int type)
+{
+    GatedPlan f{};
+    f.q.M = M; f.q.N = 2 * N; f.q.K = K; f.q.type = type;
+    f.few = M <= kFewRows;
+    if (!f.few) {
+        plan(f.q);
+        // (tiles of 64 have one fragment a wave: their pairs meet in memory)
+        f.q.parts = f.q.parts || f.q.tile == 64;
+        f.x = packed(x, ldx, M, K, type);
+        f.w = packed(weight, ldw, 2 * N, K, type);
+        f.bytes = f.x.bytes + f.w.bytes + product_bytes(f.q);
+    }
+    if (!f.q.parts) f.q.N = N;
+    return f;
+}
+
+struct GatedGradPlan {
+    GradPlan g;
+    GatedSlopeParams s;
+};
+
+GatedGradPlan gated_grad_plan(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t N, int64_t K, int type)
+{
+    GatedGradPlan p{};
+    p.g = grad_plan(nullptr, 2 * N, type, x, ldx, weight, ldw, M, 2 * N, K, type, FB_ACT_SILU);   // (an activation: dz is made)
+    p.s.M = M; p.s.N = N; p.s.ldo = p.g.ldz;
+    lay_out_pairs(p.s, type);
+    const size_t sums = aligned((size_t)p.s.down * 2 * (size_t)N * sizeof(float));
+    p.g.bytes += sums - p.g.sums;
+    p.g.sums = sums;
+    return p;
+}
+
+bool bad_pair_sizes(int64_t M, int64_t N, int64_t K) { return bad_sizes(M, N, K) || bad_width(2 * N); }
+
+int check_gated(const char *who, const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t N, int64_t K, int type, int act)
+{
+    const std::string w(who);
+    if (!known_type(type)) return fail(FB_EINVAL, w + ": unknown type");
+    if (act < FB_ACT_NONE || act > FB_ACT_SIGMOID) return fail(FB_EINVAL, w + ": unknown activation");
+    if (bad_pair_sizes(M, N, K)) return fail(FB_EINVAL, w + ": M must be 0 or more and below 2^31, N and K 1 or more, 2 N and K below 2^28");
+    if ((!x && M > 0) || !weight) return fail(FB_EINVAL, w + ": x or weight is NULL");
+    if (bad_ld(ldx, K) || bad_ld(ldw, K)) return fail(FB_EINVAL, w + ": rows of x or weight closer than K elements");
+    return FB_OK;
+}
+
+}  // namespace
+
+}  // namespace fb
+
+extern "C" {
+
+size_t fb_gated_affine_workspace_bytes(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t N, int64_t K, int type)
+{
+    using namespace fb;
+    if (bad_pair_sizes(M, N, K) || !known_type(type)) return 0;
+    return gated_plan(x, ldx, weight, ldw, M, N, K, type).bytes;
+}
+
+int fb_gated_affine(const void *x, int64_t ldx, const void *weight, int64_t ldw, const float *bias, int64_t M, int64_t N, int64_t K, int type, int act,
+                    void *y, int64_t ldy, void *preact, int64_t ldp, void *ws, size_t ws_bytes, fb_stream stream)
+{
+    using namespace fb;
+    return guarded([&]() -> int {
+        int rc = check_gated("fb_gated_affine", x, ldx, weight, ldw, M, N, K, type, act);
+        if (rc != FB_OK) return rc;
+        if (!y && M > 0) return fail(FB_EINVAL, "fb_gated_affine: y is NULL");
+        if (bad_ld(ldy, N) || (preact && bad_ld(ldp, 2 * N))) return fail(FB_EINVAL, "fb_gated_affine: rows closer than their width");
+        if (M > kFewRows ? too_long(K, type) || too_far(ldy) || (preact && too_far(ldp)) : N >= (int64_t)1 << 25)
+            return fail(FB_EUNSUPPORTED, "fb_gated_affine: rows of x and weight longer than 4 MB, rows of y or preact 2^27 elements apart, or (M <= 64) N of 2^25 and more");
+        const GatedPlan f = gated_plan(x, ldx, weight, ldw, M, N, K, type);
+        if (f.bytes && (!ws || ws_bytes < f.bytes)) return fail(FB_EINVAL, "fb_gated_affine: workspace missing or too small");
+        if (M == 0) return FB_OK;
+        hipStream_t st = (hipStream_t)stream;
+        char *xs = (char *)ws, *wts = xs + f.x.bytes;
+        Product q = f.q;
+        q.f = {bias, nullptr, 0, act, y, ldy, type, preact, ldp, nullptr};
+        if (f.few) {
+            q.N = N;
+            q.A = {x, ldx, true};
+            q.B = {weight, ldw, true};
+            return launch_few_pairs(q, st);
+        }
+        Prepare jobs;
+        if (f.x.copy) jobs.add(pack_job(f.x, x, ldx, M, K, xs), type);
+        if (f.w.copy) jobs.add(pack_job(f.w, weight, ldw, 2 * N, K, wts), type);
+        if ((rc = launch_prepare(jobs, type, type, st)) != FB_OK) return rc;
+        q.A = {f.x.copy ? xs : x, f.x.ld, true};
+        q.B = {f.w.copy ? wts : weight, f.w.ld, true};
+        q.part = (float *)(wts + f.w.bytes);
+        if (q.parts) {
+            if ((rc = launch_mfma_product(q, st)) != FB_OK) return rc;
+            return launch_gated_join(q, st);
+        }
+        if (type == FB_TYPE_F32) return launch_gated<float>(q, st);
+        return type == FB_TYPE_BF16 ? launch_gated<bf16>(q, st) : launch_gated<f16>(q, st);
+    });
+}
+
+size_t fb_gated_affine_grad_workspace_bytes(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t N, int64_t K, int type)
+{
+    using namespace fb;
+    if (bad_pair_sizes(M, N, K) || !known_type(type)) return 0;
+    return gated_grad_plan(x, ldx, weight, ldw, M, N, K, type).g.bytes;
+}
+
+int fb_gated_affine_grad(const void *dy, int64_t lddy, const void *x, int64_t ldx, const void *weight, int64_t ldw, const void *preact, int64_t ldp,
+                         int64_t M, int64_t N, int64_t K, int type, int act, void *dx, int64_t lddx, void *dweight, float *dbias, void *ws,
+                         size_t ws_bytes, fb_stream stream)
+{
+    using namespace fb;
+    return guarded([&]() -> int {
+        int rc = check_gated("fb_gated_affine_grad", x, ldx, weight, ldw, M, N, K, type, act);
+        if (rc != FB_OK) return rc;
+        if ((!dy || !preact) && M > 0) return fail(FB_EINVAL, "fb_gated_affine_grad: dy or preact is NULL");
+        if (bad_ld(lddy, N) || bad_ld(ldp, 2 * N) || (dx && bad_ld(lddx, K))) return fail(FB_EINVAL, "fb_gated_affine_grad: rows closer than their width");
+        if (!dx && !dweight && !dbias) return FB_OK;
+        if (too_long(K, type) || too_long(2 * N, type) || (dx && too_far(lddx)))
+            return fail(FB_EUNSUPPORTED, "fb_gated_affine_grad: rows of x, weight and dz longer than 4 MB, or rows of dx 2^27 elements apart");
+        GatedGradPlan p = gated_grad_plan(x, ldx, weight, ldw, M, N, K, type);
+        GradPlan &g = p.g;
+        if (!ws || ws_bytes < g.bytes) return fail(FB_EINVAL, "fb_gated_affine_grad: workspace missing or too small");
+        hipStream_t st = (hipStream_t)stream;
+        char *dz = (char *)ws, *xs = dz + g.dz, *wts = xs + g.x.bytes;
+        float *sums = (float *)(wts + g.w.bytes), *undo = (float *)(wts + g.w.bytes + g.sums);
+        float *part = (float *)((char *)undo + g.range);
+        const bool scale = g.scale && (dx || dweight) && M > 0;
+        GatedSlopeParams s = p.s;
+        s.dy = dy; s.lddy = lddy; s.z = preact; s.ldz = ldp; s.act = act;
+        s.out = dx || dweight ? dz : nullptr;
+        s.part = dbias ? sums : nullptr;
+        s.undo = undo;
+        s.peaks = scale ? (uint32_t *)(undo + 1) : nullptr;
+        if (scale) {
+            hipLaunchKernelGGL(fb_gated_peak_kernel, dim3((unsigned)s.n_peaks), dim3(1024), 0, st, s);
+            if ((rc = launched("gated peak kernel launch: ")) != FB_OK) return rc;
+        }
+        if (M > 0) {
+            const dim3 grid((unsigned)((int64_t)s.wide * s.down)), block(256);
+            if (type == FB_TYPE_F32)
+                hipLaunchKernelGGL(fb_gated_slope_kernel<float>, grid, block, 0, st, s);
+            else if (type == FB_TYPE_BF16)
+                hipLaunchKernelGGL(fb_gated_slope_kernel<bf16>, grid, block, 0, st, s);
+            else
+                hipLaunchKernelGGL(fb_gated_slope_kernel<f16>, grid, block, 0, st, s);
+            if ((rc = launched("gated slope kernel launch: ")) != FB_OK) return rc;
+        }
+        Prepare jobs;
+        if (M > 0 && dx && g.w.copy) jobs.add(pack_job(g.w, weight, ldw, 2 * N, K, wts), type);
+        if (M > 0 && dweight && g.x.copy) jobs.add(pack_job(g.x, x, ldx, M, K, xs), type);
+        if ((rc = launch_prepare(jobs, type, type, st)) != FB_OK) return rc;
+        g.dx.B = {g.w.copy ? wts : weight, g.w.ld, false};
+        g.dw.B = {g.x.copy ? xs : x, g.x.ld, false};
+        return launch_grad(g, Factor{dz, g.ldz, true}, scale ? undo : nullptr, dx, lddx, dweight, part, sums, M > 0 ? s.down : 0, dbias, st);
+    });
+}
+
+}  // extern "C"

@@ -19,13 +19,15 @@ from . import FBError, _check  # noqa: F401  (FBError: what a failing call raise
 
 F32, BF16, F16 = 0, 1, 2
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+GATED_ACTIVATIONS = {**ACTIVATIONS, "sigmoid": 4}
 NORMS = {"none": 0, "layer": 1, "rms": 2}
 TOP_MAX = 64
 
 # every symbol include/fb_layers.h declares
 SYMBOLS = ["fb_layer_norm", "fb_layer_norm_grad_workspace_bytes", "fb_layer_norm_grad", "fb_residual_norm",
            "fb_residual_norm_grad_workspace_bytes", "fb_residual_norm_grad", "fb_affine_workspace_bytes", "fb_affine",
-           "fb_affine_grad_workspace_bytes", "fb_affine_grad", "fb_token_logprobs_workspace_bytes", "fb_token_logprobs",
+           "fb_affine_grad_workspace_bytes", "fb_affine_grad", "fb_gated_affine_workspace_bytes", "fb_gated_affine",
+           "fb_gated_affine_grad_workspace_bytes", "fb_gated_affine_grad", "fb_token_logprobs_workspace_bytes", "fb_token_logprobs",
            "fb_token_logprobs_grad"]
 
 _lib = None
@@ -52,6 +54,10 @@ def lib() -> ctypes.CDLL:
         L.fb_affine.argtypes = [vp, i64, vp, i64, vp, vp, i64, i64, i64, i64, i32, i32, vp, i64, i32, vp, i64, vp, sz, vp]
         L.fb_affine_grad_workspace_bytes.argtypes = [vp, i64, i32, vp, i64, vp, i64, i64, i64, i64, i32, i32]
         L.fb_affine_grad.argtypes = [vp, i64, i32, vp, i64, vp, i64, vp, i64, i64, i64, i64, i32, i32, vp, i64, vp, vp, vp, sz, vp]
+        L.fb_gated_affine_workspace_bytes.argtypes = [vp, i64, vp, i64, i64, i64, i64, i32]
+        L.fb_gated_affine.argtypes = [vp, i64, vp, i64, vp, i64, i64, i64, i32, i32, vp, i64, vp, i64, vp, sz, vp]
+        L.fb_gated_affine_grad_workspace_bytes.argtypes = [vp, i64, vp, i64, i64, i64, i64, i32]
+        L.fb_gated_affine_grad.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i64, i64, i64, i32, i32, vp, i64, vp, vp, vp, sz, vp]
         L.fb_token_logprobs_workspace_bytes.argtypes = [i64, i64, i32, i32]
         L.fb_token_logprobs.argtypes = [vp, i64, vp, i64, i64, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]
         L.fb_token_logprobs_grad.argtypes = [vp, i64, vp, vp, vp, vp, vp, i64, i64, i32, vp, i64, vp]
@@ -285,10 +291,10 @@ def fb_residual_norm_grad(ds, dy, h, s, stats, gate=None, scale: float = 1.0, in
     return (dh, dr, dg, *sums)
 
 
-def _activation(name: str) -> int:
-    if name not in ACTIVATIONS:
-        raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}")
-    return ACTIVATIONS[name]
+def _activation(name: str, known=ACTIVATIONS) -> int:
+    if name not in known:
+        raise ValueError(f"activation must be one of {', '.join(known)}")
+    return known[name]
 
 
 def fb_affine(x, weight, bias=None, activation: str = "none", residual=None, out_dtype=None, want_preact: bool = False):
@@ -349,6 +355,55 @@ def fb_affine_grad(dy, x, weight, activation: str = "none", preact=None, want_dx
     ws, pws = _workspace(need, x)
     _check(L.fb_affine_grad(pdy, lddy, dtype, px, ldx, pw, ldw, pz, ldz, M, N, K, code, act, dx.data_ptr() if want_dx else None, K,
                             dw.data_ptr() if want_dweight else None, db.data_ptr() if want_dbias else None, pws, need, _raw_stream(dev)))
+    return dx, dw, db
+
+
+def _pairs(weight, K: int, x, dev: int):
+    """-> (address, row distance, N) of a gated layer's weight [2 N, K]."""
+    if weight.dim() != 2 or weight.shape[0] < 2 or weight.shape[0] % 2:
+        raise ValueError("weight must be [2 N, K]")
+    p, ld, _, _, _ = _rows(weight, "weight", K, x.dtype, None, dev)
+    return p, ld, int(weight.shape[0]) // 2
+
+
+def fb_gated_affine(x, weight, bias=None, activation: str = "silu", want_preact: bool = False):
+    """-> y = activation(g) * u, [..., N] of x's type, with [g, u] = x weight^T + bias, or with want_preact (y, preact).
+
+    ``x`` [..., K]; ``weight`` [2 N, K] of x's type: g's rows, then u's; ``bias`` [2 N] float32; ``activation``: as fb_affine's,
+    or "sigmoid"; preact [..., 2 N], of x's type: g, then u."""
+    L = lib()
+    code, act = _type(x, "x"), _activation(activation, GATED_ACTIVATIONS)
+    px, ldx, M, K, dev = _rows(x, "x")
+    pw, ldw, N = _pairs(weight, K, x, dev)
+    pb = _vector(bias, "bias", 2 * N, (torch.float32,), dev)
+    lead = x.shape[:-1]
+    y = _out(x, (*lead, N), x.dtype)
+    z = _out(x, (*lead, 2 * N), x.dtype) if want_preact else None
+    need = int(L.fb_gated_affine_workspace_bytes(px, ldx, pw, ldw, M, N, K, code))
+    ws, pws = _workspace(need, x)
+    _check(L.fb_gated_affine(px, ldx, pw, ldw, pb, M, N, K, code, act, y.data_ptr(), N, z.data_ptr() if want_preact else None, 2 * N, pws, need,
+                             _raw_stream(dev)))
+    return (y, z) if want_preact else y
+
+
+def fb_gated_affine_grad(dy, x, weight, preact, activation: str = "silu", want_dx: bool = True, want_dweight: bool = True, want_dbias: bool = True):
+    """-> (dx like x, dweight like weight, dbias [2 N] float32), None in the place of one that is not wanted.
+
+    ``dy`` [..., N] and ``preact`` [..., 2 N] of x's type, the latter as fb_gated_affine returned it."""
+    L = lib()
+    code, act = _type(x, "x"), _activation(activation, GATED_ACTIVATIONS)
+    px, ldx, M, K, dev = _rows(x, "x")
+    pw, ldw, N = _pairs(weight, K, x, dev)
+    lead = x.shape[:-1]
+    pdy, lddy, _, _, _ = _rows(dy, "dy", N, x.dtype, lead, dev)
+    pz, ldz, _, _, _ = _rows(preact, "preact", 2 * N, x.dtype, lead, dev)
+    dx = _out_like(x) if want_dx else None
+    dw = _out(x, (2 * N, K), x.dtype) if want_dweight else None
+    db = _out(x, (2 * N,), torch.float32) if want_dbias else None
+    need = int(L.fb_gated_affine_grad_workspace_bytes(px, ldx, pw, ldw, M, N, K, code))
+    ws, pws = _workspace(need, x)
+    _check(L.fb_gated_affine_grad(pdy, lddy, px, ldx, pw, ldw, pz, ldz, M, N, K, code, act, dx.data_ptr() if want_dx else None, K,
+                                  dw.data_ptr() if want_dweight else None, db.data_ptr() if want_dbias else None, pws, need, _raw_stream(dev)))
     return dx, dw, db
 
 
