@@ -9,6 +9,7 @@
  *   fb_affine, fb_affine_grad                     y = act(x W^T + b) + residual
  *   fb_gated_affine, fb_gated_affine_grad         y = act(x G^T + a) (x U^T + b), elementwise
  *   fb_token_logprobs, fb_token_logprobs_grad     log probabilities of given tokens, entropy, best alternatives
+ *   fb_affine_logprobs, fb_affine_logprobs_grad   log probabilities and entropy straight from hidden frames, logits never kept
  *
  * Conventions are those of fb.h: device pointers owned by the caller, kernels enqueued on `stream`, nothing allocated, freed
  * or synchronised, FB_OK or a negative code returned and never an exception, fb_last_error() says what was wrong.  A call may
@@ -216,6 +217,41 @@ int fb_token_logprobs(const void *logits, int64_t ld, const int32_t *tokens, int
 int fb_token_logprobs_grad(const void *logits, int64_t ld, const int32_t *tokens, const float *logz, const float *entropy,
                            const float *g_logprobs, const float *g_entropy, int64_t R, int64_t V, int type, void *dlogits,
                            int64_t ldd, fb_stream stream);
+
+/* Bytes of workspace fb_affine_logprobs needs for these arguments (0: bad arguments).  Matrices whose rows are not whole 16-byte pieces
+ * at multiples of 16 bytes are copied to such rows first (unless M <= 64). */
+size_t fb_affine_logprobs_workspace_bytes(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t V, int64_t K, int type);
+
+/*
+ * fb_token_logprobs of the logits  x W^T + bias,  which are formed in single precision, a tile at a time, and neither rounded nor kept:
+ *   x         [M][K] of `type`;  weight [V][K] of `type`;  bias float [V], nullable; -inf in it rules an alternative out
+ *   tokens    int32 [M]; a negative one marks a row that does not count: its x may hold anything and its outputs are 0
+ *   logprobs, entropy, logz   out, float [M], nullable; as in fb_token_logprobs, rows of nothing but -inf (logits below -1e38 among
+ *             them), of NaN or +inf and tokens of V or more too
+ * FB_EINVAL: x, weight or tokens NULL, sizes or row distances out of range, an unknown type, the workspace missing or too small.
+ * FB_EUNSUPPORTED: rows of x or weight longer than 4 MB.
+ */
+int fb_affine_logprobs(const void *x, int64_t ldx, const void *weight, int64_t ldw, const float *bias, const int32_t *tokens, int64_t M, int64_t V,
+                       int64_t K, int type, float *logprobs, float *entropy, float *logz, void *ws, size_t ws_bytes, fb_stream stream);
+
+/* Bytes of workspace fb_affine_logprobs_grad needs for these arguments (0: bad arguments).  The logits' gradient is formed for a piece of
+ * the vocabulary at a time, of up to 512 MB of `type` (at least 256 alternatives). */
+size_t fb_affine_logprobs_grad_workspace_bytes(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t V, int64_t K, int type);
+
+/*
+ * Its gradient:  dz as in fb_token_logprobs_grad, from the logits formed once more,  dx = dz W,  dweight = dz^T x,  dbias = sum over
+ * rows of dz
+ *   logz, entropy          as fb_affine_logprobs returned them (entropy may be NULL if g_entropy is)
+ *   g_logprobs, g_entropy  float [M], either nullable
+ *   dx      out, [M][K] of `type`, nullable;  dweight out, [V][K] of `type`, contiguous, nullable;  dbias out, float [V], nullable
+ * Rows that do not count and rows whose logz is -inf have dx = 0 and no part in the sums.  Where `type` has 16 bits dz is rounded to it
+ * before the two products, to FB_TYPE_F16 times a power of two for the largest |g_logprobs| + |g_entropy| (0.37 + entropy), which no |dz|
+ * exceeds (as in fb_affine_grad); dbias is summed before that.
+ * Errors as fb_affine_logprobs; FB_EUNSUPPORTED too: rows of dx 2^27 elements apart or more.
+ */
+int fb_affine_logprobs_grad(const void *x, int64_t ldx, const void *weight, int64_t ldw, const float *bias, const int32_t *tokens, const float *logz,
+                            const float *entropy, const float *g_logprobs, const float *g_entropy, int64_t M, int64_t V, int64_t K, int type,
+                            void *dx, int64_t lddx, void *dweight, float *dbias, void *ws, size_t ws_bytes, fb_stream stream);
 
 #ifdef __cplusplus
 }

@@ -28,6 +28,17 @@ struct Finish {
     const float *undo;   // nullable
 };
 
+// Log probabilities whose logits are the product's sums (see fb_vocabulary.hip).
+struct Scores {
+    const int32_t *tokens;   // [M]
+    int first;               // the number of the product's first column as a token
+    float *given;            // [M]: the tokens' logits
+    float *stats;            // [tiles across][3][M]
+    const void *rows;        // [M] fours of what the gradient takes of a row
+    bool entropy;            // the gradient has the entropy's part
+    float *sums;             // [waves down][N]: shares of the sums of the gradient's columns, nullable
+};
+
 struct Product {
     Factor A, B;
     int64_t M, N, K;     // i < M, j < N, k < K
@@ -39,6 +50,7 @@ struct Product {
     int64_t share;       // length of a share
     int tile;            // 256, 128 or 64, the side of the tiles
     bool past;           // y goes past the caches (never parts: they are joined at once)
+    Scores s;
 };
 
 int launch_mfma_product(const Product &q, hipStream_t stream);   // factors as ready() wants them
@@ -103,7 +115,7 @@ int launch_prepare(Prepare &j, int type, int dy_type, hipStream_t stream);
 
 inline size_t aligned(size_t n) { return (n + 255) & ~(size_t)255; }
 
-void plan(Product &q, int only_tile = 0);           // tiles and shares of k
+void plan(Product &q, int only_tile = 0, bool whole = false);   // tiles and shares of k (`whole`: one share)
 inline size_t product_bytes(const Product &q) { return q.parts ? aligned((size_t)q.split * (size_t)q.M * (size_t)q.N * sizeof(float)) : 0; }
 int launch_join(const Product *a, const Product *b, int type, const float *sums, int64_t rows, int64_t N, float *out, hipStream_t stream);
 

@@ -238,7 +238,7 @@ int64_t sum_rows(int64_t M, int64_t N, int type)
 // it holds at a time (1, 2 or 4) a start, an end and the latency of every step, and, where k is shared, the sums' way through
 // memory and a launch to join them.  In single precision a share is at most 4096 long, so that roundings do not pile up, as long as
 // 128 shares are enough for that (k up to 524288); with k above 4096 the sums always go through memory then, split M N floats of it.
-void plan(Product &q, int only_tile)
+void plan(Product &q, int only_tile, bool whole)
 {
     static constexpr int kSplits[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64, 96, 128};
     struct Shape {                          // (see fb_affine_mfma.hip)
@@ -255,8 +255,8 @@ void plan(Product &q, int only_tile)
         const int64_t tiles = ((q.M + sh.tile - 1) / sh.tile) * ((q.N + sh.tile - 1) / sh.tile);
         for (const int64_t split : kSplits) {
             const int64_t share = std::max<int64_t>(deep, ((q.K + split - 1) / split + deep - 1) / deep * deep);
-            if (split > 1 && (split - 1) * share >= q.K) break;
-            if (wide && share > 4096 && split < 128) continue;
+            if (split > 1 && (whole || (split - 1) * share >= q.K)) break;
+            if (wide && share > 4096 && split < 128 && !whole) continue;
             const int64_t busiest = (tiles * split + kCUs - 1) / kCUs, rounds = (busiest + sh.resident - 1) / sh.resident;
             double cost = (double)rounds * (kEnds + (double)(share / deep) * kStep) + (double)busiest * (double)share * (wide ? sh.per_k32 : sh.per_k16);
             if (split > 1) cost += kJoin + (double)(split + 1) * (double)q.M * (double)q.N * 4.0 / kBytesPerClock;
@@ -269,7 +269,7 @@ void plan(Product &q, int only_tile)
         }
     }
     q.split = std::max(q.split, 1);         // (K = 0, a gradient over no rows: sums of nothing)
-    q.parts = q.split > 1 || q.N < 4;       // (the kernel takes a residual by fours)
+    q.parts = !whole && (q.split > 1 || q.N < 4);       // (the kernel takes a residual by fours)
 }
 
 // Products whose shares are to be joined (at most two) and columns to be added up (out), in one launch.

@@ -45,7 +45,7 @@ template <class T>
 int launch(const Product &q, hipStream_t stream)
 {
     if (!q.A.along) return launch<T, false, false, kPlain>(q, stream);
-    if (!q.B.along) return launch<T, true, false, kPlain>(q, stream);
+    if (!q.B.along) return q.f.residual && !q.parts ? launch<T, true, false, FB_ACT_NONE>(q, stream) : launch<T, true, false, kPlain>(q, stream);
     if (q.parts || (q.f.act <= FB_ACT_RELU && !q.f.residual && !q.f.preact)) return launch<T, true, true, kPlain>(q, stream);
     switch (q.f.act) {
     case FB_ACT_NONE: return launch<T, true, true, FB_ACT_NONE>(q, stream);

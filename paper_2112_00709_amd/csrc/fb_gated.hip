@@ -14,16 +14,17 @@ struct Gated {
     static constexpr bool kPaired = true;
     static constexpr int kEarly = 2;
 
-    template <int FJ>
-    static __device__ __forceinline__ void early(const Product &q, int64_t j0, int wj, int lane, f32x4 (&four)[2])
+    template <int FI, int FJ>
+    static __device__ __forceinline__ void early(const Product &q, const Where &where, int lane, f32x4 (&four)[2])
     {
-        const int64_t j = j0 + wj * 32 + lane % 8 * 4;
+        if (!q.f.bias) return;
+        const int64_t j = where.j0 + where.wj * 32 + lane % 8 * 4;
         bias_of(q.f.bias, q.N, j, four[0]);
         bias_of(q.f.bias + q.N, q.N, j, four[1]);
     }
 
     template <class T, int FI, int FJ>
-    static __device__ __forceinline__ void leave(ProductArgs args, const f32x16 (&acc)[FI][FJ], const f32x4 (&bias)[2], float, const Where &where)
+    static __device__ __forceinline__ void leave(ProductArgs args, f32x16 (&acc)[FI][FJ], const f32x4 (&bias)[2], float, const Where &where)
     {
         static_assert(FJ == 2, "a fragment of either factor");
         int lane = threadIdx.x & 63;
@@ -36,21 +37,7 @@ struct Gated {
         const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)mine + (lane & 15) * FJ * 128;
 #pragma unroll 1
         for (int pass = 0; pass < 2 * FI; ++pass) {
-            if ((lane >> 4 & 1) == (pass & 1)) {
-                auto put = [&](const f32x16 (&sums)[FJ]) {
-#pragma unroll
-                    for (int y = 0; y < FJ; ++y)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const f32x4 w = {sums[y][4 * e], sums[y][4 * e + 1], sums[y][4 * e + 2], sums[y][4 * e + 3]};
-                            *(__attribute__((address_space(3))) f32x4 *)(uintptr_t)(to + ((y * 8 + 2 * e + (lane >> 5)) ^ (lane & 15)) * 16) = w;
-                        }
-                };
-                if (pass < 2) put(acc[0]);
-                else if (FI <= 2 || pass < 4) put(acc[1 % FI]);
-                else if (pass < 6) put(acc[2 % FI]);
-                else put(acc[3 % FI]);
-            }
+            put_rows<FI, FJ>(acc, pass, lane, to);
             f32x4 g[kR], u[kR];
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll

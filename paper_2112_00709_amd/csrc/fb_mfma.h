@@ -276,6 +276,28 @@ struct Where {
     float *room;
 };
 
+// Sixteen rows of a wave's sums, pass by pass, into its LDS (`to`: the lane's row there): see Finished.
+template <int FI, int FJ>
+__device__ __forceinline__ void put_rows(const f32x16 (&acc)[FI][FJ], int pass, int lane, uint32_t to)
+{
+    constexpr int kPer = FJ * 8;
+    if ((lane >> 4 & 1) != (pass & 1)) return;
+    auto put = [&](const f32x16 (&sums)[FJ]) {
+#pragma unroll
+        for (int y = 0; y < FJ; ++y)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const f32x4 w = {sums[y][4 * e], sums[y][4 * e + 1], sums[y][4 * e + 2], sums[y][4 * e + 3]};
+                const int c = (y * 8 + 2 * e + (lane >> 5)) ^ (lane & 15 & (kPer - 1));
+                *(__attribute__((address_space(3))) f32x4 *)(uintptr_t)(to + c * 16) = w;
+            }
+    };
+    if (pass < 2) put(acc[0]);
+    else if (FI <= 2 || pass < 4) put(acc[1 % FI]);
+    else if (pass < 6) put(acc[2 % FI]);
+    else put(acc[3 % FI]);
+}
+
 __device__ __forceinline__ void bias_of(const float *bias, int64_t n, int64_t j, f32x4 &four)
 {
 #pragma unroll
@@ -286,16 +308,16 @@ __device__ __forceinline__ void bias_of(const float *bias, int64_t n, int64_t j,
 template <int KIND>
 struct Finished {
     static constexpr bool kPaired = false;
-    static constexpr int kEarly = 1;       // pieces of four columns' bias that a lane asks for when a tile begins
+    static constexpr int kEarly = 1;       // fours of numbers that a lane asks for when a tile begins: its columns' bias
 
-    template <int FJ>
-    static __device__ __forceinline__ void early(const Product &q, int64_t j0, int wj, int lane, f32x4 (&four)[1])
+    template <int FI, int FJ>
+    static __device__ __forceinline__ void early(const Product &q, const Where &where, int lane, f32x4 (&four)[1])
     {
-        bias_of(q.f.bias, q.N, j0 + wj * FJ * 32 + lane % (FJ * 8) * 4, four[0]);
+        if (!q.parts && q.f.bias) bias_of(q.f.bias, q.N, where.j0 + where.wj * FJ * 32 + lane % (FJ * 8) * 4, four[0]);
     }
 
     template <class T, int FI, int FJ>
-    static __device__ __forceinline__ void leave(ProductArgs args, const f32x16 (&acc)[FI][FJ], const f32x4 (&four)[1], float undo, const Where &where)
+    static __device__ __forceinline__ void leave(ProductArgs args, f32x16 (&acc)[FI][FJ], const f32x4 (&four)[1], float undo, const Where &where)
     {
         const f32x4 bias = four[0];
         const int share = where.share;
@@ -494,8 +516,9 @@ __device__ __forceinline__ void run_tiles(const Task &task, ProductArgs args, in
         const Place p = place(in_run);
         const int steps = (int)((p.length + kDeep - 1) / kDeep);
         f32x16 acc[FI][FJ] = {};
-        f32x4 bias[WAY::kEarly] = {};
-        if (!q.parts && q.f.bias) WAY::template early<FJ>(q, p.j0, wj, lane, bias);
+        const Where where{p.share, p.i0, p.j0, wi, wj, wave, (float *)(lds_raw + 2 * (a.kBytes + b.kBytes))};
+        f32x4 four[WAY::kEarly] = {};
+        WAY::template early<FI, FJ>(q, where, lane, four);
         // One matrix instruction at a time, and behind it a read for the next 32 bytes of k, and after the meeting also a copy: in this
         // order, which the compiler left to itself does not keep (it puts the reads right before their use).
         auto times = [&](int m, int set) {
@@ -521,7 +544,7 @@ __device__ __forceinline__ void run_tiles(const Task &task, ProductArgs args, in
             __builtin_amdgcn_sched_barrier(0);
             meet();
 #pragma unroll
-            for (int e = 0; e < WAY::kEarly; ++e) asm volatile("" : "+v"(bias[e]));   // (it has come with the rest: no wait for it later, behind further copies)
+            for (int e = 0; e < WAY::kEarly; ++e) asm volatile("" : "+v"(four[e]));   // (it has come with the rest: no wait for it later, behind further copies)
             aim(turn);
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (kSlots == 1) {
@@ -542,7 +565,7 @@ __device__ __forceinline__ void run_tiles(const Task &task, ProductArgs args, in
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-        WAY::template leave<T, FI, FJ>(args, acc, bias, undo, Where{p.share, p.i0, p.j0, wi, wj, wave, (float *)(lds_raw + 2 * (a.kBytes + b.kBytes))});
+        WAY::template leave<T, FI, FJ>(args, acc, four, undo, where);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (no copy into LDS outlives the workgroup)
 }

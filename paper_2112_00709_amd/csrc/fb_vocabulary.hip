@@ -1,0 +1,722 @@
+// Log probabilities and entropy straight from hidden frames, and their gradient (fb_layers.h): fb_token_logprobs of x W^T + bias,
+// without the logits in memory.
+//
+// Forward, the product's sums never leave the registers as such: a tile leaves for each of its rows the maximum m, S = sum e^(z - m) and
+// T = sum e^(z - m) (z - m), and a second launch joins the tiles of a row.  Backward, logits are formed once more, piece by piece of
+// the vocabulary, and leave as their gradient in the factors' type; two products take that into dx and dweight.
+#include "fb_mfma.h"
+
+namespace fb {
+
+namespace {
+
+constexpr float kInf = __builtin_huge_valf(), kLn2 = 0.69314718055994530942f;
+constexpr float kOut = -1e38f;        // logits below are ruled out, as -inf is
+constexpr float kFarOut = -1e4f;      // e^this is 0, and this times a finite number is finite
+
+// S and T of one number more, or of another part: exponents are to base 2, m is as the logits are.
+struct Part {
+    float m, S, T;
+};
+
+__device__ __forceinline__ Part join(const Part &a, const Part &b)
+{
+    const float m = fmaxf(a.m, b.m);
+    // (nothing: S = 0.  NaN in S or T stays: S is not 0 then)
+    const float da = a.S == 0.0f ? 0.0f : (a.m - m) * kLog2E, db = b.S == 0.0f ? 0.0f : (b.m - m) * kLog2E;
+    const float ea = __builtin_amdgcn_exp2f(da), eb = __builtin_amdgcn_exp2f(db);
+    // (a part far below the other: 0 times a finite number)
+    return Part{m, a.S * ea + b.S * eb, fmaf(a.S, fmaxf(da, kFarOut), a.T) * ea + fmaf(b.S, fmaxf(db, kFarOut), b.T) * eb};
+}
+
+__device__ __forceinline__ float other_half_max(float v)
+{
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float other_half_sum(float v)
+{
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// The bias of a lane's four columns, -inf past the last.
+__device__ __forceinline__ void bias_or_out(const Product &q, int64_t j, f32x4 &four)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) four[e] = j + e < q.N ? (q.f.bias ? q.f.bias[j + e] : 0.0f) : -kInf;
+}
+
+// A lane has of each of its fragments' rows lane % 32 of C, columns 8 e + 4 (lane / 32) + 0 .. 3 of every 32.  Adds the bias, which
+// the wave's lanes have four by four, to all of them.
+template <int FI, int FJ>
+__device__ __forceinline__ void add_bias(f32x16 (&acc)[FI][FJ], const f32x4 &four, float *mine, int lane)
+{
+    if (lane < FJ * 8) *(f32x4 *)(mine + lane * 4) = four;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int y = 0; y < FJ; ++y)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const f32x4 b = *(const f32x4 *)(mine + (y * 8 + 2 * e + (lane >> 5)) * 4);
+#pragma unroll
+            for (int x = 0; x < FI; ++x)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[x][y][4 * e + r] += b[r];
+        }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
+// f(y, the element's place in acc[x][y]) where a row's token is among the wave's columns, in the lane that has it.  Rare: asked
+// for once a fragment.
+template <int FJ, class F>
+__device__ __forceinline__ void at_token(int token, int64_t j0, int lane, F f)
+{
+    const int64_t far = (int64_t)token - j0;
+    const int c = far >= 0 && far < FJ * 32 ? (int)far : -1;
+    if (__builtin_amdgcn_ballot_w64(c >= 0) == 0) return;
+    if (c >= 0 && (c >> 2 & 1) == lane >> 5) {
+#pragma unroll
+        for (int y = 0; y < FJ; ++y)
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+                if (c == y * 32 + (k >> 2) * 8 + (c & 4) + (k & 3)) f(y, k);
+    }
+}
+
+// Sums leave as each row's (m, S, T) over the tile's columns, and as the logits of given tokens.
+struct Reduced {
+    static constexpr bool kPaired = false;
+    static constexpr int kEarly = 2;         // bias; tokens of the lane's rows
+
+    template <int FI, int FJ>
+    static __device__ __forceinline__ void early(const Product &q, const Where &where, int lane, f32x4 (&four)[2])
+    {
+        bias_or_out(q, where.j0 + where.wj * FJ * 32 + lane % (FJ * 8) * 4, four[0]);
+        const int64_t i = where.i0 + where.wi * FI * 32 + (lane & 31);
+#pragma unroll
+        for (int x = 0; x < FI; ++x) four[1][x] = __int_as_float(i + x * 32 < q.M ? max(q.s.tokens[i + x * 32], -1) - q.s.first : -1);
+    }
+
+    template <class T, int FI, int FJ>
+    static __device__ __forceinline__ void leave(ProductArgs args, f32x16 (&acc)[FI][FJ], const f32x4 (&four)[2], float, const Where &where)
+    {
+        int lane = threadIdx.x & 63;
+        asm volatile("" : "+s"(args), "+v"(lane));
+        const int waves = blockDim.x / 64, across = FI == 4 ? 4 : 2, rows = waves / across * FI * 32;     // of the tile
+        float *mine = where.room + where.wave * FJ * 32, *parts = where.room + waves * FJ * 32;
+        const int64_t j0 = where.j0 + where.wj * FJ * 32;
+        add_bias<FI, FJ>(acc, four[0], mine, lane);
+#pragma unroll
+        for (int x = 0; x < FI; ++x) {
+            const int row = (where.wi * FI + x) * 32 + (lane & 31);
+            at_token<FJ>(__float_as_int(four[1][x]), j0, lane, [&](int y, int k) { args->s.given[where.i0 + row] = acc[x][y][k]; });
+            float m = acc[x][0][0];
+#pragma unroll
+            for (int y = 0; y < FJ; ++y)
+#pragma unroll
+                for (int k = 0; k < 16; ++k) m = fmaxf(m, acc[x][y][k]);
+            m = other_half_max(m);
+            const float from = m < kOut ? 0.0f : m;      // (their difference first: a product with m has its rounding)
+            float S = 0.0f, U = 0.0f;
+#pragma unroll
+            for (int y = 0; y < FJ; ++y)
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    const float d = (acc[x][y][k] - from) * kLog2E, e = __builtin_amdgcn_exp2f(d);
+                    S += e;
+                    U = fmaf(e, fmaxf(d, kFarOut), U);
+                }
+            S = other_half_sum(S);
+            U = other_half_sum(U);
+            if (lane < 32) {
+                float *p = parts + where.wj * 3 * rows + row;
+                p[0] = m;
+                p[rows] = S;
+                p[2 * rows] = U;
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // (the next tile's parts come behind further barriers)
+        const int64_t i = where.i0 + threadIdx.x;
+        if ((int)threadIdx.x < rows && i < args->M) {
+            Part p{-kInf, 0.0f, 0.0f};
+            for (int w = 0; w < across; ++w) {
+                const float *o = parts + w * 3 * rows + threadIdx.x;
+                p = join(p, Part{o[0], o[rows], o[2 * rows]});
+            }
+            float *out = args->s.stats + (size_t)(where.j0 / (across * FJ * 32)) * 3 * (size_t)args->M + i;
+            out[0] = p.m;
+            out[args->M] = p.S;
+            out[2 * args->M] = p.T;
+        }
+    }
+};
+
+// Sums leave as the logits' gradient, rounded to the factors' type, and as shares of its column sums before that.  Of a row there
+// are (log Z, a, h, g):  dz = g [j = token] - p (a + h log p),  a = g + h entropy.  Rows that do not count have log Z = inf and zeros.
+struct Slopes {
+    static constexpr bool kPaired = false;
+    static constexpr int kEarly = 2;
+
+    template <int FI, int FJ>
+    static __device__ __forceinline__ void early(const Product &q, const Where &where, int lane, f32x4 (&four)[2])
+    {
+        Reduced::early<FI, FJ>(q, where, lane, four);
+    }
+
+    template <class T, int FI, int FJ>
+    static __device__ __forceinline__ void leave(ProductArgs args, f32x16 (&acc)[FI][FJ], const f32x4 (&four)[2], float, const Where &where)
+    {
+        int lane = threadIdx.x & 63;
+        asm volatile("" : "+s"(args), "+v"(lane));
+        constexpr int kPer = FJ * 8, kRows = 64 / kPer, kR = 16 / kRows;
+        const int64_t M = args->M, N = args->f.ldy, i0 = where.i0 + where.wi * FI * 32, j0 = where.j0 + where.wj * FJ * 32, j = j0 + lane % kPer * 4;
+        float *mine = where.room + where.wave * 16 * FJ * 32;
+        f32x4 of_row[FI];
+#pragma unroll
+        for (int x = 0; x < FI; ++x) {
+            const int64_t i = i0 + x * 32 + (lane & 31);
+            of_row[x] = ((const f32x4 *)args->s.rows)[i < M ? i : M - 1];
+        }
+        add_bias<FI, FJ>(acc, four[0], mine, lane);
+#pragma unroll
+        for (int x = 0; x < FI; ++x) {
+            const float logz = of_row[x][0], a = of_row[x][1], h = of_row[x][2], g = of_row[x][3];
+            if (args->s.entropy) {
+#pragma unroll
+                for (int y = 0; y < FJ; ++y)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        const float d = fmaxf(acc[x][y][k] - logz, kFarOut);
+                        acc[x][y][k] = -__builtin_amdgcn_exp2f(d * kLog2E) * fmaf(h, d, a);
+                    }
+            } else {
+#pragma unroll
+                for (int y = 0; y < FJ; ++y)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) acc[x][y][k] = -__builtin_amdgcn_exp2f(fmaxf(acc[x][y][k] - logz, kFarOut) * kLog2E) * a;
+            }
+            at_token<FJ>(__float_as_int(four[1][x]), j0, lane, [&](int y, int k) { acc[x][y][k] += g; });
+        }
+        const int nj = (int)(N - j < 4 ? (N - j < 0 ? 0 : N - j) : 4), in_row = lane / kPer;
+        const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)mine + (lane & 15) * FJ * 128;
+        f32x4 sum = {};
+#pragma unroll
+        for (int pass = 0; pass < 2 * FI; ++pass) {
+            put_rows<FI, FJ>(acc, pass, lane, to);
+            f32x4 w[kR];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+            for (int r = 0; r < kR; ++r) {
+                const int row = r * kRows + in_row;
+                w[r] = *(const f32x4 *)(mine + row * FJ * 32 + ((lane % kPer) ^ (row & (kPer - 1))) * 4);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            const int64_t i = i0 + pass * 16;
+            const Spot at{i, j0, in_row, lane % kPer * 4, (int)(M - i < 16 ? M - i : 16), nj};
+#pragma unroll
+            for (int r = 0; r < kR; ++r)
+                if (r * kRows + in_row < at.rows) sum += w[r];
+            if (at.rows > in_row && nj > 0) store_rows<T, T, kR, kRows>((T *)args->f.y, args->f.ldy, at, w, false);
+        }
+        if (args->s.sums) {
+            const float undo = args->f.undo ? *args->f.undo : 1.0f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float v = sum[e];
+#pragma unroll
+                for (int step = kPer; step < 64; step *= 2) v += __shfl_xor(v, step);
+                sum[e] = v * undo;
+            }
+            if (lane < kPer) {
+                float *out = args->s.sums + (size_t)(i0 / (FI * 32)) * (size_t)args->N + j;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (j + e < args->N) out[e] = sum[e];
+            }
+        }
+    }
+};
+
+template <class T, class WAY>
+int launch_scores(const Product &q, hipStream_t stream)
+{
+    if (q.tile == 256) return launch<T, true, true, 2, 4, 4, 2, WAY>(q, stream);
+    return q.tile == 128 ? launch<T, true, true, 2, 2, 2, 2, WAY>(q, stream) : launch<T, true, true, 2, 2, 1, 1, WAY>(q, stream);
+}
+
+template <class WAY>
+int launch_scores(const Product &q, hipStream_t stream)
+{
+    if (q.type == FB_TYPE_F32) return launch_scores<float, WAY>(q, stream);
+    return q.type == FB_TYPE_BF16 ? launch_scores<bf16, WAY>(q, stream) : launch_scores<f16, WAY>(q, stream);
+}
+
+typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef f16 f16x8 __attribute__((ext_vector_type(8)));
+
+// Few rows of x: bound by reading the weight once, as fb_few_rows_kernel.  A workgroup takes 16 rows of the weight after the other, its
+// waves share k and add their sums in their order; a lane keeps (m, S, T) of its row over the columns it has seen.
+template <class T>
+__device__ __forceinline__ f32x4 multiply_few(const u32x4 &a, const u32x4 &b, f32x4 c)
+{
+    if constexpr (std::is_same<T, bf16>::value) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    } else if constexpr (std::is_same<T, f16>::value) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[e]), __uint_as_float(b[e]), c, 0, 0, 0);
+        return c;
+    }
+}
+
+template <class T, int WAVES, int TILES>
+__global__ __launch_bounds__(WAVES * 64) void fb_few_scores_kernel(Product q)
+{
+    constexpr int VE = Vec<T>::kN, kStep = 4 * VE, kAhead = TILES == 1 ? 8 : TILES == 2 ? 4 : 2;
+    __shared__ f32x4 slots[2][WAVES][TILES][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int row = lane & 15, piece = lane >> 4;
+    // (rows past the end are those of the last one: read, multiplied and not counted)
+    const T *x[TILES];
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) x[t] = (const T *)q.A.p + (t * 16 + row < q.M ? t * 16 + row : q.M - 1) * q.A.ld + piece * VE;
+    const int64_t whole = q.K / kStep * kStep, tiles = (q.N + 15) / 16, i = wave * 16 + row;
+    const int token = wave < TILES && i < q.M ? q.s.tokens[i] : -1;
+    Part part{-kInf, 0.0f, 0.0f};
+    int turn = 0;
+    for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x, turn ^= 1) {
+        const int64_t n0 = tile * 16;
+        const T *w = (const T *)q.B.p + (n0 + row < q.N ? n0 + row : q.N - 1) * q.B.ld + piece * VE;
+        f32x4 acc[TILES] = {};
+        int64_t k = (int64_t)wave * kStep;
+        for (; k + (int64_t)(kAhead - 1) * WAVES * kStep < whole; k += (int64_t)kAhead * WAVES * kStep) {
+            u32x4 a[kAhead], b[kAhead][TILES];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                a[u] = *(const u32x4_any *)(w + k + u * WAVES * kStep);
+#pragma unroll
+                for (int t = 0; t < TILES; ++t) b[u][t] = *(const u32x4_any *)(x[t] + k + u * WAVES * kStep);
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+                for (int t = 0; t < TILES; ++t) acc[t] = multiply_few<T>(a[u], b[u][t], acc[t]);
+        }
+        for (; k < q.K; k += WAVES * kStep) {
+            const int n = (int)(q.K - k - piece * VE < VE ? q.K - k - piece * VE : VE);
+            const u32x4 a = load_piece(w + k, n);
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) acc[t] = multiply_few<T>(a, load_piece(x[t] + k, n), acc[t]);
+        }
+        f32x4 bias;
+        bias_or_out(q, n0 + 4 * piece, bias);
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) slots[turn][wave][t][lane] = acc[t];
+        __syncthreads();
+        if (wave < TILES) {                    // row `row` of the wave's 16, columns n0 + 4 piece + 0 .. 3
+            f32x4 z = slots[turn][0][wave][lane];
+#pragma unroll
+            for (int v = 1; v < WAVES; ++v) z += slots[turn][v][wave][lane];
+            z += bias;
+            Part here;
+            here.m = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3]));
+            const float from = here.m < kOut ? 0.0f : here.m;
+            here.S = here.T = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float d = (z[e] - from) * kLog2E, p = __builtin_amdgcn_exp2f(d);
+                here.S += p;
+                here.T = fmaf(p, fmaxf(d, kFarOut), here.T);
+                if (token >= 0 && n0 + 4 * piece + e == token && token < q.N) q.s.given[i] = z[e];
+            }
+            part = join(part, here);
+        }
+    }
+    if (wave >= TILES) return;
+#pragma unroll
+    for (int step = 16; step < 64; step *= 2) {
+        const Part o{__shfl_xor(part.m, step), __shfl_xor(part.S, step), __shfl_xor(part.T, step)};
+        part = lane & step ? join(o, part) : join(part, o);      // (one order in both)
+    }
+    if (lane < 16 && i < q.M) {
+        float *out = q.s.stats + (size_t)blockIdx.x * 3 * (size_t)q.M + i;
+        out[0] = part.m;
+        out[q.M] = part.S;
+        out[2 * q.M] = part.T;
+    }
+}
+
+int few_groups(int64_t V) { return (int)std::min<int64_t>((V + 15) / 16, 8 * kCUs); }
+
+template <class T, int WAVES>
+int launch_few_scores(const Product &q, hipStream_t stream)
+{
+    const dim3 grid((unsigned)few_groups(q.N)), block(WAVES * 64);
+    if (q.M <= 16)
+        hipLaunchKernelGGL((fb_few_scores_kernel<T, WAVES, 1>), grid, block, 0, stream, q);
+    else if (q.M <= 32)
+        hipLaunchKernelGGL((fb_few_scores_kernel<T, WAVES, 2>), grid, block, 0, stream, q);
+    else
+        hipLaunchKernelGGL((fb_few_scores_kernel<T, WAVES, 4>), grid, block, 0, stream, q);
+    return launched("few-row scores kernel launch: ");
+}
+
+template <class T>
+int launch_few_scores(const Product &q, hipStream_t stream)
+{
+    return q.K * (int64_t)sizeof(T) <= 2048 ? launch_few_scores<T, 4>(q, stream) : launch_few_scores<T, 8>(q, stream);
+}
+
+struct EndParams {
+    const float *stats;      // [parts][3][M]
+    int64_t parts, M, V;
+    const float *given;
+    const int32_t *tokens;
+    float *logprobs, *entropy, *logz;
+};
+
+// The parts of a row joined in a fixed order: 16 rows a workgroup, 64 threads a row with every 64th part each.
+__global__ __launch_bounds__(1024) void fb_scores_end_kernel(EndParams p)
+{
+    __shared__ Part slots[64][17];
+    const int col = threadIdx.x & 15, g = threadIdx.x >> 4;
+    const int64_t i = (int64_t)blockIdx.x * 16 + col;
+    Part part{-kInf, 0.0f, 0.0f};
+    if (i < p.M) {
+        for (int64_t k = g; k < p.parts; k += 64) {
+            const float *s = p.stats + (size_t)k * 3 * (size_t)p.M + i;
+            part = join(part, Part{s[0], s[p.M], s[2 * p.M]});
+        }
+    }
+    slots[g][col] = part;
+    __syncthreads();
+    for (int n = 32; n > 0; n /= 2) {
+        if (g < n) slots[g][col] = join(slots[g][col], slots[g + n][col]);
+        __syncthreads();
+    }
+    if (g > 0 || i >= p.M) return;
+    part = slots[0][col];
+    const int token = p.tokens[i];
+    float logz = 0.0f, entropy = 0.0f, logprob = 0.0f;
+    if (token >= 0) {
+        const float log_s = logf(part.S);
+        logz = part.S == 0.0f ? -kInf : part.m + log_s;
+        entropy = part.S == 0.0f ? 0.0f : log_s - part.T * kLn2 / part.S;
+        logprob = token >= p.V ? __builtin_nanf("") : part.S == 0.0f ? -kInf : p.given[i] - logz;
+    }
+    if (p.logz) p.logz[i] = logz;
+    if (p.entropy) p.entropy[i] = entropy;
+    if (p.logprobs) p.logprobs[i] = logprob;
+}
+
+// What the gradient takes of a row, times the power of two that half precision asks for.
+struct RowParams {
+    const int32_t *tokens;
+    const float *logz, *entropy, *g, *h;
+    int64_t M;
+    f32x4 *rows;
+    uint32_t *peaks;         // half precision: of the largest finite bound of |dz|, nullable
+    int n_peaks;
+    float *undo;
+    int32_t *counts;         // negative: nothing of the row counts
+};
+
+__device__ __forceinline__ f32x4 row_of(const RowParams &p, int64_t i)
+{
+    const float logz = p.logz[i];
+    if (p.tokens[i] < 0 || logz == -kInf) return f32x4{kInf, 0.0f, 0.0f, 0.0f};
+    const float g = p.g ? p.g[i] : 0.0f, h = p.h ? p.h[i] : 0.0f;
+    return f32x4{logz, logz != logz ? logz : p.h ? fmaf(h, p.entropy[i], g) : g, h, g};
+}
+
+__global__ __launch_bounds__(256) void fb_scores_peak_kernel(RowParams p)
+{
+    __shared__ uint32_t slots[4];
+    uint32_t peak = 0;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.M; i += (int64_t)gridDim.x * 256) {
+        const f32x4 r = row_of(p, i);
+        if (r[0] == kInf) continue;
+        const uint32_t a = __float_as_uint(fabsf(r[3]) + (p.h ? fabsf(r[2]) * (0.37f + fabsf(p.entropy[i])) : 0.0f)) & 0x7fffffffu;
+        peak = a < 0x7f800000u && a > peak ? a : peak;
+    }
+    peak = max_wave_u(peak);
+    if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = peak;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < 4; ++w) peak = slots[w] > peak ? slots[w] : peak;
+        p.peaks[blockIdx.x] = peak;
+    }
+}
+
+__global__ __launch_bounds__(256) void fb_scores_rows_kernel(RowParams p)
+{
+    float scale = 1.0f;
+    if (p.peaks) {
+        float undo;
+        range_of(p.peaks, p.n_peaks, scale, undo);
+        if (blockIdx.x == 0 && threadIdx.x == 0) *p.undo = undo;
+    }
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= p.M) return;
+    f32x4 r = row_of(p, i);
+#pragma unroll
+    for (int e = 1; e < 4; ++e) r[e] *= scale;
+    p.rows[i] = r;
+    p.counts[i] = r[0] == kInf ? -1 : 0;
+}
+
+// The sum over pieces of the vocabulary, rounded to dx.
+struct RoundParams {
+    const float *sums;       // [M][K]
+    int64_t M, K, ld;
+    void *out;
+};
+
+template <class T>
+__global__ __launch_bounds__(256) void fb_scores_round_kernel(RoundParams p)
+{
+    constexpr int VE = Vec<T>::kN;
+    const int64_t pieces = (p.K + VE - 1) / VE, n = p.M * pieces;
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < n; at += (int64_t)gridDim.x * 256) {
+        const int64_t r = at / pieces, c = (at - r * pieces) * VE;
+        const int here = (int)(p.K - c < VE ? p.K - c : VE);
+        float v[VE];
+#pragma unroll
+        for (int e = 0; e < VE; e += 4) unpack<float>(load_piece(p.sums + r * p.K + c + e, here - e), v + e);
+        store_piece((T *)p.out + r * p.ld + c, here, pack<T>(v));
+    }
+}
+
+int launch_round(const RoundParams &p, int type, hipStream_t stream)
+{
+    const int64_t ve = 16 / (int64_t)type_bytes(type);
+    const dim3 grid((unsigned)std::min<int64_t>((p.M * ((p.K + ve - 1) / ve) + 255) / 256, 8 * kCUs)), block(256);
+    if (type == FB_TYPE_F32)
+        hipLaunchKernelGGL(fb_scores_round_kernel<float>, grid, block, 0, stream, p);
+    else if (type == FB_TYPE_BF16)
+        hipLaunchKernelGGL(fb_scores_round_kernel<bf16>, grid, block, 0, stream, p);
+    else
+        hipLaunchKernelGGL(fb_scores_round_kernel<f16>, grid, block, 0, stream, p);
+    return launched("scores rounding kernel launch: ");
+}
+
+struct ScorePlan {
+    Product q;
+    bool few;
+    Packed x, w;
+    int64_t parts;
+    size_t given, stats, bytes;
+};
+
+ScorePlan score_plan(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t V, int64_t K, int type)
+{
+    ScorePlan f{};
+    f.q.M = M; f.q.N = V; f.q.K = K; f.q.type = type;
+    f.few = M <= kFewRows;
+    if (f.few) {
+        f.parts = few_groups(V);
+    } else {
+        plan(f.q, 0, true);
+        f.parts = (V + f.q.tile - 1) / f.q.tile;
+        f.x = packed(x, ldx, M, K, type);
+        f.w = packed(weight, ldw, V, K, type);
+    }
+    f.given = aligned((size_t)M * sizeof(float));
+    f.stats = aligned((size_t)f.parts * 3 * (size_t)M * sizeof(float));
+    f.bytes = f.x.bytes + f.w.bytes + f.given + f.stats + 256;
+    return f;
+}
+
+// Alternatives of a piece of the vocabulary: the logits' gradient of a piece takes up to 512 MB (one piece for 69120 rows of 3000 in 16
+// bits, two of 64000 for 4095 rows) in rows of less than 4 MB, and pieces are alike.
+constexpr int64_t kPieceBytes = (int64_t)512 << 20;
+
+struct ScoreGradPlan {
+    int64_t width, pieces, ldz;
+    Product z, dx, dw;       // of a whole piece
+    Packed x, w;             // x is always copied: rows that do not count are zeros then
+    int64_t sum_rows;
+    size_t dz, rows, counts, range, sums, acc, part_x, part_w, bytes;
+};
+
+ScoreGradPlan score_grad_plan(const void *weight, int64_t ldw, int64_t M, int64_t V, int64_t K, int type)
+{
+    ScoreGradPlan g{};
+    const int64_t size = (int64_t)type_bytes(type), longest = ((int64_t)1 << 22) / size - 256;
+    const int64_t most = std::max<int64_t>(256, std::min(longest, kPieceBytes / std::max<int64_t>(1, M * size) / 256 * 256));
+    g.pieces = (V + most - 1) / most;
+    g.width = g.pieces == 1 ? V : ((V + g.pieces - 1) / g.pieces + 255) / 256 * 256;
+    g.pieces = (V + g.width - 1) / g.width;
+    g.ldz = whole_pieces(g.width, type);
+    g.z.M = M; g.z.N = g.width; g.z.K = K; g.z.type = type;
+    g.dx.M = M; g.dx.N = K; g.dx.K = g.width; g.dx.type = type;
+    g.dw.M = g.width; g.dw.N = K; g.dw.K = M; g.dw.type = type;
+    plan(g.z, 0, true);
+    plan(g.dx);
+    plan(g.dw);
+    g.x.copy = true;
+    g.x.ld = whole_pieces(K, type);
+    g.x.bytes = aligned((size_t)M * (size_t)g.x.ld * type_bytes(type));
+    g.w = packed(weight, ldw, V, K, type);
+    const int64_t fragment = g.z.tile == 256 ? 128 : g.z.tile / 2;        // rows of a wave
+    g.sum_rows = (M + g.z.tile - 1) / g.z.tile * (g.z.tile / fragment);
+    g.dz = aligned((size_t)M * (size_t)g.ldz * type_bytes(type));
+    g.rows = aligned((size_t)M * sizeof(f32x4));
+    g.counts = aligned((size_t)M * sizeof(int32_t));
+    g.range = aligned((kPeakGroups + 1) * sizeof(float));
+    g.sums = aligned((size_t)g.sum_rows * (size_t)g.width * sizeof(float));
+    g.acc = g.pieces > 1 ? aligned((size_t)M * (size_t)K * sizeof(float)) : 0;
+    g.part_x = product_bytes(g.dx);
+    g.part_w = product_bytes(g.dw);
+    g.bytes = g.x.bytes + g.w.bytes + g.dz + g.rows + g.counts + g.range + g.sums + g.acc + g.part_x + g.part_w;
+    return g;
+}
+
+int check_scores(const char *who, const void *x, int64_t ldx, const void *weight, int64_t ldw, const int32_t *tokens, int64_t M, int64_t V, int64_t K, int type)
+{
+    const std::string w(who);
+    if (!known_type(type)) return fail(FB_EINVAL, w + ": unknown type");
+    if (bad_sizes(M, V, K)) return fail(FB_EINVAL, w + ": M must be 0 or more and below 2^31, V and K 1 or more and below 2^28");
+    if (((!x || !tokens) && M > 0) || !weight) return fail(FB_EINVAL, w + ": x, weight or tokens is NULL");
+    if (bad_ld(ldx, K) || bad_ld(ldw, K)) return fail(FB_EINVAL, w + ": rows of x or weight closer than K elements");
+    if (too_long(K, type)) return fail(FB_EUNSUPPORTED, w + ": rows of x and weight longer than 4 MB");
+    return FB_OK;
+}
+
+}  // namespace
+
+}  // namespace fb
+
+extern "C" {
+
+size_t fb_affine_logprobs_workspace_bytes(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t V, int64_t K, int type)
+{
+    using namespace fb;
+    if (bad_sizes(M, V, K) || !known_type(type)) return 0;
+    return score_plan(x, ldx, weight, ldw, M, V, K, type).bytes;
+}
+
+int fb_affine_logprobs(const void *x, int64_t ldx, const void *weight, int64_t ldw, const float *bias, const int32_t *tokens, int64_t M, int64_t V,
+                       int64_t K, int type, float *logprobs, float *entropy, float *logz, void *ws, size_t ws_bytes, fb_stream stream)
+{
+    using namespace fb;
+    return guarded([&]() -> int {
+        int rc = check_scores("fb_affine_logprobs", x, ldx, weight, ldw, tokens, M, V, K, type);
+        if (rc != FB_OK) return rc;
+        const ScorePlan f = score_plan(x, ldx, weight, ldw, M, V, K, type);
+        if (!ws || ws_bytes < f.bytes) return fail(FB_EINVAL, "fb_affine_logprobs: workspace missing or too small");
+        if (M == 0) return FB_OK;
+        hipStream_t st = (hipStream_t)stream;
+        char *xs = (char *)ws, *wts = xs + f.x.bytes, *given = wts + f.w.bytes, *stats = given + f.given;
+        Product q = f.q;
+        q.f.bias = bias;
+        q.s.tokens = tokens;
+        q.s.given = (float *)given;
+        q.s.stats = (float *)stats;
+        if (f.few) {
+            q.A = {x, ldx, true};
+            q.B = {weight, ldw, true};
+            rc = type == FB_TYPE_F32 ? launch_few_scores<float>(q, st) : type == FB_TYPE_BF16 ? launch_few_scores<bf16>(q, st) : launch_few_scores<f16>(q, st);
+        } else {
+            Prepare jobs;
+            if (f.x.copy) jobs.add(pack_job(f.x, x, ldx, M, K, xs), type);
+            if (f.w.copy) jobs.add(pack_job(f.w, weight, ldw, V, K, wts), type);
+            if ((rc = launch_prepare(jobs, type, type, st)) != FB_OK) return rc;
+            q.A = {f.x.copy ? xs : x, f.x.ld, true};
+            q.B = {f.w.copy ? wts : weight, f.w.ld, true};
+            rc = launch_scores<Reduced>(q, st);
+        }
+        if (rc != FB_OK) return rc;
+        const EndParams e{q.s.stats, f.parts, M, V, q.s.given, tokens, logprobs, entropy, logz};
+        hipLaunchKernelGGL(fb_scores_end_kernel, dim3((unsigned)((M + 15) / 16)), dim3(1024), 0, st, e);
+        return launched("scores end kernel launch: ");
+    });
+}
+
+size_t fb_affine_logprobs_grad_workspace_bytes(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t V, int64_t K, int type)
+{
+    using namespace fb;
+    (void)x;
+    (void)ldx;
+    if (bad_sizes(M, V, K) || !known_type(type)) return 0;
+    return score_grad_plan(weight, ldw, M, V, K, type).bytes;
+}
+
+int fb_affine_logprobs_grad(const void *x, int64_t ldx, const void *weight, int64_t ldw, const float *bias, const int32_t *tokens, const float *logz,
+                            const float *entropy, const float *g_logprobs, const float *g_entropy, int64_t M, int64_t V, int64_t K, int type,
+                            void *dx, int64_t lddx, void *dweight, float *dbias, void *ws, size_t ws_bytes, fb_stream stream)
+{
+    using namespace fb;
+    return guarded([&]() -> int {
+        int rc = check_scores("fb_affine_logprobs_grad", x, ldx, weight, ldw, tokens, M, V, K, type);
+        if (rc != FB_OK) return rc;
+        if (M > 0 && (!logz || (g_entropy && !entropy))) return fail(FB_EINVAL, "fb_affine_logprobs_grad: logz or entropy is NULL");
+        if (dx && bad_ld(lddx, K)) return fail(FB_EINVAL, "fb_affine_logprobs_grad: rows of dx closer than K elements");
+        if (dx && too_far(lddx)) return fail(FB_EUNSUPPORTED, "fb_affine_logprobs_grad: rows of dx 2^27 elements apart");
+        if (!dx && !dweight && !dbias) return FB_OK;
+        ScoreGradPlan g = score_grad_plan(weight, ldw, M, V, K, type);
+        if (!ws || ws_bytes < g.bytes) return fail(FB_EINVAL, "fb_affine_logprobs_grad: workspace missing or too small");
+        hipStream_t st = (hipStream_t)stream;
+        char *xs = (char *)ws, *wts = xs + g.x.bytes, *dz = wts + g.w.bytes, *rows = dz + g.dz, *counts = rows + g.rows, *range = counts + g.counts, *sums = range + g.range;
+        char *acc = sums + g.sums, *part_x = acc + g.acc, *part_w = part_x + g.part_x;
+        const int64_t size = (int64_t)type_bytes(type);
+        float *undo = type == FB_TYPE_F16 ? (float *)range : nullptr;
+        if (M > 0) {
+            RowParams r{tokens, logz, entropy, g_logprobs, g_entropy, M, (f32x4 *)rows, undo ? (uint32_t *)(undo + 1) : nullptr, 0, undo, (int32_t *)counts};
+            r.n_peaks = (int)std::min<int64_t>(kPeakGroups, (M + 255) / 256);
+            if (undo) {
+                hipLaunchKernelGGL(fb_scores_peak_kernel, dim3((unsigned)r.n_peaks), dim3(256), 0, st, r);
+                if ((rc = launched("scores peak kernel launch: ")) != FB_OK) return rc;
+            }
+            hipLaunchKernelGGL(fb_scores_rows_kernel, dim3((unsigned)((M + 255) / 256)), dim3(256), 0, st, r);
+            if ((rc = launched("scores rows kernel launch: ")) != FB_OK) return rc;
+            Prepare jobs;
+            SlopeParams copy = pack_job(g.x, x, ldx, M, K, xs);
+            copy.counts = (const int32_t *)counts;
+            jobs.add(copy, type);
+            if (g.w.copy) jobs.add(pack_job(g.w, weight, ldw, V, K, wts), type);
+            if ((rc = launch_prepare(jobs, type, type, st)) != FB_OK) return rc;
+        }
+        const char *w = g.w.copy ? wts : (const char *)weight;
+        for (int64_t v0 = 0; v0 < V; v0 += g.width) {
+            const int64_t n = std::min(g.width, V - v0);
+            const bool first = v0 == 0, last = v0 + n == V;
+            Product z = g.z, qx = g.dx, qw = g.dw;
+            z.N = n; qx.K = n; qw.M = n;
+            z.A = {xs, g.x.ld, true};
+            z.B = {w + v0 * g.w.ld * size, g.w.ld, true};
+            z.f.bias = bias ? bias + v0 : nullptr;
+            z.f.y = dz; z.f.ldy = whole_pieces(n, type);
+            z.f.undo = undo;
+            z.s = {tokens, (int)v0, nullptr, nullptr, rows, g_entropy != nullptr, dbias ? (float *)sums : nullptr};
+            if (M > 0 && (rc = launch_scores<Slopes>(z, st)) != FB_OK) return rc;
+            qx.A = {dz, z.f.ldy, true};
+            qx.B = {z.B.p, g.w.ld, false};
+            qx.split = (int)((n + qx.share - 1) / qx.share);
+            qx.f.undo = undo;
+            qx.part = (float *)part_x;
+            if (g.pieces > 1) {                     // pieces add up in single precision
+                qx.f.y = acc; qx.f.ldy = K; qx.f.out_type = FB_TYPE_F32;
+                qx.f.residual = first ? nullptr : acc; qx.f.ldr = K;
+            } else {
+                qx.f.y = dx; qx.f.ldy = lddx; qx.f.out_type = type;
+            }
+            qw.A = {dz, z.f.ldy, false};
+            qw.B = {xs, g.x.ld, false};
+            qw.f.y = dweight ? (char *)dweight + v0 * K * size : nullptr; qw.f.ldy = K; qw.f.out_type = type;
+            qw.f.undo = undo;
+            qw.part = (float *)part_w;
+            const bool has_dx = dx && M > 0;
+            if (has_dx && (rc = launch_mfma_product(qx, st)) != FB_OK) return rc;
+            if (dweight && (rc = launch_mfma_product(qw, st)) != FB_OK) return rc;
+            rc = launch_join(has_dx ? &qx : nullptr, dweight ? &qw : nullptr, type, (const float *)sums, M > 0 ? g.sum_rows : 0, n, dbias ? dbias + v0 : nullptr, st);
+            if (rc != FB_OK) return rc;
+            if (last && has_dx && g.pieces > 1 && (rc = launch_round(RoundParams{(const float *)acc, M, K, lddx, dx}, type, st)) != FB_OK) return rc;
+        }
+        return FB_OK;
+    });
+}
+
+}  // extern "C"

@@ -28,7 +28,8 @@ SYMBOLS = ["fb_layer_norm", "fb_layer_norm_grad_workspace_bytes", "fb_layer_norm
            "fb_residual_norm_grad_workspace_bytes", "fb_residual_norm_grad", "fb_affine_workspace_bytes", "fb_affine",
            "fb_affine_grad_workspace_bytes", "fb_affine_grad", "fb_gated_affine_workspace_bytes", "fb_gated_affine",
            "fb_gated_affine_grad_workspace_bytes", "fb_gated_affine_grad", "fb_token_logprobs_workspace_bytes", "fb_token_logprobs",
-           "fb_token_logprobs_grad"]
+           "fb_token_logprobs_grad", "fb_affine_logprobs_workspace_bytes", "fb_affine_logprobs", "fb_affine_logprobs_grad_workspace_bytes",
+           "fb_affine_logprobs_grad"]
 
 _lib = None
 torch = None                     # loaded with the library, see lib()
@@ -61,6 +62,10 @@ def lib() -> ctypes.CDLL:
         L.fb_token_logprobs_workspace_bytes.argtypes = [i64, i64, i32, i32]
         L.fb_token_logprobs.argtypes = [vp, i64, vp, i64, i64, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]
         L.fb_token_logprobs_grad.argtypes = [vp, i64, vp, vp, vp, vp, vp, i64, i64, i32, vp, i64, vp]
+        L.fb_affine_logprobs_workspace_bytes.argtypes = [vp, i64, vp, i64, i64, i64, i64, i32]
+        L.fb_affine_logprobs.argtypes = [vp, i64, vp, i64, vp, vp, i64, i64, i64, i32, vp, vp, vp, vp, sz, vp]
+        L.fb_affine_logprobs_grad_workspace_bytes.argtypes = [vp, i64, vp, i64, i64, i64, i64, i32]
+        L.fb_affine_logprobs_grad.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, i64, i64, i64, i32, vp, i64, vp, vp, vp, sz, vp]
         for name in SYMBOLS:
             getattr(L, name).restype = sz if name.endswith("_bytes") else ctypes.c_int
         import torch as t
@@ -443,3 +448,49 @@ def fb_token_logprobs_grad(logits, tokens, logz, entropy, g_logprobs, g_entropy=
     d = _out_like(logits)
     _check(L.fb_token_logprobs_grad(p, ld, pt, pz, pe, pg, ph, R, V, code, d.data_ptr(), V, _raw_stream(dev)))
     return d
+
+
+def _scored(x, weight, tokens, bias):
+    """-> (type, x's address and row distance, rows, K, device, weight's, V, tokens' address, bias's) of arguments that the calls share."""
+    code = _type(x, "x")
+    px, ldx, M, K, dev = _rows(x, "x")
+    if weight.dim() != 2:
+        raise ValueError("weight must be [V, K]")
+    pw, ldw, _, _, _ = _rows(weight, "weight", K, x.dtype, None, dev)
+    V = int(weight.shape[0])
+    if tokens.shape != x.shape[:-1]:
+        raise ValueError("tokens must have the leading shape of x")
+    return code, px, ldx, M, K, dev, pw, ldw, V, _vector(tokens, "tokens", M, (torch.int32,), dev), _vector(bias, "bias", V, (torch.float32,), dev)
+
+
+def fb_affine_logprobs(x, weight, tokens, bias=None):
+    """fb_token_logprobs of the logits x weight^T + bias, which are not kept -> (logprobs, entropy, logz: float32 of x's leading shape).
+
+    ``x`` [..., K]; ``weight`` [V, K] of x's type; ``tokens`` int32 of the leading shape, negative where a row does not count (its
+    outputs are 0, its x may hold anything); ``bias`` [V] float32, -inf where an alternative is ruled out."""
+    L = lib()
+    code, px, ldx, M, K, dev, pw, ldw, V, pt, pb = _scored(x, weight, tokens, bias)
+    lp, ent, z = _floats(3, x, x.shape[:-1])
+    need = int(L.fb_affine_logprobs_workspace_bytes(px, ldx, pw, ldw, M, V, K, code))
+    ws, pws = _workspace(need, x)
+    _check(L.fb_affine_logprobs(px, ldx, pw, ldw, pb, pt, M, V, K, code, lp.data_ptr(), ent.data_ptr(), z.data_ptr(), pws, need, _raw_stream(dev)))
+    return lp, ent, z
+
+
+def fb_affine_logprobs_grad(x, weight, tokens, logz, entropy, g_logprobs, g_entropy=None, bias=None, want_dx: bool = True, want_dweight: bool = True,
+                            want_dbias: bool = True):
+    """-> (dx like x, dweight like weight, dbias [V] float32), None in the place of one that is not wanted, from the gradients of logprobs
+    and entropy (either None: 0) and what fb_affine_logprobs returned."""
+    L = lib()
+    code, px, ldx, M, K, dev, pw, ldw, V, pt, pb = _scored(x, weight, tokens, bias)
+    f = (torch.float32,)
+    pz, pe = _vector(logz, "logz", M, f, dev), _vector(entropy, "entropy", M, f, dev)
+    pg, ph = _vector(g_logprobs, "g_logprobs", M, f, dev), _vector(g_entropy, "g_entropy", M, f, dev)
+    dx = _out_like(x) if want_dx else None
+    dw = _out(x, (V, K), x.dtype) if want_dweight else None
+    db = _out(x, (V,), torch.float32) if want_dbias else None
+    need = int(L.fb_affine_logprobs_grad_workspace_bytes(px, ldx, pw, ldw, M, V, K, code))
+    ws, pws = _workspace(need, x)
+    _check(L.fb_affine_logprobs_grad(px, ldx, pw, ldw, pb, pt, pz, pe, pg, ph, M, V, K, code, dx.data_ptr() if want_dx else None, K,
+                                     dw.data_ptr() if want_dweight else None, db.data_ptr() if want_dbias else None, pws, need, _raw_stream(dev)))
+    return dx, dw, db
