@@ -9,10 +9,11 @@ calling ``backward`` once per sub-batch accumulates the parameter gradients of
 the whole batch (the B/F scheme of the paper's training recipe), since the
 objective is a sum over utterances.
 
-``layer_norm``, ``affine`` and ``token_logprobs`` are the operators of
-``paper_2112_00709_amd.layers`` with their gradients: what makes the network's
-output from hidden frames and takes the objective's derivative back into the
-weights, and the frame log probabilities that recipes use beside it.
+``layer_norm``, ``residual_norm``, ``affine``, ``gated_affine``, ``token_logprobs``
+and ``affine_logprobs`` are the operators of ``paper_2112_00709_amd.layers`` with
+their gradients: what makes the network's output from hidden frames and takes the
+objective's derivative back into the weights, and the frame log probabilities that
+recipes use beside it.
 """
 from __future__ import annotations
 
@@ -142,7 +143,72 @@ def _layer_functions():
             g = [None if t is None else t.contiguous() for t in (g_logprobs, g_entropy)]
             return fl.fb_token_logprobs_grad(logits, tokens, logz, entropy, *g), None, None, None
 
-    _layer_fns = _LayerNorm, _Affine, _TokenLogprobs
+    class _ResidualNorm(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, h, residual, gate, inner_weight, inner_bias, weight, bias, scale, inner, outer, eps, recording):
+            vectors = dict(scale=scale, inner=inner, inner_weight=inner_weight, inner_bias=inner_bias, outer=outer, weight=weight)
+            ctx.set_materialize_grads(False)
+            if not (recording and any(ctx.needs_input_grad[:7])):
+                return fl.fb_residual_norm(h, residual, gate, bias=bias, eps=eps, **vectors)
+            s, y, stats = fl.fb_residual_norm(h, residual, gate, bias=bias, eps=eps, want_stats=True, **vectors)
+            # (s is what the backward pass reads of its outputs; without an outer norm it reads neither)
+            ctx.save_for_backward(h, s if outer != "none" else None, stats, gate, inner_weight, inner_bias, weight)
+            ctx.rest = scale, inner, outer, [None if t is None else t.dtype for t in (inner_weight, inner_bias, weight, bias)]
+            return s, y
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, ds, dy):
+            if ds is None and dy is None:
+                return (None,) * 12
+            h, s, stats, gate, inner_weight, inner_bias, weight = ctx.saved_tensors
+            scale, inner, outer, dtypes = ctx.rest
+            need = ctx.needs_input_grad
+            ds, dy = [None if t is None else t.contiguous() for t in (ds, dy)]
+            if dy is None and outer != "none":
+                dy = torch.zeros_like(ds)
+            dh, dr, dgate, *sums = fl.fb_residual_norm_grad(ds, dy, h, s, stats, gate, scale=scale, inner=inner, inner_weight=inner_weight,
+                                                            inner_bias=inner_bias, outer=outer, weight=weight, want_dh=need[0], want_dresidual=need[1],
+                                                            want_dgate=need[2], want_dinner=need[3] or need[4], want_douter=need[5] or need[6])
+            sums = [g.to(dtype) if want else None for g, dtype, want in zip(sums, dtypes, need[3:7])]
+            return dh, dr, None if dgate is None else dgate.to(gate.dtype), *sums, None, None, None, None, None
+
+    class _GatedAffine(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, weight, bias, activation, recording):
+            if not (recording and any(ctx.needs_input_grad[:3])):
+                return fl.fb_gated_affine(x, weight, bias, activation)
+            y, preact = fl.fb_gated_affine(x, weight, bias, activation, want_preact=True)
+            ctx.save_for_backward(x, weight, preact)
+            ctx.activation = activation
+            return y
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, dy):
+            x, weight, preact = ctx.saved_tensors
+            return *fl.fb_gated_affine_grad(dy.contiguous(), x, weight, preact, ctx.activation, *ctx.needs_input_grad[:3]), None, None
+
+    class _AffineLogprobs(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, weight, bias, tokens, recording):
+            logprobs, entropy, logz = fl.fb_affine_logprobs(x, weight, tokens, bias)
+            if recording and any(ctx.needs_input_grad[:3]):
+                ctx.save_for_backward(x, weight, bias, tokens, logz.clone(), entropy.clone())
+            ctx.mark_non_differentiable(logz)
+            ctx.set_materialize_grads(False)
+            return logprobs, entropy, logz
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, g_logprobs, g_entropy, _g_logz):
+            if g_logprobs is None and g_entropy is None:
+                return None, None, None, None, None
+            x, weight, bias, tokens, logz, entropy = ctx.saved_tensors
+            g = [None if t is None else t.contiguous() for t in (g_logprobs, g_entropy)]
+            return *fl.fb_affine_logprobs_grad(x, weight, tokens, logz, entropy, *g, bias, *ctx.needs_input_grad[:3]), None, None
+
+    _layer_fns = _LayerNorm, _Affine, _TokenLogprobs, _ResidualNorm, _GatedAffine, _AffineLogprobs
     return _layer_fns
 
 
@@ -161,3 +227,21 @@ def token_logprobs(logits, tokens, top: int = 0):
     """``layers.fb_token_logprobs`` -> (logprobs, entropy, logz, top_ids, top_logprobs); the first two have gradients with
     respect to the logits, the others do not."""
     return _layer_functions()[2].apply(logits, tokens, top, _torch().is_grad_enabled())
+
+
+def residual_norm(h, residual=None, gate=None, scale: float = 1.0, inner: str = "none", inner_weight=None, inner_bias=None, outer: str = "layer",
+                  weight=None, bias=None, eps: float = 1e-5):
+    """``layers.fb_residual_norm`` -> (s, y), y None with outer "none", with its gradient with respect to h, residual, gate and the
+    norms' weights and biases.  s is read again by the backward pass where there is an outer norm: it must not be changed in place then."""
+    return _layer_functions()[3].apply(h, residual, gate, inner_weight, inner_bias, weight, bias, scale, inner, outer, eps, _torch().is_grad_enabled())
+
+
+def gated_affine(x, weight, bias=None, activation: str = "silu"):
+    """``layers.fb_gated_affine`` with its gradient with respect to x, weight and bias.  Where a gradient can follow, the forward
+    call keeps both factors before the activation, rounded to x's type."""
+    return _layer_functions()[4].apply(x, weight, bias, activation, _torch().is_grad_enabled())
+
+
+def affine_logprobs(x, weight, tokens, bias=None):
+    """``layers.fb_affine_logprobs`` -> (logprobs, entropy, logz); the first two have gradients with respect to x, weight and bias."""
+    return _layer_functions()[5].apply(x, weight, bias, tokens, _torch().is_grad_enabled())
