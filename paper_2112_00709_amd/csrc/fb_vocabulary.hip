@@ -40,31 +40,31 @@ __device__ __forceinline__ float other_half_sum(float v)
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// A lane has of each of its fragments' rows lane % 32 of C, columns 8 e + 4 (lane / 32) + 0 .. 3 of every 32.  What a row has in
+// common and what a column has go onto the sums by one matrix instruction a fragment, of two k in single precision:
+// bias[j] 1 + 1 row[i].  The columns' operand is asked for when a tile begins.
+template <int FJ>
+__device__ __forceinline__ void ask_columns(const Product &q, int64_t j0, int lane, f32x4 &of_columns)
+{
+#pragma unroll
+    for (int y = 0; y < FJ; ++y) {
+        const int64_t j = j0 + y * 32 + lane;
+        of_columns[y] = lane >= 32 ? 1.0f : j >= q.N ? -kInf : q.f.bias ? q.f.bias[j] : 0.0f;
+    }
+}
+
+template <int FJ>
+__device__ __forceinline__ void add_rank_one(f32x16 (&acc)[FJ], const f32x4 &of_columns, float of_row, int lane)
+{
+#pragma unroll
+    for (int y = 0; y < FJ; ++y) acc[y] = __builtin_amdgcn_mfma_f32_32x32x2f32(of_columns[y], lane < 32 ? 1.0f : of_row, acc[y], 0, 0, 0);
+}
+
 // The bias of a lane's four columns, -inf past the last.
 __device__ __forceinline__ void bias_or_out(const Product &q, int64_t j, f32x4 &four)
 {
 #pragma unroll
     for (int e = 0; e < 4; ++e) four[e] = j + e < q.N ? (q.f.bias ? q.f.bias[j + e] : 0.0f) : -kInf;
-}
-
-// A lane has of each of its fragments' rows lane % 32 of C, columns 8 e + 4 (lane / 32) + 0 .. 3 of every 32.  Adds the bias, which
-// the wave's lanes have four by four, to all of them.
-template <int FI, int FJ>
-__device__ __forceinline__ void add_bias(f32x16 (&acc)[FI][FJ], const f32x4 &four, float *mine, int lane)
-{
-    if (lane < FJ * 8) *(f32x4 *)(mine + lane * 4) = four;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll
-    for (int y = 0; y < FJ; ++y)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const f32x4 b = *(const f32x4 *)(mine + (y * 8 + 2 * e + (lane >> 5)) * 4);
-#pragma unroll
-            for (int x = 0; x < FI; ++x)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) acc[x][y][4 * e + r] += b[r];
-        }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
 // f(y, the element's place in acc[x][y]) where a row's token is among the wave's columns, in the lane that has it.  Rare: asked
@@ -92,7 +92,7 @@ struct Reduced {
     template <int FI, int FJ>
     static __device__ __forceinline__ void early(const Product &q, const Where &where, int lane, f32x4 (&four)[2])
     {
-        bias_or_out(q, where.j0 + where.wj * FJ * 32 + lane % (FJ * 8) * 4, four[0]);
+        ask_columns<FJ>(q, where.j0 + where.wj * FJ * 32, lane, four[0]);
         const int64_t i = where.i0 + where.wi * FI * 32 + (lane & 31);
 #pragma unroll
         for (int x = 0; x < FI; ++x) four[1][x] = __int_as_float(i + x * 32 < q.M ? max(q.s.tokens[i + x * 32], -1) - q.s.first : -1);
@@ -104,12 +104,12 @@ struct Reduced {
         int lane = threadIdx.x & 63;
         asm volatile("" : "+s"(args), "+v"(lane));
         const int waves = blockDim.x / 64, across = FI == 4 ? 4 : 2, rows = waves / across * FI * 32;     // of the tile
-        float *mine = where.room + where.wave * FJ * 32, *parts = where.room + waves * FJ * 32;
+        float *parts = where.room;
         const int64_t j0 = where.j0 + where.wj * FJ * 32;
-        add_bias<FI, FJ>(acc, four[0], mine, lane);
 #pragma unroll
         for (int x = 0; x < FI; ++x) {
             const int row = (where.wi * FI + x) * 32 + (lane & 31);
+            add_rank_one<FJ>(acc[x], four[0], 0.0f, lane);
             at_token<FJ>(__float_as_int(four[1][x]), j0, lane, [&](int y, int k) { args->s.given[where.i0 + row] = acc[x][y][k]; });
             float m = acc[x][0][0];
 #pragma unroll
@@ -153,87 +153,108 @@ struct Reduced {
 };
 
 // Sums leave as the logits' gradient, rounded to the factors' type, and as shares of its column sums before that.  Of a row there
-// are (log Z, a, h, g):  dz = g [j = token] - p (a + h log p),  a = g + h entropy.  Rows that do not count have log Z = inf and zeros.
+// are (-log Z, a, h, g):  dz = g [j = token] + p (a + h log p),  with a = -(g + h' entropy) and h = -h' for the entropy's gradient h'.  Rows
+// that do not count have log Z = inf and zeros.  A fragment's rows pass through LDS, in the factors' type, so that whole runs of a row
+// are stored; rows of dz are whole 16-byte pieces.
 struct Slopes {
     static constexpr bool kPaired = false;
-    static constexpr int kEarly = 2;
+    static constexpr int kEarly = 1;
 
     template <int FI, int FJ>
-    static __device__ __forceinline__ void early(const Product &q, const Where &where, int lane, f32x4 (&four)[2])
+    static __device__ __forceinline__ void early(const Product &q, const Where &where, int lane, f32x4 (&four)[1])
     {
-        Reduced::early<FI, FJ>(q, where, lane, four);
+        ask_columns<FJ>(q, where.j0 + where.wj * FJ * 32, lane, four[0]);
+    }
+
+    // Rows l0 .. l0 + ROWS - 1 of a fragment's 32, by the wave's `mine`: 16-byte piece c of a row lies at c ^ row.
+    template <class T, int FJ>
+    static __device__ __forceinline__ void store(const f32x16 (&v)[FJ], float *mine, T *dz, int64_t ld, int64_t i0, int64_t j0, int64_t M, int lane)
+    {
+        constexpr int VE = Vec<T>::kN, kPieces = FJ * 32 / VE, kAll = 16 * FJ * 32 * 4 / (kPieces * 16), kAtOnce = 64 / kPieces;
+        const int64_t j = j0 + lane % kPieces * VE;
+#pragma unroll
+        for (int l0 = 0; l0 < 32; l0 += kAll) {
+            const int l = (lane & 31) - l0;
+            if (l >= 0 && l < kAll) {
+                char *to = (char *)mine + l * kPieces * 16;
+#pragma unroll
+                for (int y = 0; y < FJ; ++y)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int c = (y * 32 + 8 * e + 4 * (lane >> 5)) / VE;
+                        if constexpr (sizeof(T) == 4)
+                            *(f32x4 *)(to + (c ^ (l & (kPieces - 1))) * 16) = f32x4{v[y][4 * e], v[y][4 * e + 1], v[y][4 * e + 2], v[y][4 * e + 3]};
+                        else
+                            *(u32x2 *)(to + (c ^ (l & (kPieces - 1))) * 16 + (lane >> 5) * 8) = u32x2{pack2<T>(v[y][4 * e], v[y][4 * e + 1]), pack2<T>(v[y][4 * e + 2], v[y][4 * e + 3])};
+                    }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            u32x4 w[kAll / kAtOnce];
+#pragma unroll
+            for (int r = 0; r < kAll / kAtOnce; ++r) {
+                const int row = r * kAtOnce + lane / kPieces;
+                w[r] = *(const u32x4 *)((const char *)mine + row * kPieces * 16 + ((lane % kPieces) ^ (row & (kPieces - 1))) * 16);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (j < ld) {
+                T *base = dz + (i0 + l0) * ld + j0;
+                const uint32_t off = (uint32_t)(lane / kPieces) * (uint32_t)ld + (uint32_t)(lane % kPieces * VE);
+                const int rows = (int)(M - i0 - l0 < kAll ? M - i0 - l0 : kAll);
+#pragma unroll
+                for (int r = 0; r < kAll / kAtOnce; ++r, base += kAtOnce * ld)
+                    if (r * kAtOnce + lane / kPieces < rows) *(u32x4 *)(base + off) = w[r];
+            }
+        }
     }
 
     template <class T, int FI, int FJ>
-    static __device__ __forceinline__ void leave(ProductArgs args, f32x16 (&acc)[FI][FJ], const f32x4 (&four)[2], float, const Where &where)
+    static __device__ __forceinline__ void leave(ProductArgs args, f32x16 (&acc)[FI][FJ], const f32x4 (&four)[1], float, const Where &where)
     {
         int lane = threadIdx.x & 63;
         asm volatile("" : "+s"(args), "+v"(lane));
-        constexpr int kPer = FJ * 8, kRows = 64 / kPer, kR = 16 / kRows;
-        const int64_t M = args->M, N = args->f.ldy, i0 = where.i0 + where.wi * FI * 32, j0 = where.j0 + where.wj * FJ * 32, j = j0 + lane % kPer * 4;
-        float *mine = where.room + where.wave * 16 * FJ * 32;
+        const int64_t M = args->M, i0 = where.i0 + where.wi * FI * 32, j0 = where.j0 + where.wj * FJ * 32;
+        const int64_t first = j0 + args->s.first;
         f32x4 of_row[FI];
+        int token[FI];
 #pragma unroll
         for (int x = 0; x < FI; ++x) {
             const int64_t i = i0 + x * 32 + (lane & 31);
-            of_row[x] = ((const f32x4 *)args->s.rows)[i < M ? i : M - 1];
+            of_row[x] = f32x4{-kInf, 0.0f, 0.0f, 0.0f};
+            token[x] = -1;
+            if (i < M) {
+                of_row[x] = ((const f32x4 *)args->s.rows)[i];
+                token[x] = args->s.tokens[i];
+            }
         }
-        add_bias<FI, FJ>(acc, four[0], mine, lane);
+        f32x16 sum[FJ] = {};
 #pragma unroll
         for (int x = 0; x < FI; ++x) {
-            const float logz = of_row[x][0], a = of_row[x][1], h = of_row[x][2], g = of_row[x][3];
-            if (args->s.entropy) {
+            f32x16(&v)[FJ] = acc[x];
+            add_rank_one<FJ>(v, four[0], of_row[x][0], lane);
 #pragma unroll
-                for (int y = 0; y < FJ; ++y)
+            for (int y = 0; y < FJ; ++y)
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) {
-                        const float d = fmaxf(acc[x][y][k] - logz, kFarOut);
-                        acc[x][y][k] = -__builtin_amdgcn_exp2f(d * kLog2E) * fmaf(h, d, a);
-                    }
-            } else {
+                for (int k = 0; k < 16; ++k) {
+                    const float d = fmaxf(v[y][k], kFarOut);
+                    v[y][k] = __builtin_amdgcn_exp2f(d * kLog2E) * fmaf(of_row[x][2], d, of_row[x][1]);
+                }
+            at_token<FJ>(token[x], first, lane, [&](int y, int k) { v[y][k] += of_row[x][3]; });
 #pragma unroll
-                for (int y = 0; y < FJ; ++y)
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) acc[x][y][k] = -__builtin_amdgcn_exp2f(fmaxf(acc[x][y][k] - logz, kFarOut) * kLog2E) * a;
-            }
-            at_token<FJ>(__float_as_int(four[1][x]), j0, lane, [&](int y, int k) { acc[x][y][k] += g; });
+            for (int y = 0; y < FJ; ++y) sum[y] += v[y];
+            store<T, FJ>(v, where.room + where.wave * 16 * FJ * 32, (T *)args->f.y, args->f.ldy, i0 + x * 32, j0, M, lane);
         }
-        const int nj = (int)(N - j < 4 ? (N - j < 0 ? 0 : N - j) : 4), in_row = lane / kPer;
-        const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)mine + (lane & 15) * FJ * 128;
-        f32x4 sum = {};
+        if (!args->s.sums) return;
+        const float undo = args->f.undo ? *args->f.undo : 1.0f;
+        // 32 rows of a column added: two of a lane's columns at a time over the rows of 16 lanes, so that lanes 16 .. 31 and 48 .. 63 have
+        // the second fragment's.
+        float *out = args->s.sums + (size_t)(i0 / (FI * 32)) * (size_t)args->N;
+        const int64_t j = j0 + (FJ == 2 ? (lane >> 4 & 1) * 32 : 0) + (lane >> 5) * 4;
 #pragma unroll
-        for (int pass = 0; pass < 2 * FI; ++pass) {
-            put_rows<FI, FJ>(acc, pass, lane, to);
-            f32x4 w[kR];
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll
-            for (int r = 0; r < kR; ++r) {
-                const int row = r * kRows + in_row;
-                w[r] = *(const f32x4 *)(mine + row * FJ * 32 + ((lane % kPer) ^ (row & (kPer - 1))) * 4);
-            }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            const int64_t i = i0 + pass * 16;
-            const Spot at{i, j0, in_row, lane % kPer * 4, (int)(M - i < 16 ? M - i : 16), nj};
-#pragma unroll
-            for (int r = 0; r < kR; ++r)
-                if (r * kRows + in_row < at.rows) sum += w[r];
-            if (at.rows > in_row && nj > 0) store_rows<T, T, kR, kRows>((T *)args->f.y, args->f.ldy, at, w, false);
-        }
-        if (args->s.sums) {
-            const float undo = args->f.undo ? *args->f.undo : 1.0f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float v = sum[e];
-#pragma unroll
-                for (int step = kPer; step < 64; step *= 2) v += __shfl_xor(v, step);
-                sum[e] = v * undo;
-            }
-            if (lane < kPer) {
-                float *out = args->s.sums + (size_t)(i0 / (FI * 32)) * (size_t)args->N + j;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (j + e < args->N) out[e] = sum[e];
-            }
+        for (int k = 0; k < 16; ++k) {
+            const auto two = __builtin_amdgcn_permlane16_swap(__float_as_uint(sum[0][k]), __float_as_uint(sum[FJ - 1][k]), false, false);
+            const float s = sum_row16(__uint_as_float(two[0]) + __uint_as_float(two[1])) * undo;
+            const int64_t c = j + (k >> 2) * 8 + (k & 3);
+            if ((lane & (FJ == 2 ? 15 : 31)) == 0 && c < args->N) out[c] = s;
         }
     }
 };
@@ -461,10 +482,12 @@ __global__ __launch_bounds__(256) void fb_scores_rows_kernel(RowParams p)
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= p.M) return;
     f32x4 r = row_of(p, i);
-#pragma unroll
-    for (int e = 1; e < 4; ++e) r[e] *= scale;
-    p.rows[i] = r;
     p.counts[i] = r[0] == kInf ? -1 : 0;
+    r[0] = -r[0];
+    r[1] *= -scale;
+    r[2] *= -scale;
+    r[3] *= scale;
+    p.rows[i] = r;
 }
 
 // The sum over pieces of the vocabulary, rounded to dx.
