@@ -8,73 +8,67 @@ namespace fb {
 
 namespace {
 
-// Sums of a wave leave as y = act(g) u: 16 rows of C at a time through LDS, as in Finished, the gate's 32 columns and behind
-// them the other factor's.
+// Sums of a wave leave as y = act(g) u, formed in the registers that have them, and as g and u.
 struct Gated {
     static constexpr bool kPaired = true;
-    static constexpr int kEarly = 2;
+    static constexpr int kEarly = 1;
 
     template <int FI, int FJ>
-    static __device__ __forceinline__ void early(const Product &q, const Where &where, int lane, f32x4 (&four)[2])
+    static __device__ __forceinline__ void early(const Product &q, const Where &where, int lane, f32x4 (&four)[1])
     {
         if (!q.f.bias) return;
-        const int64_t j = where.j0 + where.wj * 32 + lane % 8 * 4;
-        bias_of(q.f.bias, q.N, j, four[0]);
-        bias_of(q.f.bias + q.N, q.N, j, four[1]);
+#pragma unroll
+        for (int y = 0; y < FJ; ++y) {
+            const int64_t j = where.j0 + (where.wj * (FJ / 2) + y / 2) * 32 + lane;
+            if (lane < 32 && j < q.N) four[0][y] = q.f.bias[(y & 1) * q.N + j];
+        }
     }
 
     template <class T, int FI, int FJ>
-    static __device__ __forceinline__ void leave(ProductArgs args, f32x16 (&acc)[FI][FJ], const f32x4 (&bias)[2], float, const Where &where)
+    static __device__ __forceinline__ void leave(ProductArgs args, f32x16 (&acc)[FI][FJ], const f32x4 (&bias)[1], float, const Where &where)
     {
-        static_assert(FJ == 2, "a fragment of either factor");
+        constexpr int F = FJ / 2;
         int lane = threadIdx.x & 63;
         asm volatile("" : "+s"(args), "+v"(lane));
-        constexpr int kR = 2, kRows = 8;
-        const int64_t M = args->M, N = args->N, i0 = where.i0 + where.wi * FI * 32, j0 = where.j0 + where.wj * 32, j = j0 + lane % 8 * 4;
-        const int nj = (int)(N - j < 4 ? (N - j < 0 ? 0 : N - j) : 4), in_row = lane / 8, act = args->f.act;
+        const int64_t M = args->M, N = args->N, i0 = where.i0 + where.wi * FI * 32, j0 = where.j0 + where.wj * F * 32;
+        const int act = args->f.act;
         const bool past = args->past;
-        float *mine = where.room + where.wave * 16 * FJ * 32;
-        const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)mine + (lane & 15) * FJ * 128;
-#pragma unroll 1
-        for (int pass = 0; pass < 2 * FI; ++pass) {
-            put_rows<FI, FJ>(acc, pass, lane, to);
-            f32x4 g[kR], u[kR];
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        float *mine = where.room + where.wave * 16 * 2 * 32;
 #pragma unroll
-            for (int r = 0; r < kR; ++r) {
-                const int row = r * kRows + in_row;
-                g[r] = *(const f32x4 *)(mine + row * FJ * 32 + ((lane % 8) ^ row) * 4) + bias[0];
-                u[r] = *(const f32x4 *)(mine + row * FJ * 32 + ((lane % 8 + 8) ^ row) * 4) + bias[1];
+        for (int x = 0; x < FI; ++x) {
+            const int64_t i = i0 + x * 32;
+            if (args->f.bias) add_rank_one<FJ>(acc[x], bias[0], 0.0f, lane);
+            f32x16 g[F], u[F];
+#pragma unroll
+            for (int f = 0; f < F; ++f) {
+                g[f] = acc[x][2 * f];
+                u[f] = acc[x][2 * f + 1];
             }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            const int64_t i = i0 + pass * 16;
-            const Spot at{i, j0, in_row, (lane % 8) * 4, (int)(M - i < 16 ? M - i : 16), nj};
-            if (at.rows > in_row && nj > 0) {
-                if (args->f.preact) {
-                    store_rows<T, T, kR, kRows>((T *)args->f.preact, args->f.ldp, at, g, past);
-                    store_rows<T, T, kR, kRows>((T *)args->f.preact + N, args->f.ldp, at, u, past);
-                }
-                auto gate = [&](int which) {
-#pragma unroll
-                    for (int r = 0; r < kR; ++r)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) u[r][e] *= act_of(g[r][e], which);
-                };
-                if (act == FB_ACT_SILU) gate(FB_ACT_SILU);
-                else if (act == FB_ACT_GELU) gate(FB_ACT_GELU);
-                else if (act == FB_ACT_SIGMOID) gate(FB_ACT_SIGMOID);
-                else if (act == FB_ACT_RELU) gate(FB_ACT_RELU);
-                else gate(FB_ACT_NONE);
-                store_rows<T, T, kR, kRows>((T *)args->f.y, args->f.ldy, at, u, past);
+            if (args->f.preact) {
+                store_fragments<T, F>(g, mine, (T *)args->f.preact, args->f.ldp, i, j0, M, N, lane, past);
+                store_fragments<T, F>(u, mine, (T *)args->f.preact + N, args->f.ldp, i, j0, M, N, lane, past);
             }
+            auto gate = [&](int which) {
+#pragma unroll
+                for (int f = 0; f < F; ++f)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) u[f][k] *= act_of(g[f][k], which);
+            };
+            if (act == FB_ACT_SILU) gate(FB_ACT_SILU);
+            else if (act == FB_ACT_GELU) gate(FB_ACT_GELU);
+            else if (act == FB_ACT_SIGMOID) gate(FB_ACT_SIGMOID);
+            else if (act == FB_ACT_RELU) gate(FB_ACT_RELU);
+            else gate(FB_ACT_NONE);
+            store_fragments<T, F>(u, mine, (T *)args->f.y, args->f.ldy, i, j0, M, N, lane, past);
         }
     }
 };
 
+// Waves of 64 rows and 64 outputs: runs of 128 bytes of a row leave together.
 template <class T>
 int launch_gated(const Product &q, hipStream_t stream)
 {
-    return q.tile == 256 ? launch<T, true, true, 2, 4, 4, 2, Gated>(q, stream) : launch<T, true, true, 2, 2, 2, 2, Gated>(q, stream);
+    return q.tile == 256 ? launch<T, true, true, 4, 2, 2, 4, Gated>(q, stream) : launch<T, true, true, 2, 2, 2, 2, Gated>(q, stream);
 }
 
 // Shares of k added in their order, pair by pair, and finished.

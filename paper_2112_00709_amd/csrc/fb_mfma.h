@@ -67,13 +67,13 @@ __device__ __forceinline__ void copy_to_lds(uint32_t to, uint32_t offset, const 
 
 // One factor's way into LDS and out of it.  ROWS of the tile, NW waves that copy, F fragments of 32 rows a wave from row w0 on.
 // PAIRED: the factor is two of `n` rows, one behind the other, and the tile has as many rows of the one as of the other, 32 by 32 in
-// turn, so that a wave's two fragments are the same rows of both.  A wave's copies are 32 rows, of one of them.
+// turn, so that a wave's fragments are in twos the same rows of both.  A wave's copies are 32 rows, of one of them.
 template <class T, bool ALONG, int ROWS, int NW, int F, bool PAIRED = false>
 struct Side {
     static constexpr int kSize = sizeof(T), kDeep = kDeepOf<T>, kPiece = 16 / kSize;
     static constexpr int kBytes = ROWS * 128, kCopies = kBytes / 1024 / NW;
     static constexpr int kPer = ROWS * kSize / 16, kK = 64 / kPer;      // not ALONG: lanes a k, k a copy
-    static_assert(!PAIRED || (ALONG && F == 2 && kCopies == 4), "a wave copies 32 rows and has a fragment of each factor");
+    static_assert(!PAIRED || (ALONG && F % 2 == 0 && kCopies == 4), "a wave copies 32 rows and has as many fragments of each factor");
     uint64_t base;           // of the tile's first element at the share's first k
     uint32_t ldb;            // bytes between rows
     int rows;                // rows of the factor from the tile's first on
@@ -268,7 +268,7 @@ constexpr int kPlain = -1;
 typedef const __attribute__((address_space(4))) Product *ProductArgs;
 
 // Where a wave's sums belong: the tile's share of k, first row and column, the wave's place in the tile, and LDS for the way out (16
-// rows of its columns a wave).
+// rows of 32 or 64 sums a wave).
 struct Where {
     int share;
     int64_t i0, j0;
@@ -296,6 +296,72 @@ __device__ __forceinline__ void put_rows(const f32x16 (&acc)[FI][FJ], int pass, 
     else if (FI <= 2 || pass < 4) put(acc[1 % FI]);
     else if (pass < 6) put(acc[2 % FI]);
     else put(acc[3 % FI]);
+}
+
+// What a row has in common and what a column has go onto the sums by one matrix instruction a fragment, of two k in single
+// precision: of_columns[y] lane % 32 1 + 1 of_row.  (`of_columns`: a column's in the lower lanes, 1 in the upper ones, or 0 if rows have nothing.)
+template <int FJ>
+__device__ __forceinline__ void add_rank_one(f32x16 (&acc)[FJ], const f32x4 &of_columns, float of_row, int lane)
+{
+#pragma unroll
+    for (int y = 0; y < FJ; ++y) acc[y] = __builtin_amdgcn_mfma_f32_32x32x2f32(of_columns[y], lane < 32 ? 1.0f : of_row, acc[y], 0, 0, 0);
+}
+
+// F neighbouring fragments of 32 rows from i0 and 32 columns each from j0 on, stored as T: a lane has row lane % 32, columns
+// 8 e + 4 (lane / 32) + 0 .. 3 of every 32.  They pass through the wave's LDS (`mine`, 16 rows of F fragments in single precision) as T, so that
+// whole runs of a row are stored by 16 bytes a lane; piece c of a row lies at c ^ row there.  WHOLE: rows are whole pieces, kept in the caches.
+template <class T, int F, bool WHOLE = false>
+__device__ __forceinline__ void store_fragments(const f32x16 (&v)[F], float *mine, T *out, int64_t ld, int64_t i0, int64_t j0, int64_t M, int64_t N, int lane, bool past)
+{
+    constexpr int VE = Vec<T>::kN, kPieces = F * 32 / VE, kAll = 16 * F * 32 * 4 / (kPieces * 16), kAtOnce = 64 / kPieces, kR = kAll / kAtOnce;
+    const int64_t j = j0 + lane % kPieces * VE;
+    const int n = (int)(N - j < VE ? N - j : VE), in_row = lane / kPieces;
+#pragma unroll
+    for (int l0 = 0; l0 < 32; l0 += kAll) {
+        const int l = (lane & 31) - l0;
+        if (l >= 0 && l < kAll) {
+            char *to = (char *)mine + l * kPieces * 16;
+#pragma unroll
+            for (int y = 0; y < F; ++y)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const f32x4 four = {v[y][4 * e], v[y][4 * e + 1], v[y][4 * e + 2], v[y][4 * e + 3]};
+                    if constexpr (sizeof(T) == 4)
+                        *(f32x4 *)(to + ((y * 8 + 2 * e + (lane >> 5)) ^ (l & (kPieces - 1))) * 16) = four;
+                    else
+                        *(u32x2 *)(to + ((y * 4 + e) ^ (l & (kPieces - 1))) * 16 + (lane >> 5) * 8) = u32x2{pack2<T>(four[0], four[1]), pack2<T>(four[2], four[3])};
+                }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        u32x4 w[kR];
+#pragma unroll
+        for (int r = 0; r < kR; ++r) {
+            const int row = r * kAtOnce + in_row;
+            w[r] = *(const u32x4 *)((const char *)mine + row * kPieces * 16 + ((lane % kPieces) ^ (row & (kPieces - 1))) * 16);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        T *base = out + (i0 + l0) * ld + j0;
+        const uint32_t off = (uint32_t)in_row * (uint32_t)ld + (uint32_t)(lane % kPieces * VE);
+        const int rows = (int)(M - i0 - l0 < kAll ? M - i0 - l0 : kAll);
+        if (n == VE) {
+#pragma unroll
+            for (int r = 0; r < kR; ++r, base += kAtOnce * ld)
+                if (r * kAtOnce + in_row < rows) store_piece(base + off, VE, w[r], !WHOLE && past);
+        } else if (!WHOLE && n > 0) {
+#pragma unroll 1
+            for (int e = 0; e < n; ++e) {
+                T *p = base + off + e;
+#pragma unroll
+                for (int r = 0; r < kR; ++r, p += kAtOnce * ld) {
+                    if (r * kAtOnce + in_row >= rows) continue;
+                    if constexpr (sizeof(T) == 4)
+                        *(uint32_t *)p = e == 0 ? w[r][0] : e == 1 ? w[r][1] : w[r][2];
+                    else
+                        *(uint16_t *)p = (uint16_t)((e < 2 ? w[r][0] : e < 4 ? w[r][1] : e < 6 ? w[r][2] : w[r][3]) >> (16 * (e & 1)));
+                }
+            }
+        }
+    }
 }
 
 __device__ __forceinline__ void bias_of(const float *bias, int64_t n, int64_t j, f32x4 &four)
@@ -580,7 +646,7 @@ __global__ __launch_bounds__(WI * WJ * 64) void fb_mfma_product_kernel(Task task
 template <int WI, int WJ, int FI, int FJ>
 struct Shape {
     static constexpr int kI = WI * FI * 32, kJ = WJ * FJ * 32;
-    static constexpr size_t kBytes = (size_t)2 * (kI + kJ) * 128 + (size_t)WI * WJ * 16 * FJ * 32 * 4;
+    static constexpr size_t kBytes = (size_t)2 * (kI + kJ) * 128 + (size_t)WI * WJ * 16 * (FJ < 2 ? FJ : 2) * 32 * 4;
     static constexpr int64_t kSlots = (int64_t)kCUs * (int64_t)(kLdsBytes / kBytes);
 };
 

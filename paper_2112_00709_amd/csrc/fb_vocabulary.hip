@@ -40,9 +40,7 @@ __device__ __forceinline__ float other_half_sum(float v)
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// A lane has of each of its fragments' rows lane % 32 of C, columns 8 e + 4 (lane / 32) + 0 .. 3 of every 32.  What a row has in
-// common and what a column has go onto the sums by one matrix instruction a fragment, of two k in single precision:
-// bias[j] 1 + 1 row[i].  The columns' operand is asked for when a tile begins.
+// The columns' operand of add_rank_one, asked for when a tile begins: the bias, -inf past the last column.
 template <int FJ>
 __device__ __forceinline__ void ask_columns(const Product &q, int64_t j0, int lane, f32x4 &of_columns)
 {
@@ -51,13 +49,6 @@ __device__ __forceinline__ void ask_columns(const Product &q, int64_t j0, int la
         const int64_t j = j0 + y * 32 + lane;
         of_columns[y] = lane >= 32 ? 1.0f : j >= q.N ? -kInf : q.f.bias ? q.f.bias[j] : 0.0f;
     }
-}
-
-template <int FJ>
-__device__ __forceinline__ void add_rank_one(f32x16 (&acc)[FJ], const f32x4 &of_columns, float of_row, int lane)
-{
-#pragma unroll
-    for (int y = 0; y < FJ; ++y) acc[y] = __builtin_amdgcn_mfma_f32_32x32x2f32(of_columns[y], lane < 32 ? 1.0f : of_row, acc[y], 0, 0, 0);
 }
 
 // The bias of a lane's four columns, -inf past the last.
@@ -166,47 +157,6 @@ struct Slopes {
         ask_columns<FJ>(q, where.j0 + where.wj * FJ * 32, lane, four[0]);
     }
 
-    // Rows l0 .. l0 + ROWS - 1 of a fragment's 32, by the wave's `mine`: 16-byte piece c of a row lies at c ^ row.
-    template <class T, int FJ>
-    static __device__ __forceinline__ void store(const f32x16 (&v)[FJ], float *mine, T *dz, int64_t ld, int64_t i0, int64_t j0, int64_t M, int lane)
-    {
-        constexpr int VE = Vec<T>::kN, kPieces = FJ * 32 / VE, kAll = 16 * FJ * 32 * 4 / (kPieces * 16), kAtOnce = 64 / kPieces;
-        const int64_t j = j0 + lane % kPieces * VE;
-#pragma unroll
-        for (int l0 = 0; l0 < 32; l0 += kAll) {
-            const int l = (lane & 31) - l0;
-            if (l >= 0 && l < kAll) {
-                char *to = (char *)mine + l * kPieces * 16;
-#pragma unroll
-                for (int y = 0; y < FJ; ++y)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int c = (y * 32 + 8 * e + 4 * (lane >> 5)) / VE;
-                        if constexpr (sizeof(T) == 4)
-                            *(f32x4 *)(to + (c ^ (l & (kPieces - 1))) * 16) = f32x4{v[y][4 * e], v[y][4 * e + 1], v[y][4 * e + 2], v[y][4 * e + 3]};
-                        else
-                            *(u32x2 *)(to + (c ^ (l & (kPieces - 1))) * 16 + (lane >> 5) * 8) = u32x2{pack2<T>(v[y][4 * e], v[y][4 * e + 1]), pack2<T>(v[y][4 * e + 2], v[y][4 * e + 3])};
-                    }
-            }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            u32x4 w[kAll / kAtOnce];
-#pragma unroll
-            for (int r = 0; r < kAll / kAtOnce; ++r) {
-                const int row = r * kAtOnce + lane / kPieces;
-                w[r] = *(const u32x4 *)((const char *)mine + row * kPieces * 16 + ((lane % kPieces) ^ (row & (kPieces - 1))) * 16);
-            }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            if (j < ld) {
-                T *base = dz + (i0 + l0) * ld + j0;
-                const uint32_t off = (uint32_t)(lane / kPieces) * (uint32_t)ld + (uint32_t)(lane % kPieces * VE);
-                const int rows = (int)(M - i0 - l0 < kAll ? M - i0 - l0 : kAll);
-#pragma unroll
-                for (int r = 0; r < kAll / kAtOnce; ++r, base += kAtOnce * ld)
-                    if (r * kAtOnce + lane / kPieces < rows) *(u32x4 *)(base + off) = w[r];
-            }
-        }
-    }
-
     template <class T, int FI, int FJ>
     static __device__ __forceinline__ void leave(ProductArgs args, f32x16 (&acc)[FI][FJ], const f32x4 (&four)[1], float, const Where &where)
     {
@@ -241,7 +191,7 @@ struct Slopes {
             at_token<FJ>(token[x], first, lane, [&](int y, int k) { v[y][k] += of_row[x][3]; });
 #pragma unroll
             for (int y = 0; y < FJ; ++y) sum[y] += v[y];
-            store<T, FJ>(v, where.room + where.wave * 16 * FJ * 32, (T *)args->f.y, args->f.ldy, i0 + x * 32, j0, M, lane);
+            store_fragments<T, FJ, true>(v, where.room + where.wave * 16 * FJ * 32, (T *)args->f.y, args->f.ldy, i0 + x * 32, j0, M, args->f.ldy, lane, false);
         }
         if (!args->s.sums) return;
         const float undo = args->f.undo ? *args->f.undo : 1.0f;
