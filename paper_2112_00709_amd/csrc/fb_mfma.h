@@ -484,6 +484,33 @@ struct Finished {
     }
 };
 
+// Sums leave rounded to the factors' 16 bits, as they are or times *undo: what gradients are.
+struct Rounded {
+    static constexpr bool kPaired = false;
+    static constexpr int kEarly = 1;
+
+    template <int FI, int FJ>
+    static __device__ __forceinline__ void early(const Product &, const Where &, int, f32x4 (&)[1])
+    {
+    }
+
+    template <class T, int FI, int FJ>
+    static __device__ __forceinline__ void leave(ProductArgs args, f32x16 (&acc)[FI][FJ], const f32x4 (&)[1], float undo, const Where &where)
+    {
+        int lane = threadIdx.x & 63;
+        asm volatile("" : "+s"(args), "+v"(lane));
+        const int64_t i0 = where.i0 + where.wi * FI * 32, j0 = where.j0 + where.wj * FJ * 32;
+#pragma unroll
+        for (int x = 0; x < FI; ++x) {
+            if constexpr (std::is_same<T, f16>::value) {
+#pragma unroll
+                for (int y = 0; y < FJ; ++y) acc[x][y] *= undo;
+            }
+            store_fragments<T, FJ>(acc[x], where.room + where.wave * 16 * FJ * 32, (T *)args->f.y, args->f.ldy, i0 + x * 32, j0, args->M, args->N, lane, args->past);
+        }
+    }
+};
+
 // A product and its tiles, as a kernel gets it.
 struct Task {
     Product q;
