@@ -125,6 +125,15 @@ inline int64_t whole_pieces(int64_t width, int type)
     return (width + piece - 1) / piece * piece;
 }
 
+// The distance of rows that are made for the products: whole 128-byte lines, so that the 128 bytes of a step along k are one line and
+// not parts of two (65536 x 3000 x 1024 in bfloat16, dx: 442 us at a distance of 3000 elements, 356 at 3008; dW 391 and 361).  Rows of
+// less than 512 bytes are left at whole pieces: lines would be a quarter of them and more.
+inline int64_t line_distance(int64_t width, int type)
+{
+    const int64_t line = 128 / (int64_t)type_bytes(type);
+    return width < 4 * line ? whole_pieces(width, type) : (width + line - 1) / line * line;
+}
+
 // A matrix that the matrix units' kernel cannot take as it is, copied to rows of whole pieces (padded with zeros).
 struct Packed {
     bool copy;
@@ -136,7 +145,7 @@ inline Packed packed(const void *p, int64_t ld, int64_t rows, int64_t width, int
 {
     Packed k{};
     k.copy = !ready(p, ld, width, type);
-    k.ld = k.copy ? whole_pieces(width, type) : ld;
+    k.ld = k.copy ? line_distance(width, type) : ld;
     k.bytes = k.copy ? aligned((size_t)rows * (size_t)k.ld * type_bytes(type)) : 0;
     return k;
 }

@@ -366,7 +366,7 @@ GradPlan grad_plan(const void *dy, int64_t lddy, int dy_type, const void *x, int
     }
     g.slope = act != FB_ACT_NONE || dy_type != type || packed(dy, lddy, M, N, type).copy;
     g.scale = type == FB_TYPE_F16 && (dy_type != type || act > FB_ACT_RELU);
-    g.ldz = whole_pieces(N, type);
+    g.ldz = line_distance(N, type);
     g.dz = g.slope ? aligned((size_t)M * (size_t)g.ldz * type_bytes(type)) : 0;
     g.x = packed(x, ldx, M, K, type);
     g.w = packed(weight, ldw, N, K, type);

@@ -158,7 +158,7 @@ __global__ __launch_bounds__(256) void fb_gated_slope_kernel(GatedSlopeParams p)
     }
     if (n > 0) {
         const int64_t step = (int64_t)p.down * subs;
-        const int zeros = at + VE >= p.N ? (int)(p.ldo - 2 * p.N) : 0;       // the row's last columns, that the products read
+        const int zeros = at + VE >= p.N ? (int)((VE - 2 * p.N % VE) % VE) : 0;       // of the row's last piece, that the products read
         for (int64_t r0 = (int64_t)down * subs + sub; r0 < p.M; r0 += kPairsAhead * step) {
             u32x4 rd[kPairsAhead], rg[kPairsAhead], ru[kPairsAhead];
 #pragma unroll

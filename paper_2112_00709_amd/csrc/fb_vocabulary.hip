@@ -163,7 +163,7 @@ struct Slopes {
         int lane = threadIdx.x & 63;
         asm volatile("" : "+s"(args), "+v"(lane));
         const int64_t M = args->M, i0 = where.i0 + where.wi * FI * 32, j0 = where.j0 + where.wj * FJ * 32;
-        const int64_t first = j0 + args->s.first;
+        const int64_t first = j0 + args->s.first, wide = (args->N + Vec<T>::kN - 1) / Vec<T>::kN * Vec<T>::kN;
         f32x4 of_row[FI];
         int token[FI];
 #pragma unroll
@@ -191,7 +191,7 @@ struct Slopes {
             at_token<FJ>(token[x], first, lane, [&](int y, int k) { v[y][k] += of_row[x][3]; });
 #pragma unroll
             for (int y = 0; y < FJ; ++y) sum[y] += v[y];
-            store_fragments<T, FJ, true>(v, where.room + where.wave * 16 * FJ * 32, (T *)args->f.y, args->f.ldy, i0 + x * 32, j0, M, args->f.ldy, lane, false);
+            store_fragments<T, FJ, true>(v, where.room + where.wave * 16 * FJ * 32, (T *)args->f.y, args->f.ldy, i0 + x * 32, j0, M, wide, lane, false);
         }
         if (!args->s.sums) return;
         const float undo = args->f.undo ? *args->f.undo : 1.0f;
@@ -522,7 +522,7 @@ ScoreGradPlan score_grad_plan(const void *weight, int64_t ldw, int64_t M, int64_
     g.pieces = (V + most - 1) / most;
     g.width = g.pieces == 1 ? V : ((V + g.pieces - 1) / g.pieces + 255) / 256 * 256;
     g.pieces = (V + g.width - 1) / g.width;
-    g.ldz = whole_pieces(g.width, type);
+    g.ldz = line_distance(g.width, type);
     g.z.M = M; g.z.N = g.width; g.z.K = K; g.z.type = type;
     g.dx.M = M; g.dx.N = K; g.dx.K = g.width; g.dx.type = type;
     g.dw.M = g.width; g.dw.N = K; g.dw.K = M; g.dw.type = type;
@@ -530,7 +530,7 @@ ScoreGradPlan score_grad_plan(const void *weight, int64_t ldw, int64_t M, int64_
     plan(g.dx);
     plan(g.dw);
     g.x.copy = true;
-    g.x.ld = whole_pieces(K, type);
+    g.x.ld = line_distance(K, type);
     g.x.bytes = aligned((size_t)M * (size_t)g.x.ld * type_bytes(type));
     g.w = packed(weight, ldw, V, K, type);
     const int64_t fragment = g.z.tile == 256 ? 128 : g.z.tile / 2;        // rows of a wave
@@ -661,7 +661,7 @@ int fb_affine_logprobs_grad(const void *x, int64_t ldx, const void *weight, int6
             z.A = {xs, g.x.ld, true};
             z.B = {w + v0 * g.w.ld * size, g.w.ld, true};
             z.f.bias = bias ? bias + v0 : nullptr;
-            z.f.y = dz; z.f.ldy = whole_pieces(n, type);
+            z.f.y = dz; z.f.ldy = line_distance(n, type);
             z.f.undo = undo;
             z.s = {tokens, (int)v0, nullptr, nullptr, rows, g_entropy != nullptr, dbias ? (float *)sums : nullptr};
             if (M > 0 && (rc = launch_scores<Slopes>(z, st)) != FB_OK) return rc;
