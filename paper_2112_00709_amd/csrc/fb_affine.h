@@ -35,8 +35,8 @@ struct Scores {
     float *given;            // [M]: the tokens' logits
     float *stats;            // [tiles across][3][M]
     const void *rows;        // [M] fours of what the gradient takes of a row
-    bool entropy;            // the gradient has the entropy's part
     float *sums;             // [waves down][N]: shares of the sums of the gradient's columns, nullable
+    const uint64_t *live;    // of a product over rows, bit k % 64 of word k / 64: row k of the second factor counts; one word more; nullable
 };
 
 struct Product {
@@ -86,7 +86,6 @@ struct SlopeParams {
     const uint32_t *peaks;   // half precision: shares of the largest |dy| that sets the power of two out is taken times, nullable
     int n_peaks;
     float *undo;         // its inverse, out
-    const int32_t *counts;   // rows of out whose number here is negative are zeros, nullable
 };
 
 void lay_out(SlopeParams &p, int type);
@@ -153,7 +152,7 @@ inline Packed packed(const void *p, int64_t ld, int64_t rows, int64_t width, int
 // The job that makes the copy (nothing if none is needed).
 inline SlopeParams pack_job(const Packed &k, const void *p, int64_t ld, int64_t rows, int64_t width, void *to)
 {
-    return SlopeParams{p, nullptr, ld, 0, rows, width, k.ld, FB_ACT_NONE, to, nullptr, 0, 0, 0, nullptr, 0, nullptr, nullptr};
+    return SlopeParams{p, nullptr, ld, 0, rows, width, k.ld, FB_ACT_NONE, to, nullptr, 0, 0, 0, nullptr, 0, nullptr};
 }
 
 // What the matrix units' kernel addresses in 32 bits: 64 or 128 rows of a factor, 16 rows of what it stores or adds.

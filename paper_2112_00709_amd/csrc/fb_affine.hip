@@ -179,10 +179,6 @@ __device__ __forceinline__ void make_rows(const SlopeParams &p, int block, float
 #pragma unroll
                     for (int e = 0; e < VE; ++e) g[e] *= scale;
                 }
-                if (p.out && p.counts && r < p.M && p.counts[r] < 0) {
-#pragma unroll
-                    for (int e = 0; e < VE; ++e) g[e] = 0.0f;
-                }
                 if (p.out && r < p.M) store_piece((T *)p.out + r * p.ldo + at, VE, pack<T>(g));   // (rows of whole pieces)
             }
         }

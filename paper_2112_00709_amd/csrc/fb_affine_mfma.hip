@@ -34,11 +34,11 @@ int launch_pair(const Product &dx, const Product &dw, hipStream_t stream)
     return dx.tile == 128 ? launch_pair<T, 2, 2, 2, 2>(dx, dw, stream) : launch_pair<T, 2, 2, 1, 1>(dx, dw, stream);
 }
 
-template <class T, bool ALONG_A, bool ALONG_B, class WAY>
+template <class T, bool ALONG_A, bool ALONG_B, class WAY, bool MASKED = false>
 int launch_way(const Product &q, hipStream_t stream)
 {
-    if (q.tile == 256) return launch<T, ALONG_A, ALONG_B, 2, 4, 4, 2, WAY>(q, stream);
-    return q.tile == 128 ? launch<T, ALONG_A, ALONG_B, 2, 2, 2, 2, WAY>(q, stream) : launch<T, ALONG_A, ALONG_B, 2, 2, 1, 1, WAY>(q, stream);
+    if (q.tile == 256) return launch<T, ALONG_A, ALONG_B, 2, 4, 4, 2, WAY, MASKED>(q, stream);
+    return q.tile == 128 ? launch<T, ALONG_A, ALONG_B, 2, 2, 2, 2, WAY, MASKED>(q, stream) : launch<T, ALONG_A, ALONG_B, 2, 2, 1, 1, WAY, MASKED>(q, stream);
 }
 
 template <class T, bool ALONG_A, bool ALONG_B, int KIND>
@@ -51,17 +51,29 @@ int launch(const Product &q, hipStream_t stream)
 template <class T, bool ALONG_A>
 int launch_back(const Product &q, hipStream_t stream)
 {
-    if (q.f.residual && !q.parts) return launch<T, ALONG_A, false, FB_ACT_NONE>(q, stream);
+    if constexpr (ALONG_A) {
+        if (q.f.residual && !q.parts) return launch<T, true, false, FB_ACT_NONE>(q, stream);      // (dx in pieces)
+    }
     if constexpr (sizeof(T) == 2) {
         if (!q.parts && q.f.out_type == q.type) return launch_way<T, ALONG_A, false, Rounded>(q, stream);
     }
     return launch<T, ALONG_A, false, kPlain>(q, stream);
 }
 
+// dW where some rows do not count.
+template <class T>
+int launch_masked(const Product &q, hipStream_t stream)
+{
+    if constexpr (sizeof(T) == 2) {
+        if (!q.parts && q.f.out_type == q.type) return launch_way<T, false, false, Rounded, true>(q, stream);
+    }
+    return launch_way<T, false, false, Finished<kPlain>, true>(q, stream);
+}
+
 template <class T>
 int launch(const Product &q, hipStream_t stream)
 {
-    if (!q.A.along) return launch_back<T, false>(q, stream);
+    if (!q.A.along) return q.s.live ? launch_masked<T>(q, stream) : launch_back<T, false>(q, stream);
     if (!q.B.along) return launch_back<T, true>(q, stream);
     if (q.parts || (q.f.act <= FB_ACT_RELU && !q.f.residual && !q.f.preact)) return launch<T, true, true, kPlain>(q, stream);
     switch (q.f.act) {

@@ -68,11 +68,13 @@ __device__ __forceinline__ void copy_to_lds(uint32_t to, uint32_t offset, const 
 // One factor's way into LDS and out of it.  ROWS of the tile, NW waves that copy, F fragments of 32 rows a wave from row w0 on.
 // PAIRED: the factor is two of `n` rows, one behind the other, and the tile has as many rows of the one as of the other, 32 by 32 in
 // turn, so that a wave's fragments are in twos the same rows of both.  A wave's copies are 32 rows, of one of them.
-template <class T, bool ALONG, int ROWS, int NW, int F, bool PAIRED = false>
+// MASKED: k whose bit in Product::live is 0 are zeros, whatever they hold.
+template <class T, bool ALONG, int ROWS, int NW, int F, bool PAIRED = false, bool MASKED = false>
 struct Side {
     static constexpr int kSize = sizeof(T), kDeep = kDeepOf<T>, kPiece = 16 / kSize;
     static constexpr int kBytes = ROWS * 128, kCopies = kBytes / 1024 / NW;
     static constexpr int kPer = ROWS * kSize / 16, kK = 64 / kPer;      // not ALONG: lanes a k, k a copy
+    static_assert(!MASKED || !ALONG, "a lane copies pieces of one k");
     static_assert(!PAIRED || (ALONG && F % 2 == 0 && kCopies == 4), "a wave copies 32 rows and has as many fragments of each factor");
     uint64_t base;           // of the tile's first element at the share's first k
     uint32_t ldb;            // bytes between rows
@@ -81,6 +83,10 @@ struct Side {
     uint32_t lds;            // the first buffer
     uint32_t at[ALONG ? 4 : 2];
     int chunk;               // ALONG: a lane's piece along k
+    const __attribute__((address_space(4))) uint64_t *live;   // MASKED: of 64 k, and those of the next step
+    uint64_t bits;
+    int bit;                 // of the lane's first k, 32 k a step: in which half of `bits`
+    uint32_t dead;           // bits of the step's k, from the lane's first, inverted
 
     // What does not depend on the tile.
     __device__ __forceinline__ void start(const Factor &f, uint32_t lds_at, int wave, int w0)
@@ -111,8 +117,13 @@ struct Side {
         }
     }
 
-    __device__ __forceinline__ void tile(const Factor &f, int64_t r0, int64_t n, int64_t k0, int wave)
+    __device__ __forceinline__ void tile(const Factor &f, int64_t r0, int64_t n, int64_t k0, int wave, const uint64_t *mask)
     {
+        if constexpr (MASKED) {
+            live = (const __attribute__((address_space(4))) uint64_t *)(mask + k0 / 64);
+            bit = (int)(k0 & 32);
+            bits = *live;
+        }
         constexpr int kMost = PAIRED ? ROWS / 2 : ROWS;
         rows = (int)(n - r0 < kMost ? n - r0 : kMost);
         if (PAIRED && (wave & 1)) r0 += n;
@@ -127,6 +138,12 @@ struct Side {
     {
         uint32_t bytes;
         past = 0;
+        if constexpr (MASKED) {
+            const int lane = threadIdx.x & 63;
+            dead = ~(uint32_t)(bits >> (bit + wave * kCopies * kK + lane / kPer));
+            bit = kDeep == 64 ? 0 : bit ^ 32;
+            if (bit == 0 && left > 0) bits = *++live;        // (one word more than there are k)
+        }
         if constexpr (ALONG) {
             bytes = (uint32_t)(rows - 1) * ldb + (uint32_t)(left < kDeep ? (left + kPiece - 1) & ~(kPiece - 1) : kDeep) * kSize;   // (whole pieces)
             past = chunk * kPiece < left ? 0u : 0x80000000u;                // (`bytes` is below 2^31)
@@ -143,7 +160,9 @@ struct Side {
     __device__ __forceinline__ void copy(int u) const
     {
         constexpr int kStep = ALONG ? 8 : kK;
-        copy_to_lds(__builtin_amdgcn_readfirstlane(to + u * 1024), from[u & 1] + (uint32_t)(u * kStep) * ldb + past, buffer);
+        uint32_t offset = from[u & 1] + (uint32_t)(u * kStep) * ldb + past;
+        if constexpr (MASKED) offset |= (dead << (31 - u * kK)) & 0x80000000u;     // (beyond the buffer's end)
+        copy_to_lds(__builtin_amdgcn_readfirstlane(to + u * 1024), offset, buffer);
     }
 
     // Fragment f of step s (32 bytes along k) from buffer `b`: row lane % 32, the (lane / 32)-th 16 bytes.
@@ -519,7 +538,7 @@ struct Task {
 
 // Workgroup `block` of `blocks`: they stay and take tile after tile, so that the copies for the next tile are under way while
 // this one's sums leave.  `args`: where the kernel's argument with the product lies.
-template <class T, bool ALONG_A, bool ALONG_B, int WI, int WJ, int FI, int FJ, class WAY>
+template <class T, bool ALONG_A, bool ALONG_B, int WI, int WJ, int FI, int FJ, class WAY, bool MASKED = false>
 __device__ __forceinline__ void run_tiles(const Task &task, ProductArgs args, int block, int blocks)
 {
     const Product &q = task.q;
@@ -553,7 +572,7 @@ __device__ __forceinline__ void run_tiles(const Task &task, ProductArgs args, in
 
     constexpr int kDeep = kDeepOf<T>;
     Side<T, ALONG_A, kI, kNW, FI> a;
-    Side<T, ALONG_B, kJ, kNW, FJ, WAY::kPaired> b;
+    Side<T, ALONG_B, kJ, kNW, FJ, WAY::kPaired, MASKED> b;
     a.start(q.A, lds0, wave, wi * FI * 32);
     b.start(q.B, lds0 + 2 * a.kBytes, wave, wj * FJ * 32);
     // The copies run two steps ahead of the products, over the ends of tiles.
@@ -563,8 +582,8 @@ __device__ __forceinline__ void run_tiles(const Task &task, ProductArgs args, in
     auto enter = [&]() {
         if (ahead >= run) return;
         const Place p = place(ahead);
-        a.tile(q.A, p.i0, q.M, (int64_t)p.share * q.share, wave);
-        b.tile(q.B, p.j0, q.N, (int64_t)p.share * q.share, wave);
+        a.tile(q.A, p.i0, q.M, (int64_t)p.share * q.share, wave, nullptr);
+        b.tile(q.B, p.j0, q.N, (int64_t)p.share * q.share, wave, q.s.live);
         left = p.length;
     };
     auto aim = [&](int buffer) {
@@ -663,10 +682,10 @@ __device__ __forceinline__ void run_tiles(const Task &task, ProductArgs args, in
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (no copy into LDS outlives the workgroup)
 }
 
-template <class T, bool ALONG_A, bool ALONG_B, int WI, int WJ, int FI, int FJ, class WAY>
+template <class T, bool ALONG_A, bool ALONG_B, int WI, int WJ, int FI, int FJ, class WAY, bool MASKED>
 __global__ __launch_bounds__(WI * WJ * 64) void fb_mfma_product_kernel(Task task)
 {
-    run_tiles<T, ALONG_A, ALONG_B, WI, WJ, FI, FJ, WAY>(task, (ProductArgs)__builtin_amdgcn_kernarg_segment_ptr(), blockIdx.x, gridDim.x);
+    run_tiles<T, ALONG_A, ALONG_B, WI, WJ, FI, FJ, WAY, MASKED>(task, (ProductArgs)__builtin_amdgcn_kernarg_segment_ptr(), blockIdx.x, gridDim.x);
 }
 
 // A kernel's tile, on-chip memory and the workgroups that the GPU holds.
@@ -700,13 +719,13 @@ int take_lds(K kernel)
     return e == hipSuccess ? FB_OK : fail(FB_EHIP, std::string("hipFuncSetAttribute(LDS size): ") + hipGetErrorString(e));
 }
 
-template <class T, bool ALONG_A, bool ALONG_B, int WI, int WJ, int FI, int FJ, class WAY>
+template <class T, bool ALONG_A, bool ALONG_B, int WI, int WJ, int FI, int FJ, class WAY, bool MASKED = false>
 int launch(const Product &q, hipStream_t stream)
 {
     typedef Shape<WI, WJ, FI, FJ> S;
     const int64_t blocks = blocks_of<S>(q, WAY::kPaired);
     if (blocks >= kMostSize) return fail(FB_EUNSUPPORTED, "affine product: more than 2^31 tiles");
-    const auto kernel = fb_mfma_product_kernel<T, ALONG_A, ALONG_B, WI, WJ, FI, FJ, WAY>;
+    const auto kernel = fb_mfma_product_kernel<T, ALONG_A, ALONG_B, WI, WJ, FI, FJ, WAY, MASKED>;
     const int rc = take_lds<S>(kernel);
     if (rc != FB_OK) return rc;
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(WI * WJ * 64), S::kBytes, stream, task_of<S>(q, WAY::kPaired));

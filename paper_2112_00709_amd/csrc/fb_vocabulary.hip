@@ -391,7 +391,7 @@ struct RowParams {
     uint32_t *peaks;         // half precision: of the largest finite bound of |dz|, nullable
     int n_peaks;
     float *undo;
-    int32_t *counts;         // negative: nothing of the row counts
+    uint64_t *live;          // see Scores
 };
 
 __device__ __forceinline__ f32x4 row_of(const RowParams &p, int64_t i)
@@ -430,9 +430,11 @@ __global__ __launch_bounds__(256) void fb_scores_rows_kernel(RowParams p)
         if (blockIdx.x == 0 && threadIdx.x == 0) *p.undo = undo;
     }
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    f32x4 r = {kInf, 0.0f, 0.0f, 0.0f};
+    if (i < p.M) r = row_of(p, i);
+    const uint64_t live = __builtin_amdgcn_ballot_w64(r[0] != kInf);
+    if ((threadIdx.x & 63) == 0) p.live[i / 64] = live;
     if (i >= p.M) return;
-    f32x4 r = row_of(p, i);
-    p.counts[i] = r[0] == kInf ? -1 : 0;
     r[0] = -r[0];
     r[1] *= -scale;
     r[2] *= -scale;
@@ -509,12 +511,12 @@ constexpr int64_t kPieceBytes = (int64_t)512 << 20;
 struct ScoreGradPlan {
     int64_t width, pieces, ldz;
     Product z, dx, dw;       // of a whole piece
-    Packed x, w;             // x is always copied: rows that do not count are zeros then
+    Packed x, w;
     int64_t sum_rows;
-    size_t dz, rows, counts, range, sums, acc, part_x, part_w, bytes;
+    size_t dz, rows, live, range, sums, acc, part_x, part_w, bytes;
 };
 
-ScoreGradPlan score_grad_plan(const void *weight, int64_t ldw, int64_t M, int64_t V, int64_t K, int type)
+ScoreGradPlan score_grad_plan(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t V, int64_t K, int type)
 {
     ScoreGradPlan g{};
     const int64_t size = (int64_t)type_bytes(type), longest = ((int64_t)1 << 22) / size - 256;
@@ -529,21 +531,19 @@ ScoreGradPlan score_grad_plan(const void *weight, int64_t ldw, int64_t M, int64_
     plan(g.z, 0, true);
     plan(g.dx);
     plan(g.dw);
-    g.x.copy = true;
-    g.x.ld = line_distance(K, type);
-    g.x.bytes = aligned((size_t)M * (size_t)g.x.ld * type_bytes(type));
+    g.x = packed(x, ldx, M, K, type);
     g.w = packed(weight, ldw, V, K, type);
     const int64_t fragment = g.z.tile == 256 ? 128 : g.z.tile / 2;        // rows of a wave
     g.sum_rows = (M + g.z.tile - 1) / g.z.tile * (g.z.tile / fragment);
     g.dz = aligned((size_t)M * (size_t)g.ldz * type_bytes(type));
     g.rows = aligned((size_t)M * sizeof(f32x4));
-    g.counts = aligned((size_t)M * sizeof(int32_t));
+    g.live = aligned((size_t)((M + 255) / 256 * 4 + 1) * sizeof(uint64_t));
     g.range = aligned((kPeakGroups + 1) * sizeof(float));
     g.sums = aligned((size_t)g.sum_rows * (size_t)g.width * sizeof(float));
     g.acc = g.pieces > 1 ? aligned((size_t)M * (size_t)K * sizeof(float)) : 0;
     g.part_x = product_bytes(g.dx);
     g.part_w = product_bytes(g.dw);
-    g.bytes = g.x.bytes + g.w.bytes + g.dz + g.rows + g.counts + g.range + g.sums + g.acc + g.part_x + g.part_w;
+    g.bytes = g.x.bytes + g.w.bytes + g.dz + g.rows + g.live + g.range + g.sums + g.acc + g.part_x + g.part_w;
     return g;
 }
 
@@ -611,10 +611,8 @@ int fb_affine_logprobs(const void *x, int64_t ldx, const void *weight, int64_t l
 size_t fb_affine_logprobs_grad_workspace_bytes(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t V, int64_t K, int type)
 {
     using namespace fb;
-    (void)x;
-    (void)ldx;
     if (bad_sizes(M, V, K) || !known_type(type)) return 0;
-    return score_grad_plan(weight, ldw, M, V, K, type).bytes;
+    return score_grad_plan(x, ldx, weight, ldw, M, V, K, type).bytes;
 }
 
 int fb_affine_logprobs_grad(const void *x, int64_t ldx, const void *weight, int64_t ldw, const float *bias, const int32_t *tokens, const float *logz,
@@ -629,15 +627,15 @@ int fb_affine_logprobs_grad(const void *x, int64_t ldx, const void *weight, int6
         if (dx && bad_ld(lddx, K)) return fail(FB_EINVAL, "fb_affine_logprobs_grad: rows of dx closer than K elements");
         if (dx && too_far(lddx)) return fail(FB_EUNSUPPORTED, "fb_affine_logprobs_grad: rows of dx 2^27 elements apart");
         if (!dx && !dweight && !dbias) return FB_OK;
-        ScoreGradPlan g = score_grad_plan(weight, ldw, M, V, K, type);
+        const ScoreGradPlan g = score_grad_plan(x, ldx, weight, ldw, M, V, K, type);
         if (!ws || ws_bytes < g.bytes) return fail(FB_EINVAL, "fb_affine_logprobs_grad: workspace missing or too small");
         hipStream_t st = (hipStream_t)stream;
-        char *xs = (char *)ws, *wts = xs + g.x.bytes, *dz = wts + g.w.bytes, *rows = dz + g.dz, *counts = rows + g.rows, *range = counts + g.counts, *sums = range + g.range;
+        char *xs = (char *)ws, *wts = xs + g.x.bytes, *dz = wts + g.w.bytes, *rows = dz + g.dz, *live = rows + g.rows, *range = live + g.live, *sums = range + g.range;
         char *acc = sums + g.sums, *part_x = acc + g.acc, *part_w = part_x + g.part_x;
         const int64_t size = (int64_t)type_bytes(type);
         float *undo = type == FB_TYPE_F16 ? (float *)range : nullptr;
         if (M > 0) {
-            RowParams r{tokens, logz, entropy, g_logprobs, g_entropy, M, (f32x4 *)rows, undo ? (uint32_t *)(undo + 1) : nullptr, 0, undo, (int32_t *)counts};
+            RowParams r{tokens, logz, entropy, g_logprobs, g_entropy, M, (f32x4 *)rows, undo ? (uint32_t *)(undo + 1) : nullptr, 0, undo, (uint64_t *)live};
             r.n_peaks = (int)std::min<int64_t>(kPeakGroups, (M + 255) / 256);
             if (undo) {
                 hipLaunchKernelGGL(fb_scores_peak_kernel, dim3((unsigned)r.n_peaks), dim3(256), 0, st, r);
@@ -646,24 +644,23 @@ int fb_affine_logprobs_grad(const void *x, int64_t ldx, const void *weight, int6
             hipLaunchKernelGGL(fb_scores_rows_kernel, dim3((unsigned)((M + 255) / 256)), dim3(256), 0, st, r);
             if ((rc = launched("scores rows kernel launch: ")) != FB_OK) return rc;
             Prepare jobs;
-            SlopeParams copy = pack_job(g.x, x, ldx, M, K, xs);
-            copy.counts = (const int32_t *)counts;
-            jobs.add(copy, type);
+            if (g.x.copy) jobs.add(pack_job(g.x, x, ldx, M, K, xs), type);
             if (g.w.copy) jobs.add(pack_job(g.w, weight, ldw, V, K, wts), type);
             if ((rc = launch_prepare(jobs, type, type, st)) != FB_OK) return rc;
         }
         const char *w = g.w.copy ? wts : (const char *)weight;
+        const void *rows_of_x = g.x.copy ? xs : x;
         for (int64_t v0 = 0; v0 < V; v0 += g.width) {
             const int64_t n = std::min(g.width, V - v0);
             const bool first = v0 == 0, last = v0 + n == V;
             Product z = g.z, qx = g.dx, qw = g.dw;
             z.N = n; qx.K = n; qw.M = n;
-            z.A = {xs, g.x.ld, true};
+            z.A = {rows_of_x, g.x.ld, true};
             z.B = {w + v0 * g.w.ld * size, g.w.ld, true};
             z.f.bias = bias ? bias + v0 : nullptr;
             z.f.y = dz; z.f.ldy = line_distance(n, type);
             z.f.undo = undo;
-            z.s = {tokens, (int)v0, nullptr, nullptr, rows, g_entropy != nullptr, dbias ? (float *)sums : nullptr};
+            z.s = {tokens, (int)v0, nullptr, nullptr, rows, dbias ? (float *)sums : nullptr, nullptr};
             if (M > 0 && (rc = launch_scores<Slopes>(z, st)) != FB_OK) return rc;
             qx.A = {dz, z.f.ldy, true};
             qx.B = {z.B.p, g.w.ld, false};
@@ -677,7 +674,8 @@ int fb_affine_logprobs_grad(const void *x, int64_t ldx, const void *weight, int6
                 qx.f.y = dx; qx.f.ldy = lddx; qx.f.out_type = type;
             }
             qw.A = {dz, z.f.ldy, false};
-            qw.B = {xs, g.x.ld, false};
+            qw.B = {rows_of_x, g.x.ld, false};
+            qw.s.live = (const uint64_t *)live;
             qw.f.y = dweight ? (char *)dweight + v0 * K * size : nullptr; qw.f.ldy = K; qw.f.out_type = type;
             qw.f.undo = undo;
             qw.part = (float *)part_w;
