@@ -235,6 +235,42 @@ __device__ __forceinline__ float act_slope(float z, int act)
     return 1.0f;
 }
 
+// act(z) and act'(z) together: they share their exponentials.
+__device__ __forceinline__ void act_and_slope(float z, int act, float &value, float &slope)
+{
+    if (act == FB_ACT_GELU) {
+        float e;
+        const float h = normal_tail(z, e), p = z > 0.0f ? 1.0f - h : h;
+        value = z * p;
+        slope = fmaf(z * e, 0.39894228040143267794f, p);
+    } else if (act == FB_ACT_SILU) {
+        const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -kLog2E));
+        value = z * s;
+        slope = s * fmaf(z, 1.0f - s, 1.0f);
+    } else {
+        value = act_of(z, act);
+        slope = act_slope(z, act);
+    }
+}
+
+// A number that |act(z)| does not exceed, and is not far above it: z is where z > 0, and the least value of gelu is -0.17, of silu
+// -0.2785.  NaN for NaN.
+__device__ __forceinline__ float act_bound(float z, int act)
+{
+    if (act == FB_ACT_NONE) return fabsf(z);
+    if (act == FB_ACT_SIGMOID) return z != z ? z : 1.0f;
+    const float least = act == FB_ACT_RELU ? 0.0f : act == FB_ACT_GELU ? 0.171f : 0.279f;
+    return z < least ? least : z;
+}
+// The same of |act'(z)|.
+__device__ __forceinline__ float slope_bound(float z, int act)
+{
+    if (act == FB_ACT_NONE) return 1.0f;
+    if (act == FB_ACT_SIGMOID) return 0.25f;
+    if (act == FB_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
+    return z > 0.0f ? 1.13f : 0.51f;
+}
+
 // The power of two for a largest |dy|, and its inverse; both are normal numbers whatever the largest is.
 __device__ __forceinline__ void range_of(const uint32_t *peaks, int n, float &scale, float &undo)
 {

@@ -102,7 +102,8 @@ int launch_gated_join(const Product &q, hipStream_t stream)
 }
 
 // dz = [dy u act'(g), dy act(g)], rounded to the factors' type, and the sums of its columns before the rounding.  Bound by memory.
-// A thread has one piece of the width, of both halves; the layout of threads is that of rows of N (lay_out).
+// A thread has one piece of the width, of both halves; the layout of threads is that of rows of N (lay_out).  A row's last piece ends where
+// the row does: what it has in common with the one before is formed and stored twice, alike, and summed once.
 struct GatedSlopeParams {
     const void *dy, *z;
     int64_t lddy, ldz, M, N, ldo;
@@ -128,8 +129,10 @@ __device__ __forceinline__ void slopes_of(const u32x4 &rd, const u32x4 &rg, cons
     auto by = [&](int which) {
 #pragma unroll
         for (int e = 0; e < VE; ++e) {
-            dg[e] = d[e] * u[e] * act_slope(g[e], which);
-            du[e] = d[e] * act_of(g[e], which);
+            float value, slope;
+            act_and_slope(g[e], which, value, slope);
+            dg[e] = d[e] * u[e] * slope;
+            du[e] = d[e] * value;
         }
     };
     if (act == FB_ACT_SILU) by(FB_ACT_SILU);
@@ -146,8 +149,8 @@ __global__ __launch_bounds__(256) void fb_gated_slope_kernel(GatedSlopeParams p)
     __shared__ float slots[256][2 * VE + 1];
     const int across = blockIdx.x % p.wide, down = blockIdx.x / p.wide;
     const int lane = threadIdx.x & (p.lanes - 1), sub = threadIdx.x / p.lanes, subs = 256 / p.lanes;
-    const int64_t at = ((int64_t)across * p.lanes + lane) * VE;
-    const int n = at >= p.N ? 0 : (int)(p.N - at < VE ? p.N - at : VE);
+    const int64_t whole = p.N < VE ? 0 : p.N - VE, from = ((int64_t)across * p.lanes + lane) * VE, at = from < whole ? from : whole;
+    const int n = from >= p.N ? 0 : (int)(p.N < VE ? p.N : VE), seen = (int)(from - at);
     float sum[2 * VE] = {}, scale = 1.0f;
     if constexpr (std::is_same<T, f16>::value) {
         if (p.peaks) {
@@ -158,7 +161,7 @@ __global__ __launch_bounds__(256) void fb_gated_slope_kernel(GatedSlopeParams p)
     }
     if (n > 0) {
         const int64_t step = (int64_t)p.down * subs;
-        const int zeros = at + VE >= p.N ? (int)((VE - 2 * p.N % VE) % VE) : 0;       // of the row's last piece, that the products read
+        const int zeros = at == whole ? (int)((VE - 2 * p.N % VE) % VE) : 0;       // of the row's last piece, that the products read
         for (int64_t r0 = (int64_t)down * subs + sub; r0 < p.M; r0 += kPairsAhead * step) {
             u32x4 rd[kPairsAhead], rg[kPairsAhead], ru[kPairsAhead];
 #pragma unroll
@@ -177,7 +180,7 @@ __global__ __launch_bounds__(256) void fb_gated_slope_kernel(GatedSlopeParams p)
                 slopes_of<T>(rd[a], rg[a], ru[a], p.act, d, d + VE);
 #pragma unroll
                 for (int e = 0; e < 2 * VE; ++e) {
-                    sum[e] += d[e];
+                    sum[e] += e % VE >= seen ? d[e] : 0.0f;
                     d[e] *= scale;
                 }
                 if (!p.out) continue;
@@ -197,29 +200,32 @@ __global__ __launch_bounds__(256) void fb_gated_slope_kernel(GatedSlopeParams p)
         const int64_t col = (int64_t)across * p.lanes * VE + k;
         if (col >= p.N) continue;
         float s = 0.0f;
-        for (int i = 0; i < subs; ++i) s += slots[i * p.lanes + k / VE][half * VE + k % VE];
+        const int64_t first = col / VE * VE;
+        const int e = (int)(col - (first < whole ? first : whole));
+        for (int i = 0; i < subs; ++i) s += slots[i * p.lanes + k / VE][half * VE + e];
         p.part[(size_t)down * 2 * p.N + half * p.N + col] = s;
     }
 }
 
-// The largest finite |dz|, a share a workgroup (half precision: what fb_affine_grad finds of dy, here of dz itself, as u and act(g) are
-// not bounded).
+// The largest finite bound of |dz|, |dy| max(|u| slope_bound(g), act_bound(g)), a share a workgroup (half precision: what fb_affine_grad finds of dy,
+// here with u and act(g), which are not bounded).  Bound by memory.
 __global__ __launch_bounds__(1024) void fb_gated_peak_kernel(GatedSlopeParams p)
 {
     constexpr int VE = Vec<f16>::kN, kAhead = 2;
     __shared__ uint32_t slots[16];
     const int64_t pieces = (p.N + VE - 1) / VE, step = (int64_t)gridDim.x * 1024, down = step / pieces, across = step - down * pieces;
-    const int64_t at = (int64_t)blockIdx.x * 1024 + threadIdx.x;
+    const int64_t whole = p.N < VE ? 0 : p.N - VE, at = (int64_t)blockIdx.x * 1024 + threadIdx.x;
     int64_t r = at / pieces, c = at - r * pieces;
     uint32_t peak = 0;
     while (r < p.M) {
         u32x4 rd[kAhead], rg[kAhead], ru[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const int n = r < p.M ? (int)(p.N - c * VE) : 0;
-            rd[u] = load_piece((const f16 *)p.dy + r * p.lddy + c * VE, n);
-            rg[u] = load_piece((const f16 *)p.z + r * p.ldz + c * VE, n);
-            ru[u] = load_piece((const f16 *)p.z + r * p.ldz + p.N + c * VE, n);
+            const int64_t j = c * VE < whole ? c * VE : whole;     // (a row's last piece ends with it)
+            const int n = r < p.M ? (int)(p.N - j) : 0;
+            rd[u] = load_piece((const f16 *)p.dy + r * p.lddy + j, n);
+            rg[u] = load_piece((const f16 *)p.z + r * p.ldz + j, n);
+            ru[u] = load_piece((const f16 *)p.z + r * p.ldz + p.N + j, n);
             r += down;
             c += across;
             if (c >= pieces) {
@@ -229,12 +235,18 @@ __global__ __launch_bounds__(1024) void fb_gated_peak_kernel(GatedSlopeParams p)
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            float d[2 * VE];
-            slopes_of<f16>(rd[u], rg[u], ru[u], p.act, d, d + VE);
+            float d[VE], g[VE], v[VE];
+            unpack<f16>(rd[u], d);
+            unpack<f16>(rg[u], g);
+            unpack<f16>(ru[u], v);
 #pragma unroll
-            for (int e = 0; e < 2 * VE; ++e) {
-                const uint32_t a = __float_as_uint(d[e]) & 0x7fffffffu;
-                peak = a < 0x7f800000u && a > peak ? a : peak;
+            for (int e = 0; e < VE; ++e) {
+                const float du = d[e] * act_bound(g[e], p.act), dg = d[e] * v[e] * slope_bound(g[e], p.act);
+                uint32_t a = __float_as_uint(du) & 0x7fffffffu, b = __float_as_uint(dg) & 0x7fffffffu;
+                a = a < 0x7f800000u ? a : 0u;
+                b = b < 0x7f800000u ? b : 0u;
+                a = a > b ? a : b;
+                peak = a > peak ? a : peak;
             }
         }
     }
