@@ -10,7 +10,7 @@ namespace {
 
 // Sums of a wave leave as y = act(g) u, formed in the registers that have them, and as g and u.
 struct Gated {
-    static constexpr bool kPaired = true;
+    static constexpr bool kPaired = true, kNeverEmpty = true;
     static constexpr int kEarly = 1;
 
     template <int FI, int FJ>

@@ -61,10 +61,9 @@ __device__ __forceinline__ void unpack(const u32x4 &r, float *v)
 template <class T>
 __device__ __forceinline__ uint32_t pack2(float a, float b)
 {
-    const T h[2] = {(T)a, (T)b};
-    uint32_t u;
-    __builtin_memcpy(&u, h, 4);
-    return u;
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef T pair __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), pair));     // (one instruction for both, where there is one)
 }
 
 template <class T>

@@ -392,7 +392,7 @@ __device__ __forceinline__ void bias_of(const float *bias, int64_t n, int64_t j,
 
 template <int KIND>
 struct Finished {
-    static constexpr bool kPaired = false;
+    static constexpr bool kPaired = false, kNeverEmpty = false;
     static constexpr int kEarly = 1;       // fours of numbers that a lane asks for when a tile begins: its columns' bias
 
     template <int FI, int FJ>
@@ -505,7 +505,7 @@ struct Finished {
 
 // Sums leave rounded to the factors' 16 bits, as they are or times *undo: what gradients are.
 struct Rounded {
-    static constexpr bool kPaired = false;
+    static constexpr bool kPaired = false, kNeverEmpty = false;
     static constexpr int kEarly = 1;
 
     template <int FI, int FJ>
@@ -566,7 +566,7 @@ __device__ __forceinline__ void run_tiles(const Task &task, ProductArgs args, in
     };
 
     float undo = 1.0f;                     // (products of a half-precision gradient; shares of k leave as they are)
-    if constexpr (std::is_same<T, f16>::value && !ALONG_B) {
+    if constexpr (std::is_same<T, f16>::value && (!ALONG_B || WAY::kNeverEmpty)) {
         if (q.f.undo && !q.parts) undo = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(*q.f.undo)));
     }
 
@@ -627,6 +627,7 @@ __device__ __forceinline__ void run_tiles(const Task &task, ProductArgs args, in
     for (int in_run = block / 8; in_run < run; in_run += blocks / 8) {
         const Place p = place(in_run);
         const int steps = (int)((p.length + kDeep - 1) / kDeep);
+        if constexpr (WAY::kNeverEmpty) __builtin_assume(steps > 0);      // (or it would be waited for what `early` asks for)
         f32x16 acc[FI][FJ] = {};
         const Where where{p.share, p.i0, p.j0, wi, wj, wave, (float *)(lds_raw + 2 * (a.kBytes + b.kBytes))};
         f32x4 four[WAY::kEarly] = {};

@@ -58,26 +58,19 @@ __device__ __forceinline__ void bias_or_out(const Product &q, int64_t j, f32x4 &
     for (int e = 0; e < 4; ++e) four[e] = j + e < q.N ? (q.f.bias ? q.f.bias[j + e] : 0.0f) : -kInf;
 }
 
-// f(y, the element's place in acc[x][y]) where a row's token is among the wave's columns, in the lane that has it.  Rare: asked
-// for once a fragment.
-template <int FJ, class F>
-__device__ __forceinline__ void at_token(int token, int64_t j0, int lane, F f)
+// Which of a lane's FJ * 16 sums of a row is its token's (y 16 + k for acc[x][y][k]), -1 if it has none of them.  Few have: asked for
+// once a fragment, by a ballot.
+template <int FJ>
+__device__ __forceinline__ int place_of(int token, int64_t j0, int lane)
 {
     const int64_t far = (int64_t)token - j0;
     const int c = far >= 0 && far < FJ * 32 ? (int)far : -1;
-    if (__builtin_amdgcn_ballot_w64(c >= 0) == 0) return;
-    if (c >= 0 && (c >> 2 & 1) == lane >> 5) {
-#pragma unroll
-        for (int y = 0; y < FJ; ++y)
-#pragma unroll
-            for (int k = 0; k < 16; ++k)
-                if (c == y * 32 + (k >> 2) * 8 + (c & 4) + (k & 3)) f(y, k);
-    }
+    return c >= 0 && (c >> 2 & 1) == lane >> 5 ? (c >> 5) * 16 + (c >> 3 & 3) * 4 + (c & 3) : -1;
 }
 
 // Sums leave as each row's (m, S, T) over the tile's columns, and as the logits of given tokens.
 struct Reduced {
-    static constexpr bool kPaired = false;
+    static constexpr bool kPaired = false, kNeverEmpty = true;
     static constexpr int kEarly = 2;         // bias; tokens of the lane's rows
 
     template <int FI, int FJ>
@@ -86,7 +79,7 @@ struct Reduced {
         ask_columns<FJ>(q, where.j0 + where.wj * FJ * 32, lane, four[0]);
         const int64_t i = where.i0 + where.wi * FI * 32 + (lane & 31);
 #pragma unroll
-        for (int x = 0; x < FI; ++x) four[1][x] = __int_as_float(i + x * 32 < q.M ? max(q.s.tokens[i + x * 32], -1) - q.s.first : -1);
+        for (int x = 0; x < FI; ++x) four[1][x] = __int_as_float(q.s.tokens[i + x * 32 < q.M ? i + x * 32 : q.M - 1]);
     }
 
     template <class T, int FI, int FJ>
@@ -96,25 +89,33 @@ struct Reduced {
         asm volatile("" : "+s"(args), "+v"(lane));
         const int waves = blockDim.x / 64, across = FI == 4 ? 4 : 2, rows = waves / across * FI * 32;     // of the tile
         float *parts = where.room;
+        const float upper = lane < 32 ? 0.0f : 1.0f;
+        const f32x4 none = {upper, upper, upper, upper};
         const int64_t j0 = where.j0 + where.wj * FJ * 32;
 #pragma unroll
         for (int x = 0; x < FI; ++x) {
             const int row = (where.wi * FI + x) * 32 + (lane & 31);
             add_rank_one<FJ>(acc[x], four[0], 0.0f, lane);
-            at_token<FJ>(__float_as_int(four[1][x]), j0, lane, [&](int y, int k) { args->s.given[where.i0 + row] = acc[x][y][k]; });
+            const int place = where.i0 + row < args->M ? place_of<FJ>(__float_as_int(four[1][x]), j0, lane) : -1;
+            if (__builtin_amdgcn_ballot_w64(place >= 0)) {
+                float given = 0.0f;
+#pragma unroll
+                for (int k = 0; k < FJ * 16; ++k) given = place == k ? acc[x][k / 16][k % 16] : given;
+                if (place >= 0) args->s.given[where.i0 + row] = given;
+            }
             float m = acc[x][0][0];
 #pragma unroll
             for (int y = 0; y < FJ; ++y)
 #pragma unroll
                 for (int k = 0; k < 16; ++k) m = fmaxf(m, acc[x][y][k]);
             m = other_half_max(m);
-            const float from = m < kOut ? 0.0f : m;      // (their difference first: a product with m has its rounding)
+            add_rank_one<FJ>(acc[x], none, m < kOut ? 0.0f : -m, lane);      // (the difference first: a product with m has its rounding)
             float S = 0.0f, U = 0.0f;
 #pragma unroll
             for (int y = 0; y < FJ; ++y)
 #pragma unroll
                 for (int k = 0; k < 16; ++k) {
-                    const float d = (acc[x][y][k] - from) * kLog2E, e = __builtin_amdgcn_exp2f(d);
+                    const float d = acc[x][y][k] * kLog2E, e = __builtin_amdgcn_exp2f(d);
                     S += e;
                     U = fmaf(e, fmaxf(d, kFarOut), U);
                 }
@@ -144,67 +145,78 @@ struct Reduced {
 };
 
 // Sums leave as the logits' gradient, rounded to the factors' type, and as shares of its column sums before that.  Of a row there
-// are (-log Z, a, h, g):  dz = g [j = token] + p (a + h log p),  with a = -(g + h' entropy) and h = -h' for the entropy's gradient h'.  Rows
+// are (-log Z, a, h, g):  dz = g [j = token] + p (a + h log2 p),  with a = -(g + h' entropy) and h = -h' ln 2 for the entropy's gradient h'.  Rows
 // that do not count have log Z = inf and zeros.  A fragment's rows pass through LDS, in the factors' type, so that whole runs of a row
-// are stored; rows of dz are whole 16-byte pieces.
+// are stored; rows of dz are whole 16-byte pieces.  There are whole 256 rows and tokens (those past M do not count): they are asked for when
+// a tile begins, all at once; asked for at its end, with a condition each, they took a third of the time of 256 x 256 logits of 1024.
 struct Slopes {
-    static constexpr bool kPaired = false;
-    static constexpr int kEarly = 1;
+    static constexpr bool kPaired = false, kNeverEmpty = true;
+    static constexpr int kEarly = 6;         // columns; rows, four at most; tokens of the lane's rows
 
     template <int FI, int FJ>
-    static __device__ __forceinline__ void early(const Product &q, const Where &where, int lane, f32x4 (&four)[1])
+    static __device__ __forceinline__ void early(const Product &q, const Where &where, int lane, f32x4 (&four)[6])
     {
+        const int64_t i = where.i0 + where.wi * FI * 32 + (lane & 31);
+#pragma unroll
+        for (int x = 0; x < FI; ++x) {
+            four[1 + x] = ((const f32x4 *)q.s.rows)[i + x * 32];
+            four[5][x] = __int_as_float(q.s.tokens[i + x * 32]);
+        }
         ask_columns<FJ>(q, where.j0 + where.wj * FJ * 32, lane, four[0]);
     }
 
     template <class T, int FI, int FJ>
-    static __device__ __forceinline__ void leave(ProductArgs args, f32x16 (&acc)[FI][FJ], const f32x4 (&four)[1], float, const Where &where)
+    static __device__ __forceinline__ void leave(ProductArgs args, f32x16 (&acc)[FI][FJ], const f32x4 (&four)[6], float undo, const Where &where)
     {
         int lane = threadIdx.x & 63;
         asm volatile("" : "+s"(args), "+v"(lane));
         const int64_t M = args->M, i0 = where.i0 + where.wi * FI * 32, j0 = where.j0 + where.wj * FJ * 32;
         const int64_t first = j0 + args->s.first, wide = (args->N + Vec<T>::kN - 1) / Vec<T>::kN * Vec<T>::kN;
-        f32x4 of_row[FI];
-        int token[FI];
-#pragma unroll
-        for (int x = 0; x < FI; ++x) {
-            const int64_t i = i0 + x * 32 + (lane & 31);
-            of_row[x] = f32x4{-kInf, 0.0f, 0.0f, 0.0f};
-            token[x] = -1;
-            if (i < M) {
-                of_row[x] = ((const f32x4 *)args->s.rows)[i];
-                token[x] = args->s.tokens[i];
-            }
-        }
         f32x16 sum[FJ] = {};
+#pragma unroll
+        for (int x = 0; x < FI; ++x) add_rank_one<FJ>(acc[x], four[0], four[1 + x][0], lane);
 #pragma unroll
         for (int x = 0; x < FI; ++x) {
             f32x16(&v)[FJ] = acc[x];
-            add_rank_one<FJ>(v, four[0], of_row[x][0], lane);
+            const f32x4 of_row = four[1 + x];
 #pragma unroll
             for (int y = 0; y < FJ; ++y)
 #pragma unroll
                 for (int k = 0; k < 16; ++k) {
-                    const float d = fmaxf(v[y][k], kFarOut);
-                    v[y][k] = __builtin_amdgcn_exp2f(d * kLog2E) * fmaf(of_row[x][2], d, of_row[x][1]);
+                    const float d = fmaxf(v[y][k] * kLog2E, kFarOut);
+                    v[y][k] = __builtin_amdgcn_exp2f(d) * fmaf(of_row[2], d, of_row[1]);
                 }
-            at_token<FJ>(token[x], first, lane, [&](int y, int k) { v[y][k] += of_row[x][3]; });
+            const int place = place_of<FJ>(__float_as_int(four[5][x]), first, lane);
+            if (__builtin_amdgcn_ballot_w64(place >= 0)) {
+#pragma unroll
+                for (int k = 0; k < FJ * 16; ++k) v[k / 16][k % 16] += place == k ? of_row[3] : 0.0f;
+            }
 #pragma unroll
             for (int y = 0; y < FJ; ++y) sum[y] += v[y];
             store_fragments<T, FJ, true>(v, where.room + where.wave * 16 * FJ * 32, (T *)args->f.y, args->f.ldy, i0 + x * 32, j0, M, wide, lane, false);
         }
         if (!args->s.sums) return;
-        const float undo = args->f.undo ? *args->f.undo : 1.0f;
         // 32 rows of a column added: two of a lane's columns at a time over the rows of 16 lanes, so that lanes 16 .. 31 and 48 .. 63 have
         // the second fragment's.
-        float *out = args->s.sums + (size_t)(i0 / (FI * 32)) * (size_t)args->N;
-        const int64_t j = j0 + (FJ == 2 ? (lane >> 4 & 1) * 32 : 0) + (lane >> 5) * 4;
+        f32x4 total[4];
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
             const auto two = __builtin_amdgcn_permlane16_swap(__float_as_uint(sum[0][k]), __float_as_uint(sum[FJ - 1][k]), false, false);
-            const float s = sum_row16(__uint_as_float(two[0]) + __uint_as_float(two[1])) * undo;
-            const int64_t c = j + (k >> 2) * 8 + (k & 3);
-            if ((lane & (FJ == 2 ? 15 : 31)) == 0 && c < args->N) out[c] = s;
+            total[k / 4][k % 4] = sum_row16(__uint_as_float(two[0]) + __uint_as_float(two[1])) * undo;
+        }
+        const int64_t N = args->N, j = j0 + (FJ == 2 ? (lane >> 4 & 1) * 32 : 0) + (lane >> 5) * 4;
+        float *out = args->s.sums + (size_t)(i0 / (FI * 32)) * (size_t)N + j;
+        if ((lane & (FJ == 2 ? 15 : 31)) == 0) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (j + 8 * e + 3 < N) {
+                    *(f32x4_any *)(out + 8 * e) = total[e];
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 3; ++r)
+                        if (j + 8 * e + r < N) out[8 * e + r] = total[e][r];
+                }
+            }
         }
     }
 };
@@ -420,6 +432,7 @@ struct RowParams {
     int n_peaks;
     float *undo;
     uint64_t *live;          // see Scores
+    int32_t *picks;          // [whole 256 rows], as rows are: the tokens, -1 where a row does not count
 };
 
 __device__ __forceinline__ f32x4 row_of(const RowParams &p, int64_t i)
@@ -462,10 +475,10 @@ __global__ __launch_bounds__(256) void fb_scores_rows_kernel(RowParams p)
     if (i < p.M) r = row_of(p, i);
     const uint64_t live = __builtin_amdgcn_ballot_w64(r[0] != kInf);
     if ((threadIdx.x & 63) == 0) p.live[i / 64] = live;
-    if (i >= p.M) return;
+    p.picks[i] = r[0] != kInf ? p.tokens[i] : -1;
     r[0] = -r[0];
     r[1] *= -scale;
-    r[2] *= -scale;
+    r[2] *= -scale * kLn2;
     r[3] *= scale;
     p.rows[i] = r;
 }
@@ -541,7 +554,7 @@ struct ScoreGradPlan {
     Product z, dx, dw;       // of a whole piece
     Packed x, w;
     int64_t sum_rows;
-    size_t dz, rows, live, range, sums, acc, part_x, part_w, bytes;
+    size_t dz, rows, picks, live, range, sums, acc, part_x, part_w, bytes;
 };
 
 ScoreGradPlan score_grad_plan(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t V, int64_t K, int type)
@@ -564,14 +577,15 @@ ScoreGradPlan score_grad_plan(const void *x, int64_t ldx, const void *weight, in
     const int64_t fragment = g.z.tile == 256 ? 128 : g.z.tile / 2;        // rows of a wave
     g.sum_rows = (M + g.z.tile - 1) / g.z.tile * (g.z.tile / fragment);
     g.dz = aligned((size_t)M * (size_t)g.ldz * type_bytes(type));
-    g.rows = aligned((size_t)M * sizeof(f32x4));
+    g.rows = aligned((size_t)((M + 255) / 256 * 256) * sizeof(f32x4));
+    g.picks = aligned((size_t)((M + 255) / 256 * 256) * sizeof(int32_t));
     g.live = aligned((size_t)((M + 255) / 256 * 4 + 1) * sizeof(uint64_t));
     g.range = aligned((kPeakGroups + 1) * sizeof(float));
     g.sums = aligned((size_t)g.sum_rows * (size_t)g.width * sizeof(float));
     g.acc = g.pieces > 1 ? aligned((size_t)M * (size_t)K * sizeof(float)) : 0;
     g.part_x = product_bytes(g.dx);
     g.part_w = product_bytes(g.dw);
-    g.bytes = g.x.bytes + g.w.bytes + g.dz + g.rows + g.live + g.range + g.sums + g.acc + g.part_x + g.part_w;
+    g.bytes = g.x.bytes + g.w.bytes + g.dz + g.rows + g.picks + g.live + g.range + g.sums + g.acc + g.part_x + g.part_w;
     return g;
 }
 
@@ -657,12 +671,12 @@ int fb_affine_logprobs_grad(const void *x, int64_t ldx, const void *weight, int6
         const ScoreGradPlan g = score_grad_plan(x, ldx, weight, ldw, M, V, K, type);
         if (!ws || ws_bytes < g.bytes) return fail(FB_EINVAL, "fb_affine_logprobs_grad: workspace missing or too small");
         hipStream_t st = (hipStream_t)stream;
-        char *xs = (char *)ws, *wts = xs + g.x.bytes, *dz = wts + g.w.bytes, *rows = dz + g.dz, *live = rows + g.rows, *range = live + g.live, *sums = range + g.range;
+        char *xs = (char *)ws, *wts = xs + g.x.bytes, *dz = wts + g.w.bytes, *rows = dz + g.dz, *picks = rows + g.rows, *live = picks + g.picks, *range = live + g.live, *sums = range + g.range;
         char *acc = sums + g.sums, *part_x = acc + g.acc, *part_w = part_x + g.part_x;
         const int64_t size = (int64_t)type_bytes(type);
         float *undo = type == FB_TYPE_F16 ? (float *)range : nullptr;
         if (M > 0) {
-            RowParams r{tokens, logz, entropy, g_logprobs, g_entropy, M, (f32x4 *)rows, undo ? (uint32_t *)(undo + 1) : nullptr, 0, undo, (uint64_t *)live};
+            RowParams r{tokens, logz, entropy, g_logprobs, g_entropy, M, (f32x4 *)rows, undo ? (uint32_t *)(undo + 1) : nullptr, 0, undo, (uint64_t *)live, (int32_t *)picks};
             r.n_peaks = (int)std::min<int64_t>(kPeakGroups, (M + 255) / 256);
             if (undo) {
                 hipLaunchKernelGGL(fb_scores_peak_kernel, dim3((unsigned)r.n_peaks), dim3(256), 0, st, r);
@@ -687,7 +701,7 @@ int fb_affine_logprobs_grad(const void *x, int64_t ldx, const void *weight, int6
             z.f.bias = bias ? bias + v0 : nullptr;
             z.f.y = dz; z.f.ldy = line_distance(n, type);
             z.f.undo = undo;
-            z.s = {tokens, (int)v0, nullptr, nullptr, rows, dbias ? (float *)sums : nullptr, nullptr};
+            z.s = {(const int32_t *)picks, (int)v0, nullptr, nullptr, rows, dbias ? (float *)sums : nullptr, nullptr};
             if (M > 0 && (rc = launch_scores<Slopes>(z, st)) != FB_OK) return rc;
             qx.A = {dz, z.f.ldy, true};
             qx.B = {z.B.p, g.w.ld, false};
