@@ -234,7 +234,7 @@ int64_t sum_rows(int64_t M, int64_t N, int type)
 // it holds at a time (1, 2 or 4) a start, an end and the latency of every step, and, where k is shared, the sums' way through
 // memory and a launch to join them.  In single precision a share is at most 4096 long, so that roundings do not pile up, as long as
 // 128 shares are enough for that (k up to 524288); with k above 4096 the sums always go through memory then, split M N floats of it.
-void plan(Product &q, int only_tile, bool whole)
+double plan(Product &q, int only_tile, bool whole)
 {
     static constexpr int kSplits[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64, 96, 128};
     struct Shape {                          // (see fb_affine_mfma.hip)
@@ -266,6 +266,29 @@ void plan(Product &q, int only_tile, bool whole)
     }
     q.split = std::max(q.split, 1);         // (K = 0, a gradient over no rows: sums of nothing)
     q.parts = !whole && (q.split > 1 || q.N < 4);       // (the kernel takes a residual by fours)
+    return best;
+}
+
+// Tiles of 256 in whole rounds of workgroups, and the rows that would make a last round, which is mostly empty, by tiles that fit them:
+// 69120 x 3000 x 1024 in bfloat16 has 1080 tiles for 256 compute units: 421 us, or 354 and 50.
+int launch_dx(const Product &q, hipStream_t stream)
+{
+    const int64_t across = (q.N + 255) / 256, tiles = (q.M + 255) / 256 * across, rounds = (tiles + kCUs - 1) / kCUs;
+    const int64_t rows = (rounds - 1) * kCUs / across * 256;
+    if (q.parts || q.tile != 256 || rounds < 2 || rows <= 0 || rows >= q.M) return launch_mfma_product(q, stream);
+    Product first = q, last = q, whole = q;
+    first.M = rows;
+    last.M = q.M - rows;
+    whole.M = 256;
+    whole.N = 256;
+    constexpr double kLaunch = 5000.0;
+    if (plan(last, 0, true) + kLaunch >= plan(whole, 256, true) || last.tile == 256) return launch_mfma_product(q, stream);
+    const auto skip = [&](const void *p, int64_t ld, int type) { return p ? (const char *)p + (size_t)rows * (size_t)ld * type_bytes(type) : nullptr; };
+    last.A.p = skip(q.A.p, q.A.ld, q.type);
+    last.f.y = (void *)skip(q.f.y, q.f.ldy, q.f.out_type);
+    last.f.residual = skip(q.f.residual, q.f.ldr, q.f.out_type);
+    const int rc = launch_mfma_product(first, stream);
+    return rc == FB_OK ? launch_mfma_product(last, stream) : rc;
 }
 
 // Products whose shares are to be joined (at most two) and columns to be added up (out), in one launch.
@@ -390,7 +413,7 @@ int launch_grad(GradPlan &g, const Factor &d, const float *undo, void *dx, int64
     if (dx && dweight && g.pair) {
         if ((rc = launch_mfma_pair(g.dx, g.dw, st)) != FB_OK) return rc;
     } else {
-        if (dx && M > 0 && (rc = launch_mfma_product(g.dx, st)) != FB_OK) return rc;
+        if (dx && M > 0 && (rc = launch_dx(g.dx, st)) != FB_OK) return rc;
         if (dweight && (rc = launch_mfma_product(g.dw, st)) != FB_OK) return rc;
     }
     return launch_join(dx ? &g.dx : nullptr, dweight ? &g.dw : nullptr, type, sums, rows, N, dbias, st);

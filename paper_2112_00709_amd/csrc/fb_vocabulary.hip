@@ -721,7 +721,7 @@ int fb_affine_logprobs_grad(const void *x, int64_t ldx, const void *weight, int6
             qw.f.undo = undo;
             qw.part = (float *)part_w;
             const bool has_dx = dx && M > 0;
-            if (has_dx && (rc = launch_mfma_product(qx, st)) != FB_OK) return rc;
+            if (has_dx && (rc = launch_dx(qx, st)) != FB_OK) return rc;
             if (dweight && (rc = launch_mfma_product(qw, st)) != FB_OK) return rc;
             rc = launch_join(has_dx ? &qx : nullptr, dweight ? &qw : nullptr, type, (const float *)sums, M > 0 ? g.sum_rows : 0, n, dbias ? dbias + v0 : nullptr, st);
             if (rc != FB_OK) return rc;
