@@ -116,6 +116,7 @@ inline size_t aligned(size_t n) { return (n + 255) & ~(size_t)255; }
 
 double plan(Product &q, int only_tile = 0, bool whole = false);   // tiles and shares of k (`whole`: one share); what it takes, in clocks
 inline size_t product_bytes(const Product &q) { return q.parts ? aligned((size_t)q.split * (size_t)q.M * (size_t)q.N * sizeof(float)) : 0; }
+bool plan_back(Product &dx, Product &dw);
 int launch_dx(const Product &q, hipStream_t stream);              // by launch_mfma_product, perhaps in two
 int launch_join(const Product *a, const Product *b, int type, const float *sums, int64_t rows, int64_t N, float *out, hipStream_t stream);
 

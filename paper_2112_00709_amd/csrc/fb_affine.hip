@@ -363,26 +363,30 @@ ForwardPlan forward_plan(const void *x, int64_t ldx, const void *weight, int64_t
 
 }  // namespace
 
+// Both products of a gradient; whether they go in one launch: small ones do, by tiles of one size, as each alone would start and end by
+// itself.
+bool plan_back(Product &dx, Product &dw)
+{
+    plan(dx);
+    plan(dw);
+    if (fits_as_pair(dx, dw)) return true;
+    if (dx.tile > 128 || dw.tile > 128 || dx.tile == dw.tile) return false;
+    Product x = dx, w = dw;
+    plan(x, 64);
+    plan(w, 64);
+    if (!fits_as_pair(x, w)) return false;
+    dx = x;
+    dw = w;
+    return true;
+}
+
 GradPlan grad_plan(const void *dy, int64_t lddy, int dy_type, const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t N,
                    int64_t K, int type, int act)
 {
     GradPlan g{};
     g.dx.M = M; g.dx.N = K; g.dx.K = N; g.dx.type = type;
     g.dw.M = N; g.dw.N = K; g.dw.K = M; g.dw.type = type;
-    plan(g.dx);
-    plan(g.dw);
-    // small products go together, by tiles of one size: each alone would start and end by itself
-    g.pair = fits_as_pair(g.dx, g.dw);
-    if (!g.pair && g.dx.tile <= 128 && g.dw.tile <= 128 && g.dx.tile != g.dw.tile) {
-        Product dx = g.dx, dw = g.dw;
-        plan(dx, 64);
-        plan(dw, 64);
-        g.pair = fits_as_pair(dx, dw);
-        if (g.pair) {
-            g.dx = dx;
-            g.dw = dw;
-        }
-    }
+    g.pair = plan_back(g.dx, g.dw);
     g.slope = act != FB_ACT_NONE || dy_type != type || packed(dy, lddy, M, N, type).copy;
     g.scale = type == FB_TYPE_F16 && (dy_type != type || act > FB_ACT_RELU);
     g.ldz = line_distance(N, type);

@@ -6,32 +6,38 @@ namespace fb {
 namespace {
 
 // Both products of a gradient, dx by the first `blocks` workgroups and dW by the others: small ones fill the GPU together.
-template <class T, int WI, int WJ, int FI, int FJ>
+template <class T, int WI, int WJ, int FI, int FJ, bool MASKED>
 __global__ __launch_bounds__(WI * WJ * 64) void fb_mfma_pair_kernel(Task dx, Task dw, int blocks)
 {
     const __attribute__((address_space(4))) char *args = (const __attribute__((address_space(4))) char *)__builtin_amdgcn_kernarg_segment_ptr();
     if ((int)blockIdx.x < blocks)
         run_tiles<T, true, false, WI, WJ, FI, FJ, Finished<kPlain>>(dx, (ProductArgs)args, blockIdx.x, blocks);
     else
-        run_tiles<T, false, false, WI, WJ, FI, FJ, Finished<kPlain>>(dw, (ProductArgs)(args + sizeof(Task)), blockIdx.x - blocks, gridDim.x - blocks);
+        run_tiles<T, false, false, WI, WJ, FI, FJ, Finished<kPlain>, MASKED>(dw, (ProductArgs)(args + sizeof(Task)), blockIdx.x - blocks, gridDim.x - blocks);
 }
 
-template <class T, int WI, int WJ, int FI, int FJ>
+template <class T, int WI, int WJ, int FI, int FJ, bool MASKED>
 int launch_pair(const Product &dx, const Product &dw, hipStream_t stream)
 {
     typedef Shape<WI, WJ, FI, FJ> S;
     const int64_t first = blocks_of<S>(dx);
-    const auto kernel = fb_mfma_pair_kernel<T, WI, WJ, FI, FJ>;
+    const auto kernel = fb_mfma_pair_kernel<T, WI, WJ, FI, FJ, MASKED>;
     const int rc = take_lds<S>(kernel);
     if (rc != FB_OK) return rc;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(first + blocks_of<S>(dw))), dim3(WI * WJ * 64), S::kBytes, stream, task_of<S>(dx), task_of<S>(dw), (int)first);
     return launched("matrix product kernel launch: ");
 }
 
+template <class T, bool MASKED>
+int launch_pair(const Product &dx, const Product &dw, hipStream_t stream)
+{
+    return dx.tile == 128 ? launch_pair<T, 2, 2, 2, 2, MASKED>(dx, dw, stream) : launch_pair<T, 2, 2, 1, 1, MASKED>(dx, dw, stream);
+}
+
 template <class T>
 int launch_pair(const Product &dx, const Product &dw, hipStream_t stream)
 {
-    return dx.tile == 128 ? launch_pair<T, 2, 2, 2, 2>(dx, dw, stream) : launch_pair<T, 2, 2, 1, 1>(dx, dw, stream);
+    return dw.s.live ? launch_pair<T, true>(dx, dw, stream) : launch_pair<T, false>(dx, dw, stream);
 }
 
 template <class T, bool ALONG_A, bool ALONG_B, class WAY, bool MASKED = false>

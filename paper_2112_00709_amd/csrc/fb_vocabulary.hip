@@ -553,6 +553,7 @@ struct ScoreGradPlan {
     int64_t width, pieces, ldz;
     Product z, dx, dw;       // of a whole piece
     Packed x, w;
+    bool pair;               // both products in one launch
     int64_t sum_rows;
     size_t dz, rows, picks, live, range, sums, acc, part_x, part_w, bytes;
 };
@@ -570,8 +571,12 @@ ScoreGradPlan score_grad_plan(const void *x, int64_t ldx, const void *weight, in
     g.dx.M = M; g.dx.N = K; g.dx.K = g.width; g.dx.type = type;
     g.dw.M = g.width; g.dw.N = K; g.dw.K = M; g.dw.type = type;
     plan(g.z, 0, true);
-    plan(g.dx);
-    plan(g.dw);
+    const bool pair = plan_back(g.dx, g.dw);
+    g.pair = pair && g.pieces == 1;
+    if (pair && !g.pair) {
+        plan(g.dx);
+        plan(g.dw);
+    }
     g.x = packed(x, ldx, M, K, type);
     g.w = packed(weight, ldw, V, K, type);
     const int64_t fragment = g.z.tile == 256 ? 128 : g.z.tile / 2;        // rows of a wave
@@ -721,8 +726,12 @@ int fb_affine_logprobs_grad(const void *x, int64_t ldx, const void *weight, int6
             qw.f.undo = undo;
             qw.part = (float *)part_w;
             const bool has_dx = dx && M > 0;
-            if (has_dx && (rc = launch_dx(qx, st)) != FB_OK) return rc;
-            if (dweight && (rc = launch_mfma_product(qw, st)) != FB_OK) return rc;
+            if (g.pair && has_dx && dweight) {
+                if ((rc = launch_mfma_pair(qx, qw, st)) != FB_OK) return rc;
+            } else {
+                if (has_dx && (rc = launch_dx(qx, st)) != FB_OK) return rc;
+                if (dweight && (rc = launch_mfma_product(qw, st)) != FB_OK) return rc;
+            }
             rc = launch_join(has_dx ? &qx : nullptr, dweight ? &qw : nullptr, type, (const float *)sums, M > 0 ? g.sum_rows : 0, n, dbias ? dbias + v0 : nullptr, st);
             if (rc != FB_OK) return rc;
             if (last && has_dx && g.pieces > 1 && (rc = launch_round(RoundParams{(const float *)acc, M, K, lddx, dx}, type, st)) != FB_OK) return rc;

@@ -102,10 +102,13 @@ def _rows(t, what: str, width: Optional[int] = None, dtype=None, lead=None, devi
     n = t.numel() // w if w else 0
     if t.is_contiguous():
         return t.data_ptr(), w, n, w, on
-    if w > 1 and t.stride(-1) != 1:
+    steps = t.stride()
+    if w > 1 and steps[-1] != 1:
         raise ValueError(f"the elements of a row of {what} must be contiguous")
+    if len(shape) == 2 and n > 1 and steps[0] >= w:
+        return t.data_ptr(), steps[0], n, w, on
     ld = seen = 0                                 # the leading dimensions have to be one walk over the rows
-    for size, step in zip(reversed(shape[:-1]), reversed(t.stride()[:-1])):
+    for size, step in zip(reversed(shape[:-1]), reversed(steps[:-1])):
         if size == 1:
             continue
         if seen == 0:
@@ -286,8 +289,9 @@ def fb_residual_norm_grad(ds, dy, h, s, stats, gate=None, scale: float = 1.0, in
     dg = None
     if want_dgate and gate is not None:
         dg = _out(h, (H,), torch.float32) if one else _out_like(h)
-    sums = [_out(h, (H,), torch.float32) if kind and want else None
-            for kind, want in ((kin, want_dinner), (kin, want_dinner), (kout, want_douter), (kout, want_douter))]
+    wanted = bool(kin and want_dinner), bool(kout and want_douter)
+    made = _floats(2 * sum(wanted), h, (H,)) if any(wanted) else []
+    sums = (made[:2] if wanted[0] else [None, None]) + (made[-2:] if wanted[1] else [None, None])
     need = int(L.fb_residual_norm_grad_workspace_bytes(R, H)) if (one and dg is not None) or any(t is not None for t in sums) else 0
     ws, pws = _workspace(need, h)
     address = [None if t is None else t.data_ptr() for t in (dh, dr, dg, *sums)]
