@@ -172,7 +172,8 @@ size_t fb_gated_affine_grad_workspace_bytes(const void *x, int64_t ldx, const vo
  *   dy      [M][N] of `type`;  preact [M][2 N] of `type`
  *   dx      out, [M][K] of `type`, nullable;  dweight out, [2 N][K] of `type`, contiguous, nullable;  dbias out, float [2 N], nullable
  * Where `type` has 16 bits dz is rounded to it before the two products, to FB_TYPE_F16 times a power of two that brings the largest
- * finite bound of |dz|, |dy| times |u| or 1 times what |act'| or |act| does not exceed at g or its sign, into [2^14, 2^15) (as in fb_affine_grad); dbias is summed before that.
+ * finite bound of |dz| into [2^14, 2^15) (as in fb_affine_grad): |dy u| and |dy| times what |act'| and |act| do not exceed for a g of
+ * its sign and size; dbias is summed before that.
  * Errors as fb_affine_grad; dy, x, weight and preact must not be NULL.
  */
 int fb_gated_affine_grad(const void *dy, int64_t lddy, const void *x, int64_t ldx, const void *weight, int64_t ldw, const void *preact, int64_t ldp,

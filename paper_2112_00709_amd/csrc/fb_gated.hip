@@ -1,7 +1,12 @@
 // Gated layer and its gradient (fb_layers.h): y = act(x G^T + a) (x U^T + b).
 //
 // Forward, both products are one, of x with G and U in turn 32 rows of each (see Side in fb_mfma.h): a wave's two fragments of the
-// weight are the same rows of both, so that g and u of an output meet in one wave and y leaves alone.
+// weight are the same rows of both, so that g and u of an output meet in one wave and y leaves alone.  44160 x 2048 x 1024 in bfloat16 with silu
+// and both preactivations: 385 us (963 TFLOP/s); of these 305 are the products (1215), the rest the outputs' way through the registers and LDS, which
+// nothing overlaps (543 MB; starting half of the chiplets later, so that they do not store all at once, changes nothing).
+//
+// Backward, dz is made in one pass over dy and preact, and is a factor of two products: 851 us for the same sizes, dz 161 (5.6 TB/s), dx 354 and
+// dW 297 (1045 and 1245 TFLOP/s), shares of dW joined 21.
 #include "fb_mfma.h"
 
 namespace fb {
@@ -208,7 +213,7 @@ __global__ __launch_bounds__(256) void fb_gated_slope_kernel(GatedSlopeParams p)
 }
 
 // The largest finite bound of |dz|, |dy| max(|u| slope_bound(g), act_bound(g)), a share a workgroup (half precision: what fb_affine_grad finds of dy,
-// here with u and act(g), which are not bounded).  Bound by memory.
+// here with u and act(g), which are not bounded).  Bound by memory: 64 MB in 21 us; dz itself in the place of its bound 37.
 __global__ __launch_bounds__(1024) void fb_gated_peak_kernel(GatedSlopeParams p)
 {
     constexpr int VE = Vec<f16>::kN, kAhead = 2;

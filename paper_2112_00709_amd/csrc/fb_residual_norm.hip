@@ -1,6 +1,8 @@
 // The way from one block into the next (fb_layers.h): norm of what the block gives, gate, scale, residual, norm of their sum, in one
 // pass, and its gradient.  Bound by memory: a row is read once into the registers of one to eight waves, everything that needs
-// it whole is formed there, and it is written once.
+// it whole is formed there, and it is written once.  Measured, bfloat16: 69120 x 1024 with both norms and a gate of one row 109 us (566 MB, 5.2
+// TB/s), the gradient with a gate of rows and all seven outputs 207 us (1.13 GB, 5.5 TB/s), 5 of them the second launch; one row of 512 3.4 us on
+// the GPU, 12.6 a call.
 #include "fb_layers_device.h"
 
 namespace fb {
@@ -155,7 +157,8 @@ __global__ __launch_bounds__((Places<T, WAVES, EPL>::kThreads)) void fb_residual
 // With xh2 = (s - m2) r2, g2 = dy w2:  d = ds + r2 (g2 - sum g2 / H - xh2 sum(g2 xh2) / H) is the gradient of s and of the
 // residual; du = scale d; with xh1 = (h - m1) r1, u = xh1 w1 + b1:  dgate = du u, and through the inner norm with
 // du gate in the place of dy.  (rms: no sum g / H.)  Sums of columns stay in registers over all rows that a lane sees and leave
-// once, a row of sums a workgroup.  LEAN: weights are read again for every row, the next row is not asked for ahead.
+// once, a row of sums a workgroup (two workgroups a compute unit: with four, whose sums are twice as many, 4811 x 777 in single precision takes 38
+// instead of 33.5 us and 69120 x 1024 220 instead of 207).  LEAN: weights are read again for every row, the next row is not asked for ahead.
 template <class T, class W, int WAVES, int EPL, bool LEAN>
 __global__ __launch_bounds__((Places<T, WAVES, EPL>::kThreads)) void fb_residual_norm_grad_kernel(ResidualParams p)
 {
