@@ -686,7 +686,7 @@ int fb_affine_logprobs_grad(const void *x, int64_t ldx, const void *weight, int6
         char *range = live + g.live, *sums = range + g.range;
         char *acc = sums + g.sums, *part_x = acc + g.acc, *part_w = part_x + g.part_x;
         const int64_t size = (int64_t)type_bytes(type);
-        float *undo = type == FB_TYPE_F16 ? (float *)range : nullptr;
+        float *undo = type == FB_TYPE_F16 && M > 0 ? (float *)range : nullptr;      // (no rows: nobody sets it)
         if (M > 0) {
             RowParams r{tokens, logz, entropy, g_logprobs, g_entropy, M, (f32x4 *)rows, undo ? (uint32_t *)(undo + 1) : nullptr, 0, undo,
                         (uint64_t *)live, (int32_t *)picks};

@@ -153,3 +153,17 @@ def test_one_element_a_row(fl, dtype):
         for t in fl.fb_affine_logprobs_grad(c["x"], c["wv"], c["tokens"], logz, ent, c["g"], c["h"], c["bv"]):
             # (p = 1 to some 1e-6: the gradient of a certainty)
             assert t.abs().max() <= 1e-5 * M * 20
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("K", [3, 40])
+def test_no_rows_of_any_type(fl, dtype, K):
+    """Sums over no rows are zeros, whatever the workspace held: products that leave at once (K = 40) and by way of memory (3)."""
+    import torch
+    c = make(0, 66, K, dtype, 1)
+    out = run(fl, c)
+    for t in out:
+        assert t is not None and not t.any() and not torch.isnan(t).any()
+    none = torch.empty(0, device="cuda")
+    for t in fl.fb_affine_logprobs_grad(c["x"], c["wv"], c["tokens"], none, none, none, None, c["bv"]):
+        assert not t.any() and not torch.isnan(t).any()
