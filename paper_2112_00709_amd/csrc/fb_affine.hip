@@ -127,86 +127,11 @@ int launch_peak(const PeakParams &p, int dy_type, hipStream_t stream)
     return launched("peak kernel launch: ");
 }
 
-// dz = dy act'(z) (or a copy of dy in rows of whole pieces), rounded to the factors' type, and the sums of its columns before
-// the rounding.  Bound by memory: 44160 x 2048 in bfloat16 with max(z, 0) take 100 us, 5.4 TB/s.  A thread has one piece of the
-// width; `lanes` threads have a row side by side, so narrow rows fill the waves too, and kRowsAhead rows are asked for before the
-// first is worked on.  The sums of a workgroup's threads over its rows are added in a fixed order.
-constexpr int kRowsAhead = 4;
-
-template <class T, class D>
-__device__ __forceinline__ void make_rows(const SlopeParams &p, int block, float (*slots)[Vec<T>::kN + 1])
-{
-    constexpr int VE = Vec<T>::kN, VD = Vec<D>::kN;
-    const int across = block % p.wide, down = block / p.wide;
-    const int lane = threadIdx.x & (p.lanes - 1), sub = threadIdx.x / p.lanes, subs = 256 / p.lanes;
-    const int64_t at = ((int64_t)across * p.lanes + lane) * VE;
-    const int n = at >= p.N ? 0 : (int)(p.N - at < VE ? p.N - at : VE);
-    float sum[VE] = {}, scale = 1.0f;
-    if constexpr (std::is_same<T, f16>::value) {
-        if (p.peaks) {
-            float undo;
-            range_of(p.peaks, p.n_peaks, scale, undo);
-            if (block == 0 && threadIdx.x == 0) *p.undo = undo;
-        }
-    }
-    if (n > 0) {
-        const int64_t step = (int64_t)p.down * subs;
-        for (int64_t r0 = (int64_t)down * subs + sub; r0 < p.M; r0 += kRowsAhead * step) {
-            u32x4 rg[kRowsAhead][VE / VD], rz[kRowsAhead];
-#pragma unroll
-            for (int u = 0; u < kRowsAhead; ++u) {
-                const int64_t r = r0 + u * step;
-                const int here = r < p.M ? n : 0;
-#pragma unroll
-                for (int e = 0; e < VE / VD; ++e) rg[u][e] = load_piece((const D *)p.dy + r * p.lddy + at + e * VD, here - e * VD);
-                if (p.act != FB_ACT_NONE) rz[u] = load_piece((const T *)p.z + r * p.ldz + at, here);
-            }
-#pragma unroll
-            for (int u = 0; u < kRowsAhead; ++u) {
-                const int64_t r = r0 + u * step;
-                float g[VE];
-#pragma unroll
-                for (int e = 0; e < VE / VD; ++e) unpack<D>(rg[u][e], g + e * VD);
-                if (p.act != FB_ACT_NONE) {
-                    float z[VE];
-                    unpack<T>(rz[u], z);
-#pragma unroll
-                    for (int e = 0; e < VE; ++e) g[e] = e < n && r < p.M ? g[e] * act_slope(z[e], p.act) : 0.0f;
-                }
-#pragma unroll
-                for (int e = 0; e < VE; ++e) sum[e] += g[e];
-                if constexpr (std::is_same<T, f16>::value) {
-#pragma unroll
-                    for (int e = 0; e < VE; ++e) g[e] *= scale;
-                }
-                if (p.out && r < p.M) store_piece((T *)p.out + r * p.ldo + at, VE, pack<T>(g));   // (rows of whole pieces)
-            }
-        }
-    }
-    if (!p.part) return;
-#pragma unroll
-    for (int e = 0; e < VE; ++e) slots[threadIdx.x][e] = sum[e];
-    __syncthreads();
-    for (int c = threadIdx.x; c < p.lanes * VE; c += 256) {
-        const int64_t col = (int64_t)across * p.lanes * VE + c;
-        if (col >= p.N) continue;
-        float s = 0.0f;
-        for (int i = 0; i < subs; ++i) s += slots[i * p.lanes + c / VE][c % VE];
-        p.part[(size_t)down * p.N + col] = s;
-    }
-}
-
 template <class T, class D>
 __global__ __launch_bounds__(256) void fb_prepare_kernel(PrepareParams p)
 {
     __shared__ float slots[256][Vec<T>::kN + 1];
-    const int block = blockIdx.x;
-    if (block < p.last[0])
-        make_rows<T, D>(p.job[0], block, slots);
-    else if (block < p.last[1])
-        make_rows<T, T>(p.job[1], block - p.last[0], slots);
-    else
-        make_rows<T, T>(p.job[2], block - p.last[1], slots);
+    prepare_block<T, D>(p, blockIdx.x, slots);
 }
 
 }  // namespace
