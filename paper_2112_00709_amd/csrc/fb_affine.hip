@@ -345,7 +345,8 @@ int launch_grad(GradPlan &g, const Factor &d, const float *undo, void *dx, int64
         if (dx && M > 0 && (rc = launch_dx(g.dx, st)) != FB_OK) return rc;
         if (dweight && (rc = launch_mfma_product(g.dw, st)) != FB_OK) return rc;
     }
-    return launch_join(dx ? &g.dx : nullptr, dweight ? &g.dw : nullptr, type, sums, rows, N, dbias, st);
+    const Product joined = joined_rows(g.dx, g.twice);
+    return launch_join(dx ? &joined : nullptr, dweight ? &g.dw : nullptr, type, sums, rows, N, dbias, st);
 }
 
 namespace {

@@ -15,7 +15,7 @@ namespace {
 
 // Sums of a wave leave as y = act(g) u, formed in the registers that have them, and as g and u.
 struct Gated {
-    static constexpr bool kPaired = true, kNeverEmpty = true;
+    static constexpr bool kPaired = true, kNeverEmpty = true, kFolded = false;
     static constexpr int kEarly = 1;
 
     template <int FI, int FJ>
@@ -114,6 +114,7 @@ struct GatedSlopeParams {
     int64_t lddy, ldz, M, N, ldo;
     int act;
     void *out;               // nullable
+    int64_t low;             // rows from a row of out to the one with what it lacks, 0: none
     float *part;             // [down][2 N], nullable
     int lanes, wide, down;
     uint32_t *peaks;         // half precision: of the largest finite |dz|, see fb_affine_grad; nullable
@@ -192,6 +193,19 @@ __device__ __forceinline__ void make_pairs(const GatedSlopeParams &p, int block,
                 store_piece(out + at, n, pack<T>(d));
                 store_piece(out + p.N + at, n, pack<T>(d + VE));
                 for (int c = 0; c < zeros; ++c) out[2 * p.N + c] = (T)0.0f;
+                if constexpr (sizeof(T) == 2) {
+                    if (p.low) {
+                        out += p.low * p.ldo;
+                        float high[2 * VE];
+                        unpack<T>(pack<T>(d), high);
+                        unpack<T>(pack<T>(d + VE), high + VE);
+#pragma unroll
+                        for (int e = 0; e < 2 * VE; ++e) d[e] = lacks(d[e], high[e]);
+                        store_piece(out + at, n, pack<T>(d));
+                        store_piece(out + p.N + at, n, pack<T>(d + VE));
+                        for (int c = 0; c < zeros; ++c) out[2 * p.N + c] = (T)0.0f;
+                    }
+                }
             }
         }
     }
@@ -212,7 +226,7 @@ __device__ __forceinline__ void make_pairs(const GatedSlopeParams &p, int block,
 }
 
 // COPIES: workgroups behind those of dz copy what the products cannot take as it is (a launch less: 300 rows, N 501, K 203 in bfloat16 21.8
-// instead of 25.0 us a call, 9601 x 1111 x 777 in half precision 168 instead of 177).
+// instead of 25.0 us a call; nothing at 9601 x 1111 x 777, where both wait for memory).
 template <class T, bool COPIES>
 __global__ __launch_bounds__(256) void fb_gated_slope_kernel(GatedSlopeParams p, PrepareParams copies)
 {
@@ -329,7 +343,17 @@ struct GatedGradPlan {
 GatedGradPlan gated_grad_plan(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t N, int64_t K, int type)
 {
     GatedGradPlan p{};
-    p.g = grad_plan(nullptr, 2 * N, type, x, ldx, weight, ldw, M, 2 * N, K, type, FB_ACT_SILU);   // (an activation: dz is made)
+    const bool two = twice(M, type);
+    p.g = grad_plan(nullptr, 2 * N, type, x, ldx, weight, ldw, two ? 2 * M : M, 2 * N, K, type, FB_ACT_SILU);   // (an activation: dz is made)
+    p.g.twice = two;
+    if (two) {
+        p.g.bytes -= p.g.x.bytes + p.g.part;
+        p.g.x = packed(nullptr, K, 2 * M, K, type, true);
+        p.g.dx.parts = true;
+        p.g.part = product_bytes(p.g.dx);
+        p.g.bytes += p.g.x.bytes + p.g.part;
+    }
+    p.s.low = two ? M : 0;
     p.s.M = M; p.s.N = N; p.s.ldo = p.g.ldz;
     lay_out_pairs(p.s, type);
     const size_t sums = aligned((size_t)p.s.down * 2 * (size_t)N * sizeof(float));
@@ -446,6 +470,7 @@ int fb_gated_affine_grad(const void *dy, int64_t lddy, const void *x, int64_t ld
             Prepare copies;
             if (dx && g.w.copy) copies.add(pack_job(g.w, weight, ldw, 2 * N, K, wts), type);
             if (dweight && g.x.copy) copies.add(pack_job(g.x, x, ldx, M, K, xs), type);
+            if (dweight && g.twice) copies.add(pack_job(g.x, x, ldx, M, K, xs + (size_t)M * (size_t)g.x.ld * type_bytes(type)), type);
             rc = type == FB_TYPE_F32 ? launch_pairs<float>(s, copies, st) : type == FB_TYPE_BF16 ? launch_pairs<bf16>(s, copies, st) : launch_pairs<f16>(s, copies, st);
             if (rc != FB_OK) return rc;
         }

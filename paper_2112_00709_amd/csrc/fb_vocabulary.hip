@@ -74,7 +74,7 @@ __device__ __forceinline__ int place_of(int token, int64_t j0, int lane)
 
 // Sums leave as each row's (m, S, T) over the tile's columns, and as the logits of given tokens.
 struct Reduced {
-    static constexpr bool kPaired = false, kNeverEmpty = true;
+    static constexpr bool kPaired = false, kNeverEmpty = true, kFolded = true;
     static constexpr int kEarly = 2;         // bias; tokens of the lane's rows
 
     template <int FI, int FJ>
@@ -154,7 +154,7 @@ struct Reduced {
 // are stored; rows of dz are whole 16-byte pieces.  There are whole 256 rows and tokens (those past M do not count): they are asked for when
 // a tile begins, all at once: asked for at its end, with a condition each, each was waited for, and 69120 x 3000 x 1024 took 502 instead of 458 us.
 struct Slopes {
-    static constexpr bool kPaired = false, kNeverEmpty = true;
+    static constexpr bool kPaired = false, kNeverEmpty = true, kFolded = true;
     static constexpr int kEarly = 6;         // columns; rows, four at most; tokens of the lane's rows
 
     template <int FI, int FJ>
@@ -199,6 +199,16 @@ struct Slopes {
             for (int y = 0; y < FJ; ++y) sum[y] += v[y];
             store_fragments<T, FJ, true>(v, where.room + where.wave * 16 * FJ * 32, (T *)args->f.y, args->f.ldy, i0 + x * 32, j0, M, wide, lane,
                                          false);
+            if constexpr (FI <= 2 && sizeof(T) == 2) {
+                if (args->s.low) {
+#pragma unroll
+                    for (int y = 0; y < FJ; ++y)
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) v[y][k] = lacks(v[y][k], (float)(T)v[y][k]);
+                    store_fragments<T, FJ, true>(v, where.room + where.wave * 16 * FJ * 32, (T *)args->f.y + args->s.low * args->f.ldy, args->f.ldy,
+                                                 i0 + x * 32, j0, M, wide, lane, false);
+                }
+            }
         }
         if (!args->s.sums) return;
         // 32 rows of a column added: two of a lane's columns at a time over the rows of 16 lanes, so that lanes 16 .. 31 and 48 .. 63 have
@@ -226,10 +236,25 @@ struct Slopes {
     }
 };
 
+// Tiles of the logits' product: of 128 or 64 where a wave needs registers for a second set of sums (single precision; 256 would be 4 % faster) or
+// leaves what dz lacks.
+void plan_logits(Product &q, bool two = false)
+{
+    if (q.type != FB_TYPE_F32 && !two) {
+        plan(q, 0, true);
+        return;
+    }
+    Product small = q;
+    const double cost = plan(small, 64, true);
+    if (plan(q, 128, true) > cost) q = small;
+}
+
 template <class T, class WAY>
 int launch_scores(const Product &q, hipStream_t stream)
 {
-    if (q.tile == 256) return launch<T, true, true, 2, 4, 4, 2, WAY>(q, stream);
+    if constexpr (sizeof(T) == 2) {
+        if (q.tile == 256) return launch<T, true, true, 2, 4, 4, 2, WAY>(q, stream);
+    }
     return q.tile == 128 ? launch<T, true, true, 2, 2, 2, 2, WAY>(q, stream) : launch<T, true, true, 2, 2, 1, 1, WAY>(q, stream);
 }
 
@@ -439,6 +464,7 @@ struct RowParams {
     float *undo;
     uint64_t *live;          // see Scores
     int32_t *picks;          // [whole 256 rows], as rows are: the tokens, -1 where a row does not count
+    int low;                 // M where rows of x are there twice, see twice(); or 0
 };
 
 __device__ __forceinline__ f32x4 row_of(const RowParams &p, int64_t i)
@@ -507,7 +533,20 @@ __global__ __launch_bounds__(256) void fb_scores_rows_kernel(RowParams p, Prepar
     f32x4 r = {kInf, 0.0f, 0.0f, 0.0f};
     if (i < p.M) r = row_of(p, i);
     const uint64_t live = __builtin_amdgcn_ballot_w64(r[0] != kInf);
-    if ((threadIdx.x & 63) == 0) p.live[i / 64] = live;
+    if (p.low) {                           // (up to 128 rows, in one workgroup: once more behind the last of them)
+        __shared__ uint64_t once[4];
+        if ((threadIdx.x & 63) == 0) once[threadIdx.x >> 6] = live;
+        __syncthreads();
+        if (threadIdx.x < 4) {
+            const int back = p.low / 64, up = p.low % 64, w = (int)threadIdx.x - back;
+            uint64_t word = once[threadIdx.x];
+            if (w >= 0) word |= once[w] << up;
+            if (w >= 1 && up) word |= once[w - 1] >> (64 - up);
+            p.live[threadIdx.x] = word;
+        }
+    } else if ((threadIdx.x & 63) == 0) {
+        p.live[i / 64] = live;
+    }
     p.picks[i] = r[0] != kInf ? p.tokens[i] : -1;
     r[0] = -r[0];
     r[1] *= -scale;
@@ -591,7 +630,7 @@ ScorePlan score_plan(const void *x, int64_t ldx, const void *weight, int64_t ldw
     if (f.few) {
         f.parts = few_groups(V);
     } else {
-        plan(f.q, 0, true);
+        plan_logits(f.q);
         f.parts = (V + f.q.tile - 1) / f.q.tile;
         f.x = packed(x, ldx, M, K, type);
         f.w = packed(weight, ldw, V, K, type);
@@ -611,6 +650,7 @@ struct ScoreGradPlan {
     Product z, dx, dw;       // of a whole piece
     Packed x, w;
     bool pair;               // both products in one launch
+    bool twice;              // dz is two rows of 16 bits for each of M, see twice()
     int64_t sum_rows;
     size_t dz, rows, picks, live, range, sums, acc, part_x, part_w, bytes;
 };
@@ -627,18 +667,22 @@ ScoreGradPlan score_grad_plan(const void *x, int64_t ldx, const void *weight, in
     g.z.M = M; g.z.N = g.width; g.z.K = K; g.z.type = type;
     g.dx.M = M; g.dx.N = K; g.dx.K = g.width; g.dx.type = type;
     g.dw.M = g.width; g.dw.N = K; g.dw.K = M; g.dw.type = type;
-    plan(g.z, 0, true);
+    g.twice = twice(M, type);
+    if (g.twice) g.dx.M = g.dw.K = 2 * M;
+    plan_logits(g.z, g.twice);
     const bool pair = plan_back(g.dx, g.dw);
     g.pair = pair && g.pieces == 1;
     if (pair && !g.pair) {
         plan(g.dx);
         plan(g.dw);
     }
-    g.x = packed(x, ldx, M, K, type);
+    if (g.twice) g.dx.parts = true;
+    const int64_t rows = g.twice ? 2 * M : M;
+    g.x = packed(x, ldx, rows, K, type, g.twice);
     g.w = packed(weight, ldw, V, K, type);
     const int64_t fragment = g.z.tile == 256 ? 128 : g.z.tile / 2;        // rows of a wave
     g.sum_rows = (M + g.z.tile - 1) / g.z.tile * (g.z.tile / fragment);
-    g.dz = aligned((size_t)M * (size_t)g.ldz * type_bytes(type));
+    g.dz = aligned((size_t)rows * (size_t)g.ldz * type_bytes(type));
     g.rows = aligned((size_t)((M + 255) / 256 * 256) * sizeof(f32x4));
     g.picks = aligned((size_t)((M + 255) / 256 * 256) * sizeof(int32_t));
     g.live = aligned((size_t)((M + 255) / 256 * 4 + 1) * sizeof(uint64_t));
@@ -740,9 +784,10 @@ int fb_affine_logprobs_grad(const void *x, int64_t ldx, const void *weight, int6
         float *undo = type == FB_TYPE_F16 && M > 0 ? (float *)range : nullptr;      // (no rows: nobody sets it)
         if (M > 0) {
             RowParams r{tokens, logz, entropy, g_logprobs, g_entropy, M, (f32x4 *)rows, undo ? (uint32_t *)(undo + 1) : nullptr, 0, undo,
-                        (uint64_t *)live, (int32_t *)picks};
+                        (uint64_t *)live, (int32_t *)picks, g.twice ? (int)M : 0};
             Prepare copies;
             if (g.x.copy) copies.add(pack_job(g.x, x, ldx, M, K, xs), type);
+            if (g.twice) copies.add(pack_job(g.x, x, ldx, M, K, xs + (size_t)M * (size_t)g.x.ld * type_bytes(type)), type);
             if (g.w.copy) copies.add(pack_job(g.w, weight, ldw, V, K, wts), type);
             if ((rc = launch_rows(r, type, copies, st)) != FB_OK) return rc;
         }
@@ -758,7 +803,7 @@ int fb_affine_logprobs_grad(const void *x, int64_t ldx, const void *weight, int6
             z.f.bias = bias ? bias + v0 : nullptr;
             z.f.y = dz; z.f.ldy = line_distance(n, type);
             z.f.undo = undo;
-            z.s = {(const int32_t *)picks, (int)v0, nullptr, nullptr, rows, dbias ? (float *)sums : nullptr, nullptr};
+            z.s = {(const int32_t *)picks, (int)v0, nullptr, nullptr, rows, dbias ? (float *)sums : nullptr, nullptr, g.twice ? M : 0};
             if (M > 0 && (rc = launch_scores<Slopes>(z, st)) != FB_OK) return rc;
             qx.A = {dz, z.f.ldy, true};
             qx.B = {z.B.p, g.w.ld, false};
@@ -784,7 +829,8 @@ int fb_affine_logprobs_grad(const void *x, int64_t ldx, const void *weight, int6
                 if (has_dx && (rc = launch_dx(qx, st)) != FB_OK) return rc;
                 if (dweight && (rc = launch_mfma_product(qw, st)) != FB_OK) return rc;
             }
-            rc = launch_join(has_dx ? &qx : nullptr, dweight ? &qw : nullptr, type, (const float *)sums, M > 0 ? g.sum_rows : 0, n, dbias ? dbias + v0 : nullptr, st);
+            const Product joined = joined_rows(qx, g.twice);
+            rc = launch_join(has_dx ? &joined : nullptr, dweight ? &qw : nullptr, type, (const float *)sums, M > 0 ? g.sum_rows : 0, n, dbias ? dbias + v0 : nullptr, st);
             if (rc != FB_OK) return rc;
             if (last && has_dx && g.pieces > 1 && (rc = launch_round(RoundParams{(const float *)acc, M, K, lddx, dx}, type, st)) != FB_OK) return rc;
         }
