@@ -171,8 +171,8 @@ size_t fb_gated_affine_grad_workspace_bytes(const void *x, int64_t ldx, const vo
  * Its gradient:  dz = [dy u act'(g), dy act(g)],  dx = dz W,  dweight = dz^T x,  dbias = sum over rows of dz
  *   dy      [M][N] of `type`;  preact [M][2 N] of `type`
  *   dx      out, [M][K] of `type`, nullable;  dweight out, [2 N][K] of `type`, contiguous, nullable;  dbias out, float [2 N], nullable
- * Where `type` has 16 bits dz is rounded to it before the two products (for M <= 64 kept as two such numbers, and products of those
- * added), to FB_TYPE_F16 times a power of two that brings the largest
+ * Where `type` has 16 bits dz is rounded to it before the two products (for M <= 64, and M <= 128 if M N K <= 2^23, kept as two
+ * such numbers, and products of those added), to FB_TYPE_F16 times a power of two that brings the largest
  * finite bound of |dz| into [2^14, 2^15) (as in fb_affine_grad): |dy u| and |dy| times what |act'| and |act| do not exceed for a g of
  * its sign and size; dbias is summed before that.
  * Errors as fb_affine_grad; dy, x, weight and preact must not be NULL.
@@ -247,8 +247,8 @@ size_t fb_affine_logprobs_grad_workspace_bytes(const void *x, int64_t ldx, const
  *   g_logprobs, g_entropy  float [M], either nullable
  *   dx      out, [M][K] of `type`, nullable;  dweight out, [V][K] of `type`, contiguous, nullable;  dbias out, float [V], nullable
  * Rows that do not count and rows whose logz is -inf have dx = 0 and no part in the sums.  Where `type` has 16 bits dz is rounded to it
- * before the two products (for M <= 64 kept as two such numbers), to FB_TYPE_F16 times a power of two for the largest |g_logprobs| + |g_entropy| (0.37 + entropy), which no |dz|
- * exceeds (as in fb_affine_grad); dbias is summed before that.
+ * before the two products (for M <= 64, and M <= 128 if M V K <= 2^24, kept as two such numbers), to FB_TYPE_F16 times a power of two for
+ * the largest |g_logprobs| + |g_entropy| (0.37 + entropy), which no |dz| exceeds (as in fb_affine_grad); dbias is summed before that.
  * Errors as fb_affine_logprobs; FB_EUNSUPPORTED too: rows of dx 2^27 elements apart or more.
  */
 int fb_affine_logprobs_grad(const void *x, int64_t ldx, const void *weight, int64_t ldw, const float *bias, const int32_t *tokens, const float *logz,

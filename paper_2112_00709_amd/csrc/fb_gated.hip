@@ -343,7 +343,7 @@ struct GatedGradPlan {
 GatedGradPlan gated_grad_plan(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t N, int64_t K, int type)
 {
     GatedGradPlan p{};
-    const bool two = twice(M, type);
+    const bool two = twice(M, 2 * N, K, type);
     p.g = grad_plan(nullptr, 2 * N, type, x, ldx, weight, ldw, two ? 2 * M : M, 2 * N, K, type, FB_ACT_SILU);   // (an activation: dz is made)
     p.g.twice = two;
     if (two) {

@@ -667,7 +667,7 @@ ScoreGradPlan score_grad_plan(const void *x, int64_t ldx, const void *weight, in
     g.z.M = M; g.z.N = g.width; g.z.K = K; g.z.type = type;
     g.dx.M = M; g.dx.N = K; g.dx.K = g.width; g.dx.type = type;
     g.dw.M = g.width; g.dw.N = K; g.dw.K = M; g.dw.type = type;
-    g.twice = twice(M, type);
+    g.twice = twice(M, V, K, type);
     if (g.twice) g.dx.M = g.dw.K = 2 * M;
     plan_logits(g.z, g.twice);
     const bool pair = plan_back(g.dx, g.dw);

@@ -47,11 +47,15 @@ def products(dz, off, x, w, dtype):
     return dx, ex, dw, ew
 
 
-ROWS = [1, 2, 3, 17, 31, 32, 33, 63, 64]
+ROWS = [1, 2, 3, 17, 31, 32, 33, 63, 64, 65, 95, 127, 128]
 
 
-@pytest.mark.parametrize("M", ROWS)
-@pytest.mark.parametrize("N,K", [(5, 3), (64, 128), (77, 35), (515, 264)])
+def sizes(twice, others):
+    """Rows up to 64, and beyond in small products alone (`twice`: N stands for 2 N rows of the weight)."""
+    return [(M, N, K) for N, K in others for M in ROWS if M <= 64 or M * twice * N * K <= 2 ** 24]
+
+
+@pytest.mark.parametrize("M,N,K", sizes(2, [(5, 3), (64, 128), (77, 35), (515, 264)]))
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
 def test_gated_layer(fl, M, N, K, dtype):
     import torch
@@ -70,8 +74,7 @@ def test_gated_layer(fl, M, N, K, dtype):
             assert p is None or torch.equal(p, q)
 
 
-@pytest.mark.parametrize("M", ROWS)
-@pytest.mark.parametrize("V,K", [(3, 5), (40, 128), (1083, 29), (2050, 264)])
+@pytest.mark.parametrize("M,V,K", sizes(1, [(3, 5), (40, 128), (1083, 29), (2050, 264)]) + [(3, 2_200_000, 16), (40, 2_100_001, 9)])
 @pytest.mark.parametrize("dtype,entropy", [("bfloat16", True), ("float16", True), ("bfloat16", False)])
 def test_log_probabilities(fl, M, V, K, dtype, entropy):
     import torch
