@@ -31,8 +31,29 @@ struct ResidualParams {
     bool past;                         // outputs go past the caches
 };
 
-// What the places of a lane in a row are: WAVES waves have a row, EPL elements a lane, a piece at a time.
-template <class T, int WAVES, int EPL>
+// A piece without its first n elements (0 < n < kN), zeros behind the others.
+template <class T>
+__device__ __forceinline__ u32x4 drop(const u32x4 &r, int n)
+{
+    const int bits = n * 8 * (int)sizeof(T);
+    uint64_t lo = (uint64_t)r[1] << 32 | r[0], hi = (uint64_t)r[3] << 32 | r[2];
+    if (bits < 64) {
+        lo = lo >> bits | hi << (64 - bits);
+        hi >>= bits;
+    } else {
+        lo = hi >> (bits - 64);
+        hi = 0;
+    }
+    return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+
+// What the places of a lane in a row are: WAVES waves have a row, EPL elements a lane, a piece at a time.  A row's last piece, where it is not
+// whole, is asked for as the whole piece that ends with the row, and what other lanes have of it is dropped when it has come (it may have been
+// written in the meantime): element by element it was waited for at once, and 19904 x 2357 in bfloat16 took 182 instead of 130 us,
+// backward 500 instead of 336.
+enum Ends { kWhole, kEnding, kParts };     // rows are whole pieces; their last piece as above; element by element
+
+template <class T, int WAVES, int EPL, Ends ENDS>
 struct Places {
     static constexpr int kVE = Vec<T>::kN, kPieces = EPL / kVE, kStep = WAVES * 64;
     static constexpr int kThreads = WAVES < 4 ? 256 : WAVES * 64, kRows = kThreads / kStep;   // of a workgroup at a time
@@ -44,19 +65,63 @@ struct Places {
     __device__ __forceinline__ void ask(const void *p, int64_t r, int64_t ld, int n, u32x4 (&raw)[kPieces]) const
     {
         const T *row = (const T *)p + (n ? r * ld : 0);
+        if (ENDS == kWhole || (ENDS == kEnding && H >= kVE)) {
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) raw[i] = load_piece(row + at(i), n - at(i));
+            for (int i = 0; i < kPieces; ++i) {
+                const int c = ENDS == kEnding && at(i) > H - kVE ? H - kVE : at(i);
+                raw[i] = u32x4{0, 0, 0, 0};
+                if (at(i) < n) raw[i] = *(const u32x4_any *)(row + c);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) raw[i] = load_piece(row + at(i), n - at(i));
+        }
     }
-    __device__ __forceinline__ static void open(const u32x4 (&raw)[kPieces], float (&v)[EPL])
+    __device__ __forceinline__ void open(const u32x4 (&raw)[kPieces], float (&v)[EPL]) const
     {
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) unpack<T>(raw[i], v + i * kVE);
+        for (int i = 0; i < kPieces; ++i) {
+            const int seen = at(i) - (H - kVE);
+            u32x4 piece = raw[i];
+            if (ENDS == kEnding && seen > 0 && seen < kVE && H >= kVE) piece = drop<T>(piece, seen);
+            unpack<T>(piece, v + i * kVE);
+        }
+    }
+    // A vector of [H], at the same places; `none` where there is no vector.
+    template <class W>
+    __device__ __forceinline__ void vector(const void *w, float none, float (&v)[EPL]) const
+    {
+        constexpr int kN = Vec<W>::kN;
+        if constexpr (ENDS == kParts) {
+            load_vector<W, EPL, kVE>(w, H, kStep, lane, none, v);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+#pragma unroll
+            for (int j = 0; j < kVE; j += kN) {
+                const int c = at(i) + j;
+                u32x4 piece = {0, 0, 0, 0};
+                if (ENDS == kWhole) {
+                    if (w && c < H) piece = *(const u32x4_any *)((const W *)w + c);
+                } else if (ENDS == kEnding && H >= kN) {
+                    if (w && c < H) piece = *(const u32x4_any *)((const W *)w + (c < H - kN ? c : H - kN));
+                    if (c > H - kN && c < H) piece = drop<W>(piece, c - (H - kN));
+                } else if (w) {
+                    piece = load_piece((const W *)w + c, H - c);
+                }
+                float u[kN];
+                unpack<W>(piece, u);
+#pragma unroll
+                for (int e = 0; e < kN; ++e) v[i * kVE + j + e] = w ? u[e] : none;
+            }
+        }
     }
     __device__ __forceinline__ void store(void *p, int64_t r, int64_t ld, const float (&v)[EPL], bool past) const
     {
         T *row = (T *)p + r * ld;
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) store_piece(row + at(i), H - at(i), pack<T>(v + i * kVE), past);
+        for (int i = 0; i < kPieces; ++i) store_piece(row + at(i), ENDS != kWhole ? H - at(i) : at(i) < H ? kVE : 0, pack<T>(v + i * kVE), past);
     }
 };
 
@@ -83,22 +148,22 @@ __device__ __forceinline__ void norm_row(const P &at, int kind, float eps, float
     rstd = 1.0f / sqrtf(q[0] * inv + eps);
 }
 
-template <class T, class W, int WAVES, int EPL>
-__global__ __launch_bounds__((Places<T, WAVES, EPL>::kThreads)) void fb_residual_norm_kernel(ResidualParams p)
+template <class T, class W, int WAVES, int EPL, Ends ENDS>
+__global__ __launch_bounds__((Places<T, WAVES, EPL, ENDS>::kThreads)) void fb_residual_norm_kernel(ResidualParams p)
 {
-    typedef Places<T, WAVES, EPL> P;
-    constexpr int VE = P::kVE, NV = P::kPieces;
+    typedef Places<T, WAVES, EPL, ENDS> P;
+    constexpr int NV = P::kPieces;
     __shared__ float slots[2][P::kRows][4][WAVES][1];       // (by turns: a wave may be a row ahead of one that still reads)
     const P at(p.H);
     const bool gate_rows = p.gate && p.ldg, gate_vector = p.gate && !p.ldg;
     float w1[EPL], b1[EPL], w2[EPL], b2[EPL];
-    load_vector<W, EPL, VE>(p.inner_weight, at.H, P::kStep, at.lane, 1.0f, w1);
-    load_vector<W, EPL, VE>(p.inner_bias, at.H, P::kStep, at.lane, 0.0f, b1);
-    load_vector<W, EPL, VE>(p.weight, at.H, P::kStep, at.lane, 1.0f, w2);
-    load_vector<W, EPL, VE>(p.bias, at.H, P::kStep, at.lane, 0.0f, b2);
+    at.template vector<W>(p.inner_weight, 1.0f, w1);
+    at.template vector<W>(p.inner_bias, 0.0f, b1);
+    at.template vector<W>(p.weight, 1.0f, w2);
+    at.template vector<W>(p.bias, 0.0f, b2);
     {                                                       // a gate of one row, and the scale, go into the inner weights
         float g[EPL];
-        load_vector<W, EPL, VE>(gate_vector ? p.gate : nullptr, at.H, P::kStep, at.lane, 1.0f, g);
+        at.template vector<W>(gate_vector ? p.gate : nullptr, 1.0f, g);
 #pragma unroll
         for (int i = 0; i < EPL; ++i) {
             w1[i] *= g[i] * p.scale;
@@ -120,18 +185,18 @@ __global__ __launch_bounds__((Places<T, WAVES, EPL>::kThreads)) void fb_residual
     for (; base < p.R; base += rstep, turn ^= 1) {
         const int64_t r = base + at.sub;
         float v[EPL], x[EPL];
-        P::open(rh, v);
+        at.open(rh, v);
         float m1 = 0.0f, r1 = 1.0f, m2 = 0.0f, r2 = 1.0f;
         if (p.inner != FB_NORM_NONE) norm_row<P, WAVES, EPL>(at, p.inner, p.eps, inv, v, slots[turn][at.sub], m1, r1);
 #pragma unroll
         for (int i = 0; i < EPL; ++i) v[i] = fmaf(v[i] * r1, w1[i], b1[i]);
         if (gate_rows) {
-            P::open(rg, x);
+            at.open(rg, x);
 #pragma unroll
             for (int i = 0; i < EPL; ++i) v[i] *= x[i];
         }
         if (p.residual) {
-            P::open(rr, x);
+            at.open(rr, x);
 #pragma unroll
             for (int i = 0; i < EPL; ++i) v[i] += x[i];
         }
@@ -159,10 +224,10 @@ __global__ __launch_bounds__((Places<T, WAVES, EPL>::kThreads)) void fb_residual
 // du gate in the place of dy.  (rms: no sum g / H.)  Sums of columns stay in registers over all rows that a lane sees and leave
 // once, a row of sums a workgroup (two workgroups a compute unit: with four, whose sums are twice as many, 4811 x 777 in single precision takes 38
 // instead of 33.5 us and 69120 x 1024 220 instead of 207).  LEAN: weights are read again for every row, the next row is not asked for ahead.
-template <class T, class W, int WAVES, int EPL, bool LEAN>
-__global__ __launch_bounds__((Places<T, WAVES, EPL>::kThreads)) void fb_residual_norm_grad_kernel(ResidualParams p)
+template <class T, class W, int WAVES, int EPL, Ends ENDS, bool LEAN>
+__global__ __launch_bounds__((Places<T, WAVES, EPL, ENDS>::kThreads)) void fb_residual_norm_grad_kernel(ResidualParams p)
 {
-    typedef Places<T, WAVES, EPL> P;
+    typedef Places<T, WAVES, EPL, ENDS> P;
     constexpr int VE = P::kVE, NV = P::kPieces;
     __shared__ float slots[2][P::kRows][2][WAVES][2];
     __shared__ float joined[P::kRows == 1 ? 1 : P::kRows * P::kStep * EPL];
@@ -171,10 +236,10 @@ __global__ __launch_bounds__((Places<T, WAVES, EPL>::kThreads)) void fb_residual
     const bool need_h = inner || p.dgate || p.slot[kGate] >= 0;
     float w1[EPL], b1[EPL], w2[EPL], gv[EPL];
     auto vectors = [&]() {
-        load_vector<W, EPL, VE>(p.inner_weight, at.H, P::kStep, at.lane, 1.0f, w1);
-        load_vector<W, EPL, VE>(p.inner_bias, at.H, P::kStep, at.lane, 0.0f, b1);
-        load_vector<W, EPL, VE>(p.weight, at.H, P::kStep, at.lane, 1.0f, w2);
-        load_vector<W, EPL, VE>(gate_vector ? p.gate : nullptr, at.H, P::kStep, at.lane, 1.0f, gv);
+        at.template vector<W>(p.inner_weight, 1.0f, w1);
+        at.template vector<W>(p.inner_bias, 0.0f, b1);
+        at.template vector<W>(p.weight, 1.0f, w2);
+        at.template vector<W>(gate_vector ? p.gate : nullptr, 1.0f, gv);
     };
     if (!LEAN) vectors();
     float sum[kSums][EPL] = {};
@@ -210,9 +275,9 @@ __global__ __launch_bounds__((Places<T, WAVES, EPL>::kThreads)) void fb_residual
             ask(r);
         }
         float d[EPL], g[EPL], xh[EPL], gr[EPL];
-        P::open(rds, d);
-        P::open(rdy, g);
-        P::open(rs, xh);
+        at.open(rds, d);
+        at.open(rdy, g);
+        at.open(rs, xh);
         const float a1 = m1, c1 = r1, a2 = m2, c2 = r2;
         float t[2] = {0.0f, 0.0f};
         if (outer) {                                    // (past the row's end dy is 0, and with it every share)
@@ -230,8 +295,8 @@ __global__ __launch_bounds__((Places<T, WAVES, EPL>::kThreads)) void fb_residual
 #pragma unroll
             for (int i = 0; i < EPL; ++i) d[i] = at.in(i / VE, i % VE) ? fmaf(c2, g[i] - t0 - xh[i] * t1, d[i]) : 0.0f;
         }
-        P::open(rh, xh);
-        P::open(rg, gr);
+        at.open(rh, xh);
+        at.open(rg, gr);
         if (!LEAN) ask(r + rstep);
         if (p.dresidual && r < p.R) at.store(p.dresidual, r, p.lddr, d, p.past);
 #pragma unroll
@@ -332,17 +397,28 @@ int64_t residual_groups(int64_t R, int64_t H)
     return std::max<int64_t>(1, std::min<int64_t>((R + rows - 1) / rows, 2 * kCUs));
 }
 
+template <class T, class W, int WAVES, int EPL, Ends ENDS>
+int launch_residual(const ResidualParams &p, bool grad, hipStream_t stream)
+{
+    typedef Places<T, WAVES, EPL, ENDS> P;
+    if (grad) {
+        // (few registers: a last piece is waited for at once, 13894 x 5094 in half precision 930 instead of 1212 us)
+        constexpr bool kLean = EPL > 8;
+        hipLaunchKernelGGL((fb_residual_norm_grad_kernel<T, W, WAVES, EPL, kLean ? kParts : ENDS, kLean>), dim3((unsigned)residual_groups(p.R, p.H)),
+                           dim3(P::kThreads), 0, stream, p);
+    } else {
+        const int64_t groups = (p.R + P::kRows - 1) / P::kRows, most = (int64_t)kCUs * (P::kThreads > 256 ? 4 : 8);
+        hipLaunchKernelGGL((fb_residual_norm_kernel<T, W, WAVES, EPL, ENDS>), dim3((unsigned)std::min(groups, most)), dim3(P::kThreads), 0, stream, p);
+    }
+    return launched("residual norm kernel launch: ");
+}
+
 template <class T, class W, int WAVES, int EPL>
 int launch_residual(const ResidualParams &p, bool grad, hipStream_t stream)
 {
-    typedef Places<T, WAVES, EPL> P;
-    if (grad) {
-        hipLaunchKernelGGL((fb_residual_norm_grad_kernel<T, W, WAVES, EPL, (EPL > 8)>), dim3((unsigned)residual_groups(p.R, p.H)), dim3(P::kThreads), 0, stream, p);
-    } else {
-        const int64_t groups = (p.R + P::kRows - 1) / P::kRows, most = (int64_t)kCUs * (P::kThreads > 256 ? 4 : 8);
-        hipLaunchKernelGGL((fb_residual_norm_kernel<T, W, WAVES, EPL>), dim3((unsigned)std::min(groups, most)), dim3(P::kThreads), 0, stream, p);
-    }
-    return launched("residual norm kernel launch: ");
+    // (pieces of four elements: up to three single ones are no slower than what drops them, 4811 x 777 16 and 19 us)
+    if (p.H % Vec<T>::kN == 0) return launch_residual<T, W, WAVES, EPL, kWhole>(p, grad, stream);
+    return launch_residual<T, W, WAVES, EPL, sizeof(T) == 4 ? kParts : kEnding>(p, grad, stream);
 }
 
 template <class T, class W>
