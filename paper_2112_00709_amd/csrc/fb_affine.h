@@ -119,6 +119,7 @@ inline size_t aligned(size_t n) { return (n + 255) & ~(size_t)255; }
 double plan(Product &q, int only_tile = 0, bool whole = false);   // tiles and shares of k (`whole`: one share); what it takes, in clocks
 inline size_t product_bytes(const Product &q) { return q.parts ? aligned((size_t)q.split * (size_t)q.M * (size_t)q.N * sizeof(float)) : 0; }
 bool plan_back(Product &dx, Product &dw);
+int64_t rows_in_rounds(const Product &q, Product &last);          // rows that go in whole rounds of large tiles, before those of `last`; 0: all at once
 int launch_dx(const Product &q, hipStream_t stream);              // by launch_mfma_product, perhaps in two
 int launch_join(const Product *a, const Product *b, int type, const float *sums, int64_t rows, int64_t N, float *out, hipStream_t stream);
 
@@ -203,6 +204,19 @@ GradPlan grad_plan(const void *dy, int64_t lddy, int dy_type, const void *x, int
                    int act);
 int launch_grad(GradPlan &g, const Factor &d, const float *undo, void *dx, int64_t lddx, void *dweight, float *part, const float *sums, int64_t rows, float *dbias,
                 hipStream_t stream);
+
+// What the gradient of log probabilities from hidden frames is made of, for pieces of `width` of the vocabulary.
+struct ScoreGradPlan {
+    int64_t width, pieces, ldz;
+    Product z, dx, dw;       // of a whole piece
+    Packed x, w;
+    bool pair;               // both products in one launch
+    bool twice;              // dz is two rows of 16 bits for each of M, see twice()
+    int64_t sum_rows;
+    size_t dz, rows, picks, live, range, sums, acc, part_x, part_w, bytes;
+};
+
+ScoreGradPlan score_grad_plan(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t V, int64_t K, int type);
 
 constexpr int kPeakGroups = kCUs;    // four peaks a lane for those who need the largest
 

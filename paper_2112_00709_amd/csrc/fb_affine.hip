@@ -196,18 +196,26 @@ double plan(Product &q, int only_tile, bool whole)
 
 // Tiles of 256 in whole rounds of workgroups, and the rows that would make a last round, which is mostly empty, by tiles that fit them:
 // 69120 x 3000 x 1024 in bfloat16 has 1080 tiles for 256 compute units: 421 us, or 354 and 50.
-int launch_dx(const Product &q, hipStream_t stream)
+int64_t rows_in_rounds(const Product &q, Product &last)
 {
     const int64_t across = (q.N + 255) / 256, tiles = (q.M + 255) / 256 * across, rounds = (tiles + kCUs - 1) / kCUs;
     const int64_t rows = (rounds - 1) * kCUs / across * 256;
-    if (q.parts || q.tile != 256 || rounds < 2 || rows <= 0 || rows >= q.M) return launch_mfma_product(q, stream);
-    Product first = q, last = q, whole = q;
-    first.M = rows;
+    last = q;
+    if (q.parts || q.tile != 256 || rounds < 2 || rows <= 0 || rows >= q.M) return 0;
+    Product whole = q;
     last.M = q.M - rows;
     whole.M = 256;
     whole.N = 256;
     constexpr double kLaunch = 5000.0;
-    if (plan(last, 0, true) + kLaunch >= plan(whole, 256, true) || last.tile == 256) return launch_mfma_product(q, stream);
+    return plan(last, 0, true) + kLaunch >= plan(whole, 256, true) || last.tile == 256 ? 0 : rows;
+}
+
+int launch_dx(const Product &q, hipStream_t stream)
+{
+    Product first = q, last;
+    const int64_t rows = rows_in_rounds(q, last);
+    if (rows == 0) return launch_mfma_product(q, stream);
+    first.M = rows;
     const auto skip = [&](const void *p, int64_t ld, int type) { return p ? (const char *)p + (size_t)rows * (size_t)ld * type_bytes(type) : nullptr; };
     last.A.p = skip(q.A.p, q.A.ld, q.type);
     last.f.y = (void *)skip(q.f.y, q.f.ldy, q.f.out_type);

@@ -645,15 +645,7 @@ ScorePlan score_plan(const void *x, int64_t ldx, const void *weight, int64_t ldw
 // bits, two of 64000 for 4095 rows) in rows of less than 4 MB, and pieces are alike.
 constexpr int64_t kPieceBytes = (int64_t)512 << 20;
 
-struct ScoreGradPlan {
-    int64_t width, pieces, ldz;
-    Product z, dx, dw;       // of a whole piece
-    Packed x, w;
-    bool pair;               // both products in one launch
-    bool twice;              // dz is two rows of 16 bits for each of M, see twice()
-    int64_t sum_rows;
-    size_t dz, rows, picks, live, range, sums, acc, part_x, part_w, bytes;
-};
+}  // namespace
 
 ScoreGradPlan score_grad_plan(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t V, int64_t K, int type)
 {
@@ -694,6 +686,8 @@ ScoreGradPlan score_grad_plan(const void *x, int64_t ldx, const void *weight, in
     g.bytes = g.x.bytes + g.w.bytes + g.dz + g.rows + g.picks + g.live + g.range + g.sums + g.acc + g.part_x + g.part_w;
     return g;
 }
+
+namespace {
 
 int check_scores(const char *who, const void *x, int64_t ldx, const void *weight, int64_t ldw, const int32_t *tokens, int64_t M, int64_t V, int64_t K, int type)
 {
