@@ -536,6 +536,10 @@ struct Task {
     int tiles_i, tiles_j;
 };
 
+// Whether there are registers for a second set of sums: not beside the 128 sums a lane of 16-bit tiles of 256, which are one chain over k.
+template <class T, int FI, int FJ>
+constexpr bool kFoldsOf = sizeof(T) == 4 || FI * FJ <= 4;
+
 // Workgroup `block` of `blocks`: they stay and take tile after tile, so that the copies for the next tile are under way while
 // this one's sums leave.  `args`: where the kernel's argument with the product lies.
 template <class T, bool ALONG_A, bool ALONG_B, int WI, int WJ, int FI, int FJ, class WAY, bool MASKED = false>
@@ -629,9 +633,10 @@ __device__ __forceinline__ void run_tiles(const Task &task, ProductArgs args, in
         const int steps = (int)((p.length + kDeep - 1) / kDeep);
         if constexpr (WAY::kNeverEmpty) __builtin_assume(steps > 0);      // (or it would be waited for what `early` asks for)
         f32x16 acc[FI][FJ] = {};
-        // Single precision: sums of kFold steps are added up apart, so that their roundings do not pile up over a long k (192 x 186 x 3769:
-        // gradients 3.3e-7 off in the 2-norm instead of 1.4e-6, at the same time).
-        constexpr bool kFolds = WAY::kFolded && sizeof(T) == 4;
+        // Sums of kFold steps (256 k, of 16 bits 512) are added up apart, so that their roundings do not pile up over a long k (192 x 186 x 3769
+        // in single precision: gradients 3.3e-7 off in the 2-norm instead of 1.4e-6, at the same time; 65 x 300 x 4096 in half precision: 31 and 41
+        // instead of 29 and 39 us forward and backward, others unchanged).
+        constexpr bool kFolds = WAY::kFolded && kFoldsOf<T, FI, FJ>;
         constexpr int kFold = 8;
         f32x16 folded[kFolds ? FI : 1][kFolds ? FJ : 1] = {};
         const Where where{p.share, p.i0, p.j0, wi, wj, wave, (float *)(lds_raw + 2 * (a.kBytes + b.kBytes))};
@@ -704,7 +709,7 @@ __device__ __forceinline__ void run_tiles(const Task &task, ProductArgs args, in
 
 // (a second set of sums takes tiles of 128 two registers beyond what two workgroups a compute unit have, if they are not asked for)
 template <class T, bool ALONG_A, bool ALONG_B, int WI, int WJ, int FI, int FJ, class WAY, bool MASKED>
-__global__ __launch_bounds__(WI * WJ * 64, (WAY::kFolded && sizeof(T) == 4 && FI * FJ == 4 ? 2 : 1)) void fb_mfma_product_kernel(Task task)
+__global__ __launch_bounds__(WI * WJ * 64, (WAY::kFolded && kFoldsOf<T, FI, FJ> && FI * FJ == 4 ? 2 : 1)) void fb_mfma_product_kernel(Task task)
 {
     run_tiles<T, ALONG_A, ALONG_B, WI, WJ, FI, FJ, WAY, MASKED>(task, (ProductArgs)__builtin_amdgcn_kernarg_segment_ptr(), blockIdx.x, gridDim.x);
 }
