@@ -162,7 +162,7 @@ int64_t sum_rows(int64_t M, int64_t N, int type)
 double plan(Product &q, int only_tile, bool whole)
 {
     static constexpr int kSplits[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64, 96, 128};
-    struct Shape {                          // (see fb_affine_mfma.hip)
+    struct Shape {                          // (see fb_mfma.h)
         int tile, resident;
         double per_k16, per_k32;            // clocks of a compute unit on one k of a tile, measured
     };

@@ -295,28 +295,6 @@ struct Where {
     float *room;
 };
 
-// Sixteen rows of a wave's sums, pass by pass, into its LDS (`to`: the lane's row there): see Finished.
-template <int FI, int FJ>
-__device__ __forceinline__ void put_rows(const f32x16 (&acc)[FI][FJ], int pass, int lane, uint32_t to)
-{
-    constexpr int kPer = FJ * 8;
-    if ((lane >> 4 & 1) != (pass & 1)) return;
-    auto put = [&](const f32x16 (&sums)[FJ]) {
-#pragma unroll
-        for (int y = 0; y < FJ; ++y)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const f32x4 w = {sums[y][4 * e], sums[y][4 * e + 1], sums[y][4 * e + 2], sums[y][4 * e + 3]};
-                const int c = (y * 8 + 2 * e + (lane >> 5)) ^ (lane & 15 & (kPer - 1));
-                *(__attribute__((address_space(3))) f32x4 *)(uintptr_t)(to + c * 16) = w;
-            }
-    };
-    if (pass < 2) put(acc[0]);
-    else if (FI <= 2 || pass < 4) put(acc[1 % FI]);
-    else if (pass < 6) put(acc[2 % FI]);
-    else put(acc[3 % FI]);
-}
-
 // What a row has in common and what a column has go onto the sums by one matrix instruction a fragment, of two k in single
 // precision: of_columns[y] lane % 32 1 + 1 of_row.  (`of_columns`: a column's in the lower lanes, 1 in the upper ones, or 0 if rows have nothing.)
 template <int FJ>
