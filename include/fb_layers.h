@@ -75,7 +75,7 @@ enum { FB_NORM_NONE = 0, FB_NORM_LAYER = 1, FB_NORM_RMS = 2 };
  * where a norm is (FB_NORM_LAYER)  (x - mean) rstd weight + bias,  mean = sum x / H,  rstd = 1 / sqrt(sum (x - mean)^2 / H + eps),
  * (FB_NORM_RMS) the same with mean = 0, or (FB_NORM_NONE) x itself.
  *   h, residual, s, y   [R][H] of `type`; residual nullable (0), y needed unless outer is FB_NORM_NONE
- *   gate                [R][H] of `type`, or with ldg = 0 [H] of `wtype` for all rows; nullable (1)
+ *   gate                [R][H] of `type`, or with ldg = 0 [H] of `wtype` for all rows (for one row too); nullable (1)
  *   inner_weight, inner_bias, weight, bias   [H] of `wtype` (FB_TYPE_F32 or `type`), nullable (1 and 0), only with their norm
  *   stats               out, float [4][R]: inner mean and rstd, outer mean and rstd (0 and 1 where there is no norm, mean 0 of
  *                       FB_NORM_RMS), nullable (what fb_residual_norm_grad takes)
@@ -174,7 +174,9 @@ size_t fb_gated_affine_grad_workspace_bytes(const void *x, int64_t ldx, const vo
  * Where `type` has 16 bits dz is rounded to it before the two products (for M <= 64, and M <= 128 if M N K <= 2^23, kept as two
  * such numbers, and products of those added), to FB_TYPE_F16 times a power of two that brings the largest
  * finite bound of |dz| into [2^14, 2^15) (as in fb_affine_grad): |dy u| and |dy| times what |act'| and |act| do not exceed for a g of
- * its sign and size; dbias is summed before that.
+ * its sign and size; dbias is summed before that.  Such a rounding is off by up to half a step of each entry of dz (2^-8 of its size in
+ * FB_TYPE_BF16, 2^-11 in FB_TYPE_F16): where many entries count the products are off by 1.4 to 1.5 times their own rounding in the 2-norm, where one
+ * rules a row or a column by up to its half step beside their own rounding.
  * Errors as fb_affine_grad; dy, x, weight and preact must not be NULL.
  */
 int fb_gated_affine_grad(const void *dy, int64_t lddy, const void *x, int64_t ldx, const void *weight, int64_t ldw, const void *preact, int64_t ldp,
@@ -225,7 +227,8 @@ int fb_token_logprobs_grad(const void *logits, int64_t ld, const int32_t *tokens
 size_t fb_affine_logprobs_workspace_bytes(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t M, int64_t V, int64_t K, int type);
 
 /*
- * fb_token_logprobs of the logits  x W^T + bias,  which are formed in single precision, a tile at a time, and neither rounded nor kept:
+ * fb_token_logprobs of the logits  x W^T + bias,  which are formed in single precision, a tile at a time, and neither rounded nor kept (over
+ * a long K in shares, except where many rows of 16 bits meet many alternatives):
  *   x         [M][K] of `type`;  weight [V][K] of `type`;  bias float [V], nullable; -inf in it rules an alternative out
  *   tokens    int32 [M]; a negative one marks a row that does not count: its x may hold anything and its outputs are 0
  *   logprobs, entropy, logz   out, float [M], nullable; as in fb_token_logprobs, rows of nothing but -inf (logits below -1e38 among
@@ -249,6 +252,9 @@ size_t fb_affine_logprobs_grad_workspace_bytes(const void *x, int64_t ldx, const
  * Rows that do not count and rows whose logz is -inf have dx = 0 and no part in the sums.  Where `type` has 16 bits dz is rounded to it
  * before the two products (for M <= 64, and M <= 128 if M V K <= 2^24, kept as two such numbers), to FB_TYPE_F16 times a power of two for
  * the largest |g_logprobs| + |g_entropy| (0.37 + entropy), which no |dz| exceeds (as in fb_affine_grad); dbias is summed before that.
+ * M decides, not the rows that count.  A dz of one number is off by up to half a step (2^-8 of its size in FB_TYPE_BF16, 2^-11 in FB_TYPE_F16): dx
+ * and dweight are off by 1.5 times their own rounding in the 2-norm where many rows of different g_logprobs count, by up to 2.4 times
+ * where few do or all have one g_logprobs, whose rounding is then in every gradient (next to none where that is a power of two).
  * Errors as fb_affine_logprobs; FB_EUNSUPPORTED too: rows of dx 2^27 elements apart or more.
  */
 int fb_affine_logprobs_grad(const void *x, int64_t ldx, const void *weight, int64_t ldw, const float *bias, const int32_t *tokens, const float *logz,

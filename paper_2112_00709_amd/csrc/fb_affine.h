@@ -171,7 +171,8 @@ inline bool bad_sizes(int64_t M, int64_t N, int64_t K) { return bad_rows(M) || b
 // numbers of 16 bits each, the second what the first lacks, M rows further down.  dx adds the sums of row i and row M + i, dW takes x twice.
 // Bfloat16, log probabilities: 16 rows of 3000 x 1024 30 instead of 27 us, of 128000 x 1024 162 instead of 156; 64 rows 201 instead of 173; at
 // 128 rows it would be 276 instead of 207.  Up to 128 rows (whose bits in Scores::live one workgroup sets) that are multiplied in less time than
-// launches take have it too: 128 rows of 300 x 256 26.6 and 26.8 us, of 3000 x 1024 39 and 31.5.
+// launches take have it too: 128 rows of 300 x 256 26.6 and 26.8 us, of 3000 x 1024 39 and 31.5.  (The host knows M, not how many of the rows count: more
+// rows of which few do are left with one number, up to 2.4 times as far off as their own rounding.)
 inline bool twice(int64_t M, int64_t N, int64_t K, int type)
 {
     return type != FB_TYPE_F32 && M > 0 && (M <= 64 || (M <= 128 && N * K <= ((int64_t)1 << 24) / M));

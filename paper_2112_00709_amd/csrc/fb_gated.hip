@@ -2,11 +2,11 @@
 //
 // Forward, both products are one, of x with G and U in turn 32 rows of each (see Side in fb_mfma.h): a wave's two fragments of the
 // weight are the same rows of both, so that g and u of an output meet in one wave and y leaves alone.  44160 x 2048 x 1024 in bfloat16 with silu
-// and both preactivations: 385 us (963 TFLOP/s); of these 305 are the products (1215), the rest the outputs' way through the registers and LDS, which
+// and both preactivations: 387 us (957 TFLOP/s); of these 305 are the products (1215), the rest the outputs' way through the registers and LDS, which
 // nothing overlaps (543 MB; starting half of the chiplets later, so that they do not store all at once, changes nothing).
 //
-// Backward, dz is made in one pass over dy and preact, and is a factor of two products: 851 us for the same sizes, dz 161 (5.6 TB/s), dx 354 and
-// dW 297 (1045 and 1245 TFLOP/s), shares of dW joined 21.
+// Backward, dz is made in one pass over dy and preact, and is a factor of two products: 860 us for the same sizes, dz 163 (5.6 TB/s), dx 363 and
+// dW 306 (1020 and 1211 TFLOP/s), shares of dW joined 20.
 #include "fb_mfma.h"
 
 namespace fb {

@@ -5,9 +5,9 @@
 // T = sum e^(z - m) (z - m), and a second launch joins the tiles of a row.  Backward, logits are formed once more, piece by piece of
 // the vocabulary, and leave as their gradient in the factors' type; two products take that into dx and dweight.
 //
-// Bound by the matrix units.  Measured, bfloat16: 4095 x 128000 x 2048 forward 1850 us (1160 TFLOP/s; without the way out 1760), backward
-// 5580 (two pieces of 990 for the logits, 855 for dx, 862 for dweight, 35 to join: 1155 TFLOP/s); 69120 x 3000 x 1024 backward 1245 (logits
-// 443, dx 396, dweight 358).
+// Bound by the matrix units.  Measured, bfloat16: 4095 x 128000 x 2048 forward 1863 us (1153 TFLOP/s; without the way out 1760), backward
+// 5632 (under the profiler two pieces of 1020 for the logits, 852 for dx, 886 for dweight, 35 to join: 1144 TFLOP/s); 69120 x 3000 x 1024 backward 1251
+// (logits 463, dx 404, dweight 368).
 #include "fb_mfma.h"
 
 namespace fb {

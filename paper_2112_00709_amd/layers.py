@@ -239,7 +239,7 @@ def fb_residual_norm(h, residual=None, gate=None, scale: float = 1.0, inner: str
     mean and rstd, outer mean and rstd.
 
     ``inner``, ``outer``: "none", "layer" or "rms" (no mean); ``h``, ``residual`` [..., H], H up to 8192; ``gate`` like h, or [H] for all
-    rows; weights, biases and a gate of [H] float32 or of h's type (all of one)."""
+    rows (one of a single dimension always is); weights, biases and a gate of [H] float32 or of h's type (all of one)."""
     L = lib()
     code = _type(h, "h")
     ph, ldh, R, H, dev = _rows(h, "h")
