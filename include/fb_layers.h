@@ -252,9 +252,10 @@ size_t fb_affine_logprobs_grad_workspace_bytes(const void *x, int64_t ldx, const
  * Rows that do not count and rows whose logz is -inf have dx = 0 and no part in the sums.  Where `type` has 16 bits dz is rounded to it
  * before the two products (for M <= 64, and M <= 128 if M V K <= 2^24, kept as two such numbers), to FB_TYPE_F16 times a power of two for
  * the largest |g_logprobs| + |g_entropy| (0.37 + entropy), which no |dz| exceeds (as in fb_affine_grad); dbias is summed before that.
- * M decides, not the rows that count.  A dz of one number is off by up to half a step (2^-8 of its size in FB_TYPE_BF16, 2^-11 in FB_TYPE_F16): dx
- * and dweight are off by 1.5 times their own rounding in the 2-norm where many rows of different g_logprobs count, by up to 2.4 times
- * where few do or all have one g_logprobs, whose rounding is then in every gradient (next to none where that is a power of two).
+ * A dz of one number is rounded times the factor that makes the largest |g_logprobs| a power of two, and the products are taken times its inverse:
+ * where all rows that count have one g_logprobs, it is not rounded then.  Each entry is off by up to half a step (2^-8 of its size in
+ * FB_TYPE_BF16, 2^-11 in FB_TYPE_F16): in the 2-norm dx and dweight are off by 1.0 (one g_logprobs, small p) to 1.4 times their own
+ * rounding where many rows count, and one that hangs on a single entry by up to that half step more.
  * Errors as fb_affine_logprobs; FB_EUNSUPPORTED too: rows of dx 2^27 elements apart or more.
  */
 int fb_affine_logprobs_grad(const void *x, int64_t ldx, const void *weight, int64_t ldw, const float *bias, const int32_t *tokens, const float *logz,

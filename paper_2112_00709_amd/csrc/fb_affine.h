@@ -13,8 +13,8 @@ struct Factor {
     bool along;
 };
 
-// What becomes of the sums: y = act(sum + bias[j]) + residual, preact = sum + bias[j].  Sums of half-precision products whose first
-// factor is dz are taken times *undo before that (see fb_peak_kernel).
+// What becomes of the sums: y = act(sum + bias[j]) + residual, preact = sum + bias[j].  Sums of 16-bit products whose first
+// factor is dz are taken times *undo before that (see fb_peak_kernel and scale_of).
 struct Finish {
     const float *bias;
     const void *residual;
@@ -171,8 +171,8 @@ inline bool bad_sizes(int64_t M, int64_t N, int64_t K) { return bad_rows(M) || b
 // numbers of 16 bits each, the second what the first lacks, M rows further down.  dx adds the sums of row i and row M + i, dW takes x twice.
 // Bfloat16, log probabilities: 16 rows of 3000 x 1024 30 instead of 27 us, of 128000 x 1024 162 instead of 156; 64 rows 201 instead of 173; at
 // 128 rows it would be 276 instead of 207.  Up to 128 rows (whose bits in Scores::live one workgroup sets) that are multiplied in less time than
-// launches take have it too: 128 rows of 300 x 256 26.6 and 26.8 us, of 3000 x 1024 39 and 31.5.  (The host knows M, not how many of the rows count: more
-// rows of which few do are left with one number, up to 2.4 times as far off as their own rounding.)
+// launches take have it too: 128 rows of 300 x 256 26.6 and 26.8 us, of 3000 x 1024 39 and 31.5.  (The host knows M, not how many of the rows count:
+// see scale_of for what is done where few of many do.)
 inline bool twice(int64_t M, int64_t N, int64_t K, int type)
 {
     return type != FB_TYPE_F32 && M > 0 && (M <= 64 || (M <= 128 && N * K <= ((int64_t)1 << 24) / M));
@@ -320,8 +320,8 @@ __device__ __forceinline__ void range_of_peak(uint32_t peak, float &scale, float
     scale = __uint_as_float(up << 23);
     undo = __uint_as_float((254 - up) << 23);
 }
-// The same from shares of it.
-__device__ __forceinline__ void range_of(const uint32_t *peaks, int n, float &scale, float &undo)
+// The largest of shares of it.
+__device__ __forceinline__ uint32_t largest_of(const uint32_t *peaks, int n)
 {
     const int lane = threadIdx.x & 63;
     uint32_t peak = 0;
@@ -330,8 +330,9 @@ __device__ __forceinline__ void range_of(const uint32_t *peaks, int n, float &sc
         const uint32_t one = i + lane < n ? peaks[i + lane] : 0;
         peak = one > peak ? one : peak;
     }
-    range_of_peak(max_wave_u(peak), scale, undo);
+    return max_wave_u(peak);
 }
+__device__ __forceinline__ void range_of(const uint32_t *peaks, int n, float &scale, float &undo) { range_of_peak(largest_of(peaks, n), scale, undo); }
 
 // dz = dy act'(z) (or a copy of dy in rows of whole pieces), rounded to the factors' type, and the sums of its columns before
 // the rounding.  Bound by memory: 44160 x 2048 in bfloat16 with max(z, 0) take 100 us, 5.4 TB/s.  A thread has one piece of the

@@ -25,7 +25,7 @@ __global__ __launch_bounds__(256) void fb_join_kernel(JoinParams p)
         const Product &q = p.q[which];
         const int64_t n = q.M * q.N;
         float undo = 1.0f;
-        if constexpr (std::is_same<T, f16>::value) undo = q.f.undo ? *q.f.undo : 1.0f;
+        if constexpr (sizeof(T) == 2) undo = q.f.undo ? *q.f.undo : 1.0f;
         for (int64_t at = (int64_t)(block - first) * 256 + threadIdx.x; at < n; at += (int64_t)(p.last[which] - first) * 256) {
             float s = 0.0f;
 #pragma unroll 8

@@ -5,8 +5,8 @@
 // and both preactivations: 387 us (957 TFLOP/s); of these 305 are the products (1215), the rest the outputs' way through the registers and LDS, which
 // nothing overlaps (543 MB; starting half of the chiplets later, so that they do not store all at once, changes nothing).
 //
-// Backward, dz is made in one pass over dy and preact, and is a factor of two products: 860 us for the same sizes, dz 163 (5.6 TB/s), dx 363 and
-// dW 306 (1020 and 1211 TFLOP/s), shares of dW joined 20.
+// Backward, dz is made in one pass over dy and preact, and is a factor of two products: 855 us for the same sizes, dz 163 (5.6 TB/s), dx 362 and
+// dW 305 (1023 and 1215 TFLOP/s), shares of dW joined 20.
 #include "fb_mfma.h"
 
 namespace fb {

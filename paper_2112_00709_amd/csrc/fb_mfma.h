@@ -499,7 +499,7 @@ struct Rounded {
         const int64_t i0 = where.i0 + where.wi * FI * 32, j0 = where.j0 + where.wj * FJ * 32;
 #pragma unroll
         for (int x = 0; x < FI; ++x) {
-            if constexpr (std::is_same<T, f16>::value) {
+            if (undo != 1.0f) {
 #pragma unroll
                 for (int y = 0; y < FJ; ++y) acc[x][y] *= undo;
             }
@@ -547,8 +547,8 @@ __device__ __forceinline__ void run_tiles(const Task &task, ProductArgs args, in
         return Place{share, (int64_t)(first + v % down) * kI, (int64_t)(v / down) * (WAY::kPaired ? kJ / 2 : kJ), k0 + q.share < q.K ? q.share : q.K - k0};
     };
 
-    float undo = 1.0f;                     // (products of a half-precision gradient; shares of k leave as they are)
-    if constexpr (std::is_same<T, f16>::value && (!ALONG_B || WAY::kNeverEmpty)) {
+    float undo = 1.0f;                     // (products of a 16-bit gradient; shares of k leave as they are)
+    if constexpr (sizeof(T) == 2 && (!ALONG_B || WAY::kNeverEmpty)) {
         if (q.f.undo && !q.parts) undo = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(*q.f.undo)));
     }
 

@@ -2,7 +2,7 @@
 // pass, and its gradient.  Bound by memory: a row is read once into the registers of one to eight waves, everything that needs
 // it whole is formed there, and it is written once.  Measured, bfloat16: 69120 x 1024 with both norms and a gate of one row 108 us (566 MB, 5.3
 // TB/s), the gradient with a gate of rows and all seven outputs 205 us (1.13 GB, 5.5 TB/s), 6 of them the second launch; one row of 512 3.1 us on
-// the GPU, 12.7 a call.
+// the GPU, 12.6 a call.
 #include "fb_layers_device.h"
 
 namespace fb {

@@ -5,9 +5,9 @@
 // T = sum e^(z - m) (z - m), and a second launch joins the tiles of a row.  Backward, logits are formed once more, piece by piece of
 // the vocabulary, and leave as their gradient in the factors' type; two products take that into dx and dweight.
 //
-// Bound by the matrix units.  Measured, bfloat16: 4095 x 128000 x 2048 forward 1863 us (1153 TFLOP/s; without the way out 1760), backward
-// 5632 (under the profiler two pieces of 1020 for the logits, 852 for dx, 886 for dweight, 35 to join: 1144 TFLOP/s); 69120 x 3000 x 1024 backward 1251
-// (logits 463, dx 404, dweight 368).
+// Bound by the matrix units.  Measured, bfloat16: 4095 x 128000 x 2048 forward 1864 us (1152 TFLOP/s; without the way out 1760), backward
+// 5620 (under the profiler two pieces of 1015 for the logits, 852 for dx, 888 for dweight, 35 to join: 1146 TFLOP/s); 69120 x 3000 x 1024 backward 1258
+// (logits 458, dx 403, dweight 364, rows and the largest gradient 10).
 #include "fb_mfma.h"
 
 namespace fb {
@@ -453,61 +453,109 @@ int launch_end(const EndParams &p, hipStream_t stream)
     return launched("scores end kernel launch: ");
 }
 
-// What the gradient takes of a row, times the power of two that half precision asks for.
+// What the gradient takes of a row, times the factor that dz is rounded with (see scale_of).
 struct RowParams {
     const int32_t *tokens;
     const float *logz, *entropy, *g, *h;
     int64_t M;
     f32x4 *rows;
-    uint32_t *peaks;         // half precision: of the largest finite bound of |dz|, nullable
+    uint32_t *peaks;         // shares of the largest finite bound of |dz| and, kPeakGroups further, of the largest finite |g|; nullable
     int n_peaks;
-    float *undo;
+    float *undo;             // the factor's inverse, out; nullable (1)
     uint64_t *live;          // see Scores
     int32_t *picks;          // [whole 256 rows], as rows are: the tokens, -1 where a row does not count
     int low;                 // M where rows of x are there twice, see twice(); or 0
 };
 
-__device__ __forceinline__ f32x4 row_of(const RowParams &p, int64_t i)
+// What is known of a row (asked for whether it counts or not: all at once).
+struct Row {
+    int32_t token;
+    float logz, g, h, entropy;
+};
+
+__device__ __forceinline__ Row ask_row(const RowParams &p, int64_t i)
 {
-    const float logz = p.logz[i];
-    if (p.tokens[i] < 0 || logz == -kInf) return f32x4{kInf, 0.0f, 0.0f, 0.0f};
-    const float g = p.g ? p.g[i] : 0.0f, h = p.h ? p.h[i] : 0.0f;
-    return f32x4{logz, logz != logz ? logz : p.h ? fmaf(h, p.entropy[i], g) : g, h, g};
+    return Row{p.tokens[i], p.logz[i], p.g ? p.g[i] : 0.0f, p.h ? p.h[i] : 0.0f, p.h ? p.entropy[i] : 0.0f};
+}
+
+__device__ __forceinline__ f32x4 row_of(const RowParams &p, const Row &r)
+{
+    if (r.token < 0 || r.logz == -kInf) return f32x4{kInf, 0.0f, 0.0f, 0.0f};
+    return f32x4{r.logz, r.logz != r.logz ? r.logz : p.h ? fmaf(r.h, r.entropy, r.g) : r.g, r.h, r.g};
 }
 
 // What no |dz| of the row exceeds, if it is finite, as a whole number that is larger where it is.
-__device__ __forceinline__ uint32_t bound_of(const RowParams &p, int64_t i)
+__device__ __forceinline__ uint32_t bound_of(const RowParams &p, const Row &row, const f32x4 &r)
 {
-    const f32x4 r = row_of(p, i);
     if (r[0] == kInf) return 0u;
-    const uint32_t a = __float_as_uint(fabsf(r[3]) + (p.h ? fabsf(r[2]) * (0.37f + fabsf(p.entropy[i])) : 0.0f)) & 0x7fffffffu;
+    const uint32_t a = __float_as_uint(fabsf(r[3]) + (p.h ? fabsf(r[2]) * (0.37f + fabsf(row.entropy)) : 0.0f)) & 0x7fffffffu;
     return a < 0x7f800000u ? a : 0u;
 }
 
-// The largest bound of every `step`-th row from `from` on, in thread 0.
-__device__ __forceinline__ uint32_t peak_of(const RowParams &p, int64_t from, int64_t step, uint32_t (&slots)[4])
+// The largest bound and |g| of rows that count.
+struct Peaks {
+    uint32_t bound, g;
+};
+
+// Those of every `step`-th row from `from` on.
+__device__ __forceinline__ Peaks peaks_of(const RowParams &p, int64_t from, int64_t step, uint32_t (&slots)[2][4])
 {
-    uint32_t peak = 0;
-#pragma unroll 4
-    for (int64_t i = from; i < p.M; i += step) {
-        const uint32_t a = bound_of(p, i);
-        peak = a > peak ? a : peak;
+    constexpr int kAhead = 8;
+    Peaks peak{0, 0};
+    for (int64_t i = from; i < p.M; i += kAhead * step) {
+        Row row[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) row[u] = ask_row(p, i + u * step < p.M ? i + u * step : p.M - 1);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const f32x4 r = row_of(p, row[u]);
+            const uint32_t a = bound_of(p, row[u], r);
+            uint32_t b = __float_as_uint(r[3]) & 0x7fffffffu;
+            b = b < 0x7f800000u ? b : 0u;
+            peak.bound = a > peak.bound ? a : peak.bound;
+            peak.g = b > peak.g ? b : peak.g;
+        }
     }
-    peak = max_wave_u(peak);
-    if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = peak;
+    peak.bound = max_wave_u(peak.bound);
+    peak.g = max_wave_u(peak.g);
+    if ((threadIdx.x & 63) == 0) {
+        slots[0][threadIdx.x >> 6] = peak.bound;
+        slots[1][threadIdx.x >> 6] = peak.g;
+    }
     __syncthreads();
-    for (int w = 0; w < 4; ++w) peak = slots[w] > peak ? slots[w] : peak;
+    for (int w = 0; w < 4; ++w) {
+        peak.bound = slots[0][w] > peak.bound ? slots[0][w] : peak.bound;
+        peak.g = slots[1][w] > peak.g ? slots[1][w] : peak.g;
+    }
     return peak;
 }
 
 __global__ __launch_bounds__(256) void fb_scores_peak_kernel(RowParams p)
 {
-    __shared__ uint32_t slots[4];
-    const uint32_t peak = peak_of(p, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256, slots);
-    if (threadIdx.x == 0) p.peaks[blockIdx.x] = peak;
+    __shared__ uint32_t slots[2][4];
+    const Peaks peak = peaks_of(p, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256, slots);
+    if (threadIdx.x == 0) {
+        p.peaks[blockIdx.x] = peak.bound;
+        p.peaks[kPeakGroups + blockIdx.x] = peak.g;
+    }
 }
 
-// Rows the way the gradient takes them, 256 a workgroup; in half precision few of them (kPeakAlone) are looked through for the largest bound by
+// The factor that dz is rounded with, and its inverse.  A row's largest entry is mostly its token's, g (1 - p) with a small p, and where g is one number in
+// all rows, or few rows count, the rounding of that entry would be in every gradient (300 rows, g = -1 / 300, V 128000, in bfloat16: dx and dweight 2.6e-3
+// off in the 2-norm, their own rounding is 1.7e-3).  Taken times 1 / m, where m is the mantissa of the largest |g|, 1 <= m < 2, such a g is a power of two
+// and 1 - p rounds to 1; smaller ones lie in the halves of two powers of two where a step is less of the number.  In half precision times a power
+// of two too, for the bound's sake.  Where dz is two numbers there is nothing to gain: m = 1.
+template <class T>
+__device__ __forceinline__ void scale_of(const Peaks &peak, bool twice, float &scale, float &undo)
+{
+    const float m = twice || peak.g < 0x00800000u ? 1.0f : __uint_as_float((peak.g & 0x007fffffu) | 0x3f800000u), part = 1.0f / m;
+    scale = undo = 1.0f;
+    if constexpr (std::is_same<T, f16>::value) range_of_peak(__float_as_uint(__uint_as_float(peak.bound) * part), scale, undo);
+    scale *= part;
+    undo *= m;
+}
+
+// Rows the way the gradient takes them, 256 a workgroup; in 16 bits few of them (kPeakAlone) are looked through for the largest bound and |g| by
 // every workgroup.  Workgroups behind those copy what the products cannot take as it is.
 template <class T>
 __global__ __launch_bounds__(256) void fb_scores_rows_kernel(RowParams p, PrepareParams copies)
@@ -519,19 +567,25 @@ __global__ __launch_bounds__(256) void fb_scores_rows_kernel(RowParams p, Prepar
         return;
     }
     float scale = 1.0f;
-    if constexpr (std::is_same<T, f16>::value) {
-        float undo;
+    if (sizeof(T) == 2 && p.undo) {
+        Peaks peak;
         if (p.peaks) {
-            range_of(p.peaks, p.n_peaks, scale, undo);
+            peak = Peaks{largest_of(p.peaks, p.n_peaks), largest_of(p.peaks + kPeakGroups, p.n_peaks)};
         } else {
-            __shared__ uint32_t of_waves[4];
-            range_of_peak(peak_of(p, threadIdx.x, 256, of_waves), scale, undo);
+            __shared__ uint32_t of_waves[2][4];
+            peak = peaks_of(p, threadIdx.x, 256, of_waves);
         }
+        float undo;
+        scale_of<T>(peak, p.low != 0, scale, undo);
         if (blockIdx.x == 0 && threadIdx.x == 0) *p.undo = undo;
     }
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    Row row{-1, 0.0f, 0.0f, 0.0f, 0.0f};
     f32x4 r = {kInf, 0.0f, 0.0f, 0.0f};
-    if (i < p.M) r = row_of(p, i);
+    if (i < p.M) {
+        row = ask_row(p, i);
+        r = row_of(p, row);
+    }
     const uint64_t live = __builtin_amdgcn_ballot_w64(r[0] != kInf);
     if (p.low) {                           // (up to 128 rows, in one workgroup: once more behind the last of them)
         __shared__ uint64_t once[4];
@@ -547,7 +601,7 @@ __global__ __launch_bounds__(256) void fb_scores_rows_kernel(RowParams p, Prepar
     } else if ((threadIdx.x & 63) == 0) {
         p.live[i / 64] = live;
     }
-    p.picks[i] = r[0] != kInf ? p.tokens[i] : -1;
+    p.picks[i] = r[0] != kInf ? row.token : -1;
     r[0] = -r[0];
     r[1] *= -scale;
     r[2] *= -scale * kLn2;
@@ -555,13 +609,13 @@ __global__ __launch_bounds__(256) void fb_scores_rows_kernel(RowParams p, Prepar
     p.rows[i] = r;
 }
 
-// (half precision, a launch less: 2000 rows, V 300, K 256 25.4 instead of 29.3 us a call, 300 rows 24.9 instead of 28.6)
-constexpr int64_t kPeakAlone = 2048;
+// (a launch less: 4095 rows, V 300, K 256 in bfloat16 28 instead of 30 us a call, 8000 rows 36 either way, 12000 43 and 40.5)
+constexpr int64_t kPeakAlone = 8192;
 
 int launch_rows(RowParams r, int type, const Prepare &copies, hipStream_t stream)
 {
     const unsigned blocks = (unsigned)((r.M + 255) / 256);
-    if (type == FB_TYPE_F16 && r.M > kPeakAlone) {
+    if (r.undo && r.M > kPeakAlone) {
         r.n_peaks = (int)std::min<int64_t>(kPeakGroups, blocks);
         hipLaunchKernelGGL(fb_scores_peak_kernel, dim3((unsigned)r.n_peaks), dim3(256), 0, stream, r);
         const int rc = launched("scores peak kernel launch: ");
@@ -678,7 +732,7 @@ ScoreGradPlan score_grad_plan(const void *x, int64_t ldx, const void *weight, in
     g.rows = aligned((size_t)((M + 255) / 256 * 256) * sizeof(f32x4));
     g.picks = aligned((size_t)((M + 255) / 256 * 256) * sizeof(int32_t));
     g.live = aligned((size_t)((M + 255) / 256 * 4 + 1) * sizeof(uint64_t));
-    g.range = aligned((kPeakGroups + 1) * sizeof(float));
+    g.range = aligned((2 * kPeakGroups + 1) * sizeof(float));
     g.sums = aligned((size_t)g.sum_rows * (size_t)g.width * sizeof(float));
     g.acc = g.pieces > 1 ? aligned((size_t)M * (size_t)K * sizeof(float)) : 0;
     g.part_x = product_bytes(g.dx);
@@ -775,7 +829,7 @@ int fb_affine_logprobs_grad(const void *x, int64_t ldx, const void *weight, int6
         char *range = live + g.live, *sums = range + g.range;
         char *acc = sums + g.sums, *part_x = acc + g.acc, *part_w = part_x + g.part_x;
         const int64_t size = (int64_t)type_bytes(type);
-        float *undo = type == FB_TYPE_F16 && M > 0 ? (float *)range : nullptr;      // (no rows: nobody sets it)
+        float *undo = M > 0 && (type == FB_TYPE_F16 || (type == FB_TYPE_BF16 && !g.twice)) ? (float *)range : nullptr;      // (no rows: nobody sets it)
         if (M > 0) {
             RowParams r{tokens, logz, entropy, g_logprobs, g_entropy, M, (f32x4 *)rows, undo ? (uint32_t *)(undo + 1) : nullptr, 0, undo,
                         (uint64_t *)live, (int32_t *)picks, g.twice ? (int)M : 0};
